@@ -477,6 +477,159 @@ int lif_softplus_grad(const float* x, const float* grad_d, float* grad_x, size_t
                       lif_stream_t stream);
 
 /* --------------------------------------------------------------------- */
+/* Sequences of binned input and rows of logits.                           */
+/*                                                                         */
+/* A spike train counted in time bins is a dense sequence.  The calls      */
+/* below run a leaky integrator whose leak is a function of the input over */
+/* such sequences (lif_gated_*), read class or token probabilities off     */
+/* rows of logits (lif_token_logprobs), and train rows of logits on the    */
+/* most likely alternatives of a teacher (lif_distill_top).  Their large   */
+/* arrays hold one of three types; states, statistics, losses and sums are */
+/* float32 or wider, and a result in a 16-bit type is rounded once.        */
+/* No output may overlap an input or another output (lif_gated_step's      */
+/* state, updated in place, is the one exception).                         */
+/* --------------------------------------------------------------------- */
+#define LIF_F32  0
+#define LIF_BF16 1
+#define LIF_F16  2
+
+/* Gated leaky integrator: for each sample b and channel d, over the steps
+ * t = 0 .. n - 1 with n = length[b] clamped into [0, T] (length NULL: T),
+ *   a = 1 / (1 + e^{-f}),   h_t = a h_{t-1} + (1 - a) x_t   (LIF_GATED_COUPLED)
+ *                           h_t = a h_{t-1} + x_t           (without the flag)
+ * from h_{-1} = h_first[b][d] (NULL: 0).  The coupled form is the exact step
+ * of tau dh/dt = -h + x over one bin of length -tau log a.
+ *   x, f     [B][T][D] of p->dtype, rows of D contiguous elements; batch and
+ *            time strides in elements, >= 0 (0 repeats one row)
+ *   h        [B][T][D] contiguous, of p->dtype; 0 at steps t >= n; may be NULL
+ *   h_last   float [B][D] h_{n-1} (h_first where n = 0); may be NULL
+ *   marks    float [B][ceil(T / LIF_GATED_MARK)][D] the state entering step
+ *            t = 0, LIF_GATED_MARK, 2 LIF_GATED_MARK, ... (where t >= n the
+ *            last state); the backward pass needs them; may be NULL
+ * Values of x and f at steps t >= n have no effect.  A NaN or infinity at an
+ * earlier step reaches that channel's later states only.
+ *
+ * lif_gated_scan_backward: for L with dL/dh = grad_h ([B][T][D] of p->dtype,
+ * rows contiguous, strides g_batch and g_time; NULL: 0) and dL/dh_last =
+ * grad_last (float [B][D]; NULL: 0), from the forward's marks,
+ *   lambda_t = dL/dh_t + a_{t+1} lambda_{t+1}   (lambda_{n-1} += grad_last)
+ *   grad_x       [B][T][D] contiguous: lambda (1 - a), or lambda (free form)
+ *   grad_f       [B][T][D] contiguous: lambda (h_{t-1} - x) a (1 - a), or
+ *                lambda h_{t-1} a (1 - a)
+ *   grad_h_first float [B][D]: a_0 lambda_0 (grad_last where n = 0); may be
+ *                NULL
+ * grad_x and grad_f are 0 at steps t >= n.  Where one row of x or f serves
+ * several steps or samples (stride 0), the caller sums their gradients.
+ *
+ * lif_gated_step: one step for B running streams whose states are rows of
+ * state (float [n_slots][D], updated in place): stream b's is row slot[b]
+ * (NULL: row b, n_slots >= B).  p->T is 1; x, f are [B][D] with strides
+ * x_batch, f_batch; h [B][D] contiguous gets the new state.  The slots of
+ * one call must be distinct; a stream whose slot lies outside [0, n_slots)
+ * is left out (its h is 0).
+ *
+ * ws: lif_gated_scan_workspace_size(p) bytes, for the forward and the
+ * backward pass (0 for many shapes; ws may then be NULL).  All three are
+ * bitwise reproducible.
+ * Errors: LIF_ERR_ARG (null pointers, sizes, flags, dtype, strides),
+ * LIF_ERR_SIZE (B * D >= 2^31 or B * T * D >= 2^48), LIF_ERR_WORKSPACE. */
+#define LIF_GATED_MARK 64
+#define LIF_GATED_COUPLED 1u
+typedef struct lif_gated_params {
+    int32_t  B, T, D;            /* samples, steps, channels; T or B may be 0       */
+    int32_t  dtype;              /* LIF_F32, LIF_BF16 or LIF_F16                    */
+    uint32_t flags;              /* LIF_GATED_COUPLED                               */
+    int32_t  reserved;           /* must be 0                                       */
+    int64_t  x_batch, x_time;    /* strides of x in elements                        */
+    int64_t  f_batch, f_time;    /* strides of f                                    */
+    int64_t  g_batch, g_time;    /* strides of grad_h (backward pass)               */
+} lif_gated_params;
+
+size_t lif_gated_scan_workspace_size(const lif_gated_params* p);
+int lif_gated_scan(const void* x, const void* f, const int32_t* length, const float* h_first,
+                   const lif_gated_params* p, void* h, float* h_last, float* marks, void* ws, size_t ws_bytes,
+                   lif_stream_t stream);
+int lif_gated_scan_backward(const void* x, const void* f, const int32_t* length, const float* marks,
+                            const void* grad_h, const float* grad_last, const lif_gated_params* p, void* grad_x,
+                            void* grad_f, float* grad_h_first, void* ws, size_t ws_bytes, lif_stream_t stream);
+int lif_gated_step(const void* x, const void* f, const int32_t* slot, float* state, int n_slots,
+                   const lif_gated_params* p, void* h, lif_stream_t stream);
+
+/* Rows of logits: R rows of V logits of p->dtype, each row contiguous, rows
+ * p->stride elements apart; z = logits / p->temperature, p = softmax(z) over
+ * the row.
+ *
+ * lif_token_logprobs:
+ *   token    int32 [R] the given class or token of each row; a value outside
+ *            [0, V) marks a row without one (its logp is 0 and grad_logp has
+ *            no effect there); may be NULL (no row has one)
+ *   logp     float [R] log p[token]
+ *   entropy  float [R] -sum_j p_j log p_j
+ *   lse      float [R] log sum_j e^{z_j}
+ *   top_logp float [R][k], top_idx int32 [R][k]: the k largest logits of the
+ *            row as log probabilities, largest first, equal logits in order
+ *            of their index; k = p->k may be 0
+ *   grad     [R][V] of p->dtype, rows p->grad_stride elements apart: for L
+ *            with dL/dlogp = grad_logp and dL/dentropy = grad_entropy (float
+ *            [R] each; NULL: 0),
+ *              (grad_logp (1[j = token] - p_j)
+ *               - grad_entropy p_j (log p_j + entropy)) / temperature
+ * Every output may be NULL (top_logp and top_idx both or neither when k > 0).
+ *
+ * lif_distill_top: a teacher's list of k = p->k classes per row,
+ *   teacher_idx  int32 [R][k] distinct classes; a value outside [0, V) marks
+ *                an unused entry
+ *   teacher_logp float [R][k] their log probabilities, at the temperature of
+ *                the loss (lif_token_logprobs' top_* at that temperature)
+ *   weight       float [R] weight of each row in the gradient (NULL: 1)
+ *   loss         float [R] the divergence sum_c q_c (log q_c - log p_c), not
+ *                weighted; may be NULL
+ *   grad         [R][V] of p->dtype, rows p->grad_stride apart: the gradient
+ *                of sum_r weight_r loss_r; may be NULL
+ * over the listed classes c with q = e^{teacher_logp} made to sum to 1; with
+ * LIF_DISTILL_TAIL, q is kept as it is and all classes that are not listed
+ * form one further class, q_rest = 1 - sum q (a q_rest below
+ * LIF_DISTILL_TAIL_MIN counts as 0: it is not told apart from the rounding
+ * of the listed ones).  A class listed twice has the sum of its entries
+ * (q and q log q of each).  A row whose list has no mass (every entry unused
+ * or of probability 0) has loss 0 and gradient 0.
+ *
+ * Values that are not finite: a logit of -infinity has p = 0 and no part in
+ * any sum (as a token its logp is -infinity, in a teacher's list with q > 0
+ * the loss is +infinity).  A row with nothing above -infinity has lse and all
+ * log probabilities -infinity, entropy 0 and gradient 0.  A row with a NaN or
+ * +infinity has NaN for everything but top_idx, in which NaN ranks below
+ * -infinity.  (The zeros of a row without a token or without a list's mass
+ * stay.)
+ *
+ * ws: lif_rows_workspace_size(p) bytes for either call (0 for many shapes;
+ * ws may then be NULL).  Both are bitwise reproducible.
+ * Errors: LIF_ERR_ARG (null pointers, sizes, flags, dtype, stride < V,
+ * k > V, a temperature outside [2^-20, 2^20]), LIF_ERR_SIZE (k >
+ * LIF_TOP_MAX), LIF_ERR_WORKSPACE. */
+#define LIF_TOP_MAX 128
+#define LIF_DISTILL_TAIL 1u
+#define LIF_DISTILL_TAIL_MIN (1.0 / 1048576.0)
+typedef struct lif_rows_params {
+    int32_t  R, V;               /* rows (may be 0) and logits of a row (>= 1)      */
+    int32_t  k;                  /* alternatives, or entries of a teacher's list    */
+    int32_t  dtype;              /* LIF_F32, LIF_BF16 or LIF_F16                    */
+    int64_t  stride;             /* elements between rows of logits, >= V           */
+    int64_t  grad_stride;        /* elements between rows of grad, >= V             */
+    double   temperature;
+    uint32_t flags;              /* LIF_DISTILL_TAIL                                */
+    int32_t  reserved;           /* must be 0                                       */
+} lif_rows_params;
+
+size_t lif_rows_workspace_size(const lif_rows_params* p);
+int lif_token_logprobs(const void* logits, const int32_t* token, const lif_rows_params* p, float* logp,
+                       float* entropy, float* lse, float* top_logp, int32_t* top_idx, const float* grad_logp,
+                       const float* grad_entropy, void* grad, void* ws, size_t ws_bytes, lif_stream_t stream);
+int lif_distill_top(const void* logits, const float* teacher_logp, const int32_t* teacher_idx,
+                    const lif_rows_params* p, const float* weight, float* loss, void* grad, void* ws,
+                    size_t ws_bytes, lif_stream_t stream);
+
+/* --------------------------------------------------------------------- */
 /* Optional kernel timer (host-side state, off by default).  When enabled, */
 /* every kernel launched by this library is launched with a pair of HIP    */
 /* events that its own dispatch records (hipExtLaunchKernel), so each      */

@@ -4,10 +4,11 @@ Argument marshalling only: every step of the forward and backward passes runs
 in the library's HIP kernels.  PyTorch supplies device memory and the current
 HIP stream.  The entry points carry the C names of ``include/lif.h``
 (``lif_layer_forward``, ``lif_layer_forward_sequential``,
-``lif_layer_backward``, ``lif_merge_spikes``, ``lif_first_spike_ce``, the
-workspace-size queries, ``lif_version``); ``forward``/``backward``/``merge``
-are conveniences that allocate outputs and workspace as torch tensors and
-call them.
+``lif_layer_backward``, ``lif_merge_spikes``, ``lif_first_spike_ce``,
+``lif_gated_scan``, ``lif_token_logprobs``, ``lif_distill_top``, the
+workspace-size queries, ``lif_version``); ``forward``/``backward``/``merge``/
+``gated_scan``/``token_logprobs``/``distill_top`` are conveniences that
+allocate outputs and workspace as torch tensors and call them.
 
 Importing this module does not touch the GPU.  Loading the library fails
 loudly (``LibraryMissing``) if ``liblif.so`` has not been built: there is no
@@ -15,6 +16,7 @@ fallback implementation.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -55,8 +57,17 @@ EXPORTED = ["lif_version", "lif_layer_forward_workspace_size", "lif_layer_forwar
             "lif_layer_backward_delayed_workspace_size", "lif_layer_backward_delayed",
             "lif_spike_count_reg_delayed_workspace_size", "lif_spike_count_reg_delayed",
             "lif_spike_count_reg_delayed_backward",
-            "lif_add", "lif_softplus", "lif_softplus_grad", "lif_timer_enable", "lif_timer_read"]
+            "lif_add", "lif_softplus", "lif_softplus_grad",
+            "lif_gated_scan_workspace_size", "lif_gated_scan", "lif_gated_scan_backward", "lif_gated_step",
+            "lif_rows_workspace_size", "lif_token_logprobs", "lif_distill_top",
+            "lif_timer_enable", "lif_timer_read"]
 LIF_LI_MAX_CLASSES = 64
+LIF_F32, LIF_BF16, LIF_F16 = 0, 1, 2
+LIF_GATED_MARK = 64
+LIF_GATED_COUPLED = 1
+LIF_TOP_MAX = 128
+LIF_DISTILL_TAIL = 1
+LIF_DISTILL_TAIL_MIN = 2.0 ** -20
 
 
 class LibraryMissing(RuntimeError):
@@ -120,6 +131,19 @@ class LiParams:
 class lif_adam_params(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double)]
+
+
+class lif_gated_params(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("reserved", ctypes.c_int32), ("x_batch", ctypes.c_int64),
+                ("x_time", ctypes.c_int64), ("f_batch", ctypes.c_int64), ("f_time", ctypes.c_int64),
+                ("g_batch", ctypes.c_int64), ("g_time", ctypes.c_int64)]
+
+
+class lif_rows_params(ctypes.Structure):
+    _fields_ = [("R", ctypes.c_int32), ("V", ctypes.c_int32), ("k", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("stride", ctypes.c_int64), ("grad_stride", ctypes.c_int64), ("temperature", ctypes.c_double),
+                ("flags", ctypes.c_uint32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -212,6 +236,21 @@ def load(path: Optional[str] = None):
     lib.lif_softplus.argtypes = [_P, _P, _SZ, ctypes.c_double, _P]
     lib.lif_softplus_grad.restype = _I
     lib.lif_softplus_grad.argtypes = [_P, _P, _P, _SZ, ctypes.c_double, _P]
+    gp, rp = ctypes.POINTER(lif_gated_params), ctypes.POINTER(lif_rows_params)
+    lib.lif_gated_scan_workspace_size.restype = _SZ
+    lib.lif_gated_scan_workspace_size.argtypes = [gp]
+    lib.lif_gated_scan.restype = _I
+    lib.lif_gated_scan.argtypes = [_P, _P, _P, _P, gp, _P, _P, _P, _P, _SZ, _P]
+    lib.lif_gated_scan_backward.restype = _I
+    lib.lif_gated_scan_backward.argtypes = [_P, _P, _P, _P, _P, _P, gp, _P, _P, _P, _P, _SZ, _P]
+    lib.lif_gated_step.restype = _I
+    lib.lif_gated_step.argtypes = [_P, _P, _P, _P, _I, gp, _P, _P]
+    lib.lif_rows_workspace_size.restype = _SZ
+    lib.lif_rows_workspace_size.argtypes = [rp]
+    lib.lif_token_logprobs.restype = _I
+    lib.lif_token_logprobs.argtypes = [_P, _P, rp, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
+    lib.lif_distill_top.restype = _I
+    lib.lif_distill_top.argtypes = [_P, _P, _P, rp, _P, _P, _P, _P, _SZ, _P]
     lib.lif_timer_enable.restype = None
     lib.lif_timer_enable.argtypes = [_I]
     lib.lif_timer_read.restype = _I
@@ -351,6 +390,34 @@ def lif_softplus(*args) -> int:
 
 def lif_softplus_grad(*args) -> int:
     return load().lif_softplus_grad(*args)
+
+
+def lif_gated_scan_workspace_size(p: lif_gated_params) -> int:
+    return load().lif_gated_scan_workspace_size(ctypes.byref(p))
+
+
+def lif_gated_scan(*args) -> int:
+    return load().lif_gated_scan(*args)
+
+
+def lif_gated_scan_backward(*args) -> int:
+    return load().lif_gated_scan_backward(*args)
+
+
+def lif_gated_step(*args) -> int:
+    return load().lif_gated_step(*args)
+
+
+def lif_rows_workspace_size(p: lif_rows_params) -> int:
+    return load().lif_rows_workspace_size(ctypes.byref(p))
+
+
+def lif_token_logprobs(*args) -> int:
+    return load().lif_token_logprobs(*args)
+
+
+def lif_distill_top(*args) -> int:
+    return load().lif_distill_top(*args)
 
 
 def lif_timer_enable(on: bool) -> None:
@@ -754,3 +821,223 @@ def softplus_grad(x, grad_d, beta: float, stream=None):
     _check("lif_softplus_grad", lif_softplus_grad(_ptr(x), _ptr(grad_d), _ptr(gx), x.numel(), float(beta),
                                                   _stream(stream)))
     return gx
+
+
+# ---------------------------------------------------------------------------
+# sequences of binned input and rows of logits
+# ---------------------------------------------------------------------------
+
+_DTYPES = None
+
+
+def _dtype_code(name, t):
+    global _DTYPES
+    torch = _torch()
+    if _DTYPES is None:
+        _DTYPES = {torch.float32: LIF_F32, torch.bfloat16: LIF_BF16, torch.float16: LIF_F16}
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _on(dev, stream):
+    """The context that an operator's buffers and launches belong to: the
+    inputs' GPU, and `stream` when one is given (memory is then taken for that
+    stream, which has to wait for the inputs)."""
+    torch = _torch()
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    if dev.index is not None and dev.index != torch.cuda.current_device():
+        return torch.cuda.device(dev)
+    return contextlib.nullcontext()
+
+
+def _expect(name, t, shape, dtype, dev):
+    """A contiguous device tensor of this shape and type (None stays None)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} on {dev}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.contiguous()
+
+
+def _rows_of(name, t, shape, dtype, dev):
+    """A device tensor of this shape and type whose last axis is contiguous
+    (a copy of one that is not)."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} on {dev}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
+
+
+def _workspace(need, ws, dev):
+    """(pointer, bytes, the tensor that holds them) of a workspace."""
+    if need == 0:
+        return None, 0, None
+    if ws is None or ws.numel() * ws.element_size() < need or ws.device != dev:
+        ws = _torch().empty(need, dtype=_torch().uint8, device=dev)
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
+
+
+@dataclass
+class GatedOut:
+    h: "object"              # [B, T, D], the inputs' type; None when not asked for
+    h_last: "object"         # float32 [B, D]
+    marks: "object" = None   # float32 [B, ceil(T / 64), D]: the states that the backward pass starts from
+
+
+def _gated_inputs(x, f, length):
+    if x.dim() != 3 or not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor [B, T, D]")
+    code = _dtype_code("x", x)
+    x = _rows_of("x", x, x.shape, x.dtype, x.device)
+    f = _rows_of("f", f, x.shape, x.dtype, x.device)
+    B, T, D = x.shape
+    return x, f, _expect("length", length, (B,), _torch().int32, x.device), code, B, T, D
+
+
+def gated_scan(x, f, length=None, h_first=None, coupled: bool = True, marks: bool = False, states: bool = True,
+               stream=None, ws=None) -> GatedOut:
+    """Run lif_gated_scan: a leaky integrator with the gate sigmoid(f) over
+    sequences x, f [B, T, D] (any batch and time strides), length int32 [B],
+    h_first float32 [B, D].  marks=True keeps what gated_scan_backward needs;
+    states=False returns the last state only."""
+    torch = _torch()
+    x, f, length, code, B, T, D = _gated_inputs(x, f, length)
+    dev = x.device
+    h_first = _expect("h_first", h_first, (B, D), torch.float32, dev)
+    p = lif_gated_params(B, T, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), x.stride(1), f.stride(0),
+                         f.stride(1), 0, 0)
+    with _on(dev, stream):
+        h = torch.empty((B, T, D), dtype=x.dtype, device=dev) if states else None
+        last = torch.empty((B, D), dtype=torch.float32, device=dev)
+        mk = torch.empty((B, -(-T // LIF_GATED_MARK), D), dtype=torch.float32, device=dev) if marks else None
+        wp, wn, ws = _workspace(lif_gated_scan_workspace_size(p), ws, dev)
+        rc = lif_gated_scan(x.data_ptr(), f.data_ptr(), _ptr(length), _ptr(h_first), ctypes.byref(p), _ptr(h),
+                            last.data_ptr(), _ptr(mk), wp, wn, _stream(stream))
+    _check("lif_gated_scan", rc)
+    return GatedOut(h, last, mk)
+
+
+def gated_scan_backward(x, f, marks, grad_h=None, grad_last=None, length=None, coupled: bool = True, stream=None,
+                        ws=None):
+    """Run lif_gated_scan_backward with the forward's inputs and its marks;
+    returns (grad_x, grad_f, grad_h_first)."""
+    torch = _torch()
+    x, f, length, code, B, T, D = _gated_inputs(x, f, length)
+    dev = x.device
+    marks = _expect("marks", marks, (B, -(-T // LIF_GATED_MARK), D), torch.float32, dev)
+    if marks is None:
+        raise ValueError("the backward pass needs the forward's marks (gated_scan with marks=True)")
+    if grad_h is not None:
+        grad_h = _rows_of("grad_h", grad_h, x.shape, x.dtype, dev)
+    grad_last = _expect("grad_last", grad_last, (B, D), torch.float32, dev)
+    p = lif_gated_params(B, T, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), x.stride(1), f.stride(0),
+                         f.stride(1), *((0, 0) if grad_h is None else grad_h.stride()[:2]))
+    with _on(dev, stream):
+        gx = torch.empty((B, T, D), dtype=x.dtype, device=dev)
+        gf = torch.empty((B, T, D), dtype=x.dtype, device=dev)
+        g0 = torch.empty((B, D), dtype=torch.float32, device=dev)
+        wp, wn, ws = _workspace(lif_gated_scan_workspace_size(p), ws, dev)
+        rc = lif_gated_scan_backward(x.data_ptr(), f.data_ptr(), _ptr(length), marks.data_ptr(), _ptr(grad_h),
+                                     _ptr(grad_last), ctypes.byref(p), gx.data_ptr(), gf.data_ptr(), g0.data_ptr(),
+                                     wp, wn, _stream(stream))
+    _check("lif_gated_scan_backward", rc)
+    return gx, gf, g0
+
+
+def gated_step(x, f, state, slot=None, coupled: bool = True, stream=None):
+    """Run lif_gated_step: one step of B streams, x and f [B, D]; their states
+    are rows slot (int32 [B], distinct; None: rows 0 .. B - 1) of state
+    (float32 [n_slots, D]), updated in place.  Returns h [B, D]."""
+    torch = _torch()
+    if x.dim() != 2 or not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor [B, D]")
+    code, dev = _dtype_code("x", x), x.device
+    x = _rows_of("x", x, x.shape, x.dtype, dev)
+    f = _rows_of("f", f, x.shape, x.dtype, dev)
+    B, D = x.shape
+    if state.dim() != 2 or state.shape[1] != D or state.dtype != torch.float32 or state.device != dev or \
+            not state.is_contiguous():
+        raise ValueError(f"state must be a contiguous float32 tensor [n_slots, {D}] on {dev}")
+    slot = _expect("slot", slot, (B,), torch.int32, dev)
+    p = lif_gated_params(B, 1, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), 0, f.stride(0), 0, 0, 0)
+    with _on(dev, stream):
+        h = torch.empty((B, D), dtype=x.dtype, device=dev)
+        rc = lif_gated_step(x.data_ptr(), f.data_ptr(), _ptr(slot), state.data_ptr(), state.shape[0], ctypes.byref(p),
+                            h.data_ptr(), _stream(stream))
+    _check("lif_gated_step", rc)
+    return h
+
+
+@dataclass
+class LogprobOut:
+    logp: "object"               # float32 [R] log probability of the given token (0 where there is none)
+    entropy: "object"            # float32 [R]
+    lse: "object"                # float32 [R]
+    top_logp: "object" = None    # float32 [R, k], largest first
+    top_idx: "object" = None     # int32 [R, k]
+    grad: "object" = None        # [R, V] of the logits' type
+
+
+def _row_params(logits, k, temperature, flags):
+    if logits.dim() != 2 or not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor [R, V]")
+    code = _dtype_code("logits", logits)
+    R, V = logits.shape
+    if (V > 1 and logits.stride(1) != 1) or (R > 1 and logits.stride(0) < V):
+        logits = logits.contiguous()
+    return logits, lif_rows_params(R, V, int(k), code, logits.stride(0) if R > 1 else V, V, float(temperature), flags,
+                                   0), R, V
+
+
+def token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 1.0, grad_logp=None, grad_entropy=None,
+                   stream=None, ws=None) -> LogprobOut:
+    """Run lif_token_logprobs on logits [R, V] (rows contiguous, any row
+    stride): log probabilities of tokens (int32 [R]; outside [0, V): none),
+    entropies, the k likeliest alternatives, and, when grad_logp or
+    grad_entropy (float32 [R]) is given, the gradient to the logits."""
+    torch = _torch()
+    logits, p, R, V = _row_params(logits, k, temperature, 0)
+    dev = logits.device
+    tokens = _expect("tokens", tokens, (R,), torch.int32, dev)
+    grad_logp = _expect("grad_logp", grad_logp, (R,), torch.float32, dev)
+    grad_entropy = _expect("grad_entropy", grad_entropy, (R,), torch.float32, dev)
+    with _on(dev, stream):
+        logp, ent, lse = torch.empty((3, R), dtype=torch.float32, device=dev).unbind(0)
+        tv = ti = grad = None
+        if k > 0:
+            tv = torch.empty((R, k), dtype=torch.float32, device=dev)
+            ti = torch.empty((R, k), dtype=torch.int32, device=dev)
+        if grad_logp is not None or grad_entropy is not None:
+            grad = torch.empty((R, V), dtype=logits.dtype, device=dev)
+        wp, wn, ws = _workspace(lif_rows_workspace_size(p), ws, dev)
+        rc = lif_token_logprobs(logits.data_ptr(), _ptr(tokens), ctypes.byref(p), logp.data_ptr(), ent.data_ptr(),
+                                lse.data_ptr(), _ptr(tv), _ptr(ti), _ptr(grad_logp), _ptr(grad_entropy), _ptr(grad),
+                                wp, wn, _stream(stream))
+    _check("lif_token_logprobs", rc)
+    return LogprobOut(logp, ent, lse, tv, ti, grad)
+
+
+def distill_top(logits, teacher_logp, teacher_idx, temperature: float = 1.0, tail: bool = False, weight=None,
+                want_grad: bool = True, stream=None, ws=None):
+    """Run lif_distill_top on a student's logits [R, V] and a teacher's list
+    (float32 and int32 [R, k]); returns (loss float32 [R], grad [R, V] of the
+    logits' type or None), the gradient of sum_r weight_r loss_r."""
+    torch = _torch()
+    if teacher_idx.dim() != 2:
+        raise ValueError("teacher_idx must be [R, k]")
+    logits, p, R, V = _row_params(logits, teacher_idx.shape[1], temperature, LIF_DISTILL_TAIL if tail else 0)
+    dev = logits.device
+    teacher_logp = _expect("teacher_logp", teacher_logp, (R, p.k), torch.float32, dev)
+    teacher_idx = _expect("teacher_idx", teacher_idx, (R, p.k), torch.int32, dev)
+    weight = _expect("weight", weight, (R,), torch.float32, dev)
+    with _on(dev, stream):
+        loss = torch.empty(R, dtype=torch.float32, device=dev)
+        grad = torch.empty((R, V), dtype=logits.dtype, device=dev) if want_grad else None
+        wp, wn, ws = _workspace(lif_rows_workspace_size(p), ws, dev)
+        rc = lif_distill_top(logits.data_ptr(), teacher_logp.data_ptr(), teacher_idx.data_ptr(), ctypes.byref(p),
+                             _ptr(weight), loss.data_ptr(), _ptr(grad), wp, wn, _stream(stream))
+    _check("lif_distill_top", rc)
+    return loss, grad

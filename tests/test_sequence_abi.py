@@ -1,0 +1,123 @@
+"""Host-side refusals of the sequence and answer operators (no GPU needed):
+argument errors are found before anything is launched."""
+import ctypes
+
+import pytest
+
+import paper_2603_13283_amd as L
+
+F = ctypes.c_void_p(0x1000)      # never dereferenced: validation fails first
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return L.load()
+
+
+def _gp(**kw):
+    d = dict(B=2, T=10, D=8, dtype=0, flags=1, reserved=0, x_batch=80, x_time=8, f_batch=80, f_time=8, g_batch=80,
+             g_time=8)
+    d.update(kw)
+    return L.lif_gated_params(*(d[k] for k, _ in L.lif_gated_params._fields_))
+
+
+GATED_BAD = [(dict(B=-1), L.LIF_ERR_ARG), (dict(T=-1), L.LIF_ERR_ARG), (dict(D=0), L.LIF_ERR_ARG),
+             (dict(dtype=3), L.LIF_ERR_ARG), (dict(dtype=-1), L.LIF_ERR_ARG), (dict(flags=2), L.LIF_ERR_ARG),
+             (dict(reserved=1), L.LIF_ERR_ARG), (dict(x_time=-8), L.LIF_ERR_ARG), (dict(g_batch=-1), L.LIF_ERR_ARG),
+             (dict(B=1 << 16, D=1 << 15), L.LIF_ERR_SIZE),
+             (dict(B=1 << 10, D=1 << 20, T=1 << 18), L.LIF_ERR_SIZE)]
+
+
+@pytest.mark.parametrize("kw,code", GATED_BAD)
+def test_gated_sizes(lib, kw, code):
+    p = _gp(**kw)
+    ref = ctypes.byref(p)
+    assert L.lif_gated_scan(F, F, None, None, ref, F, F, F, F, 1 << 40, None) == code
+    assert L.lif_gated_scan_backward(F, F, None, F, F, F, ref, F, F, F, F, 1 << 40, None) == code
+    assert L.lif_gated_step(F, F, None, F, 1 << 30, ref, F, None) in (code, L.LIF_ERR_ARG)
+    assert L.lif_gated_scan_workspace_size(p) == 0
+
+
+def test_gated_pointers(lib):
+    p = ctypes.byref(_gp())
+    ok = 1 << 40
+    assert L.lif_gated_scan(F, F, None, None, None, F, F, F, F, ok, None) == L.LIF_ERR_ARG
+    assert L.lif_gated_scan(None, F, None, None, p, F, F, F, F, ok, None) == L.LIF_ERR_ARG
+    assert L.lif_gated_scan(F, None, None, None, p, F, F, F, F, ok, None) == L.LIF_ERR_ARG
+    assert L.lif_gated_scan(F, F, None, None, p, None, None, None, F, ok, None) == L.LIF_ERR_ARG
+    for i in (0, 1, 3, 7, 8):                     # x, f, marks, grad_x, grad_f
+        a = [F, F, None, F, F, F, p, F, F, F, F, ok, None]
+        a[i] = None
+        assert L.lif_gated_scan_backward(*a) == L.LIF_ERR_ARG
+    one = ctypes.byref(_gp(T=1))
+    assert L.lif_gated_step(F, F, F, F, 8, p, F, None) == L.LIF_ERR_ARG           # T is not 1
+    assert L.lif_gated_step(F, F, None, F, 1, one, F, None) == L.LIF_ERR_ARG      # fewer states than streams
+    assert L.lif_gated_step(F, F, F, F, -1, one, F, None) == L.LIF_ERR_ARG
+    for i in (0, 1, 3, 6):                        # x, f, state, h
+        a = [F, F, F, F, 8, one, F, None]
+        a[i] = None
+        assert L.lif_gated_step(*a) == L.LIF_ERR_ARG
+
+
+def test_gated_workspace(lib):
+    """A long sequence of few channels is shared out over workgroups and needs
+    a workspace; too small a one is refused."""
+    p = _gp(B=1, T=60000, D=64, x_batch=0, f_batch=0, g_batch=0)
+    need = L.lif_gated_scan_workspace_size(p)
+    if need:
+        ref = ctypes.byref(p)
+        assert L.lif_gated_scan(F, F, None, None, ref, F, F, F, F, need - 1, None) == L.LIF_ERR_WORKSPACE
+        assert L.lif_gated_scan(F, F, None, None, ref, F, F, F, None, 0, None) == L.LIF_ERR_ARG
+        assert L.lif_gated_scan_backward(F, F, None, F, F, F, ref, F, F, F, F, need - 1, None) == L.LIF_ERR_WORKSPACE
+    # nothing to do: no samples
+    assert L.lif_gated_scan(None, None, None, None, ctypes.byref(_gp(B=0)), F, F, F, None, 0, None) == L.LIF_OK
+
+
+def _rp(**kw):
+    d = dict(R=4, V=100, k=5, dtype=0, stride=100, grad_stride=100, temperature=1.0, flags=0, reserved=0)
+    d.update(kw)
+    return L.lif_rows_params(*(d[k] for k, _ in L.lif_rows_params._fields_))
+
+
+ROWS_BAD = [(dict(R=-1), L.LIF_ERR_ARG), (dict(V=0), L.LIF_ERR_ARG), (dict(k=-1), L.LIF_ERR_ARG),
+            (dict(k=101), L.LIF_ERR_ARG), (dict(dtype=7), L.LIF_ERR_ARG), (dict(stride=99), L.LIF_ERR_ARG),
+            (dict(grad_stride=99), L.LIF_ERR_ARG), (dict(temperature=0.0), L.LIF_ERR_ARG),
+            (dict(temperature=-1.0), L.LIF_ERR_ARG), (dict(temperature=float("nan")), L.LIF_ERR_ARG),
+            (dict(temperature=float("inf")), L.LIF_ERR_ARG), (dict(temperature=1e-9), L.LIF_ERR_ARG),
+            (dict(flags=2), L.LIF_ERR_ARG), (dict(reserved=1), L.LIF_ERR_ARG),
+            (dict(V=1000, stride=1000, grad_stride=1000, k=129), L.LIF_ERR_SIZE)]
+
+
+@pytest.mark.parametrize("kw,code", ROWS_BAD)
+def test_rows_sizes(lib, kw, code):
+    p = _rp(**kw)
+    ref = ctypes.byref(p)
+    assert L.lif_token_logprobs(F, F, ref, F, F, F, F, F, F, F, F, F, 1 << 40, None) == code
+    assert L.lif_distill_top(F, F, F, ref, F, F, F, F, 1 << 40, None) == code
+    assert L.lif_rows_workspace_size(p) == 0
+
+
+def test_rows_pointers(lib):
+    p, ok = ctypes.byref(_rp()), 1 << 40
+    assert L.lif_token_logprobs(F, F, None, F, F, F, F, F, F, F, F, F, ok, None) == L.LIF_ERR_ARG
+    assert L.lif_token_logprobs(None, F, p, F, F, F, F, F, F, F, F, F, ok, None) == L.LIF_ERR_ARG
+    assert L.lif_token_logprobs(F, F, p, F, F, F, F, None, F, F, F, F, ok, None) == L.LIF_ERR_ARG
+    assert L.lif_token_logprobs(F, F, p, F, F, F, None, F, F, F, F, F, ok, None) == L.LIF_ERR_ARG
+    tail = ctypes.byref(_rp(flags=L.LIF_DISTILL_TAIL))    # a flag of the other call
+    assert L.lif_token_logprobs(F, F, tail, F, F, F, F, F, F, F, F, F, ok, None) == L.LIF_ERR_ARG
+    for i in (0, 1, 2):                           # logits, teacher_logp, teacher_idx
+        a = [F, F, F, p, F, F, F, F, ok, None]
+        a[i] = None
+        assert L.lif_distill_top(*a) == L.LIF_ERR_ARG
+    assert L.lif_distill_top(F, F, F, p, F, None, None, F, ok, None) == L.LIF_ERR_ARG     # nothing asked for
+    assert L.lif_distill_top(None, None, None, ctypes.byref(_rp(R=0)), None, F, F, None, 0, None) == L.LIF_OK
+
+
+def test_rows_workspace(lib):
+    p = _rp(R=1, V=200000, stride=200000, grad_stride=200000)
+    need = L.lif_rows_workspace_size(p)
+    if need:
+        ref = ctypes.byref(p)
+        assert L.lif_token_logprobs(F, F, ref, F, F, F, F, F, F, F, F, F, need - 1, None) == L.LIF_ERR_WORKSPACE
+        assert L.lif_token_logprobs(F, F, ref, F, F, F, F, F, F, F, F, None, 0, None) == L.LIF_ERR_ARG
+        assert L.lif_distill_top(F, F, F, ref, F, F, F, F, need - 1, None) == L.LIF_ERR_WORKSPACE
