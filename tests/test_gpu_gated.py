@@ -147,6 +147,7 @@ def test_long_sequences_of_few_channels(env, split):
     n = np.array([T - 17] + [T // 3] * (B - 1))
     run(env, x, f, "f32", n=n, h0=h0, gh=gh, gl=gl, label="long")
     run(env, x, f, "f32", gh=gh, coupled=False, label="long, no first state")
+    run(env, x, f, "f32", gl=gl, label="long, a gradient of the last state only")
 
 
 def test_strides_offsets_and_expanded_inputs(env):
