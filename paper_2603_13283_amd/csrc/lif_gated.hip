@@ -26,6 +26,9 @@ namespace {
 
 constexpr int kTS = 8;            // steps of a wave in a tile
 constexpr int kMaxWaves = 8;      // waves of a workgroup
+constexpr int kSplitColumns = 256;   // fewer columns than this share out the time axis,
+constexpr int kSplitGroups = 1024;   // over about this many workgroups,
+constexpr int kSplitBlocks = 2;      // each with at least this many blocks of LIF_GATED_MARK steps
 static_assert(LIF_GATED_MARK % kTS == 0 && kTS * kMaxWaves == LIF_GATED_MARK,
               "a mark is the state entering some wave's first step, and a backward tile starts at one");
 
@@ -46,8 +49,13 @@ __device__ __forceinline__ int steps_of(const int32_t* __restrict__ length, int 
     return length ? min(max(length[b], 0), T) : T;
 }
 
-// What a launch works on: `groups` = B * D / CPL lanes in all, `S` segments of
-// `seg_len` steps (a multiple of LIF_GATED_MARK) of the time axis.
+// The wave's index in its workgroup, in a scalar register.
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+
+// What a launch works on: `groups` = B * ceil(D / CPL) lanes in all, `S`
+// segments of `seg_len` steps (a multiple of LIF_GATED_MARK) of the time axis.
+// Where CPL does not divide D, a sample's last group starts at D - CPL: the
+// channels that it shares with the group before get the same bits twice.
 struct Geometry {
     int B, T, D, groups, per_sample, S, seg_len;
     int64_t x_batch, x_time, f_batch, f_time, g_batch, g_time;
@@ -63,14 +71,14 @@ struct Place {
 };
 
 template <int CPL>
-__device__ __forceinline__ Place place_of(const Geometry& g, const int32_t* __restrict__ length, int lane)
+__device__ __forceinline__ Place place_of(const Geometry& g, const int32_t* __restrict__ length, int column, int lane)
 {
     Place p;
-    const int64_t at = (int64_t)blockIdx.x * kWave + lane;
+    const int64_t at = (int64_t)column * kWave + lane;
     p.live = at < g.groups;
     const int cg = p.live ? (int)at : g.groups - 1;
     p.b = cg / g.per_sample;
-    p.d = (cg - p.b * g.per_sample) * CPL;
+    p.d = min((cg - p.b * g.per_sample) * CPL, g.D - CPL);
     p.c = (int64_t)p.b * g.D + p.d;
     p.n = steps_of(length, p.b, g.T);
     p.n_min = p.n_max = p.n;
@@ -84,87 +92,153 @@ __device__ __forceinline__ Place place_of(const Geometry& g, const int32_t* __re
 }
 
 // The raw elements of a wave's TS steps of two or three inputs.
-template <typename E, int CPL, int N>
+template <typename E, int CPL, int TS, int N>
 struct Raw {
-    E v[N][kTS][CPL];
+    E v[N][TS][CPL];
 };
 
-// Loads steps t .. t + TS - 1 (those below the lane's n) of one input.
-template <typename E, int CPL>
-__device__ __forceinline__ void load_steps(E (&v)[kTS][CPL], const E* __restrict__ base, int64_t stride, int t,
+// A row stride that the compiler takes for a new value each time: otherwise it
+// keeps the multiples of every stride for all TS steps in scalar registers
+// across the loops below, and spills them.
+__device__ __forceinline__ int64_t fresh(int64_t stride)
+{
+    asm volatile("" : "+s"(stride));
+    return stride;
+}
+
+// Loads steps t .. t + TS - 1 of one input; steps at or past the lane's n get
+// `rest`.  With f = +infinity (a = 1, 1 - a = 0 exactly), x = 0 and grad_h = 0
+// there, such a step is the identity in every composition below.
+template <typename E, int CPL, int TS>
+__device__ __forceinline__ void load_steps(E (&v)[TS][CPL], const E* __restrict__ base, int64_t stride, int t,
+                                           const Place& p, float rest)
+{
+    stride = fresh(stride);
+    const E* at = base + (int64_t)t * stride;
+    if (t + TS <= p.n_min) {
+#pragma unroll
+        for (int i = 0; i < TS; ++i, at += stride) load_elems<E, CPL>(at, v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < TS; ++i, at += stride) {
+#pragma unroll
+            for (int k = 0; k < CPL; ++k) v[i][k] = from_f32<E>(rest);
+            if (t + i < p.n) load_elems<E, CPL>(at, v[i]);
+        }
+    }
+}
+
+// The same for x or grad_h; 0 where there is none.
+template <typename E, int CPL, int TS>
+__device__ __forceinline__ void load_input(E (&v)[TS][CPL], const E* in, int64_t at, int64_t stride, int t,
                                            const Place& p)
 {
-    const E* at = base + (int64_t)t * stride;
-    if (t + kTS <= p.n_min) {
+    if (in) {
+        load_steps<E, CPL, TS>(v, in + at, stride, t, p, 0.0f);
+    } else {
 #pragma unroll
-        for (int i = 0; i < kTS; ++i) load_elems<E, CPL>(at + i * stride, v[i]);
-    } else if (t < p.n_max) {
+        for (int i = 0; i < TS; ++i)
 #pragma unroll
-        for (int i = 0; i < kTS; ++i)
-            if (t + i < p.n) load_elems<E, CPL>(at + i * stride, v[i]);
+            for (int k = 0; k < CPL; ++k) v[i][k] = from_f32<E>(0.0f);
     }
 }
 
-// The state that enters a segment: h_first (or grad_last) carried through the
-// maps of the segments before it in the direction of the walk, `count` of
-// them from `from` on, one every `step`.
-template <int CPL>
-__device__ __forceinline__ void fold_segments(float (&c)[CPL], const float2* __restrict__ maps, int64_t chans,
-                                              int64_t at, int from, int count, int step)
+// A wave's TS steps of the forward recurrence: gates and inputs of the raw
+// elements, and the composed map.
+template <typename E, int CPL, int TS, bool COUPLED>
+__device__ __forceinline__ void compose_steps(const Raw<E, CPL, TS, 2>& r, float (&a)[TS][CPL], float (&u)[TS][CPL],
+                                              float (&A)[CPL], float (&H)[CPL])
 {
-#pragma unroll 4
-    for (int s = 0; s < count; ++s) {
-        const float2* q = maps + (int64_t)(from + s * step) * chans + at;
 #pragma unroll
-        for (int k = 0; k < CPL; ++k) c[k] = fmaf(q[k].x, c[k], q[k].y);
+    for (int k = 0; k < CPL; ++k) A[k] = 1.0f, H[k] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < TS; ++i)
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) {
+            float na;
+            gate(to_f32(r.v[0][i][k]), a[i][k], na);
+            const float v = to_f32(r.v[1][i][k]);
+            u[i][k] = COUPLED ? na * v : v;
+            H[k] = fmaf(a[i][k], H[k], u[i][k]);
+            A[k] *= a[i][k];
+        }
+}
+
+// Runs a wave's steps from the state `h` that enters them, and stores them.
+template <typename E, int CPL, int TS>
+__device__ __forceinline__ void run_steps(float (&h)[CPL], const float (&a)[TS][CPL], const float (&u)[TS][CPL], int t,
+                                          const Place& p, const Geometry& g, E* __restrict__ out,
+                                          float* __restrict__ mk)
+{
+    if (!p.live) return;
+    if (mk && t % LIF_GATED_MARK == 0 && t < g.T)
+        store_elems<float, CPL>(mk + (int64_t)(t / LIF_GATED_MARK) * g.D, h);
+    if (!out) return;
+    const int64_t row = fresh(g.D);
+    E* at = out + t * row;
+    const bool full = t + TS <= p.n_min;
+#pragma unroll
+    for (int i = 0; i < TS; ++i, at += row) {
+        E o[CPL];
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) {
+            h[k] = fmaf(a[i][k], h[k], u[i][k]);
+            o[k] = from_f32<E>(h[k]);
+        }
+        if (!full) {
+            if (t + i >= g.T) return;
+#pragma unroll
+            for (int k = 0; k < CPL; ++k) o[k] = t + i < p.n ? o[k] : from_f32<E>(0.0f);
+        }
+        store_elems<E, CPL>(at, o);
     }
 }
 
-// Composed maps of whole segments, where the time axis is shared out over
-// workgroups: segment blockIdx.y's map of h (forward: inputs f and x) or of mu
-// (REVERSE: inputs f and grad_h).  Each wave takes a contiguous part of the
-// segment with no barrier; the waves' maps meet once at the end.
+// Where there are few channels, the time axis is cut into segments that
+// workgroups share out: a first launch composes each segment's map, a second
+// one works on all segments at once, each from the state that the maps before
+// it carry to it.  x and f (backward: f and grad_h) are then read twice, the
+// second time in part from the cache behind the L2s.
+
+// The composed map of segment blockIdx.y (plus one, backward): of h from f and
+// x, or (REVERSE) of mu from f and grad_h.  Each wave takes a contiguous part
+// of the segment without a barrier; the waves' maps meet once at the end.
 template <typename E, int CPL, bool COUPLED, bool REVERSE>
 __global__ __launch_bounds__(kMaxWaves* kWave) void k_segment_maps(const E* __restrict__ in, const E* __restrict__ f,
                                                                    const int32_t* __restrict__ length, Geometry g,
                                                                    float2* __restrict__ maps)
 {
+    constexpr int TS = kTS;
     __shared__ float2 sh[kMaxWaves][CPL][kWave];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+    const int lane = threadIdx.x & 63, w = wave_index();
     const int seg = REVERSE ? blockIdx.y + 1 : blockIdx.y;       // the walk's last segment needs no map
-    const Place p = place_of<CPL>(g, length, lane);
+    const Place p = place_of<CPL>(g, length, blockIdx.x, lane);
     const int64_t in_batch = REVERSE ? g.g_batch : g.x_batch, in_time = REVERSE ? g.g_time : g.x_time;
-    const E* in0 = in ? in + p.b * in_batch + p.d : nullptr;     // no grad_h: 0
-    const E* f0 = f + p.b * g.f_batch + p.d;
-    const int part = g.seg_len / nw;                             // a multiple of TS
+    const int part = g.seg_len / kMaxWaves;                      // a multiple of TS
     const int t0 = seg * g.seg_len + w * part;
-    const int t1 = min(t0 + part, g.T);
+    const int blocks = (min(t0 + part, p.n_max) - t0 + TS - 1) / TS;
     float A[CPL], H[CPL];
 #pragma unroll
     for (int k = 0; k < CPL; ++k) A[k] = 1.0f, H[k] = 0.0f;
-    const int blocks = t1 > t0 ? (min(t1, p.n_max) - t0 + kTS - 1) / kTS : 0;
-    Raw<E, CPL, 2> cur, nxt;
-    auto at = [&](int j) { return REVERSE ? t0 + (blocks - 1 - j) * kTS : t0 + j * kTS; };
-    auto load = [&](Raw<E, CPL, 2>& r, int j) {
-        load_steps<E, CPL>(r.v[0], f0, g.f_time, at(j), p);
-        if (in0) load_steps<E, CPL>(r.v[1], in0, in_time, at(j), p);
+    Raw<E, CPL, TS, 2> cur, nxt;
+    auto load = [&](Raw<E, CPL, TS, 2>& r, int j) {
+        const int t = t0 + (REVERSE ? blocks - 1 - j : j) * TS;
+        load_steps<E, CPL, TS>(r.v[0], f + p.b * g.f_batch + p.d, g.f_time, t, p, INFINITY);
+        load_input<E, CPL, TS>(r.v[1], in, p.b * in_batch + p.d, in_time, t, p);
     };
     if (blocks > 0) load(cur, 0);
     for (int j = 0; j < blocks; ++j) {
         if (j + 1 < blocks) load(nxt, j + 1);
-        const int t = at(j);
 #pragma unroll
-        for (int q = 0; q < kTS; ++q) {
-            const int i = REVERSE ? kTS - 1 - q : q;
-            if (t + i < p.n) {
+        for (int q = 0; q < TS; ++q) {
+            const int i = REVERSE ? TS - 1 - q : q;
 #pragma unroll
-                for (int k = 0; k < CPL; ++k) {
-                    float a, na;
-                    gate(to_f32(cur.v[0][i][k]), a, na);
-                    const float v = in0 ? to_f32(cur.v[1][i][k]) : 0.0f;
-                    H[k] = REVERSE ? a * (H[k] + v) : fmaf(a, H[k], COUPLED ? na * v : v);
-                    A[k] *= a;
-                }
+            for (int k = 0; k < CPL; ++k) {
+                float a, na;
+                gate(to_f32(cur.v[0][i][k]), a, na);
+                const float v = to_f32(cur.v[1][i][k]);
+                H[k] = REVERSE ? a * (H[k] + v) : fmaf(a, H[k], COUPLED ? na * v : v);
+                A[k] *= a;
             }
         }
         cur = nxt;
@@ -176,16 +250,48 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_segment_maps(const E* __re
 #pragma unroll
         for (int k = 0; k < CPL; ++k) {
             float a = 1.0f, h = 0.0f;
-            for (int q = 0; q < nw; ++q) {
-                const float2 m = sh[REVERSE ? nw - 1 - q : q][k][lane];
+            for (int q = 0; q < kMaxWaves; ++q) {
+                const float2 m = sh[REVERSE ? kMaxWaves - 1 - q : q][k][lane];
                 h = fmaf(m.x, h, m.y);
                 a *= m.x;
             }
-            maps[(int64_t)seg * ((int64_t)g.B * g.D) + p.c + k] = make_float2(a, h);
+            maps[(int64_t)seg * g.B * g.D + p.c + k] = make_float2(a, h);
         }
     }
 }
 
+// c: the first state c carried through the maps of `count` segments, from
+// segment `from` on in direction `step`.  Each of the nw waves composes a part
+// of them, all its loads in flight at once, and the parts meet in LDS.
+template <int CPL>
+__device__ __forceinline__ void carry_to_segment(float (&c)[CPL], const float2* __restrict__ maps, int64_t chans,
+                                                 int64_t at, int from, int count, int step,
+                                                 float2 (*sh)[CPL][kWave], int lane, int w, int nw)
+{
+    if (count == 0) return;
+    float A[CPL], H[CPL];
+#pragma unroll
+    for (int k = 0; k < CPL; ++k) A[k] = 1.0f, H[k] = 0.0f;
+    const int q1 = count * (w + 1) / nw;
+#pragma unroll 8
+    for (int q = count * w / nw; q < q1; ++q) {
+        const float2* m = maps + (int64_t)(from + q * step) * chans + at;
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) {
+            H[k] = fmaf(m[k].x, H[k], m[k].y);
+            A[k] *= m[k].x;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < CPL; ++k) sh[w][k][lane] = make_float2(A[k], H[k]);
+    __syncthreads();
+    for (int q = 0; q < nw; ++q)
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) c[k] = fmaf(sh[q][k][lane].x, c[k], sh[q][k][lane].y);
+    __syncthreads();
+}
+
+// A workgroup walks its column of channels through its segment.
 template <typename E, int CPL, bool COUPLED>
 __global__ __launch_bounds__(kMaxWaves* kWave) void k_scan(const E* __restrict__ x, const E* __restrict__ f,
                                                            const int32_t* __restrict__ length,
@@ -193,53 +299,36 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_scan(const E* __restrict__
                                                            const float2* __restrict__ maps, E* __restrict__ h_out,
                                                            float* __restrict__ h_last, float* __restrict__ marks)
 {
+    constexpr int TS = kTS;
     __shared__ float2 sh[2][kMaxWaves][CPL][kWave];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
-    const int seg = blockIdx.y, tile = nw * kTS;
-    const int64_t chans = (int64_t)g.B * g.D;
-    const Place p = place_of<CPL>(g, length, lane);
+    const int lane = threadIdx.x & 63, w = wave_index(), nw = blockDim.x >> 6;
+    const int seg = blockIdx.y, tile = nw * TS;
     const int t0 = seg * g.seg_len, t1 = min(t0 + g.seg_len, g.T);
-    const E* x0 = x + p.b * g.x_batch + p.d;
-    const E* f0 = f + p.b * g.f_batch + p.d;
+    const Place p = place_of<CPL>(g, length, blockIdx.x, lane);
     E* out = h_out ? h_out + (int64_t)p.b * g.T * g.D + p.d : nullptr;
     const int nm = (g.T + LIF_GATED_MARK - 1) / LIF_GATED_MARK;
     float* mk = marks ? marks + (int64_t)p.b * nm * g.D + p.d : nullptr;
 
-    Raw<E, CPL, 2> cur, nxt;
-    auto load = [&](Raw<E, CPL, 2>& r, int t) {
-        load_steps<E, CPL>(r.v[0], f0, g.f_time, t, p);
-        load_steps<E, CPL>(r.v[1], x0, g.x_time, t, p);
+    Raw<E, CPL, TS, 2> cur, nxt;
+    auto load = [&](Raw<E, CPL, TS, 2>& r, int t) {
+        load_steps<E, CPL, TS>(r.v[0], f + p.b * g.f_batch + p.d, g.f_time, t, p, INFINITY);
+        load_steps<E, CPL, TS>(r.v[1], x + p.b * g.x_batch + p.d, g.x_time, t, p, 0.0f);
     };
-    if (t0 + w * kTS < t1) load(cur, t0 + w * kTS);
+    load(cur, t0 + w * TS);
 
     float c[CPL];                       // the state carried into the tile, the same in every wave
 #pragma unroll
     for (int k = 0; k < CPL; ++k) c[k] = h_first ? h_first[p.c + k] : 0.0f;
-    fold_segments<CPL>(c, maps, chans, p.c, 0, seg, 1);
+    carry_to_segment<CPL>(c, maps, (int64_t)g.B * g.D, p.c, 0, seg, 1, sh[0], lane, w, nw);
 
     int buf = 0;
     for (int tt = t0; tt < t1; tt += tile, buf ^= 1) {
-        const int t = tt + w * kTS;
-        float a[kTS][CPL], u[kTS][CPL], in[CPL];
+        const int t = tt + w * TS;
+        float a[TS][CPL], u[TS][CPL], in[CPL];
         if (tt < p.n_max) {
             if (tt + tile < t1) load(nxt, t + tile);
             float A[CPL], H[CPL];
-#pragma unroll
-            for (int k = 0; k < CPL; ++k) A[k] = 1.0f, H[k] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kTS; ++i) {
-                const bool on = t + i < p.n;
-#pragma unroll
-                for (int k = 0; k < CPL; ++k) {
-                    float s, ns;
-                    gate(to_f32(cur.v[0][i][k]), s, ns);
-                    const float v = to_f32(cur.v[1][i][k]);
-                    a[i][k] = on ? s : 1.0f;
-                    u[i][k] = on ? (COUPLED ? ns * v : v) : 0.0f;
-                    H[k] = fmaf(a[i][k], H[k], u[i][k]);
-                    A[k] *= a[i][k];
-                }
-            }
+            compose_steps<E, CPL, TS, COUPLED>(cur, a, u, A, H);
 #pragma unroll
             for (int k = 0; k < CPL; ++k) sh[buf][w][k][lane] = make_float2(A[k], H[k]);
             __syncthreads();
@@ -257,33 +346,95 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_scan(const E* __restrict__
             for (int k = 0; k < CPL; ++k) {
                 in[k] = c[k];
 #pragma unroll
-                for (int i = 0; i < kTS; ++i) a[i][k] = 1.0f, u[i][k] = 0.0f;
+                for (int i = 0; i < TS; ++i) a[i][k] = 1.0f, u[i][k] = 0.0f;
             }
         }
-        if (p.live) {
-            if (mk && t % LIF_GATED_MARK == 0 && t < g.T) store_elems<float, CPL>(mk + (int64_t)(t / LIF_GATED_MARK) * g.D, in);
-            if (out) {
-#pragma unroll
-                for (int i = 0; i < kTS; ++i) {
-                    E o[CPL];
-#pragma unroll
-                    for (int k = 0; k < CPL; ++k) {
-                        in[k] = fmaf(a[i][k], in[k], u[i][k]);
-                        o[k] = from_f32<E>(t + i < p.n ? in[k] : 0.0f);
-                    }
-                    if (t + i < t1) store_elems<E, CPL>(out + (int64_t)(t + i) * g.D, o);
-                }
-            }
-        }
+        run_steps<E, CPL, TS>(in, a, u, t, p, g, out, mk);
         cur = nxt;
     }
     if (h_last && seg == g.S - 1 && w == 0 && p.live) store_elems<float, CPL>(h_last + p.c, c);
 }
 
-// Backward: tiles of LIF_GATED_MARK steps from the last to the first.  The
-// states of a tile are recomputed from its mark, so h is not read; both
-// directions' maps meet in the same LDS exchange (their products A are the
-// same).
+// Backward, a wave's TS steps: the gates, the composed map of h (A, H) and of
+// mu (A, M; the products are the same).
+template <typename E, int CPL, int TS, bool COUPLED>
+__device__ __forceinline__ void compose_back(const Raw<E, CPL, TS, 3>& r, float (&a)[TS][CPL], float (&na)[TS][CPL],
+                                             float (&A)[CPL], float (&H)[CPL], float (&M)[CPL])
+{
+#pragma unroll
+    for (int k = 0; k < CPL; ++k) A[k] = 1.0f, H[k] = 0.0f, M[k] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < TS; ++i)
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) {
+            gate(to_f32(r.v[0][i][k]), a[i][k], na[i][k]);
+            const float v = to_f32(r.v[1][i][k]);
+            H[k] = fmaf(a[i][k], H[k], COUPLED ? na[i][k] * v : v);
+            A[k] *= a[i][k];
+        }
+#pragma unroll
+    for (int i = TS - 1; i >= 0; --i)
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) M[k] = a[i][k] * (M[k] + to_f32(r.v[2][i][k]));
+}
+
+// Runs a wave's steps from the entering state h upwards and from the adjoint
+// lam (mu of the last step) downwards, and stores the gradients.
+template <typename E, int CPL, int TS, bool COUPLED>
+__device__ __forceinline__ void run_back(const Raw<E, CPL, TS, 3>& r, float (&h)[CPL], float (&lam)[CPL],
+                                         const float (&a)[TS][CPL], const float (&na)[TS][CPL], int t, const Place& p,
+                                         const Geometry& g, E* __restrict__ grad_x, E* __restrict__ grad_f)
+{
+    float df[TS][CPL];                  // d h_t / d f_t
+#pragma unroll
+    for (int i = 0; i < TS; ++i)
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) {
+            const float v = to_f32(r.v[1][i][k]);
+            df[i][k] = (COUPLED ? h[k] - v : h[k]) * (a[i][k] * na[i][k]);
+            h[k] = fmaf(a[i][k], h[k], COUPLED ? na[i][k] * v : v);
+        }
+    if (!p.live) return;
+    const int64_t row = fresh(g.D);
+    const int64_t last = ((int64_t)p.b * g.T + t + TS - 1) * row + p.d;
+    E *to_x = grad_x + last, *to_f = grad_f + last;
+    const bool full = t + TS <= p.n_min;
+#pragma unroll
+    for (int i = TS - 1; i >= 0; --i, to_x -= row, to_f -= row) {
+        E ox[CPL], of[CPL];
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) {
+            lam[k] += to_f32(r.v[2][i][k]);
+            ox[k] = from_f32<E>(COUPLED ? lam[k] * na[i][k] : lam[k]);
+            of[k] = from_f32<E>(lam[k] * df[i][k]);
+            lam[k] *= a[i][k];
+        }
+        if (!full) {
+            if (t + i >= g.T) continue;
+#pragma unroll
+            for (int k = 0; k < CPL; ++k) {
+                ox[k] = t + i < p.n ? ox[k] : from_f32<E>(0.0f);
+                of[k] = t + i < p.n ? of[k] : from_f32<E>(0.0f);
+            }
+        }
+        store_elems<E, CPL>(to_x, ox);
+        store_elems<E, CPL>(to_f, of);
+    }
+}
+
+// The three inputs of a backward tile.
+template <typename E, int CPL, int TS>
+__device__ __forceinline__ void load_back(Raw<E, CPL, TS, 3>& r, const E* f, const E* x, const E* gh,
+                                          const Geometry& g, int t, const Place& p)
+{
+    load_steps<E, CPL, TS>(r.v[0], f + p.b * g.f_batch + p.d, g.f_time, t, p, INFINITY);
+    load_steps<E, CPL, TS>(r.v[1], x + p.b * g.x_batch + p.d, g.x_time, t, p, 0.0f);
+    load_input<E, CPL, TS>(r.v[2], gh, p.b * g.g_batch + p.d, g.g_time, t, p);
+}
+
+// Backward: tiles of LIF_GATED_MARK steps of the segment from the last to the
+// first.  The states of a tile are recomputed from its mark, so h is not read;
+// both directions' maps meet in the same LDS exchange.
 template <typename E, int CPL, bool COUPLED>
 __global__ __launch_bounds__(kMaxWaves* kWave) void k_back(const E* __restrict__ x, const E* __restrict__ f,
                                                            const int32_t* __restrict__ length,
@@ -293,76 +444,49 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_back(const E* __restrict__
                                                            const float2* __restrict__ maps, E* __restrict__ grad_x,
                                                            E* __restrict__ grad_f, float* __restrict__ grad_first)
 {
+    constexpr int TS = kTS, tile = LIF_GATED_MARK;
     __shared__ float sh[2][kMaxWaves][CPL][3][kWave];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    __shared__ float2 sh_maps[kMaxWaves][CPL][kWave];
+    const int lane = threadIdx.x & 63, w = wave_index();
     const int seg = blockIdx.y;
-    constexpr int tile = kMaxWaves * kTS;
-    const int64_t chans = (int64_t)g.B * g.D;
-    const Place p = place_of<CPL>(g, length, lane);
     const int t0 = seg * g.seg_len, t1 = min(t0 + g.seg_len, g.T);
-    const E* x0 = x + p.b * g.x_batch + p.d;
-    const E* f0 = f + p.b * g.f_batch + p.d;
-    const E* g0 = grad_h ? grad_h + p.b * g.g_batch + p.d : nullptr;
-    const int64_t row0 = (int64_t)p.b * g.T * g.D + p.d;
+    const Place p = place_of<CPL>(g, length, blockIdx.x, lane);
     const int nm = (g.T + LIF_GATED_MARK - 1) / LIF_GATED_MARK;
     const float* mk = marks + (int64_t)p.b * nm * g.D + p.d;
 
-    Raw<E, CPL, 3> cur, nxt;
+    Raw<E, CPL, TS, 3> cur, nxt;
     float h_cur[CPL], h_nxt[CPL];
-    auto load = [&](Raw<E, CPL, 3>& r, float (&h)[CPL], int tt) {
-        load_steps<E, CPL>(r.v[0], f0, g.f_time, tt + w * kTS, p);
-        load_steps<E, CPL>(r.v[1], x0, g.x_time, tt + w * kTS, p);
-        if (g0) load_steps<E, CPL>(r.v[2], g0, g.g_time, tt + w * kTS, p);
+    auto load = [&](Raw<E, CPL, TS, 3>& r, float (&h)[CPL], int tt) {
+        load_back<E, CPL, TS>(r, f, x, grad_h, g, tt + w * TS, p);
         load_elems<float, CPL>(mk + (int64_t)(tt / LIF_GATED_MARK) * g.D, h);
     };
-    int tt = t1 > t0 ? t0 + (t1 - t0 - 1) / tile * tile : t0 - tile;
+    int tt = t0 + (t1 - t0 + tile - 1) / tile * tile - tile;
     if (tt >= t0) load(cur, h_cur, tt);
 
     float mu[CPL];                      // the adjoint carried into the tile from the later side
 #pragma unroll
     for (int k = 0; k < CPL; ++k) mu[k] = grad_last ? grad_last[p.c + k] : 0.0f;
-    fold_segments<CPL>(mu, maps, chans, p.c, g.S - 1, g.S - 1 - seg, -1);
+    carry_to_segment<CPL>(mu, maps, (int64_t)g.B * g.D, p.c, g.S - 1, g.S - 1 - seg, -1, sh_maps, lane, w, kMaxWaves);
 
     int buf = 0;
     for (; tt >= t0; tt -= tile, buf ^= 1) {
-        const int t = tt + w * kTS;
+        const int t = tt + w * TS;
+        if (tt > t0) load(nxt, h_nxt, tt - tile);
         if (tt >= p.n_max) {            // past every lane's length
-            if (tt - tile >= t0) load(nxt, h_nxt, tt - tile);
-            if (p.live) {
-                E o[CPL];
+            const int64_t row = ((int64_t)p.b * g.T + t) * g.D + p.d;
+            E o[CPL];
 #pragma unroll
-                for (int k = 0; k < CPL; ++k) o[k] = from_f32<E>(0.0f);
+            for (int k = 0; k < CPL; ++k) o[k] = from_f32<E>(0.0f);
+            if (p.live)
 #pragma unroll
-                for (int i = 0; i < kTS; ++i)
-                    if (t + i < t1) {
-                        store_elems<E, CPL>(grad_x + row0 + (int64_t)(t + i) * g.D, o);
-                        store_elems<E, CPL>(grad_f + row0 + (int64_t)(t + i) * g.D, o);
+                for (int i = 0; i < TS; ++i)
+                    if (t + i < g.T) {
+                        store_elems<E, CPL>(grad_x + row + (int64_t)i * g.D, o);
+                        store_elems<E, CPL>(grad_f + row + (int64_t)i * g.D, o);
                     }
-            }
         } else {
-            if (tt - tile >= t0) load(nxt, h_nxt, tt - tile);
-            float a[kTS][CPL], na[kTS][CPL], A[CPL], H[CPL], M[CPL];
-#pragma unroll
-            for (int k = 0; k < CPL; ++k) A[k] = 1.0f, H[k] = 0.0f, M[k] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kTS; ++i) {
-                const bool on = t + i < p.n;
-#pragma unroll
-                for (int k = 0; k < CPL; ++k) {
-                    float s, ns;
-                    gate(to_f32(cur.v[0][i][k]), s, ns);
-                    a[i][k] = on ? s : 1.0f;
-                    na[i][k] = on ? ns : 0.0f;
-                    const float v = to_f32(cur.v[1][i][k]);
-                    H[k] = fmaf(a[i][k], H[k], on ? (COUPLED ? ns * v : v) : 0.0f);
-                    A[k] *= a[i][k];
-                }
-            }
-#pragma unroll
-            for (int i = kTS - 1; i >= 0; --i)
-#pragma unroll
-                for (int k = 0; k < CPL; ++k)
-                    M[k] = a[i][k] * (M[k] + (g0 && t + i < p.n ? to_f32(cur.v[2][i][k]) : 0.0f));
+            float a[TS][CPL], na[TS][CPL], A[CPL], H[CPL], M[CPL], h[CPL], lam[CPL];
+            compose_back<E, CPL, TS, COUPLED>(cur, a, na, A, H, M);
 #pragma unroll
             for (int k = 0; k < CPL; ++k) {
                 sh[buf][w][k][0][lane] = A[k];
@@ -370,7 +494,6 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_back(const E* __restrict__
                 sh[buf][w][k][2][lane] = M[k];
             }
             __syncthreads();
-            float h[CPL], lam[CPL];
 #pragma unroll
             for (int k = 0; k < CPL; ++k) {
                 h[k] = h_cur[k];
@@ -380,33 +503,7 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_back(const E* __restrict__
                     mu[k] = fmaf(sh[buf][q][k][0][lane], mu[k], sh[buf][q][k][2][lane]);
                 }
             }
-            float before[kTS][CPL];
-#pragma unroll
-            for (int i = 0; i < kTS; ++i)
-#pragma unroll
-                for (int k = 0; k < CPL; ++k) {
-                    before[i][k] = h[k];
-                    const float v = to_f32(cur.v[1][i][k]);
-                    h[k] = fmaf(a[i][k], h[k], t + i < p.n ? (COUPLED ? na[i][k] * v : v) : 0.0f);
-                }
-#pragma unroll
-            for (int i = kTS - 1; i >= 0; --i) {
-                E ox[CPL], of[CPL];
-                const bool on = t + i < p.n;
-#pragma unroll
-                for (int k = 0; k < CPL; ++k) {
-                    if (g0 && on) lam[k] += to_f32(cur.v[2][i][k]);
-                    const float v = to_f32(cur.v[1][i][k]);
-                    ox[k] = from_f32<E>(on ? (COUPLED ? lam[k] * na[i][k] : lam[k]) : 0.0f);
-                    of[k] = from_f32<E>(on ? lam[k] * (COUPLED ? before[i][k] - v : before[i][k]) *
-                                                 (a[i][k] * na[i][k]) : 0.0f);
-                    lam[k] *= a[i][k];
-                }
-                if (p.live && t + i < t1) {
-                    store_elems<E, CPL>(grad_x + row0 + (int64_t)(t + i) * g.D, ox);
-                    store_elems<E, CPL>(grad_f + row0 + (int64_t)(t + i) * g.D, of);
-                }
-            }
+            run_back<E, CPL, TS, COUPLED>(cur, h, lam, a, na, t, p, g, grad_x, grad_f);
         }
         cur = nxt;
 #pragma unroll
@@ -461,35 +558,43 @@ int check_gated(const lif_gated_params* p)
     return LIF_OK;
 }
 
-// Channels per lane and segments of the time axis.
+// The way a call takes: channels per lane and segments of the time axis.
 struct Plan {
-    int cpl;
+    int cpl, columns;
     Geometry g;
 };
 
-Plan plan_of(const lif_gated_params& p)
+Plan plan_of(const lif_gated_params& p, bool back)
 {
     Plan q;
-    const int64_t chans = (int64_t)p.B * p.D;
-    // the widest group of up to 8 bytes that divides a row and leaves two workgroups for every CU
-    q.cpl = p.dtype == LIF_F32 ? 2 : 4;
-    while (q.cpl > 1 && (p.D % q.cpl != 0 || chans / q.cpl < 512 * kWave)) q.cpl >>= 1;
+    auto groups = [&](int cpl) { return (int64_t)p.B * ((p.D + cpl - 1) / cpl); };
+    auto columns = [&](int cpl) { return (int)((groups(cpl) + kWave - 1) / kWave); };
+    const int blocks = (p.T + LIF_GATED_MARK - 1) / LIF_GATED_MARK;
+    // The widest group of up to 8 bytes that leaves two workgroups for every
+    // CU; or, forward, two channels where the time axis is long enough to be
+    // shared out further (backward they cost the registers of half the waves:
+    // 60000 x 512 bf16 67 -> 82 us).
+    q.cpl = p.dtype == LIF_F32 || back ? 2 : 4;
+    auto fits = [&](int cpl) {
+        return p.D >= cpl && (columns(cpl) >= 512 || (cpl == 2 && !back &&
+                                                      (int64_t)columns(2) * (blocks / kSplitBlocks) >= kSplitGroups));
+    };
+    while (q.cpl > 1 && !fits(q.cpl)) q.cpl >>= 1;
+    q.columns = columns(q.cpl);
+    int S = 1;
+    if (q.columns < kSplitColumns && blocks >= 2 * kSplitBlocks) {
+        S = (kSplitGroups + q.columns - 1) / q.columns;
+        if (S > blocks / kSplitBlocks) S = blocks / kSplitBlocks;
+    }
+    const int per = blocks > 0 ? (blocks + S - 1) / S : 1;
     Geometry& g = q.g;
+    g.seg_len = per * LIF_GATED_MARK;
+    g.S = blocks > 0 ? (blocks + per - 1) / per : 1;
     g.B = p.B;
     g.T = p.T;
     g.D = p.D;
-    g.groups = (int)(chans / q.cpl);
-    g.per_sample = p.D / q.cpl;
-    const int columns = (g.groups + kWave - 1) / kWave;
-    const int blocks = (p.T + LIF_GATED_MARK - 1) / LIF_GATED_MARK;
-    int S = 1;
-    if (columns < 128 && blocks > 4) {
-        S = (1024 + columns - 1) / columns;
-        if (S > (blocks + 3) / 4) S = (blocks + 3) / 4;
-    }
-    const int per = S > 0 ? (blocks + S - 1) / S : 1;
-    g.seg_len = (per > 0 ? per : 1) * LIF_GATED_MARK;
-    g.S = p.T > 0 ? (p.T + g.seg_len - 1) / g.seg_len : 1;
+    g.groups = (int)groups(q.cpl);
+    g.per_sample = (p.D + q.cpl - 1) / q.cpl;
     g.x_batch = p.x_batch;
     g.x_time = p.x_time;
     g.f_batch = p.f_batch;
@@ -499,7 +604,7 @@ Plan plan_of(const lif_gated_params& p)
     return q;
 }
 
-size_t ws_size(const Plan& q) { return q.g.S > 1 ? (size_t)q.g.S * q.g.B * q.g.D * sizeof(float2) : 0; }
+size_t maps_size(const Plan& q) { return q.g.S > 1 ? (size_t)q.g.S * q.g.B * q.g.D * sizeof(float2) : 0; }
 
 template <int N> struct Int { static constexpr int value = N; };
 
@@ -523,8 +628,10 @@ template <typename Fn> void dispatch(const Plan& q, const lif_gated_params& p, F
 
 extern "C" size_t lif_gated_scan_workspace_size(const lif_gated_params* p)
 {
-    if (lif::check_gated(p) != LIF_OK) return 0;
-    return lif::ws_size(lif::plan_of(*p));
+    using namespace lif;
+    if (check_gated(p) != LIF_OK) return 0;
+    const size_t a = maps_size(plan_of(*p, false)), b = maps_size(plan_of(*p, true));
+    return a > b ? a : b;
 }
 
 extern "C" int lif_gated_scan(const void* x, const void* f, const int32_t* length, const float* h_first,
@@ -537,24 +644,23 @@ extern "C" int lif_gated_scan(const void* x, const void* f, const int32_t* lengt
     const int64_t chans = (int64_t)p->B * p->D;
     if (chans * p->T > 0 && (!x || !f)) return LIF_ERR_ARG;
     if (chans > 0 && !h && !h_last && !marks) return LIF_ERR_ARG;
-    const Plan q = plan_of(*p);
-    const size_t need = ws_size(q);
-    if (need > 0 && !ws) return LIF_ERR_ARG;
+    const size_t need = lif_gated_scan_workspace_size(p);
+    if (need > 0 && (!ws || (uintptr_t)ws % sizeof(float2))) return LIF_ERR_ARG;
     if (ws_bytes < need) return LIF_ERR_WORKSPACE;
     if (chans == 0) return LIF_OK;
-    const Geometry& g = q.g;
-    const unsigned columns = (unsigned)((g.groups + kWave - 1) / kWave);
+    const Plan q = plan_of(*p, false);
+    const hipStream_t s = (hipStream_t)stream;
     int nw = 1;                          // no more waves than the sequence has groups of TS steps
     while (nw < kMaxWaves && nw * kTS < p->T) nw *= 2;
     dispatch(q, *p, [&](auto e, auto cpl, auto coupled) {
         using E = decltype(e);
         constexpr int C = decltype(cpl)::value;
         constexpr bool K = decltype(coupled)::value;
-        if (g.S > 1)
-            TIMED_LAUNCH("gated_maps", (k_segment_maps<E, C, K, false>), dim3(columns, g.S - 1), dim3(kMaxWaves * kWave),
-                         0, (hipStream_t)stream, (const E*)x, (const E*)f, length, g, (float2*)ws);
-        TIMED_LAUNCH("gated_scan", (k_scan<E, C, K>), dim3(columns, g.S), dim3(nw * kWave), 0, (hipStream_t)stream,
-                     (const E*)x, (const E*)f, length, h_first, g, (const float2*)ws, (E*)h, h_last, marks);
+        if (q.g.S > 1)
+            TIMED_LAUNCH("gated_maps", (k_segment_maps<E, C, K, false>), dim3(q.columns, q.g.S - 1),
+                         dim3(kMaxWaves * kWave), 0, s, (const E*)x, (const E*)f, length, q.g, (float2*)ws);
+        TIMED_LAUNCH("gated_scan", (k_scan<E, C, K>), dim3(q.columns, q.g.S), dim3(nw * kWave), 0, s, (const E*)x,
+                     (const E*)f, length, h_first, q.g, (const float2*)ws, (E*)h, h_last, marks);
     });
     return check_launch();
 }
@@ -569,24 +675,24 @@ extern "C" int lif_gated_scan_backward(const void* x, const void* f, const int32
     if (rc) return rc;
     const int64_t chans = (int64_t)p->B * p->D;
     if (chans * p->T > 0 && (!x || !f || !marks || !grad_x || !grad_f)) return LIF_ERR_ARG;
-    const Plan q = plan_of(*p);
-    const size_t need = ws_size(q);
-    if (need > 0 && !ws) return LIF_ERR_ARG;
+    const size_t need = lif_gated_scan_workspace_size(p);
+    if (need > 0 && (!ws || (uintptr_t)ws % sizeof(float2))) return LIF_ERR_ARG;
     if (ws_bytes < need) return LIF_ERR_WORKSPACE;
     if (chans == 0) return LIF_OK;
-    const Geometry& g = q.g;
-    const unsigned columns = (unsigned)((g.groups + kWave - 1) / kWave);
+    const Plan q = plan_of(*p, true);
+    const hipStream_t s = (hipStream_t)stream;
     dispatch(q, *p, [&](auto e, auto cpl, auto coupled) {
         using E = decltype(e);
         constexpr int C = decltype(cpl)::value;
         constexpr bool K = decltype(coupled)::value;
-        if (g.S > 1)
-            TIMED_LAUNCH("gated_maps_back", (k_segment_maps<E, C, K, true>), dim3(columns, g.S - 1),
-                         dim3(kMaxWaves * kWave), 0, (hipStream_t)stream, (const E*)grad_h, (const E*)f, length, g,
-                         (float2*)ws);
-        TIMED_LAUNCH("gated_back", (k_back<E, C, K>), dim3(columns, g.S), dim3(kMaxWaves * kWave), 0,
-                     (hipStream_t)stream, (const E*)x, (const E*)f, length, marks, (const E*)grad_h, grad_last, g,
-                     (const float2*)ws, (E*)grad_x, (E*)grad_f, grad_h_first);
+        if constexpr (C <= 2) {
+            if (q.g.S > 1)
+                TIMED_LAUNCH("gated_maps_back", (k_segment_maps<E, C, K, true>), dim3(q.columns, q.g.S - 1),
+                             dim3(kMaxWaves * kWave), 0, s, (const E*)grad_h, (const E*)f, length, q.g, (float2*)ws);
+            TIMED_LAUNCH("gated_back", (k_back<E, C, K>), dim3(q.columns, q.g.S), dim3(kMaxWaves * kWave), 0, s,
+                         (const E*)x, (const E*)f, length, marks, (const E*)grad_h, grad_last, q.g, (const float2*)ws,
+                         (E*)grad_x, (E*)grad_f, grad_h_first);
+        }
     });
     return check_launch();
 }
