@@ -20,15 +20,23 @@
 // products keeps a state's rounding that of the recurrence.
 #include "lif_host.hpp"
 #include "lif_types.hpp"
+#include "lif_walk.hpp"
 
 namespace lif {
 namespace {
 
 constexpr int kTS = 8;            // steps of a wave in a tile
 constexpr int kMaxWaves = 8;      // waves of a workgroup
-constexpr int kSplitColumns = 256;   // fewer columns than this share out the time axis,
-constexpr int kSplitGroups = 1024;   // over about this many workgroups,
-constexpr int kSplitBlocks = 2;      // each with at least this many blocks of LIF_GATED_MARK steps
+// The time axis is shared out where one step of one input has less than
+// kSplitBytes, over about kSplitGroups workgroups that take at least
+// kSplitBlocks blocks of LIF_GATED_MARK steps each.  32 KB a step (32 x 256
+// f32, 1000 steps): forward and backward 70 -> 55 us; 40 KB (20 x 1000 bf16,
+// 3000 steps): forward 114 -> 133, backward 199 -> 200.  Short sequences gain
+// from it at narrower steps only: 30 KB, 500 steps 40 -> 52 us, 2 KB 32 -> 24.
+constexpr int64_t kSplitBytes = 36 << 10;
+constexpr int kSplitGroups = 1024;
+constexpr int kSplitBlocks = 2;
+constexpr int kSplitMin = 8;         // fewer blocks than this are not shared out
 static_assert(LIF_GATED_MARK % kTS == 0 && kTS * kMaxWaves == LIF_GATED_MARK,
               "a mark is the state entering some wave's first step, and a backward tile starts at one");
 
@@ -57,9 +65,22 @@ __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstl
 // Where CPL does not divide D, a sample's last group starts at D - CPL: the
 // channels that it shares with the group before get the same bits twice.
 struct Geometry {
-    int B, T, D, groups, per_sample, S, seg_len;
+    int B, T, D, groups, per_sample, columns, S, seg_len;
+    bool shared_lines;            // rows are not whole cache lines
     int64_t x_batch, x_time, f_batch, f_time, g_batch, g_time;
 };
+
+// A workgroup's column of 64 lanes and segment.  Where rows are not multiples
+// of a cache line, neighbouring columns write parts of the same lines: they
+// then go to one XCD, so that the parts meet in its L2 (4 x 8192 x 1001 bf16,
+// forward and backward 227 -> 191 us; for whole lines the order of launch is
+// better, 65521 x 512 bf16 87 -> 76 us).
+__device__ __forceinline__ void work_item(const Geometry& g, int& column, int& segment)
+{
+    const int at = g.shared_lines ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x;
+    segment = at / g.columns;
+    column = at - segment * g.columns;
+}
 
 // A lane's place: sample b, first channel d, flat channel c = b * D + d, the
 // sample's steps n and the smallest and largest n of the wave.  Lanes past
@@ -200,8 +221,8 @@ __device__ __forceinline__ void run_steps(float (&h)[CPL], const float (&a)[TS][
 // it carry to it.  x and f (backward: f and grad_h) are then read twice, the
 // second time in part from the cache behind the L2s.
 
-// The composed map of segment blockIdx.y (plus one, backward): of h from f and
-// x, or (REVERSE) of mu from f and grad_h.  Each wave takes a contiguous part
+// The composed map of a segment: of h from f and x, or (REVERSE) of mu from f
+// and grad_h.  Each wave takes a contiguous part
 // of the segment without a barrier; the waves' maps meet once at the end.
 template <typename E, int CPL, bool COUPLED, bool REVERSE>
 __global__ __launch_bounds__(kMaxWaves* kWave) void k_segment_maps(const E* __restrict__ in, const E* __restrict__ f,
@@ -211,8 +232,10 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_segment_maps(const E* __re
     constexpr int TS = kTS;
     __shared__ float2 sh[kMaxWaves][CPL][kWave];
     const int lane = threadIdx.x & 63, w = wave_index();
-    const int seg = REVERSE ? blockIdx.y + 1 : blockIdx.y;       // the walk's last segment needs no map
-    const Place p = place_of<CPL>(g, length, blockIdx.x, lane);
+    int column, seg;
+    work_item(g, column, seg);
+    if (REVERSE) ++seg;                                          // the walk's last segment needs no map
+    const Place p = place_of<CPL>(g, length, column, lane);
     const int64_t in_batch = REVERSE ? g.g_batch : g.x_batch, in_time = REVERSE ? g.g_time : g.x_time;
     const int part = g.seg_len / kMaxWaves;                      // a multiple of TS
     const int t0 = seg * g.seg_len + w * part;
@@ -302,9 +325,11 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_scan(const E* __restrict__
     constexpr int TS = kTS;
     __shared__ float2 sh[2][kMaxWaves][CPL][kWave];
     const int lane = threadIdx.x & 63, w = wave_index(), nw = blockDim.x >> 6;
-    const int seg = blockIdx.y, tile = nw * TS;
+    int column, seg;
+    work_item(g, column, seg);
+    const int tile = nw * TS;
     const int t0 = seg * g.seg_len, t1 = min(t0 + g.seg_len, g.T);
-    const Place p = place_of<CPL>(g, length, blockIdx.x, lane);
+    const Place p = place_of<CPL>(g, length, column, lane);
     E* out = h_out ? h_out + (int64_t)p.b * g.T * g.D + p.d : nullptr;
     const int nm = (g.T + LIF_GATED_MARK - 1) / LIF_GATED_MARK;
     float* mk = marks ? marks + (int64_t)p.b * nm * g.D + p.d : nullptr;
@@ -448,9 +473,10 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_back(const E* __restrict__
     __shared__ float sh[2][kMaxWaves][CPL][3][kWave];
     __shared__ float2 sh_maps[kMaxWaves][CPL][kWave];
     const int lane = threadIdx.x & 63, w = wave_index();
-    const int seg = blockIdx.y;
+    int column, seg;
+    work_item(g, column, seg);
     const int t0 = seg * g.seg_len, t1 = min(t0 + g.seg_len, g.T);
-    const Place p = place_of<CPL>(g, length, blockIdx.x, lane);
+    const Place p = place_of<CPL>(g, length, column, lane);
     const int nm = (g.T + LIF_GATED_MARK - 1) / LIF_GATED_MARK;
     const float* mk = marks + (int64_t)p.b * nm * g.D + p.d;
 
@@ -560,30 +586,38 @@ int check_gated(const lif_gated_params* p)
 
 // The way a call takes: channels per lane and segments of the time axis.
 struct Plan {
-    int cpl, columns;
+    int cpl;
     Geometry g;
 };
 
 Plan plan_of(const lif_gated_params& p, bool back)
 {
     Plan q;
+    const int64_t elem = p.dtype == LIF_F32 ? 4 : 2;
     auto groups = [&](int cpl) { return (int64_t)p.B * ((p.D + cpl - 1) / cpl); };
     auto columns = [&](int cpl) { return (int)((groups(cpl) + kWave - 1) / kWave); };
     const int blocks = (p.T + LIF_GATED_MARK - 1) / LIF_GATED_MARK;
-    // The widest group of up to 8 bytes that leaves two workgroups for every
-    // CU; or, forward, two channels where the time axis is long enough to be
-    // shared out further (backward they cost the registers of half the waves:
-    // 60000 x 512 bf16 67 -> 82 us).
-    q.cpl = p.dtype == LIF_F32 || back ? 2 : 4;
+    const bool split = blocks >= kSplitMin && p.B * (int64_t)p.D * elem < kSplitBytes * (blocks < 16 ? blocks : 16) / 16;
+    // The widest group that leaves enough workgroups: four channels take 136
+    // registers, so they pay from two workgroups per CU on (128 x 1000 x 512
+    // bf16, ragged, 256 columns: 74 us, 66 with two channels); two 16-bit
+    // channels fill a 4-byte load (157 columns: 114 us, 126 with one); two
+    // float32 ones from 256 columns on (76 us, 81 with one; at 192 columns 102
+    // and 95).  Where the time axis is shared out, two channels if that still
+    // gives all workgroups (65521 x 512 bf16: 76 us, 85 with one).  Backward
+    // always one: two halve the waves (60000 x 512 67 -> 82, 128 x 1000 x 512
+    // 145 -> 151 us).
+    q.cpl = back ? 1 : elem == 4 ? 2 : 4;
     auto fits = [&](int cpl) {
-        return p.D >= cpl && (columns(cpl) >= 512 || (cpl == 2 && !back &&
-                                                      (int64_t)columns(2) * (blocks / kSplitBlocks) >= kSplitGroups));
+        if (p.D < cpl) return false;
+        if (split) return cpl == 2 && (int64_t)columns(2) * (blocks / kSplitBlocks) >= kSplitGroups;
+        return columns(cpl) >= (cpl == 4 ? 512 : elem == 4 ? 256 : 150);
     };
     while (q.cpl > 1 && !fits(q.cpl)) q.cpl >>= 1;
-    q.columns = columns(q.cpl);
+    q.g.columns = columns(q.cpl);
     int S = 1;
-    if (q.columns < kSplitColumns && blocks >= 2 * kSplitBlocks) {
-        S = (kSplitGroups + q.columns - 1) / q.columns;
+    if (split) {
+        S = (kSplitGroups + q.g.columns - 1) / q.g.columns;
         if (S > blocks / kSplitBlocks) S = blocks / kSplitBlocks;
     }
     const int per = blocks > 0 ? (blocks + S - 1) / S : 1;
@@ -595,6 +629,7 @@ Plan plan_of(const lif_gated_params& p, bool back)
     g.D = p.D;
     g.groups = (int)groups(q.cpl);
     g.per_sample = (p.D + q.cpl - 1) / q.cpl;
+    g.shared_lines = p.D * elem % 128 != 0;
     g.x_batch = p.x_batch;
     g.x_time = p.x_time;
     g.f_batch = p.f_batch;
@@ -657,9 +692,9 @@ extern "C" int lif_gated_scan(const void* x, const void* f, const int32_t* lengt
         constexpr int C = decltype(cpl)::value;
         constexpr bool K = decltype(coupled)::value;
         if (q.g.S > 1)
-            TIMED_LAUNCH("gated_maps", (k_segment_maps<E, C, K, false>), dim3(q.columns, q.g.S - 1),
+            TIMED_LAUNCH("gated_maps", (k_segment_maps<E, C, K, false>), dim3(q.g.columns * (q.g.S - 1)),
                          dim3(kMaxWaves * kWave), 0, s, (const E*)x, (const E*)f, length, q.g, (float2*)ws);
-        TIMED_LAUNCH("gated_scan", (k_scan<E, C, K>), dim3(q.columns, q.g.S), dim3(nw * kWave), 0, s, (const E*)x,
+        TIMED_LAUNCH("gated_scan", (k_scan<E, C, K>), dim3(q.g.columns * q.g.S), dim3(nw * kWave), 0, s, (const E*)x,
                      (const E*)f, length, h_first, q.g, (const float2*)ws, (E*)h, h_last, marks);
     });
     return check_launch();
@@ -685,11 +720,11 @@ extern "C" int lif_gated_scan_backward(const void* x, const void* f, const int32
         using E = decltype(e);
         constexpr int C = decltype(cpl)::value;
         constexpr bool K = decltype(coupled)::value;
-        if constexpr (C <= 2) {
+        if constexpr (C == 1) {
             if (q.g.S > 1)
-                TIMED_LAUNCH("gated_maps_back", (k_segment_maps<E, C, K, true>), dim3(q.columns, q.g.S - 1),
+                TIMED_LAUNCH("gated_maps_back", (k_segment_maps<E, C, K, true>), dim3(q.g.columns * (q.g.S - 1)),
                              dim3(kMaxWaves * kWave), 0, s, (const E*)grad_h, (const E*)f, length, q.g, (float2*)ws);
-            TIMED_LAUNCH("gated_back", (k_back<E, C, K>), dim3(q.columns, q.g.S), dim3(kMaxWaves * kWave), 0, s,
+            TIMED_LAUNCH("gated_back", (k_back<E, C, K>), dim3(q.g.columns * q.g.S), dim3(kMaxWaves * kWave), 0, s,
                          (const E*)x, (const E*)f, length, marks, (const E*)grad_h, grad_last, q.g, (const float2*)ws,
                          (E*)grad_x, (E*)grad_f, grad_h_first);
         }
