@@ -606,7 +606,8 @@ int lif_gated_step(const void* x, const void* f, const int32_t* slot, float* sta
  * ws may then be NULL).  Both are bitwise reproducible.
  * Errors: LIF_ERR_ARG (null pointers, sizes, flags, dtype, stride < V,
  * k > V, a temperature outside [2^-20, 2^20]), LIF_ERR_SIZE (k >
- * LIF_TOP_MAX), LIF_ERR_WORKSPACE. */
+ * LIF_TOP_MAX, V > 2^24, R * V beyond 2^31 segments of a row),
+ * LIF_ERR_WORKSPACE. */
 #define LIF_TOP_MAX 128
 #define LIF_DISTILL_TAIL 1u
 #define LIF_DISTILL_TAIL_MIN (1.0 / 1048576.0)

@@ -4,211 +4,1117 @@
 // (lif_distill_top), each with its gradient.
 //
 // With m the row's largest logit and c = log2(e) / temperature, every term
-// is e_j = 2^{(x_j - m) c}; S = sum e_j gives p_j = e_j / S and
-// lse = m / temperature + log S.
+// is e_j = 2^{z_j} with z_j = (x_j - m) c <= 0; S = sum e_j and U = sum e_j z_j
+// give p_j = e_j / S, lse = m / temperature + log S and the entropy
+// log S - log(2) U / S.  m is subtracted before the product, so that rows of
+// huge logits (masks at the type's lowest value) stay exact.
+//
+// Rows of up to kNarrow logits: a workgroup stages many rows in LDS with
+// contiguous loads, and a few lanes work on each (k_narrow_*).  Longer rows:
+// a workgroup holds a row in registers, so that the logits are read once for
+// the maximum, the sums, the alternatives and the gradient (k_wide_*).  Where
+// there are few rows, or a row does not fit, the row is cut into segments: a
+// first launch leaves each segment's statistics and alternatives, a second
+// one joins them and writes the results (and the gradient, from a second read).
 #include "lif_host.hpp"
 #include "lif_types.hpp"
+
+#include <type_traits>
 
 namespace lif {
 namespace {
 
-constexpr int kRowThreads = 256;
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kNegInf = -INFINITY;
+constexpr int kNarrow = 256;            // longest row of the narrow kernels
+constexpr int kNarrowThreads = 256;
+constexpr int kMaxV = 1 << 24;
+constexpr int kCand = 512;              // candidates of a top-k selection held in LDS
+
+// A row's result from its maximum and sums.
+struct RowStat {
+    float m;                            // largest logit, 0 where nothing is above -infinity
+    float s, ls;                        // S and its logarithm
+    float H;                            // entropy
+    bool empty;                         // nothing above -infinity
+};
 
 struct RowArgs {
     int R, V, k;
     int64_t stride, grad_stride;
-    float c, inv_t;             // log2(e) / temperature, 1 / temperature
+    float c, inv_t;                     // log2(e) / temperature, 1 / temperature
     double inv_td;
     bool tail;
+    int nseg, seg;                      // segments of a row and their length
 };
 
-// Orders float32 values as unsigned integers; -0 and +0 are equal, a NaN
-// ranks below -infinity.
+__device__ __forceinline__ float z_of(float x, float m, float c) { return (x - m) * c; }
+__device__ __forceinline__ float pow2(float z) { return __builtin_amdgcn_exp2f(z); }
+// z where it is multiplied by e: -infinity (e = 0) must not give a NaN.
+__device__ __forceinline__ float z_finite(float z) { return fmaxf(z, -200.0f); }
+
+__device__ __forceinline__ RowStat row_stat(float m, float s, float u)
+{
+    RowStat r;
+    r.m = m == kNegInf ? 0.0f : m;
+    r.s = s;
+    r.empty = s == 0.0f;
+    r.ls = r.empty ? kNegInf : logf(s);
+    r.H = r.empty ? 0.0f : r.ls - kLn2 * (u / s);
+    return r;
+}
+__device__ __forceinline__ float row_logp(const RowStat& r, const RowArgs& a, float x)
+{
+    return r.empty ? kNegInf : (x - r.m) * a.inv_t - r.ls;
+}
+__device__ __forceinline__ float row_lse(const RowStat& r, const RowArgs& a)
+{
+    return r.empty ? kNegInf : (float)((double)r.m * a.inv_td + (double)r.ls);
+}
+
+// Orders float32 values as unsigned integers: -0 and +0 are equal, a NaN
+// ranks below -infinity, 0 is left for "none".
 __device__ __forceinline__ uint32_t order_key(float v)
 {
-    if (v != v) return 0;
+    if (v != v) return 1;
     const uint32_t u = __float_as_uint(v + 0.0f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
-
-__device__ __forceinline__ float wave_sum(float v)
+__device__ __forceinline__ float key_value(uint32_t k)
 {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    if (k == 1) return NAN;
+    return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
+}
+// Larger logits first, then smaller indices.
+using Cand = unsigned long long;
+__device__ __forceinline__ Cand make_cand(float v, int j) { return ((Cand)order_key(v) << 32) | (0xffffffffu - (uint32_t)j); }
+__device__ __forceinline__ int cand_index(Cand c) { return (int)(0xffffffffu - (uint32_t)c); }
+__device__ __forceinline__ float cand_value(Cand c) { return key_value((uint32_t)(c >> 32)); }
+
+// ---------------------------------------------------------------------------
+// Sums and maxima over lanes: within 16 lanes by DPP (pairs, quads, mirrored
+// halves), over the wave's four rows of 16 by lane reads.  The result is the
+// same in all lanes, and the order of a sum is fixed.
+// ---------------------------------------------------------------------------
+template <int Ctrl> __device__ __forceinline__ float dpp(float v)
+{
+    const int i = __float_as_int(v);
+    return __int_as_float(__builtin_amdgcn_update_dpp(i, i, Ctrl, 0xf, 0xf, false));
+}
+template <int Ctrl> __device__ __forceinline__ int dpp(int v)
+{
+    return __builtin_amdgcn_update_dpp(v, v, Ctrl, 0xf, 0xf, false);
+}
+// Combines with the lanes of a group of L <= 16 (aligned) lanes.
+template <int L, typename V, typename Op> __device__ __forceinline__ V over_lanes(V v, Op op)
+{
+    if constexpr (L >= 2) v = op(v, dpp<0xb1>(v));          // quad_perm 1,0,3,2
+    if constexpr (L >= 4) v = op(v, dpp<0x4e>(v));          // quad_perm 2,3,0,1
+    if constexpr (L >= 8) v = op(v, dpp<0x141>(v));         // mirrored in 8
+    if constexpr (L >= 16) v = op(v, dpp<0x140>(v));        // mirrored in 16
     return v;
 }
-__device__ __forceinline__ float wave_max(float v)
+struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct Min { __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); } };
+
+template <typename Op> __device__ __forceinline__ float over_wave(float v, Op op)
 {
-    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
+    v = over_lanes<16>(v, op);
+    const int i = __float_as_int(v);
+    const float a = __int_as_float(__builtin_amdgcn_readlane(i, 0)), b = __int_as_float(__builtin_amdgcn_readlane(i, 16));
+    const float c = __int_as_float(__builtin_amdgcn_readlane(i, 32)), d = __int_as_float(__builtin_amdgcn_readlane(i, 48));
+    return op(op(a, b), op(c, d));
 }
 
-struct Shared {
-    float part[4][kRowThreads / 64];
-    unsigned long long best[kRowThreads / 64];
-};
+// ---------------------------------------------------------------------------
+// Narrow rows.  A workgroup takes kNarrowThreads / L rows, L lanes a row; lane
+// l of a row holds its elements j = l + L i.  The rows pass through LDS, with
+// a row length of an odd multiple of L words, so that the lanes of a wave read
+// different banks.
+// ---------------------------------------------------------------------------
+constexpr int kNarrowPer = 32;          // at most this many elements a lane: one bit each in a mask
 
-__device__ __forceinline__ float block_sum(float v, float* part)
+__host__ __device__ __forceinline__ int narrow_pitch(int V, int L) { return ((V + L - 1) / L | 1) * L; }
+
+// Calls fn(row, element) for the elements of `rows` rows: thread by thread
+// along the rows, so that several short rows lie side by side in a wave.
+template <typename Fn> __device__ __forceinline__ void each_staged(int rows, int V, Fn&& fn)
 {
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float s = 0.0f;
-    for (int i = 0; i < kRowThreads / 64; ++i) s += part[i];
-    return s;
+    const int dr = kNarrowThreads / V, dj = kNarrowThreads - dr * V;
+    int r = (int)threadIdx.x / V, j = (int)threadIdx.x - r * V;
+    while (r < rows) {
+        fn(r, j);
+        r += dr;
+        j += dj;
+        if (j >= V) j -= V, ++r;
+    }
 }
-__device__ __forceinline__ float block_max(float v, float* part)
-{
-    v = wave_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float s = part[0];
-    for (int i = 1; i < kRowThreads / 64; ++i) s = fmaxf(s, part[i]);
-    return s;
-}
-
-// (x - m) c; 0 for the row's largest logits, also where they are infinite
-// or the row has nothing above -infinity.
-__device__ __forceinline__ float log2_term(float x, float m, float c) { return (x - m) * c; }
-
 template <typename E>
-__global__ __launch_bounds__(kRowThreads) void k_token_logprobs(
+__device__ __forceinline__ void stage_rows(const E* __restrict__ in, int64_t stride, int rows, int V, int pitch,
+                                           float* sh)
+{
+    each_staged(rows, V, [&](int r, int j) { sh[r * pitch + j] = to_f32(in[r * stride + j]); });
+}
+template <typename E>
+__device__ __forceinline__ void unstage_rows(E* __restrict__ out, int64_t stride, int rows, int V, int pitch,
+                                             const float* sh)
+{
+    each_staged(rows, V, [&](int r, int j) { out[r * stride + j] = from_f32<E>(sh[r * pitch + j]); });
+}
+
+template <typename E, int L>
+__global__ __launch_bounds__(kNarrowThreads) void k_narrow_logprobs(
     const E* __restrict__ logits, const int32_t* __restrict__ token, RowArgs a, float* __restrict__ logp,
     float* __restrict__ entropy, float* __restrict__ lse, float* __restrict__ top_logp, int32_t* __restrict__ top_idx,
     const float* __restrict__ g_logp, const float* __restrict__ g_ent, E* __restrict__ grad)
 {
-    __shared__ Shared sh;
-    const int r = blockIdx.x, tid = threadIdx.x;
-    const E* x = logits + r * a.stride;
-    float m = kNegInf;
-    for (int j = tid; j < a.V; j += kRowThreads) m = fmaxf(m, to_f32(x[j]));
-    m = block_max(m, sh.part[0]);
+    extern __shared__ float sh[];
+    constexpr int per_group = kNarrowThreads / L;
+    const int64_t row0 = (int64_t)blockIdx.x * per_group;
+    const int rows = (int)min((int64_t)per_group, a.R - row0);
+    const int pitch = narrow_pitch(a.V, L);
+    stage_rows(logits + row0 * a.stride, a.stride, rows, a.V, pitch, sh);
+    __syncthreads();
+    const int rl = threadIdx.x / L, l = threadIdx.x % L;
+    const int64_t r = row0 + rl;
+    float* x = sh + rl * pitch + l;
+    const int n = rl < rows ? (a.V - l + L - 1) / L : 0;       // this lane's elements x[L i]
+    float m = kNegInf, s = 0.0f, u = 0.0f;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, x[L * i]);
+    m = over_lanes<L>(m, Max());
     const float ms = m == kNegInf ? 0.0f : m;
-    float s = 0.0f, u = 0.0f;
-    for (int j = tid; j < a.V; j += kRowThreads) {
-        const float z = log2_term(to_f32(x[j]), ms, a.c), e = exp2f(z);
+    for (int i = 0; i < n; ++i) {
+        const float z = z_of(x[L * i], ms, a.c), e = pow2(z);
         s += e;
-        u = fmaf(e, fmaxf(z, -200.0f), u);
+        u = fmaf(e, z_finite(z), u);
     }
-    s = block_sum(s, sh.part[0]);
-    u = block_sum(u, sh.part[1]);
-    const bool empty = s == 0.0f;
-    const float ls = empty ? kNegInf : logf(s);
-    const float H = empty ? 0.0f : ls - kLn2 * (u / s);
-    const int tok = token ? token[r] : -1;
-    const bool there = tok >= 0 && tok < a.V;
-    if (tid == 0) {
-        if (logp) logp[r] = !there ? 0.0f : empty ? kNegInf : (to_f32(x[tok]) - ms) * a.inv_t - ls;
-        if (entropy) entropy[r] = H;
-        if (lse) lse[r] = empty ? kNegInf : (float)((double)ms * a.inv_td + (double)ls);
+    s = over_lanes<L>(s, Add());
+    u = over_lanes<L>(u, Add());
+    const RowStat st = row_stat(m, s, u);
+    int tok = -1;
+    bool there = false;
+    if (rl < rows) {
+        tok = token ? token[r] : -1;
+        there = tok >= 0 && tok < a.V;
+        if (l == 0) {
+            if (logp) logp[r] = there ? row_logp(st, a, sh[rl * pitch + tok]) : 0.0f;
+            if (entropy) entropy[r] = st.H;
+            if (lse) lse[r] = row_lse(st, a);
+        }
     }
-    unsigned long long last = ~0ull;
-    for (int i = 0; i < a.k; ++i) {          // the largest key below the last one
-        unsigned long long best = 0;
-        for (int j = tid; j < a.V; j += kRowThreads) {
-            const unsigned long long key = ((unsigned long long)order_key(to_f32(x[j])) << 32) | (0xffffffffu - (uint32_t)j);
-            if (key < last && key > best) best = key;
+    uint32_t taken = 0;                         // elements already given out
+    for (int q = 0; q < a.k; ++q) {
+        // the largest left, ties and NaN by index: (v, j), j = V while there is none
+        float v = kNegInf;
+        int at = -1;
+        for (int i = 0; i < n; ++i) {
+            const float w = x[L * i];
+            if (!(taken >> i & 1) && (w > v || (at < 0 && w == w))) v = w, at = i;
         }
-        for (int o = 32; o; o >>= 1) {
-            const unsigned long long w = __shfl_xor(best, o);
-            best = w > best ? w : best;
+        int j = at < 0 ? a.V : l + L * at;
+        auto better = [&](float w, int o) {
+            if (o < a.V && (j == a.V || w > v || (w == v && o < j))) v = w, j = o;
+        };
+        if constexpr (L >= 2) better(dpp<0xb1>(v), dpp<0xb1>(j));
+        if constexpr (L >= 4) better(dpp<0x4e>(v), dpp<0x4e>(j));
+        if constexpr (L >= 8) better(dpp<0x141>(v), dpp<0x141>(j));
+        if constexpr (L >= 16) better(dpp<0x140>(v), dpp<0x140>(j));
+        if (j == a.V) {                         // only NaN left: by index
+            int first = a.V;
+            for (int i = n - 1; i >= 0; --i)
+                if (!(taken >> i & 1)) first = l + L * i;
+            j = over_lanes<L>(first, [](int p, int o) { return min(p, o); });
+            v = NAN;
         }
-        __syncthreads();
-        if ((tid & 63) == 0) sh.best[tid >> 6] = best;
-        __syncthreads();
-        for (int q = 0; q < kRowThreads / 64; ++q) best = sh.best[q] > best ? sh.best[q] : best;
-        last = best;
-        if (tid == 0) {
-            const int j = (int)(0xffffffffu - (uint32_t)best);
-            top_idx[(int64_t)r * a.k + i] = j;
-            top_logp[(int64_t)r * a.k + i] = empty ? kNegInf : (to_f32(x[j]) - ms) * a.inv_t - ls;
+        if (rl < rows) {
+            if (j % L == l) taken |= 1u << (j / L);
+            if (l == 0) {
+                top_idx[r * a.k + q] = j;
+                top_logp[r * a.k + q] = row_logp(st, a, v);
+            }
         }
     }
     if (!grad) return;
-    const float g = there && g_logp ? g_logp[r] : 0.0f, ge = g_ent ? g_ent[r] : 0.0f;
-    const float inv_s = empty ? 0.0f : 1.0f / s;
-    for (int j = tid; j < a.V; j += kRowThreads) {
-        const float z = log2_term(to_f32(x[j]), ms, a.c);
-        const float p = exp2f(z) * inv_s;
-        const float lp = empty ? 0.0f : fmaf(kLn2, fmaxf(z, -200.0f), -ls);
-        float v = -p * fmaf(ge, lp + H, g);
-        if (there && j == tok && !empty) v += g;
-        grad[r * a.grad_stride + j] = from_f32<E>(v * a.inv_t);
+    const float g = there && g_logp ? g_logp[r] : 0.0f, ge = rl < rows && g_ent ? g_ent[r] : 0.0f;
+    const float inv_s = st.empty ? 0.0f : 1.0f / st.s;
+    for (int i = 0; i < n; ++i) {
+        const float z = z_of(x[L * i], st.m, a.c), p = pow2(z) * inv_s;
+        const float lp = st.empty ? 0.0f : fmaf(kLn2, z_finite(z), -st.ls);
+        float v = -p * fmaf(ge, lp + st.H, g);
+        if (there && l + L * i == tok && !st.empty) v += g;
+        x[L * i] = v * a.inv_t;
+    }
+    __syncthreads();
+    unstage_rows(grad + row0 * a.grad_stride, a.grad_stride, rows, a.V, pitch, sh);
+}
+
+// The teacher's side of a row: sums over its used entries.
+struct Teacher {
+    double sq;                          // sum of q
+    bool none;                          // no mass
+    double q_rest, scale;               // the tail's share; what q is multiplied by
+};
+__device__ __forceinline__ Teacher teacher_of(double sq, bool tail, bool all_listed)
+{
+    Teacher t;
+    t.sq = sq;
+    t.none = sq == 0.0;
+    t.q_rest = tail && 1.0 - sq >= LIF_DISTILL_TAIL_MIN && !all_listed ? 1.0 - sq : 0.0;
+    t.scale = tail || t.none ? 1.0 : 1.0 / sq;
+    return t;
+}
+// One entry's share q (log q - log p) of the loss; lp the student's log p.
+__device__ __forceinline__ double entry_loss(double q, double log_q, double lp)
+{
+    return q > 0.0 ? q * (log_q - lp) : q != q ? q : 0.0;
+}
+__device__ __forceinline__ double tail_loss(const Teacher& t, float s_rest, const RowStat& st)
+{
+    if (!(t.q_rest > 0.0)) return 0.0;
+    const double lp = st.empty ? (double)kNegInf : (double)logf(s_rest) - (double)st.ls;
+    return t.q_rest * (log(t.q_rest) - lp);
+}
+// dloss/dz_j = e_j c_top - q_j for a listed class, e_j c_rest for another.
+__device__ __forceinline__ void grad_factors(const Teacher& t, const RowStat& st, float s_rest, float& c_top,
+                                             float& c_rest)
+{
+    const double mass = t.scale == 1.0 && !t.none ? t.sq + t.q_rest : 1.0;
+    c_top = t.none || st.empty ? 0.0f : (float)(mass / (double)st.s);
+    c_rest = c_top;
+    if (!t.none && !st.empty && t.q_rest > 0.0 && s_rest > 0.0f)
+        c_rest = (float)(mass / (double)st.s - t.q_rest / (double)s_rest);
+}
+
+template <typename E, int L>
+__global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __restrict__ logits,
+                                                                   const float* __restrict__ t_logp,
+                                                                   const int32_t* __restrict__ t_idx, RowArgs a,
+                                                                   const float* __restrict__ weight,
+                                                                   float* __restrict__ loss, E* __restrict__ grad)
+{
+    extern __shared__ float sh[];
+    constexpr int per_group = kNarrowThreads / L;
+    const int64_t row0 = (int64_t)blockIdx.x * per_group;
+    const int rows = (int)min((int64_t)per_group, a.R - row0);
+    const int pitch = narrow_pitch(a.V, L);
+    stage_rows(logits + row0 * a.stride, a.stride, rows, a.V, pitch, sh);
+    __syncthreads();
+    const int rl = threadIdx.x / L, l = threadIdx.x % L;
+    const int64_t r = row0 + rl;
+    float* row = sh + rl * pitch;
+    float* x = row + l;
+    const int n = rl < rows ? (a.V - l + L - 1) / L : 0;
+    const int k = rl < rows ? a.k : 0;
+    const int32_t* idx = t_idx + r * a.k;
+    const float* lt = t_logp + r * a.k;
+    uint32_t listed = 0;                        // this lane's elements that the teacher lists
+    double sq = 0.0;                            // the same order of sums in every lane
+    for (int i = 0; i < k; ++i) {
+        const int j = idx[i];
+        if (j < 0 || j >= a.V) continue;
+        if (j % L == l) listed |= 1u << (j / L);
+        sq += (double)expf(lt[i]);
+    }
+    float m = kNegInf, s_top = 0.0f, s_rest = 0.0f;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, x[L * i]);
+    m = over_lanes<L>(m, Max());
+    const float ms = m == kNegInf ? 0.0f : m;
+    for (int i = 0; i < n; ++i) {
+        const float e = pow2(z_of(x[L * i], ms, a.c));
+        if (listed >> i & 1) s_top += e;
+        else s_rest += e;
+    }
+    s_top = over_lanes<L>(s_top, Add());
+    s_rest = over_lanes<L>(s_rest, Add());
+    const int n_top = over_lanes<L>((int)__popc(listed), [](int p, int o) { return p + o; });
+    const RowStat st = row_stat(m, s_top + s_rest, 0.0f);
+    const Teacher t = teacher_of(sq, a.tail, n_top == a.V);
+    const double log_scale = t.scale == 1.0 ? 0.0 : log(t.scale);
+    if (loss) {
+        double v = 0.0;
+        for (int i = l; i < k; i += L) {
+            const int j = idx[i];
+            if (j < 0 || j >= a.V) continue;
+            const double lp = st.empty ? (double)kNegInf
+                                       : ((double)row[j] - (double)st.m) * a.inv_td - (double)st.ls;
+            v += entry_loss((double)expf(lt[i]) * t.scale, (double)lt[i] + log_scale, lp);
+        }
+        for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o);
+        if (l == 0 && rl < rows) loss[r] = t.none ? 0.0f : (float)(v + tail_loss(t, s_rest, st));
+    }
+    if (!grad) return;
+    float c_top, c_rest;
+    grad_factors(t, st, s_rest, c_top, c_rest);
+    const float w = rl < rows ? (weight ? weight[r] : 1.0f) * a.inv_t : 0.0f;
+    const bool dead = t.none || st.empty;
+    for (int i = 0; i < n; ++i) {
+        const float e = pow2(z_of(x[L * i], st.m, a.c));
+        x[L * i] = dead ? 0.0f : e * ((listed >> i & 1) ? c_top : c_rest);
+    }
+    // the lanes of a row hold its elements apart, so every element is changed by one lane
+    for (int i = 0; i < k && !dead; ++i) {
+        const int j = idx[i];
+        if (j >= 0 && j < a.V && j % L == l) row[j] -= (float)((double)expf(lt[i]) * t.scale);
+    }
+    for (int i = 0; i < n; ++i) x[L * i] *= dead ? 0.0f : w;
+    __syncthreads();
+    unstage_rows(grad + row0 * a.grad_stride, a.grad_stride, rows, a.V, pitch, sh);
+}
+
+// ---------------------------------------------------------------------------
+// Wide rows.  A workgroup of NT threads holds a segment in registers: NV
+// vectors of 16 bytes a thread, vector i of thread t at element
+// (i NT + t) VEC.  Elements past the segment count as -infinity.
+// ---------------------------------------------------------------------------
+template <typename E> constexpr int kVec = 16 / (int)sizeof(E);
+
+// Four words at an address that is aligned to one element.
+template <typename E> struct __attribute__((packed, aligned(sizeof(E)))) Words {
+    uint32_t w[4];
+};
+
+// Element e of four words.
+template <typename E> __device__ __forceinline__ float unpack(const uint32_t (&w)[4], int e)
+{
+    if constexpr (sizeof(E) == 4) return __uint_as_float(w[e]);
+    const uint32_t u = w[e >> 1];
+    if constexpr (std::is_same<E, bf16>::value) return __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
+    else return (float)__builtin_bit_cast(f16, (uint16_t)(e & 1 ? u >> 16 : u));
+}
+template <typename E> __device__ __forceinline__ uint32_t pack_pair(float a, float b)
+{
+    const uint32_t lo = __builtin_bit_cast(uint16_t, from_f32<E>(a)), hi = __builtin_bit_cast(uint16_t, from_f32<E>(b));
+    return lo | hi << 16;
+}
+
+template <typename E, int NT, int NV> struct Held {
+    static constexpr int VEC = kVec<E>;
+    uint32_t v[NV][4];
+    int len;                            // elements of the segment
+
+    __device__ __forceinline__ int first(int i) const { return (i * NT + (int)threadIdx.x) * VEC; }
+    // whether any thread of the workgroup holds elements in vector i
+    __device__ __forceinline__ bool any(int i) const { return i * NT * VEC < len; }
+    __device__ __forceinline__ float get(int i, int e) const { return unpack<E>(v[i], e); }
+
+    __device__ __forceinline__ void load(const E* __restrict__ x, int n)
+    {
+        len = n;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (!any(i)) continue;
+            const int j = first(i);
+            if (j + VEC <= n) {
+                const Words<E> q = *reinterpret_cast<const Words<E>*>(x + j);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[i][k] = q.w[k];
+            } else {
+                float f[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f[e] = j + e < n ? to_f32(x[j + e]) : kNegInf;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if constexpr (sizeof(E) == 4) v[i][k] = __float_as_uint(f[k]);
+                    else v[i][k] = pack_pair<E>(f[2 * k], f[2 * k + 1]);
+            }
+        }
+    }
+    // From here on the elements and the length count as new values to the
+    // compiler, which otherwise keeps all elements unpacked, and a mask for
+    // every vector, in registers from one pass to the next.
+    __device__ __forceinline__ void fresh()
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(v[i][k]));
+        asm volatile("" : "+s"(len));
+    }
+    // vm: the largest element of each vector; returns the thread's largest.
+    __device__ __forceinline__ float maxima(float (&vm)[NV])
+    {
+        float m = kNegInf;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            vm[i] = kNegInf;
+            if (!any(i)) continue;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) vm[i] = fmaxf(vm[i], get(i, e));
+            m = fmaxf(m, vm[i]);
+        }
+        fresh();
+        return m;
+    }
+    // Calls fn(element) for each element.
+    template <typename Fn> __device__ __forceinline__ void each(Fn&& fn)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (!any(i)) continue;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) fn(get(i, e));
+        }
+        fresh();
+    }
+    // Takes out the elements of vector i that `bits` names.
+    __device__ __forceinline__ void drop(int i, uint32_t bits)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if constexpr (sizeof(E) == 4) {
+                if (bits >> k & 1) v[i][k] = __float_as_uint(kNegInf);
+            } else {
+                const uint32_t none = pack_pair<E>(kNegInf, kNegInf);
+                if (bits >> (2 * k) & 1) v[i][k] = (v[i][k] & 0xffff0000u) | (none & 0xffffu);
+                if (bits >> (2 * k + 1) & 1) v[i][k] = (v[i][k] & 0xffffu) | (none & 0xffff0000u);
+            }
+    }
+    // Stores fn(element) for each element of the segment.
+    template <typename Fn> __device__ __forceinline__ void store(E* __restrict__ out, Fn&& fn)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (!any(i)) continue;
+            const int j = first(i);
+            float f[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[e] = fn(get(i, e));
+            if (j + VEC <= len) {
+                Words<E> q;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if constexpr (sizeof(E) == 4) q.w[k] = __float_as_uint(f[k]);
+                    else q.w[k] = pack_pair<E>(f[2 * k], f[2 * k + 1]);
+                *reinterpret_cast<Words<E>*>(out + j) = q;
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (j + e < len) out[j + e] = from_f32<E>(f[e]);
+            }
+        }
+    }
+};
+
+constexpr int kGroups = 256;            // groups whose maxima bound the k-th largest logit
+
+template <int NT> struct WideLds {
+    float part[3][NT / 64];
+    float group[kGroups];
+    float bound;                        // at least k logits reach it, or -infinity
+    int count;
+    Cand cand[kCand];
+};
+
+// Maximum over the workgroup.
+template <int NT, typename Op> __device__ __forceinline__ float join_parts(const float* part, Op op)
+{
+    float v = part[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) v = op(v, part[i]);
+    return v;
+}
+
+// A value that at least k logits of the segment reach, from the maxima of
+// disjoint groups of threads: the k-th largest of them, nearly (ten halvings
+// of the interval between the smallest and the largest).  -infinity where
+// fewer than k groups have anything above it.  Run by one wave.
+template <int NG> __device__ __forceinline__ float bound_of_kth(const float* group, int k, int lane)
+{
+    constexpr int N = NG / 64;
+    float v[N], lo = INFINITY, hi = kNegInf;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = group[i * 64 + lane];
+        hi = fmaxf(hi, v[i]);
+        lo = fminf(lo, v[i] > kNegInf ? v[i] : INFINITY);
+    }
+    hi = over_wave(hi, Max());
+    lo = over_wave(lo, Min());
+    auto reach = [&](float b) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __popcll(__ballot(v[i] >= b));
+        return n;
+    };
+    if (!(lo < INFINITY) || reach(lo) < k) return kNegInf;
+    for (int i = 0; i < 10; ++i) {
+        const float mid = 0.5f * lo + 0.5f * hi;
+        if (reach(mid) >= k) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// The elements j .. j + VEC - 1 of a segment for which fn(element) holds, one
+// bit each.  A selection reads the few vectors that it needs again (from the
+// L2): indexing the held ones by a loop's variable would cost more.
+template <typename E, typename Fn>
+__device__ __forceinline__ uint32_t which(const E* __restrict__ x, int j, int len, Fn&& fn)
+{
+    constexpr int VEC = kVec<E>;
+    uint32_t hit = 0;
+    if (j + VEC <= len) {
+        const Words<E> q = *reinterpret_cast<const Words<E>*>(x + j);
+        uint32_t v[4] = {q.w[0], q.w[1], q.w[2], q.w[3]};
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) hit |= fn(unpack<E>(v, e)) ? 1u << e : 0u;
+    } else {
+        for (int e = 0; j + e < len; ++e) hit |= fn(to_f32(x[j + e])) ? 1u << e : 0u;
+    }
+    return hit;
+}
+
+// Collects the logits that reach `from` (not NaN) in LDS; returns their
+// number, of which the first kCand are there.
+template <typename E, int NT, int NV>
+__device__ __forceinline__ int collect(const float (&vm)[NV], const E* __restrict__ x, int len, float from,
+                                       WideLds<NT>& sh)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    uint32_t vectors = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) vectors |= vm[i] >= from ? 1u << i : 0u;
+    for (; vectors; vectors &= vectors - 1) {
+        const int j = (__builtin_ctz(vectors) * NT + (int)threadIdx.x) * kVec<E>;
+        for (uint32_t hit = which(x, j, len, [&](float v) { return v >= from; }); hit; hit &= hit - 1) {
+            const int e = j + __builtin_ctz(hit), at = atomicAdd(&sh.count, 1);
+            if (at < kCand) sh.cand[at] = make_cand(to_f32(x[e]), e);
+        }
+    }
+    __syncthreads();
+    return sh.count;
+}
+
+// Ranks the n collected candidates and gives out the first k.
+template <int NT, typename Out>
+__device__ __forceinline__ void rank_collected(const WideLds<NT>& sh, int n, int k, Out&& out)
+{
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const Cand c = sh.cand[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += sh.cand[j] > c;
+        if (rank < k) out(rank, c);
     }
 }
 
-template <typename E>
-__global__ __launch_bounds__(kRowThreads) void k_distill(const E* __restrict__ logits,
-                                                         const float* __restrict__ t_logp,
-                                                         const int32_t* __restrict__ t_idx, RowArgs a,
-                                                         const float* __restrict__ weight, float* __restrict__ loss,
-                                                         E* __restrict__ grad)
+// Gives out the logits that equal t (NaN: the NaN ones) in the order of their
+// indices, from rank n on, until k are out; returns the number that are out.
+template <typename E, int NT, typename Out>
+__device__ __forceinline__ int fill_equal(const E* __restrict__ x, int len, float t, int n, int k, WideLds<NT>& sh,
+                                          Out&& out)
 {
-    __shared__ Shared sh;
-    __shared__ int li[LIF_TOP_MAX];
-    __shared__ float lq[LIF_TOP_MAX], lt[LIF_TOP_MAX];
-    const int r = blockIdx.x, tid = threadIdx.x;
-    const E* x = logits + r * a.stride;
-    if (tid < a.k) {
-        const int j = t_idx[(int64_t)r * a.k + tid];
-        const bool used = j >= 0 && j < a.V;
-        li[tid] = used ? j : -1;
-        lt[tid] = used ? t_logp[(int64_t)r * a.k + tid] : kNegInf;
-        lq[tid] = used ? expf(lt[tid]) : 0.0f;
-    }
-    float m = kNegInf;
-    for (int j = tid; j < a.V; j += kRowThreads) m = fmaxf(m, to_f32(x[j]));
-    m = block_max(m, sh.part[0]);
-    const float ms = m == kNegInf ? 0.0f : m;
-    double sq = 0.0;
-    for (int i = 0; i < a.k; ++i) sq += (double)lq[i];
-    float s_top = 0.0f, s_rest = 0.0f;
-    int n_top = 0;
-    for (int j = tid; j < a.V; j += kRowThreads) {
-        const float e = exp2f(log2_term(to_f32(x[j]), ms, a.c));
-        bool in = false;
-        for (int i = 0; i < a.k; ++i) in |= li[i] == j;
-        if (in) { s_top += e; ++n_top; } else s_rest += e;
-    }
-    s_top = block_sum(s_top, sh.part[0]);
-    s_rest = block_sum(s_rest, sh.part[1]);
-    const float n_in = block_sum((float)n_top, sh.part[2]);
-    const float s = s_top + s_rest;
-    const bool empty = s == 0.0f, none = sq == 0.0;
-    const float ls = empty ? kNegInf : logf(s);
-    double q_rest = 0.0;
-    if (a.tail && 1.0 - sq >= LIF_DISTILL_TAIL_MIN && n_in < (float)a.V) q_rest = 1.0 - sq;
-    const double scale = a.tail ? 1.0 : 1.0 / sq;
-    if (tid == 0 && loss) {
-        double v = 0.0;
-        for (int i = 0; i < a.k && !none; ++i) {
-            const double q = (double)lq[i] * scale;
-            if (q > 0.0) {
-                const double lp = empty ? (double)kNegInf
-                                        : ((double)to_f32(x[li[i]]) - (double)ms) * a.inv_td - (double)ls;
-                v += q * ((double)lt[i] + log(scale) - lp);
-            } else if (q != q) v = q;
+    const int lane = threadIdx.x & 63, w = (int)threadIdx.x >> 6;
+    for (int base = 0; base < len && n < k; base += NT * kVec<E>) {
+        const int j0 = base + (int)threadIdx.x * kVec<E>;
+        uint32_t hit = which(x, j0, len, [&](float v) { return v == t || (t != t && v != v); });
+        const int mine = __popc(hit);
+        int upto = mine;                // of this wave's lanes so far
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o);
+            if (lane >= o) upto += v;
         }
-        if (!none && q_rest > 0.0) v += q_rest * (log(q_rest) - (empty ? (double)kNegInf : log((double)s_rest) - log((double)s)));
-        loss[r] = (float)v;
+        __syncthreads();
+        if (lane == 63) sh.part[0][w] = __int_as_float(upto);
+        __syncthreads();
+        int rank = n + upto - mine;
+        for (int q = 0; q < NT / 64; ++q) {
+            const int c = __float_as_int(sh.part[0][q]);
+            if (q < w) rank += c;
+            n += c;
+        }
+        for (; hit && rank < k; hit &= hit - 1, ++rank) out(rank, make_cand(t, j0 + __builtin_ctz(hit)));
+    }
+    return min(n, k);
+}
+
+// Number of logits that reach v, over the workgroup.
+template <typename E, int NT>
+__device__ __forceinline__ int count_reaching(const E* __restrict__ x, int len, float v, WideLds<NT>& sh)
+{
+    int n = 0;
+    for (int j = (int)threadIdx.x * kVec<E>; j < len; j += NT * kVec<E>)
+        n += __popc(which(x, j, len, [&](float u) { return u >= v; }));
+    for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.part[0][threadIdx.x >> 6] = __int_as_float(n);
+    __syncthreads();
+    n = 0;
+    for (int q = 0; q < NT / 64; ++q) n += __float_as_int(sh.part[0][q]);
+    return n;
+}
+
+// Gives out(rank, candidate) for the k largest logits of the segment (k <= its
+// length); candidate indices count from the segment's start.
+//
+// The logits that reach the bound are collected in LDS, a little more than k
+// of them as a rule, and each finds its rank by counting those before it.
+// Two things need more.  Fewer than k groups hold anything above -infinity
+// (rows masked to few classes): all such logits are collected, and the places
+// that they leave go to the others in the order of their indices.  More than
+// kCand reach the bound (many equal logits, as in an untrained layer's rows):
+// the bound is raised by halving the interval of keys up to the maximum until
+// few enough reach it, or until it is the k-th largest value itself; then the
+// larger ones are ranked and equal ones fill up by index.
+template <typename E, int NT, int NV, typename Out>
+__device__ __forceinline__ void select_top(const float (&vm)[NV], float m, const E* __restrict__ x, int len, int k,
+                                           WideLds<NT>& sh, Out&& out)
+{
+    float bound = sh.bound;
+    if (bound == kNegInf) bound = key_value(order_key(kNegInf) + 1);
+    int n = collect<E, NT, NV>(vm, x, len, bound, sh);
+    if (n > kCand) {
+        uint32_t lo = order_key(bound), hi = order_key(m) + 1;     // n reach lo; none reach hi
+        while (hi - lo > 1 && n > kCand) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            const int c = count_reaching<E, NT>(x, len, key_value(mid), sh);
+            if (c >= k) lo = mid, n = c;
+            else hi = mid;
+        }
+        const float t = key_value(lo);
+        if (n > kCand) {                // hi = lo + 1: the k-th largest is t
+            n = 0;
+            if (t < m) {
+                n = collect<E, NT, NV>(vm, x, len, key_value(hi), sh);
+                rank_collected<NT>(sh, n, k, out);
+            }
+            fill_equal<E, NT>(x, len, t, n, k, sh, out);
+            return;
+        }
+        n = collect<E, NT, NV>(vm, x, len, t, sh);
+    }
+    rank_collected<NT>(sh, n, k, out);
+    if (n < k) n = fill_equal<E, NT>(x, len, kNegInf, n, k, sh, out);
+    if (n < k) fill_equal<E, NT>(x, len, NAN, n, k, sh, out);
+}
+
+struct LogprobOutputs {
+    float *logp, *entropy, *lse, *top_logp;
+    int32_t* top_idx;
+    const float *g_logp, *g_ent;
+};
+
+// A segment's statistics for the join.
+struct Part {
+    float m, s, u, pad;
+};
+
+template <typename E, int NT, int NV>
+__global__ __launch_bounds__(NT) void k_wide_logprobs(const E* __restrict__ logits, const int32_t* __restrict__ token,
+                                                      RowArgs a, LogprobOutputs o, E* __restrict__ grad,
+                                                      Part* __restrict__ parts, Cand* __restrict__ lists)
+{
+    __shared__ WideLds<NT> sh;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int r = blockIdx.x / a.nseg, sg = blockIdx.x - r * a.nseg;
+    const int j0 = sg * a.seg;
+    const E* x = logits + r * a.stride + j0;
+    Held<E, NT, NV> h;
+    h.load(x, min(a.seg, a.V - j0));
+    float vm[NV];
+    float m = h.maxima(vm);
+    const int k = min(a.k, h.len);
+    if (k > 0) {                        // the maxima of kGroups groups: adjacent threads, or one wave's vectors
+        if constexpr (NT >= kGroups) {
+            constexpr int T = NT / kGroups;
+            const float g = over_lanes<T>(m, Max());
+            if (tid % T == 0) sh.group[tid / T] = g;
+        } else {
+            static_assert(NT * NV == kGroups, "one group a vector");
+#pragma unroll
+            for (int i = 0; i < NV; ++i) sh.group[i * NT + tid] = vm[i];
+        }
+    }
+    m = over_wave(m, Max());
+    if (lane == 0) sh.part[0][w] = m;
+    __syncthreads();
+    m = join_parts<NT>(sh.part[0], Max());
+    const float ms = m == kNegInf ? 0.0f : m;
+    float s = 0.0f, u = 0.0f;
+    h.each([&](float v) {
+        const float z = z_of(v, ms, a.c), e = pow2(z);
+        s += e;
+        u = fmaf(e, z_finite(z), u);
+    });
+    s = over_wave(s, Add());
+    u = over_wave(u, Add());
+    if (lane == 0) sh.part[1][w] = s, sh.part[2][w] = u;
+    if (k > 0 && w == 0) {
+        const float b = bound_of_kth<kGroups>(sh.group, k, lane);
+        if (lane == 0) sh.bound = b;
+    }
+    __syncthreads();
+    s = join_parts<NT>(sh.part[1], Add());
+    u = join_parts<NT>(sh.part[2], Add());
+    if (a.nseg > 1) {
+        const int64_t at = (int64_t)r * a.nseg + sg;
+        if (tid == 0) parts[at] = Part{m, s, u, 0.0f};
+        if (a.k > 0) {
+            Cand* list = lists + at * a.k;
+            for (int i = k + tid; i < a.k; i += NT) list[i] = 0;
+            select_top<E, NT, NV>(vm, m, x, h.len, k, sh, [&](int rank, Cand c) {
+                list[rank] = c - (Cand)j0;          // the index counts from the row's start
+            });
+        }
+        return;
+    }
+    const RowStat st = row_stat(m, s, u);
+    const int tok = token ? token[r] : -1;
+    const bool there = tok >= 0 && tok < a.V;
+    if (tid == 0) {
+        if (o.logp) o.logp[r] = there ? row_logp(st, a, to_f32(x[tok])) : 0.0f;
+        if (o.entropy) o.entropy[r] = st.H;
+        if (o.lse) o.lse[r] = row_lse(st, a);
+    }
+    if (k > 0)
+        select_top<E, NT, NV>(vm, m, x, h.len, k, sh, [&](int rank, Cand c) {
+            o.top_idx[(int64_t)r * a.k + rank] = cand_index(c);
+            o.top_logp[(int64_t)r * a.k + rank] = row_logp(st, a, cand_value(c));
+        });
+    if (!grad) return;
+    E* out = grad + r * a.grad_stride;
+    const float g = there && o.g_logp ? o.g_logp[r] : 0.0f, ge = o.g_ent ? o.g_ent[r] : 0.0f;
+    const float inv_s = st.empty ? 0.0f : a.inv_t / st.s, k0 = st.empty ? 0.0f : fmaf(ge, st.H - st.ls, g);
+    auto value = [&](float v) {
+        const float z = z_of(v, st.m, a.c);
+        return -(pow2(z) * inv_s) * fmaf(ge * kLn2, z_finite(z), k0);
+    };
+    h.store(out, value);
+    __syncthreads();
+    if (tid == 0 && there && !st.empty) out[tok] = from_f32<E>(value(to_f32(x[tok])) + g * a.inv_t);
+}
+
+// Joins the statistics of a row's segments: m, s and u of the whole row, the
+// same in every thread.
+template <int NT>
+__device__ __forceinline__ void join_row(const Part* __restrict__ parts, int nseg, float c, float& m, float& s, float& u,
+                                         float (*part)[NT / 64])
+{
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    m = kNegInf;
+    for (int i = tid; i < nseg; i += NT) m = fmaxf(m, parts[i].m);
+    m = over_wave(m, Max());
+    if (lane == 0) part[0][w] = m;
+    __syncthreads();
+    m = join_parts<NT>(part[0], Max());
+    const float ms = m == kNegInf ? 0.0f : m;
+    s = u = 0.0f;
+    for (int i = tid; i < nseg; i += NT) {
+        const Part p = parts[i];
+        // a segment without anything above -infinity has s = u = 0 (or a NaN)
+        const float d = p.m == kNegInf ? 0.0f : z_of(p.m, ms, c), f = pow2(d);
+        s += p.s * f;
+        u += f * fmaf(p.s, z_finite(d), p.u);
+    }
+    s = over_wave(s, Add());
+    u = over_wave(u, Add());
+    if (lane == 0) part[1][w] = s, part[2][w] = u;
+    __syncthreads();
+    s = join_parts<NT>(part[1], Add());
+    u = join_parts<NT>(part[2], Add());
+    __syncthreads();
+}
+
+constexpr int kJoinThreads = 256;
+constexpr int kJoinHeads = 2048;        // list heads whose k-th largest bounds the row's
+
+struct JoinLds {
+    float part[3][kJoinThreads / 64];
+    Cand bound;
+    int count;
+    Cand cand[kJoinHeads];
+};
+
+// The k largest of the sorted lists of a row's segments: the k-th largest of
+// the lists' first entries bounds the row's k-th largest from below; what
+// reaches it is collected and ranked by counting.
+template <typename Out>
+__device__ __forceinline__ void join_lists(const Cand* __restrict__ lists, int nseg, int k, JoinLds& sh, Out&& out)
+{
+    const int tid = threadIdx.x;
+    const int heads = min(k, min(2 * k / nseg + 2, kJoinHeads / nseg));      // of each list; nseg <= kJoinHeads / 2
+    const int nh = heads * nseg;
+    for (int i = tid; i < nh; i += kJoinThreads) sh.cand[i] = lists[(int64_t)(i / heads) * k + i % heads];
+    if (tid == 0) sh.bound = 1, sh.count = 0;
+    __syncthreads();
+    if (nh >= k)
+        for (int i = tid; i < nh; i += kJoinThreads) {
+            const Cand c = sh.cand[i];
+            int rank = 0;
+            for (int j = 0; j < nh; ++j) rank += sh.cand[j] > c;
+            if (rank == k - 1 && c) sh.bound = c;
+        }
+    __syncthreads();
+    const Cand bound = sh.bound;
+    for (int i = tid; i < nseg * k; i += kJoinThreads) {
+        const Cand c = lists[i];
+        if (c >= bound) {
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < kJoinHeads) sh.cand[at] = c;
+        }
+    }
+    __syncthreads();
+    const int n = sh.count;
+    if (n <= kJoinHeads) {
+        for (int i = tid; i < n; i += kJoinThreads) {
+            const Cand c = sh.cand[i];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += sh.cand[j] > c;
+            if (rank < k) out(rank, c);
+        }
+        return;
+    }
+    for (int i = tid; i < nseg * k; i += kJoinThreads) {        // more than fit: counted in memory
+        const Cand c = lists[i];
+        if (c < bound) continue;
+        int rank = 0;
+        for (int j = 0; j < nseg * k && rank < k; ++j) rank += lists[j] > c;
+        if (rank < k) out(rank, c);
+    }
+}
+
+// Second launch over a row's segments: grid (segments that write the
+// gradient, or one) x rows.
+template <typename E>
+__global__ __launch_bounds__(kJoinThreads) void k_join_logprobs(const E* __restrict__ logits,
+                                                                const int32_t* __restrict__ token, RowArgs a,
+                                                                LogprobOutputs o, E* __restrict__ grad, int pieces,
+                                                                int piece, const Part* __restrict__ parts,
+                                                                const Cand* __restrict__ lists)
+{
+    __shared__ JoinLds sh;
+    const int tid = threadIdx.x;
+    const int r = blockIdx.x / pieces, pc = blockIdx.x - r * pieces;
+    const E* x = logits + r * a.stride;
+    float m, s, u;
+    join_row<kJoinThreads>(parts + (int64_t)r * a.nseg, a.nseg, a.c, m, s, u, sh.part);
+    const RowStat st = row_stat(m, s, u);
+    const int tok = token ? token[r] : -1;
+    const bool there = tok >= 0 && tok < a.V;
+    if (pc == 0) {
+        if (tid == 0) {
+            if (o.logp) o.logp[r] = there ? row_logp(st, a, to_f32(x[tok])) : 0.0f;
+            if (o.entropy) o.entropy[r] = st.H;
+            if (o.lse) o.lse[r] = row_lse(st, a);
+        }
+        if (a.k > 0)
+            join_lists(lists + (int64_t)r * a.nseg * a.k, a.nseg, a.k, sh, [&](int rank, Cand c) {
+                o.top_idx[(int64_t)r * a.k + rank] = cand_index(c);
+                o.top_logp[(int64_t)r * a.k + rank] = row_logp(st, a, cand_value(c));
+            });
     }
     if (!grad) return;
-    const float w = (weight ? weight[r] : 1.0f) * a.inv_t;
-    const double mass = a.tail ? sq + q_rest : 1.0;
-    const float c_top = none || empty ? 0.0f : (float)(mass / (double)s);
-    const float c_rest = none || empty ? 0.0f : q_rest > 0.0 && s_rest > 0.0f ? (float)(mass / (double)s - q_rest / (double)s_rest) : c_top;
-    for (int j = tid; j < a.V; j += kRowThreads) {
-        const float e = exp2f(log2_term(to_f32(x[j]), ms, a.c));
-        double q = 0.0;
-        bool in = false;
-        for (int i = 0; i < a.k; ++i)
-            if (li[i] == j) { in = true; q += (double)lq[i] * scale; }
-        const float v = none || empty ? 0.0f : in ? fmaf(e, c_top, -(float)q) : e * c_rest;
-        grad[r * a.grad_stride + j] = from_f32<E>(v * w);
+    E* out = grad + r * a.grad_stride;
+    const float g = there && o.g_logp ? o.g_logp[r] : 0.0f, ge = o.g_ent ? o.g_ent[r] : 0.0f;
+    const float inv_s = st.empty ? 0.0f : a.inv_t / st.s, k0 = st.empty ? 0.0f : fmaf(ge, st.H - st.ls, g);
+    auto value = [&](float v) {
+        const float z = z_of(v, st.m, a.c);
+        return -(pow2(z) * inv_s) * fmaf(ge * kLn2, z_finite(z), k0);
+    };
+    const int j0 = pc * piece, j1 = min(j0 + piece, a.V);
+    for (int j = j0; j < j1; j += kJoinThreads * kVec<E>) {
+        Held<E, kJoinThreads, 1> h;
+        h.load(x + j, j1 - j);
+        h.store(out + j, value);
     }
+    __syncthreads();
+    if (tid == 0 && there && !st.empty && tok >= j0 && tok < j1)
+        out[tok] = from_f32<E>(value(to_f32(x[tok])) + g * a.inv_t);
+}
+
+// ---------------------------------------------------------------------------
+// Distillation of wide rows.  The listed classes are found with a bitmap in
+// LDS and taken out of the held elements (set to -infinity) before the sums,
+// so that the sum over the others is summed directly; the listed logits are
+// read one by one.  Their gradients are written last.
+// ---------------------------------------------------------------------------
+template <int NT> struct ListLds {
+    int idx[LIF_TOP_MAX];               // -1: unused
+    float lt[LIF_TOP_MAX], q[LIF_TOP_MAX], x[LIF_TOP_MAX];
+    double sq, v;
+    int distinct;
+    float part[3][NT / 64];
+};
+
+// Reads the teacher's list and the student's logits at it (NT >= 64 threads).
+template <typename E, int NT>
+__device__ __forceinline__ void read_list(ListLds<NT>& sh, const E* __restrict__ row, const int32_t* __restrict__ idx,
+                                          const float* __restrict__ lt, int k, int V)
+{
+    for (int i = threadIdx.x; i < k; i += NT) {
+        const int j = idx[i];
+        const bool used = j >= 0 && j < V;
+        sh.idx[i] = used ? j : -1;
+        sh.lt[i] = used ? lt[i] : kNegInf;
+        sh.q[i] = used ? expf(lt[i]) : 0.0f;
+        sh.x[i] = used ? to_f32(row[j]) : kNegInf;
+    }
+}
+
+// Sums over the list, by one wave: q, and the terms e of distinct classes.
+// Entries that repeat an earlier one count once in the latter.
+template <int NT>
+__device__ __forceinline__ float sum_list(ListLds<NT>& sh, int k, float m, float c, int lane)
+{
+    double sq = 0.0;
+    float e = 0.0f;
+    int n = 0;
+    for (int i = lane; i < k; i += 64) {
+        sq += (double)sh.q[i];
+        const int j = sh.idx[i];
+        bool first = j >= 0;
+        for (int p = 0; p < i; ++p) first &= sh.idx[p] != j;
+        if (first) e += pow2(z_of(sh.x[i], m, c)), ++n;
+    }
+    for (int o = 32; o; o >>= 1) sq += __shfl_xor(sq, o), n += __shfl_xor(n, o);
+    if (lane == 0) sh.sq = sq, sh.distinct = n;
+    return over_wave(e, Add());
+}
+
+// The loss of a row, by one wave.
+template <int NT>
+__device__ __forceinline__ double list_loss(const ListLds<NT>& sh, int k, const RowArgs& a, const RowStat& st,
+                                            const Teacher& t, float s_rest, int lane)
+{
+    const double log_scale = t.scale == 1.0 ? 0.0 : log(t.scale);
+    double v = 0.0;
+    for (int i = lane; i < k; i += 64) {
+        if (sh.idx[i] < 0) continue;
+        const double lp = st.empty ? (double)kNegInf : ((double)sh.x[i] - (double)st.m) * a.inv_td - (double)st.ls;
+        v += entry_loss((double)sh.q[i] * t.scale, (double)sh.lt[i] + log_scale, lp);
+    }
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    return t.none ? 0.0 : v + tail_loss(t, s_rest, st);
+}
+
+// The gradients at the listed classes in [j0, j1), after those of the others.
+template <typename E, int NT>
+__device__ __forceinline__ void store_listed(const ListLds<NT>& sh, int k, const RowArgs& a, const RowStat& st,
+                                             const Teacher& t, float c_top, float w, int j0, int j1,
+                                             E* __restrict__ out)
+{
+    for (int i = threadIdx.x; i < k; i += NT) {
+        const int j = sh.idx[i];
+        if (j < j0 || j >= j1) continue;
+        double q = 0.0;                 // repeated entries write the same value
+        for (int p = 0; p < k; ++p)
+            if (sh.idx[p] == j) q += (double)sh.q[p];
+        const float v = t.none || st.empty ? 0.0f : fmaf(pow2(z_of(sh.x[i], st.m, a.c)), c_top, -(float)(q * t.scale));
+        out[j] = from_f32<E>(v * (t.none || st.empty ? 0.0f : w));
+    }
+}
+
+template <typename E, int NT, int NV>
+__global__ __launch_bounds__(NT) void k_wide_distill(const E* __restrict__ logits, const float* __restrict__ t_logp,
+                                                     const int32_t* __restrict__ t_idx, RowArgs a,
+                                                     const float* __restrict__ weight, float* __restrict__ loss,
+                                                     E* __restrict__ grad, Part* __restrict__ parts)
+{
+    constexpr int VEC = kVec<E>;
+    __shared__ ListLds<NT> sh;
+    __shared__ uint32_t bits[NT * NV * VEC / 32];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int r = blockIdx.x / a.nseg, sg = blockIdx.x - r * a.nseg;
+    const int j0 = sg * a.seg;
+    const E* row = logits + r * a.stride;
+    Held<E, NT, NV> h;
+    h.load(row + j0, min(a.seg, a.V - j0));
+    for (int i = tid; i < (h.len + 31) / 32; i += NT) bits[i] = 0;
+    read_list<E, NT>(sh, row, t_idx + (int64_t)r * a.k, t_logp + (int64_t)r * a.k, a.k, a.V);
+    __syncthreads();
+    for (int i = tid; i < a.k; i += NT) {
+        const int j = sh.idx[i] - j0;
+        if (sh.idx[i] >= 0 && j >= 0 && j < h.len) atomicOr(&bits[j >> 5], 1u << (j & 31));
+    }
+    float vm[NV];
+    float m = over_wave(h.maxima(vm), Max());
+    if (lane == 0) sh.part[0][w] = m;
+    __syncthreads();
+    m = join_parts<NT>(sh.part[0], Max());
+    const float ms = m == kNegInf ? 0.0f : m;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (!h.any(i) || h.first(i) >= h.len) continue;
+        const uint32_t b = bits[h.first(i) >> 5] >> (h.first(i) & 31) & ((1u << VEC) - 1u);
+        if (b) h.drop(i, b);
+    }
+    float s = 0.0f;
+    h.each([&](float v) { s += pow2(z_of(v, ms, a.c)); });
+    s = over_wave(s, Add());
+    if (lane == 0) sh.part[1][w] = s;
+    if (a.nseg > 1) {
+        __syncthreads();
+        if (tid == 0) parts[(int64_t)r * a.nseg + sg] = Part{m, join_parts<NT>(sh.part[1], Add()), 0.0f, 0.0f};
+        return;
+    }
+    if (w == 0) {
+        const float e = sum_list<NT>(sh, a.k, ms, a.c, lane);
+        if (lane == 0) sh.part[2][0] = e;
+    }
+    __syncthreads();
+    const float s_rest = join_parts<NT>(sh.part[1], Add()), s_top = sh.part[2][0];
+    const RowStat st = row_stat(m, s_top + s_rest, 0.0f);
+    const Teacher t = teacher_of(sh.sq, a.tail, sh.distinct == a.V);
+    if (loss && w == 0) {
+        const double v = list_loss<NT>(sh, a.k, a, st, t, s_rest, lane);
+        if (lane == 0) loss[r] = (float)v;
+    }
+    if (!grad) return;
+    float c_top, c_rest;
+    grad_factors(t, st, s_rest, c_top, c_rest);
+    const float wt = (weight ? weight[r] : 1.0f) * a.inv_t, f = t.none || st.empty ? 0.0f : c_rest * wt;
+    E* out = grad + r * a.grad_stride;
+    // a row without a gradient may hold a NaN, which 0 f would keep
+    if (t.none || st.empty) h.store(out, [&](float) { return 0.0f; });
+    else h.store(out, [&](float v) { return pow2(z_of(v, st.m, a.c)) * f; });
+    __syncthreads();
+    store_listed<E, NT>(sh, a.k, a, st, t, c_top, wt, 0, a.V, out);
+}
+
+template <typename E>
+__global__ __launch_bounds__(kJoinThreads) void k_join_distill(const E* __restrict__ logits,
+                                                               const float* __restrict__ t_logp,
+                                                               const int32_t* __restrict__ t_idx, RowArgs a,
+                                                               const float* __restrict__ weight,
+                                                               float* __restrict__ loss, E* __restrict__ grad,
+                                                               int pieces, int piece, const Part* __restrict__ parts)
+{
+    constexpr int NT = kJoinThreads;
+    __shared__ ListLds<NT> sh;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int r = blockIdx.x / pieces, pc = blockIdx.x - r * pieces;
+    const E* row = logits + r * a.stride;
+    read_list<E, NT>(sh, row, t_idx + (int64_t)r * a.k, t_logp + (int64_t)r * a.k, a.k, a.V);
+    float m, s_rest, u;
+    join_row<NT>(parts + (int64_t)r * a.nseg, a.nseg, a.c, m, s_rest, u, sh.part);
+    const float ms = m == kNegInf ? 0.0f : m;
+    if (w == 0) {
+        const float e = sum_list<NT>(sh, a.k, ms, a.c, lane);
+        if (lane == 0) sh.part[2][0] = e;
+    }
+    __syncthreads();
+    const RowStat st = row_stat(m, sh.part[2][0] + s_rest, 0.0f);
+    const Teacher t = teacher_of(sh.sq, a.tail, sh.distinct == a.V);
+    if (loss && pc == 0 && w == 0) {
+        const double v = list_loss<NT>(sh, a.k, a, st, t, s_rest, lane);
+        if (lane == 0) loss[r] = (float)v;
+    }
+    if (!grad) return;
+    float c_top, c_rest;
+    grad_factors(t, st, s_rest, c_top, c_rest);
+    const float wt = (weight ? weight[r] : 1.0f) * a.inv_t, f = t.none || st.empty ? 0.0f : c_rest * wt;
+    E* out = grad + r * a.grad_stride;
+    const int j0 = pc * piece, j1 = min(j0 + piece, a.V);
+    for (int j = j0; j < j1; j += NT * kVec<E>) {
+        Held<E, NT, 1> h;
+        h.load(row + j, j1 - j);
+        if (t.none || st.empty) h.store(out + j, [&](float) { return 0.0f; });
+        else h.store(out + j, [&](float v) { return pow2(z_of(v, st.m, a.c)) * f; });
+    }
+    __syncthreads();
+    store_listed<E, NT>(sh, a.k, a, st, t, c_top, wt, j0, j1, out);
 }
 
 int check_rows(const lif_rows_params* p)
@@ -218,13 +1124,26 @@ int check_rows(const lif_rows_params* p)
     if (p->flags & ~LIF_DISTILL_TAIL) return LIF_ERR_ARG;
     if (p->stride < p->V || p->grad_stride < p->V) return LIF_ERR_ARG;
     if (!(p->temperature >= 1.0 / 1048576.0 && p->temperature <= 1048576.0)) return LIF_ERR_ARG;
-    if (p->k > LIF_TOP_MAX) return LIF_ERR_SIZE;
+    if (p->k > LIF_TOP_MAX || p->V > kMaxV) return LIF_ERR_SIZE;
     return LIF_OK;
 }
 
-RowArgs row_args(const lif_rows_params& p)
-{
+// Workgroup shapes of the wide kernels: threads and vectors a thread.
+struct Shape {
+    int nt, nv;
+};
+constexpr Shape kShapes[] = {{64, 4}, {256, 4}, {512, 8}, {512, 16}, {1024, 16}};
+constexpr int kNumShapes = sizeof(kShapes) / sizeof(kShapes[0]);
+
+struct RowPlan {
     RowArgs a;
+    int shape;                          // -1: narrow
+};
+
+RowPlan plan_rows(const lif_rows_params& p)
+{
+    RowPlan q;
+    RowArgs& a = q.a;
     a.R = p.R;
     a.V = p.V;
     a.k = p.k;
@@ -234,7 +1153,74 @@ RowArgs row_args(const lif_rows_params& p)
     a.inv_t = (float)(1.0 / p.temperature);
     a.inv_td = 1.0 / p.temperature;
     a.tail = p.flags & LIF_DISTILL_TAIL;
-    return a;
+    a.nseg = 1;
+    a.seg = p.V;
+    q.shape = -1;
+    if (p.V <= kNarrow) return q;
+    const int vec = p.dtype == LIF_F32 ? 4 : 8;
+    auto holds = [&](int s) { return kShapes[s].nt * kShapes[s].nv * vec; };
+    int seg = p.V;
+    if (seg > holds(kNumShapes - 1)) seg = holds(2);            // does not fit: segments of a middling size
+    // few rows: enough segments for two workgroups on every CU, of 512 vectors at least
+    if (p.R > 0 && p.R < 256 && seg > 512 * vec) {
+        const int want = (512 + p.R - 1) / p.R;
+        int few = (p.V + want - 1) / want;
+        few = few < 512 * vec ? 512 * vec : few;
+        if (few < seg) seg = few;
+    }
+    a.nseg = (p.V + seg - 1) / seg;
+    a.seg = ((p.V + a.nseg - 1) / a.nseg + vec - 1) / vec * vec;
+    a.nseg = (p.V + a.seg - 1) / a.seg;
+    for (q.shape = 0; holds(q.shape) < a.seg;) ++q.shape;
+    return q;
+}
+
+size_t rows_ws(const RowPlan& q)
+{
+    return q.a.nseg > 1 ? (size_t)q.a.R * q.a.nseg * (sizeof(Part) + (size_t)q.a.k * sizeof(Cand)) : 0;
+}
+
+// Calls fn(element, threads, vectors) with types that carry them.
+template <int N> struct Int { static constexpr int value = N; };
+template <typename Fn> void with_shape(int dtype, int shape, Fn&& fn)
+{
+    with_dtype(dtype, [&](auto e) {
+        switch (shape) {
+            case 0: fn(e, Int<kShapes[0].nt>(), Int<kShapes[0].nv>()); break;
+            case 1: fn(e, Int<kShapes[1].nt>(), Int<kShapes[1].nv>()); break;
+            case 2: fn(e, Int<kShapes[2].nt>(), Int<kShapes[2].nv>()); break;
+            case 3: fn(e, Int<kShapes[3].nt>(), Int<kShapes[3].nv>()); break;
+            default: fn(e, Int<kShapes[4].nt>(), Int<kShapes[4].nv>()); break;
+        }
+    });
+}
+// Lanes for a narrow row: up to 24 elements a lane.
+template <typename Fn> void with_lanes(int dtype, int V, Fn&& fn)
+{
+    with_dtype(dtype, [&](auto e) {
+        if (V <= 24) fn(e, Int<1>());
+        else if (V <= 48) fn(e, Int<2>());
+        else if (V <= 96) fn(e, Int<4>());
+        else if (V <= 192) fn(e, Int<8>());
+        else fn(e, Int<16>());
+    });
+}
+static_assert((kNarrow + 15) / 16 <= kNarrowPer && 24 <= kNarrowPer, "a lane's elements have a bit each");
+
+size_t narrow_lds(int V, int L) { return (size_t)(kNarrowThreads / L) * narrow_pitch(V, L) * sizeof(float); }
+
+// The pieces of a row that the second launch writes gradients of.
+void gradient_pieces(const RowArgs& a, bool grad, int elem, int& pieces, int& piece)
+{
+    const int unit = kJoinThreads * (16 / elem);                // one vector a thread
+    pieces = 1;
+    piece = a.V;
+    if (!grad) return;
+    const int units = (a.V + unit - 1) / unit;
+    int want = a.R >= 1024 ? 1 : (1024 + a.R - 1) / a.R;
+    if (want > units) want = units;
+    piece = (units + want - 1) / want * unit;
+    pieces = (a.V + piece - 1) / piece;
 }
 
 }  // namespace
@@ -243,7 +1229,7 @@ RowArgs row_args(const lif_rows_params& p)
 extern "C" size_t lif_rows_workspace_size(const lif_rows_params* p)
 {
     if (lif::check_rows(p) != LIF_OK) return 0;
-    return 0;
+    return lif::rows_ws(lif::plan_rows(*p));
 }
 
 extern "C" int lif_token_logprobs(const void* logits, const int32_t* token, const lif_rows_params* p, float* logp,
@@ -256,17 +1242,39 @@ extern "C" int lif_token_logprobs(const void* logits, const int32_t* token, cons
     if (rc) return rc;
     if ((p->R > 0 && !logits) || (p->flags & LIF_DISTILL_TAIL)) return LIF_ERR_ARG;
     if (p->k > 0 && p->R > 0 && (!top_logp != !top_idx)) return LIF_ERR_ARG;
-    const size_t need = lif_rows_workspace_size(p);
-    if (need > 0 && !ws) return LIF_ERR_ARG;
+    RowPlan q = plan_rows(*p);
+    const size_t need = rows_ws(q);
+    if (need > 0 && (!ws || (uintptr_t)ws % sizeof(Part))) return LIF_ERR_ARG;
     if (ws_bytes < need) return LIF_ERR_WORKSPACE;
     if (p->R == 0) return LIF_OK;
-    RowArgs a = row_args(*p);
+    RowArgs& a = q.a;
     if (!top_idx) a.k = 0;
-    with_dtype(p->dtype, [&](auto tag) {
-        using E = decltype(tag);
-        TIMED_LAUNCH("token_logprobs", k_token_logprobs<E>, dim3(p->R), dim3(kRowThreads), 0, (hipStream_t)stream,
-                     (const E*)logits, token, a, logp, entropy, lse, top_logp, top_idx, grad_logp, grad_entropy,
-                     (E*)grad);
+    const hipStream_t s = (hipStream_t)stream;
+    if (q.shape < 0) {
+        with_lanes(p->dtype, p->V, [&](auto e, auto l) {
+            using E = decltype(e);
+            constexpr int L = decltype(l)::value, per = kNarrowThreads / L;
+            TIMED_LAUNCH("token_logprobs", (k_narrow_logprobs<E, L>), dim3((a.R + per - 1) / per),
+                         dim3(kNarrowThreads), narrow_lds(a.V, L), s, (const E*)logits, token, a, logp, entropy, lse,
+                         top_logp, top_idx, grad_logp, grad_entropy, (E*)grad);
+        });
+        return check_launch();
+    }
+    if ((int64_t)a.R * a.nseg >= ((int64_t)1 << 31)) return LIF_ERR_SIZE;
+    const LogprobOutputs o{logp, entropy, lse, top_logp, top_idx, grad_logp, grad_entropy};
+    Part* parts = (Part*)ws;
+    Cand* lists = (Cand*)(parts + (size_t)a.R * a.nseg);
+    with_shape(p->dtype, q.shape, [&](auto e, auto nt, auto nv) {
+        using E = decltype(e);
+        constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+        TIMED_LAUNCH("token_logprobs", (k_wide_logprobs<E, NT, NV>), dim3(a.R * a.nseg), dim3(NT), 0, s,
+                     (const E*)logits, token, a, o, (E*)grad, parts, lists);
+        if (a.nseg > 1) {
+            int pieces, piece;
+            gradient_pieces(a, grad != nullptr, sizeof(E), pieces, piece);
+            TIMED_LAUNCH("token_logprobs_join", (k_join_logprobs<E>), dim3(a.R * pieces), dim3(kJoinThreads), 0, s,
+                         (const E*)logits, token, a, o, (E*)grad, pieces, piece, parts, lists);
+        }
     });
     return check_launch();
 }
@@ -279,15 +1287,35 @@ extern "C" int lif_distill_top(const void* logits, const float* teacher_logp, co
     const int rc = check_rows(p);
     if (rc) return rc;
     if (p->R > 0 && (!logits || (!loss && !grad) || (p->k > 0 && (!teacher_logp || !teacher_idx)))) return LIF_ERR_ARG;
-    const size_t need = lif_rows_workspace_size(p);
-    if (need > 0 && !ws) return LIF_ERR_ARG;
+    const RowPlan q = plan_rows(*p);
+    const size_t need = rows_ws(q);
+    if (need > 0 && (!ws || (uintptr_t)ws % sizeof(Part))) return LIF_ERR_ARG;
     if (ws_bytes < need) return LIF_ERR_WORKSPACE;
     if (p->R == 0) return LIF_OK;
-    const RowArgs a = row_args(*p);
-    with_dtype(p->dtype, [&](auto tag) {
-        using E = decltype(tag);
-        TIMED_LAUNCH("distill_top", k_distill<E>, dim3(p->R), dim3(kRowThreads), 0, (hipStream_t)stream,
-                     (const E*)logits, teacher_logp, teacher_idx, a, weight, loss, (E*)grad);
+    const RowArgs& a = q.a;
+    const hipStream_t s = (hipStream_t)stream;
+    if (q.shape < 0) {
+        with_lanes(p->dtype, p->V, [&](auto e, auto l) {
+            using E = decltype(e);
+            constexpr int L = decltype(l)::value, per = kNarrowThreads / L;
+            TIMED_LAUNCH("distill_top", (k_narrow_distill<E, L>), dim3((a.R + per - 1) / per), dim3(kNarrowThreads),
+                         narrow_lds(a.V, L), s, (const E*)logits, teacher_logp, teacher_idx, a, weight, loss, (E*)grad);
+        });
+        return check_launch();
+    }
+    if ((int64_t)a.R * a.nseg >= ((int64_t)1 << 31)) return LIF_ERR_SIZE;
+    Part* parts = (Part*)ws;
+    with_shape(p->dtype, q.shape, [&](auto e, auto nt, auto nv) {
+        using E = decltype(e);
+        constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+        TIMED_LAUNCH("distill_top", (k_wide_distill<E, NT, NV>), dim3(a.R * a.nseg), dim3(NT), 0, s, (const E*)logits,
+                     teacher_logp, teacher_idx, a, weight, loss, (E*)grad, parts);
+        if (a.nseg > 1) {
+            int pieces, piece;
+            gradient_pieces(a, grad != nullptr, sizeof(E), pieces, piece);
+            TIMED_LAUNCH("distill_join", (k_join_distill<E>), dim3(a.R * pieces), dim3(kJoinThreads), 0, s,
+                         (const E*)logits, teacher_logp, teacher_idx, a, weight, loss, (E*)grad, pieces, piece, parts);
+        }
     });
     return check_launch();
 }
