@@ -3,11 +3,10 @@
 // (lif_token_logprobs), and distillation from a teacher's likeliest classes
 // (lif_distill_top), each with its gradient.
 //
-// With m the row's largest logit and c = log2(e) / temperature, every term
-// is e_j = 2^{z_j} with z_j = (x_j - m) c <= 0; S = sum e_j and U = sum e_j z_j
-// give p_j = e_j / S, lse = m / temperature + log S and the entropy
-// log S - log(2) U / S.  m is subtracted before the product, so that rows of
-// huge logits (masks at the type's lowest value) stay exact.
+// With m the row's largest logit, c = log2(e) / temperature and o = m c
+// rounded, every term is e_j = 2^{z_j} with z_j = x_j c - o, one FMA;
+// S = sum e_j and U = sum e_j z_j give p_j = e_j / S, the entropy
+// log S - log(2) U / S, and, with the rounding error of o put back, lse.
 //
 // Rows of up to kNarrow logits: a workgroup stages many rows in LDS with
 // contiguous loads, and a few lanes work on each (k_narrow_*).  Longer rows:
@@ -31,36 +30,53 @@ constexpr int kNarrowThreads = 256;
 constexpr int kMaxV = 1 << 24;
 constexpr int kCand = 512;              // candidates of a top-k selection held in LDS
 
-// A row's result from its maximum and sums.
-struct RowStat {
-    float m;                            // largest logit, 0 where nothing is above -infinity
-    float s, ls;                        // S and its logarithm
-    float H;                            // entropy
-    bool empty;                         // nothing above -infinity
-};
-
 struct RowArgs {
     int R, V, k;
     int64_t stride, grad_stride;
-    float c, inv_t;                     // log2(e) / temperature, 1 / temperature
+    float c, c_pow2, inv_t;             // log2(e) / temperature, a power of two from there on, 1 / temperature
     double inv_td;
     bool tail;
     int nseg, seg;                      // segments of a row and their length
 };
 
-__device__ __forceinline__ float z_of(float x, float m, float c) { return (x - m) * c; }
+// The exponents of a row: z = x c - o, for the largest logit m.  The rounding
+// of o multiplies all terms by the same factor, below 2^64 while |m| c < 2^30.
+// From there on (rows masked by the type's lowest value, say) logits that
+// differ lie at least 64 / c apart, so that the largest ones alone count: any
+// power of two from c on makes the products exact, e = 1 for those and below
+// 2^-64 for others, and 2^-60 one that does not overflow from |m| = 2^100 on.
+struct Exponent {
+    float m, c, o;                      // m is 0 where nothing is above -infinity
+    bool plain;                         // c is the row's
+    __device__ __forceinline__ Exponent(float largest, const RowArgs& a)
+    {
+        m = largest == kNegInf ? 0.0f : largest;
+        plain = fabsf(m * a.c) < 0x1p30f;
+        c = plain ? a.c : fabsf(m) < 0x1p100f ? a.c_pow2 : 0x1p-60f;
+        o = m * c;
+    }
+    __device__ __forceinline__ float z(float x) const { return fmaf(x, c, -o); }
+};
 __device__ __forceinline__ float pow2(float z) { return __builtin_amdgcn_exp2f(z); }
 // z where it is multiplied by e: -infinity (e = 0) must not give a NaN.
 __device__ __forceinline__ float z_finite(float z) { return fmaxf(z, -200.0f); }
 
-__device__ __forceinline__ RowStat row_stat(float m, float s, float u)
+// A row's result from its exponents and sums.
+struct RowStat {
+    float m, s;
+    float lz, ls;                       // log S as summed, and with the rounding of o put back
+    float H;                            // entropy
+    bool empty;                         // nothing above -infinity
+};
+__device__ __forceinline__ RowStat row_stat(const Exponent& x, float s, float u)
 {
     RowStat r;
-    r.m = m == kNegInf ? 0.0f : m;
+    r.m = x.m;
     r.s = s;
     r.empty = s == 0.0f;
-    r.ls = r.empty ? kNegInf : logf(s);
-    r.H = r.empty ? 0.0f : r.ls - kLn2 * (u / s);
+    r.lz = r.empty ? kNegInf : logf(s);
+    r.ls = r.lz - kLn2 * fmaf(x.m, x.c, -x.o);
+    r.H = r.empty ? 0.0f : r.lz - kLn2 * (u / s);
     return r;
 }
 __device__ __forceinline__ float row_logp(const RowStat& r, const RowArgs& a, float x)
@@ -182,16 +198,15 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_logprobs(
     const int n = rl < rows ? (a.V - l + L - 1) / L : 0;       // this lane's elements x[L i]
     float m = kNegInf, s = 0.0f, u = 0.0f;
     for (int i = 0; i < n; ++i) m = fmaxf(m, x[L * i]);
-    m = over_lanes<L>(m, Max());
-    const float ms = m == kNegInf ? 0.0f : m;
+    const Exponent ex(over_lanes<L>(m, Max()), a);
     for (int i = 0; i < n; ++i) {
-        const float z = z_of(x[L * i], ms, a.c), e = pow2(z);
+        const float z = ex.z(x[L * i]), e = pow2(z);
         s += e;
         u = fmaf(e, z_finite(z), u);
     }
     s = over_lanes<L>(s, Add());
     u = over_lanes<L>(u, Add());
-    const RowStat st = row_stat(m, s, u);
+    const RowStat st = row_stat(ex, s, u);
     int tok = -1;
     bool there = false;
     if (rl < rows) {
@@ -239,8 +254,8 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_logprobs(
     const float g = there && g_logp ? g_logp[r] : 0.0f, ge = rl < rows && g_ent ? g_ent[r] : 0.0f;
     const float inv_s = st.empty ? 0.0f : 1.0f / st.s;
     for (int i = 0; i < n; ++i) {
-        const float z = z_of(x[L * i], st.m, a.c), p = pow2(z) * inv_s;
-        const float lp = st.empty ? 0.0f : fmaf(kLn2, z_finite(z), -st.ls);
+        const float z = ex.z(x[L * i]), p = pow2(z) * inv_s;
+        const float lp = st.empty ? 0.0f : fmaf(kLn2, z_finite(z), -st.lz);
         float v = -p * fmaf(ge, lp + st.H, g);
         if (there && l + L * i == tok && !st.empty) v += g;
         x[L * i] = v * a.inv_t;
@@ -272,7 +287,7 @@ __device__ __forceinline__ double entry_loss(double q, double log_q, double lp)
 __device__ __forceinline__ double tail_loss(const Teacher& t, float s_rest, const RowStat& st)
 {
     if (!(t.q_rest > 0.0)) return 0.0;
-    const double lp = st.empty ? (double)kNegInf : (double)logf(s_rest) - (double)st.ls;
+    const double lp = st.empty ? (double)kNegInf : (double)logf(s_rest) - (double)st.lz;
     return t.q_rest * (log(t.q_rest) - lp);
 }
 // dloss/dz_j = e_j c_top - q_j for a listed class, e_j c_rest for another.
@@ -318,17 +333,16 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
     }
     float m = kNegInf, s_top = 0.0f, s_rest = 0.0f;
     for (int i = 0; i < n; ++i) m = fmaxf(m, x[L * i]);
-    m = over_lanes<L>(m, Max());
-    const float ms = m == kNegInf ? 0.0f : m;
+    const Exponent ex(over_lanes<L>(m, Max()), a);
     for (int i = 0; i < n; ++i) {
-        const float e = pow2(z_of(x[L * i], ms, a.c));
+        const float e = pow2(ex.z(x[L * i]));
         if (listed >> i & 1) s_top += e;
         else s_rest += e;
     }
     s_top = over_lanes<L>(s_top, Add());
     s_rest = over_lanes<L>(s_rest, Add());
     const int n_top = over_lanes<L>((int)__popc(listed), [](int p, int o) { return p + o; });
-    const RowStat st = row_stat(m, s_top + s_rest, 0.0f);
+    const RowStat st = row_stat(ex, s_top + s_rest, 0.0f);
     const Teacher t = teacher_of(sq, a.tail, n_top == a.V);
     const double log_scale = t.scale == 1.0 ? 0.0 : log(t.scale);
     if (loss) {
@@ -349,7 +363,7 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
     const float w = rl < rows ? (weight ? weight[r] : 1.0f) * a.inv_t : 0.0f;
     const bool dead = t.none || st.empty;
     for (int i = 0; i < n; ++i) {
-        const float e = pow2(z_of(x[L * i], st.m, a.c));
+        const float e = pow2(ex.z(x[L * i]));
         x[L * i] = dead ? 0.0f : e * ((listed >> i & 1) ? c_top : c_rest);
     }
     // the lanes of a row hold its elements apart, so every element is changed by one lane
@@ -365,7 +379,10 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
 // ---------------------------------------------------------------------------
 // Wide rows.  A workgroup of NT threads holds a segment in registers: NV
 // vectors of 16 bytes a thread, vector i of thread t at element
-// (i NT + t) VEC.  Elements past the segment count as -infinity.
+// (i NT + t) VEC, at whatever address that is: the order of a row's sums does
+// not depend on where the row lies.  (Rows off the 16-byte grid cost more:
+// 4096 x 50021 bf16 138 us, 112 for 50048.)  What a vector holds past the
+// segment counts as -infinity.
 // ---------------------------------------------------------------------------
 template <typename E> constexpr int kVec = 16 / (int)sizeof(E);
 
@@ -400,7 +417,7 @@ template <typename E, int NT, int NV> struct Held {
 
     __device__ __forceinline__ void load(const E* __restrict__ x, int n)
     {
-        len = n;
+        len = __builtin_amdgcn_readfirstlane(n);               // the same in all threads
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (!any(i)) continue;
@@ -702,7 +719,7 @@ struct Part {
 };
 
 template <typename E, int NT, int NV>
-__global__ __launch_bounds__(NT) void k_wide_logprobs(const E* __restrict__ logits, const int32_t* __restrict__ token,
+__global__ __launch_bounds__(NT, 4) void k_wide_logprobs(const E* __restrict__ logits, const int32_t* __restrict__ token,
                                                       RowArgs a, LogprobOutputs o, E* __restrict__ grad,
                                                       Part* __restrict__ parts, Cand* __restrict__ lists)
 {
@@ -731,10 +748,10 @@ __global__ __launch_bounds__(NT) void k_wide_logprobs(const E* __restrict__ logi
     if (lane == 0) sh.part[0][w] = m;
     __syncthreads();
     m = join_parts<NT>(sh.part[0], Max());
-    const float ms = m == kNegInf ? 0.0f : m;
+    const Exponent ex(m, a);
     float s = 0.0f, u = 0.0f;
     h.each([&](float v) {
-        const float z = z_of(v, ms, a.c), e = pow2(z);
+        const float z = ex.z(v), e = pow2(z);
         s += e;
         u = fmaf(e, z_finite(z), u);
     });
@@ -760,7 +777,7 @@ __global__ __launch_bounds__(NT) void k_wide_logprobs(const E* __restrict__ logi
         }
         return;
     }
-    const RowStat st = row_stat(m, s, u);
+    const RowStat st = row_stat(ex, s, u);
     const int tok = token ? token[r] : -1;
     const bool there = tok >= 0 && tok < a.V;
     if (tid == 0) {
@@ -776,9 +793,9 @@ __global__ __launch_bounds__(NT) void k_wide_logprobs(const E* __restrict__ logi
     if (!grad) return;
     E* out = grad + r * a.grad_stride;
     const float g = there && o.g_logp ? o.g_logp[r] : 0.0f, ge = o.g_ent ? o.g_ent[r] : 0.0f;
-    const float inv_s = st.empty ? 0.0f : a.inv_t / st.s, k0 = st.empty ? 0.0f : fmaf(ge, st.H - st.ls, g);
+    const float inv_s = st.empty ? 0.0f : a.inv_t / st.s, k0 = st.empty ? 0.0f : fmaf(ge, st.H - st.lz, g);
     auto value = [&](float v) {
-        const float z = z_of(v, st.m, a.c);
+        const float z = ex.z(v);
         return -(pow2(z) * inv_s) * fmaf(ge * kLn2, z_finite(z), k0);
     };
     h.store(out, value);
@@ -786,25 +803,28 @@ __global__ __launch_bounds__(NT) void k_wide_logprobs(const E* __restrict__ logi
     if (tid == 0 && there && !st.empty) out[tok] = from_f32<E>(value(to_f32(x[tok])) + g * a.inv_t);
 }
 
-// Joins the statistics of a row's segments: m, s and u of the whole row, the
+// Joins the statistics of a row's segments: the row's exponents, s and u, the
 // same in every thread.
 template <int NT>
-__device__ __forceinline__ void join_row(const Part* __restrict__ parts, int nseg, float c, float& m, float& s, float& u,
-                                         float (*part)[NT / 64])
+__device__ __forceinline__ Exponent join_row(const Part* __restrict__ parts, const RowArgs& a, float& s, float& u,
+                                             float (*part)[NT / 64])
 {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    m = kNegInf;
-    for (int i = tid; i < nseg; i += NT) m = fmaxf(m, parts[i].m);
+    float m = kNegInf;
+    for (int i = tid; i < a.nseg; i += NT) m = fmaxf(m, parts[i].m);
     m = over_wave(m, Max());
     if (lane == 0) part[0][w] = m;
     __syncthreads();
-    m = join_parts<NT>(part[0], Max());
-    const float ms = m == kNegInf ? 0.0f : m;
+    const Exponent ex(join_parts<NT>(part[0], Max()), a);
     s = u = 0.0f;
-    for (int i = tid; i < nseg; i += NT) {
+    for (int i = tid; i < a.nseg; i += NT) {
         const Part p = parts[i];
+        const Exponent own(p.m, a);
         // a segment without anything above -infinity has s = u = 0 (or a NaN)
-        const float d = p.m == kNegInf ? 0.0f : z_of(p.m, ms, c), f = pow2(d);
+        float d = own.o - ex.o;
+        if (p.m == kNegInf || own.m == ex.m) d = 0.0f;
+        else if (!own.plain || !ex.plain) d = -200.0f;
+        const float f = pow2(d);
         s += p.s * f;
         u += f * fmaf(p.s, z_finite(d), p.u);
     }
@@ -815,6 +835,7 @@ __device__ __forceinline__ void join_row(const Part* __restrict__ parts, int nse
     s = join_parts<NT>(part[1], Add());
     u = join_parts<NT>(part[2], Add());
     __syncthreads();
+    return ex;
 }
 
 constexpr int kJoinThreads = 256;
@@ -888,9 +909,9 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_logprobs(const E* __restr
     const int tid = threadIdx.x;
     const int r = blockIdx.x / pieces, pc = blockIdx.x - r * pieces;
     const E* x = logits + r * a.stride;
-    float m, s, u;
-    join_row<kJoinThreads>(parts + (int64_t)r * a.nseg, a.nseg, a.c, m, s, u, sh.part);
-    const RowStat st = row_stat(m, s, u);
+    float s, u;
+    const Exponent ex = join_row<kJoinThreads>(parts + (int64_t)r * a.nseg, a, s, u, sh.part);
+    const RowStat st = row_stat(ex, s, u);
     const int tok = token ? token[r] : -1;
     const bool there = tok >= 0 && tok < a.V;
     if (pc == 0) {
@@ -908,9 +929,9 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_logprobs(const E* __restr
     if (!grad) return;
     E* out = grad + r * a.grad_stride;
     const float g = there && o.g_logp ? o.g_logp[r] : 0.0f, ge = o.g_ent ? o.g_ent[r] : 0.0f;
-    const float inv_s = st.empty ? 0.0f : a.inv_t / st.s, k0 = st.empty ? 0.0f : fmaf(ge, st.H - st.ls, g);
+    const float inv_s = st.empty ? 0.0f : a.inv_t / st.s, k0 = st.empty ? 0.0f : fmaf(ge, st.H - st.lz, g);
     auto value = [&](float v) {
-        const float z = z_of(v, st.m, a.c);
+        const float z = ex.z(v);
         return -(pow2(z) * inv_s) * fmaf(ge * kLn2, z_finite(z), k0);
     };
     const int j0 = pc * piece, j1 = min(j0 + piece, a.V);
@@ -932,44 +953,42 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_logprobs(const E* __restr
 // ---------------------------------------------------------------------------
 template <int NT> struct ListLds {
     int idx[LIF_TOP_MAX];               // -1: unused
+    int first[LIF_TOP_MAX];             // the one entry of its class that counts there
     float lt[LIF_TOP_MAX], q[LIF_TOP_MAX], x[LIF_TOP_MAX];
-    double sq, v;
-    int distinct;
+    double sq;
+    int used, distinct;
     float part[3][NT / 64];
 };
 
-// Reads the teacher's list and the student's logits at it (NT >= 64 threads).
-template <typename E, int NT>
-__device__ __forceinline__ void read_list(ListLds<NT>& sh, const E* __restrict__ row, const int32_t* __restrict__ idx,
-                                          const float* __restrict__ lt, int k, int V)
+// Entry i of the teacher's list and the student's logit there.
+template <int NT>
+__device__ __forceinline__ void keep_entry(ListLds<NT>& sh, int i, int j, float lt, float x)
 {
-    for (int i = threadIdx.x; i < k; i += NT) {
-        const int j = idx[i];
-        const bool used = j >= 0 && j < V;
-        sh.idx[i] = used ? j : -1;
-        sh.lt[i] = used ? lt[i] : kNegInf;
-        sh.q[i] = used ? expf(lt[i]) : 0.0f;
-        sh.x[i] = used ? to_f32(row[j]) : kNegInf;
-    }
+    const bool used = j >= 0;
+    sh.idx[i] = j;
+    sh.lt[i] = used ? lt : kNegInf;
+    sh.q[i] = used ? expf(lt) : 0.0f;
+    sh.x[i] = used ? x : kNegInf;
 }
 
 // Sums over the list, by one wave: q, and the terms e of distinct classes.
-// Entries that repeat an earlier one count once in the latter.
 template <int NT>
-__device__ __forceinline__ float sum_list(ListLds<NT>& sh, int k, float m, float c, int lane)
+__device__ __forceinline__ float sum_list(ListLds<NT>& sh, int k, const Exponent& ex, int lane)
 {
     double sq = 0.0;
     float e = 0.0f;
-    int n = 0;
+    int used = 0, distinct = 0;
     for (int i = lane; i < k; i += 64) {
         sq += (double)sh.q[i];
-        const int j = sh.idx[i];
-        bool first = j >= 0;
-        for (int p = 0; p < i; ++p) first &= sh.idx[p] != j;
-        if (first) e += pow2(z_of(sh.x[i], m, c)), ++n;
+        used += sh.idx[i] >= 0;
+        if (sh.first[i]) e += pow2(ex.z(sh.x[i])), ++distinct;
     }
-    for (int o = 32; o; o >>= 1) sq += __shfl_xor(sq, o), n += __shfl_xor(n, o);
-    if (lane == 0) sh.sq = sq, sh.distinct = n;
+    for (int o = 32; o; o >>= 1) {
+        sq += __shfl_xor(sq, o);
+        used += __shfl_xor(used, o);
+        distinct += __shfl_xor(distinct, o);
+    }
+    if (lane == 0) sh.sq = sq, sh.used = used, sh.distinct = distinct;
     return over_wave(e, Add());
 }
 
@@ -991,23 +1010,27 @@ __device__ __forceinline__ double list_loss(const ListLds<NT>& sh, int k, const 
 
 // The gradients at the listed classes in [j0, j1), after those of the others.
 template <typename E, int NT>
-__device__ __forceinline__ void store_listed(const ListLds<NT>& sh, int k, const RowArgs& a, const RowStat& st,
+__device__ __forceinline__ void store_listed(const ListLds<NT>& sh, int k, const Exponent& ex, const RowStat& st,
                                              const Teacher& t, float c_top, float w, int j0, int j1,
                                              E* __restrict__ out)
 {
+    const bool dead = t.none || st.empty;
     for (int i = threadIdx.x; i < k; i += NT) {
         const int j = sh.idx[i];
         if (j < j0 || j >= j1) continue;
-        double q = 0.0;                 // repeated entries write the same value
-        for (int p = 0; p < k; ++p)
-            if (sh.idx[p] == j) q += (double)sh.q[p];
-        const float v = t.none || st.empty ? 0.0f : fmaf(pow2(z_of(sh.x[i], st.m, a.c)), c_top, -(float)(q * t.scale));
-        out[j] = from_f32<E>(v * (t.none || st.empty ? 0.0f : w));
+        double q = (double)sh.q[i];
+        if (sh.distinct < sh.used) {    // repeated entries write the same value
+            q = 0.0;
+            for (int p = 0; p < k; ++p)
+                if (sh.idx[p] == j) q += (double)sh.q[p];
+        }
+        const float v = dead ? 0.0f : fmaf(pow2(ex.z(sh.x[i])), c_top, -(float)(q * t.scale));
+        out[j] = from_f32<E>(dead ? 0.0f : v * w);
     }
 }
 
 template <typename E, int NT, int NV>
-__global__ __launch_bounds__(NT) void k_wide_distill(const E* __restrict__ logits, const float* __restrict__ t_logp,
+__global__ __launch_bounds__(NT, 4) void k_wide_distill(const E* __restrict__ logits, const float* __restrict__ t_logp,
                                                      const int32_t* __restrict__ t_idx, RowArgs a,
                                                      const float* __restrict__ weight, float* __restrict__ loss,
                                                      E* __restrict__ grad, Part* __restrict__ parts)
@@ -1019,21 +1042,45 @@ __global__ __launch_bounds__(NT) void k_wide_distill(const E* __restrict__ logit
     const int r = blockIdx.x / a.nseg, sg = blockIdx.x - r * a.nseg;
     const int j0 = sg * a.seg;
     const E* row = logits + r * a.stride;
+    static_assert(NT >= 64 && LIF_TOP_MAX <= 128, "at most two entries a thread");
+    // the list first: its loads are short, and the logits there are on their
+    // way with the row
+    int ej[2] = {-1, -1};
+    float el[2], ex_[2];
+#pragma unroll
+    for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q) {
+        const int i = tid + q * NT;
+        if (i >= a.k) continue;
+        const int j = t_idx[(int64_t)r * a.k + i];
+        el[q] = t_logp[(int64_t)r * a.k + i];
+        if (j >= 0 && j < a.V) {
+            ej[q] = j;
+            ex_[q] = to_f32(row[j]);
+        }
+    }
     Held<E, NT, NV> h;
     h.load(row + j0, min(a.seg, a.V - j0));
     for (int i = tid; i < (h.len + 31) / 32; i += NT) bits[i] = 0;
-    read_list<E, NT>(sh, row, t_idx + (int64_t)r * a.k, t_logp + (int64_t)r * a.k, a.k, a.V);
+#pragma unroll
+    for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q)
+        if (tid + q * NT < a.k) keep_entry(sh, tid + q * NT, ej[q], el[q], ex_[q]);
     __syncthreads();
-    for (int i = tid; i < a.k; i += NT) {
-        const int j = sh.idx[i] - j0;
-        if (sh.idx[i] >= 0 && j >= 0 && j < h.len) atomicOr(&bits[j >> 5], 1u << (j & 31));
+#pragma unroll
+    for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q) {
+        const int i = tid + q * NT, j = ej[q] - j0;
+        if (i >= a.k) continue;
+        bool first = false;
+        if (ej[q] >= 0 && j >= 0 && j < h.len) {
+            first = !(atomicOr(&bits[j >> 5], 1u << (j & 31)) >> (j & 31) & 1);
+        }
+        sh.first[i] = first;
     }
     float vm[NV];
     float m = over_wave(h.maxima(vm), Max());
     if (lane == 0) sh.part[0][w] = m;
     __syncthreads();
     m = join_parts<NT>(sh.part[0], Max());
-    const float ms = m == kNegInf ? 0.0f : m;
+    const Exponent ex(m, a);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         if (!h.any(i) || h.first(i) >= h.len) continue;
@@ -1041,7 +1088,7 @@ __global__ __launch_bounds__(NT) void k_wide_distill(const E* __restrict__ logit
         if (b) h.drop(i, b);
     }
     float s = 0.0f;
-    h.each([&](float v) { s += pow2(z_of(v, ms, a.c)); });
+    h.each([&](float v) { s += pow2(ex.z(v)); });
     s = over_wave(s, Add());
     if (lane == 0) sh.part[1][w] = s;
     if (a.nseg > 1) {
@@ -1050,27 +1097,28 @@ __global__ __launch_bounds__(NT) void k_wide_distill(const E* __restrict__ logit
         return;
     }
     if (w == 0) {
-        const float e = sum_list<NT>(sh, a.k, ms, a.c, lane);
+        const float e = sum_list<NT>(sh, a.k, ex, lane);
         if (lane == 0) sh.part[2][0] = e;
     }
     __syncthreads();
     const float s_rest = join_parts<NT>(sh.part[1], Add()), s_top = sh.part[2][0];
-    const RowStat st = row_stat(m, s_top + s_rest, 0.0f);
+    const RowStat st = row_stat(ex, s_top + s_rest, 0.0f);
     const Teacher t = teacher_of(sh.sq, a.tail, sh.distinct == a.V);
+    if (grad) {
+        float c_top, c_rest;
+        grad_factors(t, st, s_rest, c_top, c_rest);
+        const float wt = (weight ? weight[r] : 1.0f) * a.inv_t, f = t.none || st.empty ? 0.0f : c_rest * wt;
+        E* out = grad + r * a.grad_stride;
+        // a row without a gradient may hold a NaN, which 0 f would keep
+        if (t.none || st.empty) h.store(out, [&](float) { return 0.0f; });
+        else h.store(out, [&](float v) { return pow2(ex.z(v)) * f; });
+        __syncthreads();
+        store_listed<E, NT>(sh, a.k, ex, st, t, c_top, wt, 0, a.V, out);
+    }
     if (loss && w == 0) {
         const double v = list_loss<NT>(sh, a.k, a, st, t, s_rest, lane);
         if (lane == 0) loss[r] = (float)v;
     }
-    if (!grad) return;
-    float c_top, c_rest;
-    grad_factors(t, st, s_rest, c_top, c_rest);
-    const float wt = (weight ? weight[r] : 1.0f) * a.inv_t, f = t.none || st.empty ? 0.0f : c_rest * wt;
-    E* out = grad + r * a.grad_stride;
-    // a row without a gradient may hold a NaN, which 0 f would keep
-    if (t.none || st.empty) h.store(out, [&](float) { return 0.0f; });
-    else h.store(out, [&](float v) { return pow2(z_of(v, st.m, a.c)) * f; });
-    __syncthreads();
-    store_listed<E, NT>(sh, a.k, a, st, t, c_top, wt, 0, a.V, out);
 }
 
 template <typename E>
@@ -1086,16 +1134,25 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_distill(const E* __restri
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int r = blockIdx.x / pieces, pc = blockIdx.x - r * pieces;
     const E* row = logits + r * a.stride;
-    read_list<E, NT>(sh, row, t_idx + (int64_t)r * a.k, t_logp + (int64_t)r * a.k, a.k, a.V);
-    float m, s_rest, u;
-    join_row<NT>(parts + (int64_t)r * a.nseg, a.nseg, a.c, m, s_rest, u, sh.part);
-    const float ms = m == kNegInf ? 0.0f : m;
+    for (int i = tid; i < a.k; i += NT) {
+        const int j = t_idx[(int64_t)r * a.k + i];
+        const bool used = j >= 0 && j < a.V;
+        keep_entry(sh, i, used ? j : -1, t_logp[(int64_t)r * a.k + i], used ? to_f32(row[j]) : 0.0f);
+    }
+    __syncthreads();
+    for (int i = tid; i < a.k; i += NT) {
+        bool first = sh.idx[i] >= 0;
+        for (int p = 0; p < i; ++p) first &= sh.idx[p] != sh.idx[i];
+        sh.first[i] = first;
+    }
+    float s_rest, u;
+    const Exponent ex = join_row<NT>(parts + (int64_t)r * a.nseg, a, s_rest, u, sh.part);
     if (w == 0) {
-        const float e = sum_list<NT>(sh, a.k, ms, a.c, lane);
+        const float e = sum_list<NT>(sh, a.k, ex, lane);
         if (lane == 0) sh.part[2][0] = e;
     }
     __syncthreads();
-    const RowStat st = row_stat(m, sh.part[2][0] + s_rest, 0.0f);
+    const RowStat st = row_stat(ex, sh.part[2][0] + s_rest, 0.0f);
     const Teacher t = teacher_of(sh.sq, a.tail, sh.distinct == a.V);
     if (loss && pc == 0 && w == 0) {
         const double v = list_loss<NT>(sh, a.k, a, st, t, s_rest, lane);
@@ -1111,10 +1168,10 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_distill(const E* __restri
         Held<E, NT, 1> h;
         h.load(row + j, j1 - j);
         if (t.none || st.empty) h.store(out + j, [&](float) { return 0.0f; });
-        else h.store(out + j, [&](float v) { return pow2(z_of(v, st.m, a.c)) * f; });
+        else h.store(out + j, [&](float v) { return pow2(ex.z(v)) * f; });
     }
     __syncthreads();
-    store_listed<E, NT>(sh, a.k, a, st, t, c_top, wt, j0, j1, out);
+    store_listed<E, NT>(sh, a.k, ex, st, t, c_top, wt, j0, j1, out);
 }
 
 int check_rows(const lif_rows_params* p)
@@ -1150,6 +1207,7 @@ RowPlan plan_rows(const lif_rows_params& p)
     a.stride = p.stride;
     a.grad_stride = p.grad_stride;
     a.c = (float)(1.4426950408889634074 / p.temperature);
+    a.c_pow2 = (float)exp2(ceil(log2((double)a.c)));
     a.inv_t = (float)(1.0 / p.temperature);
     a.inv_td = 1.0 / p.temperature;
     a.tail = p.flags & LIF_DISTILL_TAIL;
