@@ -26,7 +26,7 @@ namespace {
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kNegInf = -INFINITY;
 constexpr int kNarrow = 256;            // longest row of the narrow kernels
-constexpr int kNarrowThreads = 256;
+constexpr int kNarrowThreads = 128;
 constexpr int kMaxV = 1 << 24;
 constexpr int kCand = 512;              // candidates of a top-k selection held in LDS
 
@@ -101,6 +101,11 @@ __device__ __forceinline__ float key_value(uint32_t k)
     if (k == 1) return NAN;
     return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
 }
+// The same order as signed integers, with a value below all for an element
+// that is out.
+constexpr int kTaken = INT32_MIN;
+__device__ __forceinline__ int signed_key(float v) { return (int)(order_key(v) ^ 0x80000000u); }
+__device__ __forceinline__ float signed_value(int k) { return key_value((uint32_t)k ^ 0x80000000u); }
 // Larger logits first, then smaller indices.
 using Cand = unsigned long long;
 __device__ __forceinline__ Cand make_cand(float v, int j) { return ((Cand)order_key(v) << 32) | (0xffffffffu - (uint32_t)j); }
@@ -197,8 +202,10 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_logprobs(
     float* x = sh + rl * pitch + l;
     const int n = rl < rows ? (a.V - l + L - 1) / L : 0;       // this lane's elements x[L i]
     float m = kNegInf, s = 0.0f, u = 0.0f;
+#pragma unroll 4
     for (int i = 0; i < n; ++i) m = fmaxf(m, x[L * i]);
     const Exponent ex(over_lanes<L>(m, Max()), a);
+#pragma unroll 4
     for (int i = 0; i < n; ++i) {
         const float z = ex.z(x[L * i]), e = pow2(z);
         s += e;
@@ -218,36 +225,36 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_logprobs(
             if (lse) lse[r] = row_lse(st, a);
         }
     }
-    uint32_t taken = 0;                         // elements already given out
-    for (int q = 0; q < a.k; ++q) {
-        // the largest left, ties and NaN by index: (v, j), j = V while there is none
-        float v = kNegInf;
-        int at = -1;
-        for (int i = 0; i < n; ++i) {
-            const float w = x[L * i];
-            if (!(taken >> i & 1) && (w > v || (at < 0 && w == w))) v = w, at = i;
-        }
-        int j = at < 0 ? a.V : l + L * at;
-        auto better = [&](float w, int o) {
-            if (o < a.V && (j == a.V || w > v || (w == v && o < j))) v = w, j = o;
-        };
-        if constexpr (L >= 2) better(dpp<0xb1>(v), dpp<0xb1>(j));
-        if constexpr (L >= 4) better(dpp<0x4e>(v), dpp<0x4e>(j));
-        if constexpr (L >= 8) better(dpp<0x141>(v), dpp<0x141>(j));
-        if constexpr (L >= 16) better(dpp<0x140>(v), dpp<0x140>(j));
-        if (j == a.V) {                         // only NaN left: by index
-            int first = a.V;
-            for (int i = n - 1; i >= 0; --i)
-                if (!(taken >> i & 1)) first = l + L * i;
-            j = over_lanes<L>(first, [](int p, int o) { return min(p, o); });
-            v = NAN;
-        }
-        if (rl < rows) {
-            if (j % L == l) taken |= 1u << (j / L);
-            if (l == 0) {
-                top_idx[r * a.k + q] = j;
-                top_logp[r * a.k + q] = row_logp(st, a, v);
+    if (a.k > 0) {                              // the elements become their keys
+        int* key = reinterpret_cast<int*>(x);
+        for (int i = 0; i < n; ++i) key[L * i] = signed_key(x[L * i]);
+        for (int q = 0; q < a.k; ++q) {
+            int best = kTaken, at = 0;          // equal ones by index
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                const int w = key[L * i];
+                if (w > best) best = w, at = i;
             }
+            int j = l + L * at;
+            auto better = [&](int w, int o) {
+                if (w > best || (w == best && o < j)) best = w, j = o;
+            };
+            if constexpr (L >= 2) better(dpp<0xb1>(best), dpp<0xb1>(j));
+            if constexpr (L >= 4) better(dpp<0x4e>(best), dpp<0x4e>(j));
+            if constexpr (L >= 8) better(dpp<0x141>(best), dpp<0x141>(j));
+            if constexpr (L >= 16) better(dpp<0x140>(best), dpp<0x140>(j));
+            if (rl < rows) {
+                if (j % L == l) key[j - l] = kTaken;
+                if (l == 0) {
+                    top_idx[r * a.k + q] = j;
+                    top_logp[r * a.k + q] = row_logp(st, a, signed_value(best));
+                }
+            }
+        }
+        if (grad) {                             // the elements again
+            __syncthreads();
+            stage_rows(logits + row0 * a.stride, a.stride, rows, a.V, pitch, sh);
+            __syncthreads();
         }
     }
     if (!grad) return;
@@ -287,18 +294,19 @@ __device__ __forceinline__ double entry_loss(double q, double log_q, double lp)
 __device__ __forceinline__ double tail_loss(const Teacher& t, float s_rest, const RowStat& st)
 {
     if (!(t.q_rest > 0.0)) return 0.0;
-    const double lp = st.empty ? (double)kNegInf : (double)logf(s_rest) - (double)st.lz;
-    return t.q_rest * (log(t.q_rest) - lp);
+    const float lp = st.empty ? kNegInf : logf(s_rest) - st.lz;
+    return t.q_rest * (double)(logf((float)t.q_rest) - lp);
 }
 // dloss/dz_j = e_j c_top - q_j for a listed class, e_j c_rest for another.
 __device__ __forceinline__ void grad_factors(const Teacher& t, const RowStat& st, float s_rest, float& c_top,
                                              float& c_rest)
 {
     const double mass = t.scale == 1.0 && !t.none ? t.sq + t.q_rest : 1.0;
-    c_top = t.none || st.empty ? 0.0f : (float)(mass / (double)st.s);
+    c_top = t.none || st.empty ? 0.0f : (float)mass / st.s;
     c_rest = c_top;
+    // mass / S - q_rest / s_rest: the difference, which may be small, in float64
     if (!t.none && !st.empty && t.q_rest > 0.0 && s_rest > 0.0f)
-        c_rest = (float)(mass / (double)st.s - t.q_rest / (double)s_rest);
+        c_rest = (float)(mass * (double)s_rest - t.q_rest * (double)st.s) / st.s / s_rest;
 }
 
 template <typename E, int L>
@@ -324,16 +332,20 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
     const int32_t* idx = t_idx + r * a.k;
     const float* lt = t_logp + r * a.k;
     uint32_t listed = 0;                        // this lane's elements that the teacher lists
-    double sq = 0.0;                            // the same order of sums in every lane
+#pragma unroll 4
     for (int i = 0; i < k; ++i) {
         const int j = idx[i];
-        if (j < 0 || j >= a.V) continue;
-        if (j % L == l) listed |= 1u << (j / L);
-        sq += (double)expf(lt[i]);
+        if (j >= 0 && j < a.V && j % L == l) listed |= 1u << (j / L);
     }
+    double sq = 0.0;
+    for (int i = l; i < k; i += L)
+        if (idx[i] >= 0 && idx[i] < a.V) sq += (double)expf(lt[i]);
+    for (int o = 1; o < L; o <<= 1) sq += __shfl_xor(sq, o);
     float m = kNegInf, s_top = 0.0f, s_rest = 0.0f;
+#pragma unroll 4
     for (int i = 0; i < n; ++i) m = fmaxf(m, x[L * i]);
     const Exponent ex(over_lanes<L>(m, Max()), a);
+#pragma unroll 4
     for (int i = 0; i < n; ++i) {
         const float e = pow2(ex.z(x[L * i]));
         if (listed >> i & 1) s_top += e;
@@ -344,7 +356,7 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
     const int n_top = over_lanes<L>((int)__popc(listed), [](int p, int o) { return p + o; });
     const RowStat st = row_stat(ex, s_top + s_rest, 0.0f);
     const Teacher t = teacher_of(sq, a.tail, n_top == a.V);
-    const double log_scale = t.scale == 1.0 ? 0.0 : log(t.scale);
+    const double log_scale = t.scale == 1.0 ? 0.0 : (double)logf((float)t.scale);
     if (loss) {
         double v = 0.0;
         for (int i = l; i < k; i += L) {
@@ -362,6 +374,8 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
     grad_factors(t, st, s_rest, c_top, c_rest);
     const float w = rl < rows ? (weight ? weight[r] : 1.0f) * a.inv_t : 0.0f;
     const bool dead = t.none || st.empty;
+    c_top *= w;
+    c_rest *= w;
     for (int i = 0; i < n; ++i) {
         const float e = pow2(ex.z(x[L * i]));
         x[L * i] = dead ? 0.0f : e * ((listed >> i & 1) ? c_top : c_rest);
@@ -369,9 +383,8 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
     // the lanes of a row hold its elements apart, so every element is changed by one lane
     for (int i = 0; i < k && !dead; ++i) {
         const int j = idx[i];
-        if (j >= 0 && j < a.V && j % L == l) row[j] -= (float)((double)expf(lt[i]) * t.scale);
+        if (j >= 0 && j < a.V && j % L == l) row[j] -= (float)((double)expf(lt[i]) * t.scale) * w;
     }
-    for (int i = 0; i < n; ++i) x[L * i] *= dead ? 0.0f : w;
     __syncthreads();
     unstage_rows(grad + row0 * a.grad_stride, a.grad_stride, rows, a.V, pitch, sh);
 }
@@ -997,7 +1010,7 @@ template <int NT>
 __device__ __forceinline__ double list_loss(const ListLds<NT>& sh, int k, const RowArgs& a, const RowStat& st,
                                             const Teacher& t, float s_rest, int lane)
 {
-    const double log_scale = t.scale == 1.0 ? 0.0 : log(t.scale);
+    const double log_scale = t.scale == 1.0 ? 0.0 : (double)logf((float)t.scale);
     double v = 0.0;
     for (int i = lane; i < k; i += 64) {
         if (sh.idx[i] < 0) continue;
@@ -1252,18 +1265,20 @@ template <typename Fn> void with_shape(int dtype, int shape, Fn&& fn)
         }
     });
 }
-// Lanes for a narrow row: up to 24 elements a lane.
+// Lanes for a narrow row: up to 16 elements a lane (128000 x 20 f32 with 5
+// alternatives: 12 us; with up to 24 elements 14.5, with up to 6 13;
+// 200000 x 40 f32 distillation 40, 35, 55).
 template <typename Fn> void with_lanes(int dtype, int V, Fn&& fn)
 {
     with_dtype(dtype, [&](auto e) {
-        if (V <= 24) fn(e, Int<1>());
-        else if (V <= 48) fn(e, Int<2>());
-        else if (V <= 96) fn(e, Int<4>());
-        else if (V <= 192) fn(e, Int<8>());
+        if (V <= 16) fn(e, Int<1>());
+        else if (V <= 32) fn(e, Int<2>());
+        else if (V <= 64) fn(e, Int<4>());
+        else if (V <= 128) fn(e, Int<8>());
         else fn(e, Int<16>());
     });
 }
-static_assert((kNarrow + 15) / 16 <= kNarrowPer && 24 <= kNarrowPer, "a lane's elements have a bit each");
+static_assert((kNarrow + 15) / 16 <= kNarrowPer && 16 <= kNarrowPer, "a lane's elements have a bit each");
 
 size_t narrow_lds(int V, int L) { return (size_t)(kNarrowThreads / L) * narrow_pitch(V, L) * sizeof(float); }
 
