@@ -18,6 +18,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 import os
 from dataclasses import dataclass
@@ -828,35 +829,42 @@ def softplus_grad(x, grad_d, beta: float, stream=None):
 # ---------------------------------------------------------------------------
 
 _DTYPES = None
+_HERE = contextlib.nullcontext()
 
 
 def _dtype_code(name, t):
     global _DTYPES
-    torch = _torch()
     if _DTYPES is None:
+        torch = _torch()
         _DTYPES = {torch.float32: LIF_F32, torch.bfloat16: LIF_BF16, torch.float16: LIF_F16}
-    if t.dtype not in _DTYPES:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
-    return _DTYPES[t.dtype]
+    return code
 
 
-def _on(dev, stream):
+def _on(torch, dev, stream):
     """The context that an operator's buffers and launches belong to: the
     inputs' GPU, and `stream` when one is given (memory is then taken for that
     stream, which has to wait for the inputs)."""
-    torch = _torch()
     if stream is not None:
         return torch.cuda.stream(stream)
-    if dev.index is not None and dev.index != torch.cuda.current_device():
+    if dev.index != torch._C._cuda_getDevice():
         return torch.cuda.device(dev)
-    return contextlib.nullcontext()
+    return _HERE
+
+
+def _raw_stream(torch, dev, stream) -> int:
+    """The HIP stream of a call (without the objects that _stream makes: these
+    calls are short)."""
+    return torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
 
 
 def _expect(name, t, shape, dtype, dev):
     """A contiguous device tensor of this shape and type (None stays None)."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != dev:
+    if t.shape != shape or t.dtype != dtype or t.device != dev:
         raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} on {dev}, "
                          f"not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.contiguous()
@@ -865,18 +873,30 @@ def _expect(name, t, shape, dtype, dev):
 def _rows_of(name, t, shape, dtype, dev):
     """A device tensor of this shape and type whose last axis is contiguous
     (a copy of one that is not)."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != dev:
+    if t.shape != shape or t.dtype != dtype or t.device != dev:
         raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} on {dev}, "
                          f"not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
 
 
-def _workspace(need, ws, dev):
+@functools.lru_cache(maxsize=256)
+def _gated_ws(B, T, D, dtype) -> int:
+    """lif_gated_scan_workspace_size: it depends on sizes and type only."""
+    return lif_gated_scan_workspace_size(lif_gated_params(B, T, D, dtype, 0, 0, 0, 0, 0, 0, 0, 0))
+
+
+@functools.lru_cache(maxsize=256)
+def _rows_ws(R, V, k, dtype) -> int:
+    """lif_rows_workspace_size: it depends on sizes and type only."""
+    return lif_rows_workspace_size(lif_rows_params(R, V, k, dtype, V, V, 1.0, 0, 0))
+
+
+def _workspace(torch, need, ws, dev):
     """(pointer, bytes, the tensor that holds them) of a workspace."""
     if need == 0:
         return None, 0, None
     if ws is None or ws.numel() * ws.element_size() < need or ws.device != dev:
-        ws = _torch().empty(need, dtype=_torch().uint8, device=dev)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
     return ws.data_ptr(), ws.numel() * ws.element_size(), ws
 
 
@@ -909,13 +929,13 @@ def gated_scan(x, f, length=None, h_first=None, coupled: bool = True, marks: boo
     h_first = _expect("h_first", h_first, (B, D), torch.float32, dev)
     p = lif_gated_params(B, T, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), x.stride(1), f.stride(0),
                          f.stride(1), 0, 0)
-    with _on(dev, stream):
+    with _on(torch, dev, stream):
         h = torch.empty((B, T, D), dtype=x.dtype, device=dev) if states else None
         last = torch.empty((B, D), dtype=torch.float32, device=dev)
         mk = torch.empty((B, -(-T // LIF_GATED_MARK), D), dtype=torch.float32, device=dev) if marks else None
-        wp, wn, ws = _workspace(lif_gated_scan_workspace_size(p), ws, dev)
+        wp, wn, ws = _workspace(torch, _gated_ws(B, T, D, code), ws, dev)
         rc = lif_gated_scan(x.data_ptr(), f.data_ptr(), _ptr(length), _ptr(h_first), ctypes.byref(p), _ptr(h),
-                            last.data_ptr(), _ptr(mk), wp, wn, _stream(stream))
+                            last.data_ptr(), _ptr(mk), wp, wn, _raw_stream(torch, dev, stream))
     _check("lif_gated_scan", rc)
     return GatedOut(h, last, mk)
 
@@ -935,14 +955,14 @@ def gated_scan_backward(x, f, marks, grad_h=None, grad_last=None, length=None, c
     grad_last = _expect("grad_last", grad_last, (B, D), torch.float32, dev)
     p = lif_gated_params(B, T, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), x.stride(1), f.stride(0),
                          f.stride(1), *((0, 0) if grad_h is None else grad_h.stride()[:2]))
-    with _on(dev, stream):
+    with _on(torch, dev, stream):
         gx = torch.empty((B, T, D), dtype=x.dtype, device=dev)
         gf = torch.empty((B, T, D), dtype=x.dtype, device=dev)
         g0 = torch.empty((B, D), dtype=torch.float32, device=dev)
-        wp, wn, ws = _workspace(lif_gated_scan_workspace_size(p), ws, dev)
+        wp, wn, ws = _workspace(torch, _gated_ws(B, T, D, code), ws, dev)
         rc = lif_gated_scan_backward(x.data_ptr(), f.data_ptr(), _ptr(length), marks.data_ptr(), _ptr(grad_h),
                                      _ptr(grad_last), ctypes.byref(p), gx.data_ptr(), gf.data_ptr(), g0.data_ptr(),
-                                     wp, wn, _stream(stream))
+                                     wp, wn, _raw_stream(torch, dev, stream))
     _check("lif_gated_scan_backward", rc)
     return gx, gf, g0
 
@@ -963,10 +983,10 @@ def gated_step(x, f, state, slot=None, coupled: bool = True, stream=None):
         raise ValueError(f"state must be a contiguous float32 tensor [n_slots, {D}] on {dev}")
     slot = _expect("slot", slot, (B,), torch.int32, dev)
     p = lif_gated_params(B, 1, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), 0, f.stride(0), 0, 0, 0)
-    with _on(dev, stream):
+    with _on(torch, dev, stream):
         h = torch.empty((B, D), dtype=x.dtype, device=dev)
         rc = lif_gated_step(x.data_ptr(), f.data_ptr(), _ptr(slot), state.data_ptr(), state.shape[0], ctypes.byref(p),
-                            h.data_ptr(), _stream(stream))
+                            h.data_ptr(), _raw_stream(torch, dev, stream))
     _check("lif_gated_step", rc)
     return h
 
@@ -1004,7 +1024,7 @@ def token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 1.0, gr
     tokens = _expect("tokens", tokens, (R,), torch.int32, dev)
     grad_logp = _expect("grad_logp", grad_logp, (R,), torch.float32, dev)
     grad_entropy = _expect("grad_entropy", grad_entropy, (R,), torch.float32, dev)
-    with _on(dev, stream):
+    with _on(torch, dev, stream):
         logp, ent, lse = torch.empty((3, R), dtype=torch.float32, device=dev).unbind(0)
         tv = ti = grad = None
         if k > 0:
@@ -1012,10 +1032,10 @@ def token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 1.0, gr
             ti = torch.empty((R, k), dtype=torch.int32, device=dev)
         if grad_logp is not None or grad_entropy is not None:
             grad = torch.empty((R, V), dtype=logits.dtype, device=dev)
-        wp, wn, ws = _workspace(lif_rows_workspace_size(p), ws, dev)
+        wp, wn, ws = _workspace(torch, _rows_ws(R, V, p.k, p.dtype), ws, dev)
         rc = lif_token_logprobs(logits.data_ptr(), _ptr(tokens), ctypes.byref(p), logp.data_ptr(), ent.data_ptr(),
                                 lse.data_ptr(), _ptr(tv), _ptr(ti), _ptr(grad_logp), _ptr(grad_entropy), _ptr(grad),
-                                wp, wn, _stream(stream))
+                                wp, wn, _raw_stream(torch, dev, stream))
     _check("lif_token_logprobs", rc)
     return LogprobOut(logp, ent, lse, tv, ti, grad)
 
@@ -1033,11 +1053,11 @@ def distill_top(logits, teacher_logp, teacher_idx, temperature: float = 1.0, tai
     teacher_logp = _expect("teacher_logp", teacher_logp, (R, p.k), torch.float32, dev)
     teacher_idx = _expect("teacher_idx", teacher_idx, (R, p.k), torch.int32, dev)
     weight = _expect("weight", weight, (R,), torch.float32, dev)
-    with _on(dev, stream):
+    with _on(torch, dev, stream):
         loss = torch.empty(R, dtype=torch.float32, device=dev)
         grad = torch.empty((R, V), dtype=logits.dtype, device=dev) if want_grad else None
-        wp, wn, ws = _workspace(lif_rows_workspace_size(p), ws, dev)
+        wp, wn, ws = _workspace(torch, _rows_ws(R, V, p.k, p.dtype), ws, dev)
         rc = lif_distill_top(logits.data_ptr(), teacher_logp.data_ptr(), teacher_idx.data_ptr(), ctypes.byref(p),
-                             _ptr(weight), loss.data_ptr(), _ptr(grad), wp, wn, _stream(stream))
+                             _ptr(weight), loss.data_ptr(), _ptr(grad), wp, wn, _raw_stream(torch, dev, stream))
     _check("lif_distill_top", rc)
     return loss, grad
