@@ -393,9 +393,8 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
 // Wide rows.  A workgroup of NT threads holds a segment in registers: NV
 // vectors of 16 bytes a thread, vector i of thread t at element
 // (i NT + t) VEC, at whatever address that is: the order of a row's sums does
-// not depend on where the row lies.  (Rows off the 16-byte grid cost more:
-// 4096 x 50021 bf16 138 us, 112 for 50048.)  What a vector holds past the
-// segment counts as -infinity.
+// not depend on where the row lies.  What a vector holds past the segment
+// counts as -infinity.
 // ---------------------------------------------------------------------------
 template <typename E> constexpr int kVec = 16 / (int)sizeof(E);
 
@@ -428,27 +427,90 @@ template <typename E, int NT, int NV> struct Held {
     __device__ __forceinline__ bool any(int i) const { return i * NT * VEC < len; }
     __device__ __forceinline__ float get(int i, int e) const { return unpack<E>(v[i], e); }
 
+    // The vector at element j, element by element.
+    __device__ __forceinline__ void load_each(uint32_t (&w)[4], const E* __restrict__ x, int j) const
+    {
+        float f[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = j + e < len ? to_f32(x[j + e]) : kNegInf;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if constexpr (sizeof(E) == 4) w[k] = __float_as_uint(f[k]);
+            else w[k] = pack_pair<E>(f[2 * k], f[2 * k + 1]);
+    }
+    // Whole vectors are loaded wide.  The one that the segment's end cuts is read
+    // by its thread apart and put in its place afterwards: a branch for it at
+    // every vector makes the code outgrow the instruction cache (4096 x 50048
+    // bf16 distillation 168 -> 212 us).
+    //
+    // Rows of 16-bit elements off the 4-byte grid: wide loads there take a
+    // quarter longer (4096 x 50001 bf16 111 us, 91 for 50002).  So a thread
+    // loads from one element before its vector, on the grid, gets the last
+    // element from the next lane's first word, and shifts; every thread ends
+    // up with the elements that it has in any other row.  The first vector is
+    // then read like the last.
     __device__ __forceinline__ void load(const E* __restrict__ x, int n)
     {
         len = __builtin_amdgcn_readfirstlane(n);               // the same in all threads
+        const bool odd = sizeof(E) == 2 && ((uintptr_t)x & 2);
+        const int cut = len / VEC;                             // the vector that the end cuts, if any
+        const bool mine = len % VEC && (int)threadIdx.x == cut % NT;
+        uint32_t edge[4], head[4];
+        if (!odd) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (!any(i)) continue;
-            const int j = first(i);
-            if (j + VEC <= n) {
-                const Words<E> q = *reinterpret_cast<const Words<E>*>(x + j);
+            for (int i = 0; i < NV; ++i) load_wide(i, x, 0);
+            if (mine) load_each(edge, x, cut * VEC);
+        } else {
+            const bool last = (threadIdx.x & 63) == 63;
+            uint32_t end[NV];                                  // the last element, where the next lane has it not
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[i][k] = q.w[k];
-            } else {
-                float f[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] = j + e < n ? to_f32(x[j + e]) : kNegInf;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if constexpr (sizeof(E) == 4) v[i][k] = __float_as_uint(f[k]);
-                    else v[i][k] = pack_pair<E>(f[2 * k], f[2 * k + 1]);
+            for (int i = 0; i < NV; ++i) {
+                load_wide(i, x, 1);
+                end[i] = 0;
+                const int j = first(i);
+                if (j + VEC <= len && (last || j + 2 * VEC > len))
+                    end[i] = *reinterpret_cast<const uint16_t*>(x + j + VEC - 1);
             }
+            if (mine) load_each(edge, x, cut * VEC);
+            if (threadIdx.x == 0) load_each(head, x, 0);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int j = first(i);
+                const uint32_t next = (uint32_t)dpp<0x130>((int)v[i][0]);      // of the next lane
+                const uint32_t tail = last || j + 2 * VEC > len ? end[i] : next;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t u = __builtin_amdgcn_alignbyte(k < 3 ? v[i][k + 1] : tail, v[i][k], 2);
+                    v[i][k] = j + VEC <= len ? u : none();
+                }
+            }
+            if (threadIdx.x == 0)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[0][k] = head[k];
         }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i == cut / NT && mine)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[i][k] = edge[k];
+    }
+    // Vector i from `back` elements before its place, if the segment has all of
+    // its elements (and, with back, it is not the first).
+    __device__ __forceinline__ void load_wide(int i, const E* __restrict__ x, int back)
+    {
+        const int j = first(i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[i][k] = none();
+        if (j + VEC <= len && j >= back) {
+            const Words<E> q = *reinterpret_cast<const Words<E>*>(x + j - back);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[i][k] = q.w[k];
+        }
+    }
+    static __device__ __forceinline__ uint32_t none()
+    {
+        if constexpr (sizeof(E) == 4) return __float_as_uint(kNegInf);
+        else return pack_pair<E>(kNegInf, kNegInf);
     }
     // From here on the elements and the length count as new values to the
     // compiler, which otherwise keeps all elements unpacked, and a mask for
@@ -495,34 +557,30 @@ template <typename E, int NT, int NV> struct Held {
             if constexpr (sizeof(E) == 4) {
                 if (bits >> k & 1) v[i][k] = __float_as_uint(kNegInf);
             } else {
-                const uint32_t none = pack_pair<E>(kNegInf, kNegInf);
-                if (bits >> (2 * k) & 1) v[i][k] = (v[i][k] & 0xffff0000u) | (none & 0xffffu);
-                if (bits >> (2 * k + 1) & 1) v[i][k] = (v[i][k] & 0xffffu) | (none & 0xffff0000u);
+                if (bits >> (2 * k) & 1) v[i][k] = (v[i][k] & 0xffff0000u) | (none() & 0xffffu);
+                if (bits >> (2 * k + 1) & 1) v[i][k] = (v[i][k] & 0xffffu) | (none() & 0xffff0000u);
             }
     }
-    // Stores fn(element) for each element of the segment.
-    template <typename Fn> __device__ __forceinline__ void store(E* __restrict__ out, Fn&& fn)
+    // Stores fn(element) for each element of the segment, which is x's.
+    template <typename Fn>
+    __device__ __forceinline__ void store(E* __restrict__ out, const E* __restrict__ x, Fn&& fn)
     {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (!any(i)) continue;
             const int j = first(i);
+            if (!any(i) || j + VEC > len) continue;
             float f[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) f[e] = fn(get(i, e));
-            if (j + VEC <= len) {
-                Words<E> q;
+            Words<E> q;
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if constexpr (sizeof(E) == 4) q.w[k] = __float_as_uint(f[k]);
-                    else q.w[k] = pack_pair<E>(f[2 * k], f[2 * k + 1]);
-                *reinterpret_cast<Words<E>*>(out + j) = q;
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (j + e < len) out[j + e] = from_f32<E>(f[e]);
-            }
+            for (int k = 0; k < 4; ++k)
+                if constexpr (sizeof(E) == 4) q.w[k] = __float_as_uint(f[k]);
+                else q.w[k] = pack_pair<E>(f[2 * k], f[2 * k + 1]);
+            *reinterpret_cast<Words<E>*>(out + j) = q;
         }
+        const int j = len / VEC * VEC + (int)threadIdx.x;      // the vector that the end cuts
+        if (j < len) out[j] = from_f32<E>(fn(to_f32(x[j])));
     }
 };
 
@@ -811,7 +869,7 @@ __global__ __launch_bounds__(NT, 4) void k_wide_logprobs(const E* __restrict__ l
         const float z = ex.z(v);
         return -(pow2(z) * inv_s) * fmaf(ge * kLn2, z_finite(z), k0);
     };
-    h.store(out, value);
+    h.store(out, x, value);
     __syncthreads();
     if (tid == 0 && there && !st.empty) out[tok] = from_f32<E>(value(to_f32(x[tok])) + g * a.inv_t);
 }
@@ -951,7 +1009,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_logprobs(const E* __restr
     for (int j = j0; j < j1; j += kJoinThreads * kVec<E>) {
         Held<E, kJoinThreads, 1> h;
         h.load(x + j, j1 - j);
-        h.store(out + j, value);
+        h.store(out + j, x + j, value);
     }
     __syncthreads();
     if (tid == 0 && there && !st.empty && tok >= j0 && tok < j1)
@@ -1056,23 +1114,24 @@ __global__ __launch_bounds__(NT, 4) void k_wide_distill(const E* __restrict__ lo
     const int j0 = sg * a.seg;
     const E* row = logits + r * a.stride;
     static_assert(NT >= 64 && LIF_TOP_MAX <= 128, "at most two entries a thread");
-    // the list first: its loads are short, and the logits there are on their
-    // way with the row
+    // the list's loads first: they are short, and the logits that it names are
+    // on their way right behind the row
     int ej[2] = {-1, -1};
     float el[2], ex_[2];
 #pragma unroll
     for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q) {
         const int i = tid + q * NT;
         if (i >= a.k) continue;
-        const int j = t_idx[(int64_t)r * a.k + i];
+        ej[q] = t_idx[(int64_t)r * a.k + i];
         el[q] = t_logp[(int64_t)r * a.k + i];
-        if (j >= 0 && j < a.V) {
-            ej[q] = j;
-            ex_[q] = to_f32(row[j]);
-        }
     }
     Held<E, NT, NV> h;
     h.load(row + j0, min(a.seg, a.V - j0));
+#pragma unroll
+    for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q) {
+        if (ej[q] < 0 || ej[q] >= a.V) ej[q] = -1;
+        else ex_[q] = to_f32(row[ej[q]]);
+    }
     for (int i = tid; i < (h.len + 31) / 32; i += NT) bits[i] = 0;
 #pragma unroll
     for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q)
@@ -1123,8 +1182,8 @@ __global__ __launch_bounds__(NT, 4) void k_wide_distill(const E* __restrict__ lo
         const float wt = (weight ? weight[r] : 1.0f) * a.inv_t, f = t.none || st.empty ? 0.0f : c_rest * wt;
         E* out = grad + r * a.grad_stride;
         // a row without a gradient may hold a NaN, which 0 f would keep
-        if (t.none || st.empty) h.store(out, [&](float) { return 0.0f; });
-        else h.store(out, [&](float v) { return pow2(ex.z(v)) * f; });
+        if (t.none || st.empty) h.store(out, row, [&](float) { return 0.0f; });
+        else h.store(out, row, [&](float v) { return pow2(ex.z(v)) * f; });
         __syncthreads();
         store_listed<E, NT>(sh, a.k, ex, st, t, c_top, wt, 0, a.V, out);
     }
@@ -1180,8 +1239,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_distill(const E* __restri
     for (int j = j0; j < j1; j += NT * kVec<E>) {
         Held<E, NT, 1> h;
         h.load(row + j, j1 - j);
-        if (t.none || st.empty) h.store(out + j, [&](float) { return 0.0f; });
-        else h.store(out + j, [&](float v) { return pow2(ex.z(v)) * f; });
+        if (t.none || st.empty) h.store(out + j, row + j, [&](float) { return 0.0f; });
+        else h.store(out + j, row + j, [&](float v) { return pow2(ex.z(v)) * f; });
     }
     __syncthreads();
     store_listed<E, NT>(sh, a.k, ex, st, t, c_top, wt, j0, j1, out);
