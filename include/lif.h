@@ -532,7 +532,8 @@ int lif_softplus_grad(const float* x, const float* grad_d, float* grad_x, size_t
  * backward pass (0 for many shapes; ws may then be NULL).  All three are
  * bitwise reproducible.
  * Errors: LIF_ERR_ARG (null pointers, sizes, flags, dtype, strides),
- * LIF_ERR_SIZE (B * D >= 2^31 or B * T * D >= 2^48), LIF_ERR_WORKSPACE. */
+ * LIF_ERR_SIZE (B * D >= 2^28, T > 2^30 or B * T * D >= 2^48),
+ * LIF_ERR_WORKSPACE. */
 #define LIF_GATED_MARK 64
 #define LIF_GATED_COUPLED 1u
 typedef struct lif_gated_params {
@@ -606,8 +607,9 @@ int lif_gated_step(const void* x, const void* f, const int32_t* slot, float* sta
  * ws may then be NULL).  Both are bitwise reproducible.
  * Errors: LIF_ERR_ARG (null pointers, sizes, flags, dtype, stride < V,
  * k > V, a temperature outside [2^-20, 2^20]), LIF_ERR_SIZE (k >
- * LIF_TOP_MAX, V > 2^24, R * V beyond 2^31 segments of a row),
- * LIF_ERR_WORKSPACE. */
+ * LIF_TOP_MAX, V > 2^24, or more rows than one launch of fewer than 2^32
+ * threads takes, at up to 16 threads a row of 256 logits or fewer and 1024 a
+ * longer one), LIF_ERR_WORKSPACE. */
 #define LIF_TOP_MAX 128
 #define LIF_DISTILL_TAIL 1u
 #define LIF_DISTILL_TAIL_MIN (1.0 / 1048576.0)

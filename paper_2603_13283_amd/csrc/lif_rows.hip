@@ -152,7 +152,9 @@ template <typename Op> __device__ __forceinline__ float over_wave(float v, Op op
 // Narrow rows.  A workgroup takes kNarrowThreads / L rows, L lanes a row; lane
 // l of a row holds its elements j = l + L i.  The rows pass through LDS, with
 // a row length of an odd multiple of L words, so that the lanes of a wave read
-// different banks.
+// different banks.  Bound by instructions (vector units busy for two thirds of
+// the time): 128000 x 20 f32 with 5 alternatives 12 us, 17 MB; with a wave a
+// row it would be 128000 waves of one element a lane.
 // ---------------------------------------------------------------------------
 constexpr int kNarrowPer = 32;          // at most this many elements a lane: one bit each in a mask
 
@@ -390,7 +392,15 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
 }
 
 // ---------------------------------------------------------------------------
-// Wide rows.  A workgroup of NT threads holds a segment in registers: NV
+// Wide rows, read once.  At 2 bytes a logit the vector units take nearly as
+// long as the memory (about 11 instructions a logit, one of them an
+// exponential, against 14 that fit the time of its load), so two workgroups
+// share a CU and one computes while the other loads: rows of 65536 16-bit
+// logits take 64 of 128 registers.  4096 x 50048 bf16 with 5 alternatives
+// 96 us, 410 MB at 4.3 TB/s; gradient of 4096 x 32768 f32 200 us, 1.07 GB at
+// 5.4 TB/s; distillation 4096 x 50048 bf16 165 us, 820 MB at 5.0 TB/s.
+//
+// A workgroup of NT threads holds a segment in registers: NV
 // vectors of 16 bytes a thread, vector i of thread t at element
 // (i NT + t) VEC, at whatever address that is: the order of a row's sums does
 // not depend on where the row lies.  What a vector holds past the segment
@@ -1310,6 +1320,14 @@ size_t rows_ws(const RowPlan& q)
     return q.a.nseg > 1 ? (size_t)q.a.R * q.a.nseg * (sizeof(Part) + (size_t)q.a.k * sizeof(Cand)) : 0;
 }
 
+// A launch has fewer than 2^32 threads.
+bool too_many(const RowPlan& q)
+{
+    // a narrow row takes up to 16 threads; the join's 256 a row are fewer than the segments' in all
+    const int64_t per_row = q.shape < 0 ? 16 : (int64_t)q.a.nseg * kShapes[q.shape].nt;
+    return (int64_t)q.a.R * per_row > ((int64_t)1 << 32) - 1024;
+}
+
 // Calls fn(element, threads, vectors) with types that carry them.
 template <int N> struct Int { static constexpr int value = N; };
 template <typename Fn> void with_shape(int dtype, int shape, Fn&& fn)
@@ -1382,17 +1400,17 @@ extern "C" int lif_token_logprobs(const void* logits, const int32_t* token, cons
     RowArgs& a = q.a;
     if (!top_idx) a.k = 0;
     const hipStream_t s = (hipStream_t)stream;
+    if (too_many(q)) return LIF_ERR_SIZE;
     if (q.shape < 0) {
         with_lanes(p->dtype, p->V, [&](auto e, auto l) {
             using E = decltype(e);
             constexpr int L = decltype(l)::value, per = kNarrowThreads / L;
-            TIMED_LAUNCH("token_logprobs", (k_narrow_logprobs<E, L>), dim3((a.R + per - 1) / per),
+            TIMED_LAUNCH("token_logprobs", (k_narrow_logprobs<E, L>), dim3((unsigned)(((int64_t)a.R + per - 1) / per)),
                          dim3(kNarrowThreads), narrow_lds(a.V, L), s, (const E*)logits, token, a, logp, entropy, lse,
                          top_logp, top_idx, grad_logp, grad_entropy, (E*)grad);
         });
         return check_launch();
     }
-    if ((int64_t)a.R * a.nseg >= ((int64_t)1 << 31)) return LIF_ERR_SIZE;
     const LogprobOutputs o{logp, entropy, lse, top_logp, top_idx, grad_logp, grad_entropy};
     Part* parts = (Part*)ws;
     Cand* lists = (Cand*)(parts + (size_t)a.R * a.nseg);
@@ -1426,16 +1444,16 @@ extern "C" int lif_distill_top(const void* logits, const float* teacher_logp, co
     if (p->R == 0) return LIF_OK;
     const RowArgs& a = q.a;
     const hipStream_t s = (hipStream_t)stream;
+    if (too_many(q)) return LIF_ERR_SIZE;
     if (q.shape < 0) {
         with_lanes(p->dtype, p->V, [&](auto e, auto l) {
             using E = decltype(e);
             constexpr int L = decltype(l)::value, per = kNarrowThreads / L;
-            TIMED_LAUNCH("distill_top", (k_narrow_distill<E, L>), dim3((a.R + per - 1) / per), dim3(kNarrowThreads),
+            TIMED_LAUNCH("distill_top", (k_narrow_distill<E, L>), dim3((unsigned)(((int64_t)a.R + per - 1) / per)), dim3(kNarrowThreads),
                          narrow_lds(a.V, L), s, (const E*)logits, teacher_logp, teacher_idx, a, weight, loss, (E*)grad);
         });
         return check_launch();
     }
-    if ((int64_t)a.R * a.nseg >= ((int64_t)1 << 31)) return LIF_ERR_SIZE;
     Part* parts = (Part*)ws;
     with_shape(p->dtype, q.shape, [&](auto e, auto nt, auto nv) {
         using E = decltype(e);

@@ -25,7 +25,8 @@ GATED_BAD = [(dict(B=-1), L.LIF_ERR_ARG), (dict(T=-1), L.LIF_ERR_ARG), (dict(D=0
              (dict(dtype=3), L.LIF_ERR_ARG), (dict(dtype=-1), L.LIF_ERR_ARG), (dict(flags=2), L.LIF_ERR_ARG),
              (dict(reserved=1), L.LIF_ERR_ARG), (dict(x_time=-8), L.LIF_ERR_ARG), (dict(g_batch=-1), L.LIF_ERR_ARG),
              (dict(B=1 << 16, D=1 << 15), L.LIF_ERR_SIZE),
-             (dict(B=1 << 10, D=1 << 20, T=1 << 18), L.LIF_ERR_SIZE)]
+             (dict(B=1 << 10, D=1 << 20, T=1 << 18), L.LIF_ERR_SIZE), (dict(B=1 << 14, D=1 << 14), L.LIF_ERR_SIZE),
+             (dict(B=1, D=1, T=(1 << 30) + 1), L.LIF_ERR_SIZE), (dict(B=1 << 12, D=1 << 10, T=1 << 26), L.LIF_ERR_SIZE)]
 
 
 @pytest.mark.parametrize("kw,code", GATED_BAD)
@@ -85,7 +86,8 @@ ROWS_BAD = [(dict(R=-1), L.LIF_ERR_ARG), (dict(V=0), L.LIF_ERR_ARG), (dict(k=-1)
             (dict(temperature=-1.0), L.LIF_ERR_ARG), (dict(temperature=float("nan")), L.LIF_ERR_ARG),
             (dict(temperature=float("inf")), L.LIF_ERR_ARG), (dict(temperature=1e-9), L.LIF_ERR_ARG),
             (dict(flags=2), L.LIF_ERR_ARG), (dict(reserved=1), L.LIF_ERR_ARG),
-            (dict(V=1000, stride=1000, grad_stride=1000, k=129), L.LIF_ERR_SIZE)]
+            (dict(V=1000, stride=1000, grad_stride=1000, k=129), L.LIF_ERR_SIZE),
+            (dict(V=(1 << 24) + 1, stride=1 << 25, grad_stride=1 << 25), L.LIF_ERR_SIZE)]
 
 
 @pytest.mark.parametrize("kw,code", ROWS_BAD)
@@ -111,6 +113,14 @@ def test_rows_pointers(lib):
         assert L.lif_distill_top(*a) == L.LIF_ERR_ARG
     assert L.lif_distill_top(F, F, F, p, F, None, None, F, ok, None) == L.LIF_ERR_ARG     # nothing asked for
     assert L.lif_distill_top(None, None, None, ctypes.byref(_rp(R=0)), None, F, F, None, 0, None) == L.LIF_OK
+
+
+@pytest.mark.parametrize("R,V", [((1 << 31) - 1, 20), ((1 << 31) - 1, 200), (1 << 27, 300), (1 << 22, 131072)])
+def test_rows_that_one_launch_does_not_take(lib, R, V):
+    p = _rp(R=R, V=V, stride=V, grad_stride=V)
+    ref = ctypes.byref(p)
+    assert L.lif_token_logprobs(F, F, ref, F, F, F, F, F, F, F, F, F, 1 << 60, None) == L.LIF_ERR_SIZE
+    assert L.lif_distill_top(F, F, F, ref, F, F, F, F, 1 << 60, None) == L.LIF_ERR_SIZE
 
 
 def test_rows_workspace(lib):
