@@ -843,14 +843,16 @@ def _dtype_code(name, t):
     return code
 
 
-def _on(torch, dev, stream):
-    """The context that an operator's buffers and launches belong to: the
-    inputs' GPU, and `stream` when one is given (memory is then taken for that
-    stream, which has to wait for the inputs)."""
+def _on(torch, t, stream):
+    """The context that an operator's copies, buffers and launches belong to:
+    the GPU of its input t, and `stream` when one is given (memory is then
+    taken for that stream, which has to wait for the inputs)."""
+    if not t.is_cuda:
+        raise ValueError(f"a CUDA tensor is needed, not one on {t.device}")
     if stream is not None:
         return torch.cuda.stream(stream)
-    if dev.index != torch._C._cuda_getDevice():
-        return torch.cuda.device(dev)
+    if t.device.index != torch._C._cuda_getDevice():
+        return torch.cuda.device(t.device)
     return _HERE
 
 
@@ -924,20 +926,20 @@ def gated_scan(x, f, length=None, h_first=None, coupled: bool = True, marks: boo
     h_first float32 [B, D].  marks=True keeps what gated_scan_backward needs;
     states=False returns the last state only."""
     torch = _torch()
-    x, f, length, code, B, T, D = _gated_inputs(x, f, length)
-    dev = x.device
-    h_first = _expect("h_first", h_first, (B, D), torch.float32, dev)
-    p = lif_gated_params(B, T, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), x.stride(1), f.stride(0),
-                         f.stride(1), 0, 0)
-    with _on(torch, dev, stream):
+    with _on(torch, x, stream):
+        x, f, length, code, B, T, D = _gated_inputs(x, f, length)
+        dev = x.device
+        h_first = _expect("h_first", h_first, (B, D), torch.float32, dev)
+        p = lif_gated_params(B, T, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), x.stride(1),
+                             f.stride(0), f.stride(1), 0, 0)
         h = torch.empty((B, T, D), dtype=x.dtype, device=dev) if states else None
         last = torch.empty((B, D), dtype=torch.float32, device=dev)
         mk = torch.empty((B, -(-T // LIF_GATED_MARK), D), dtype=torch.float32, device=dev) if marks else None
         wp, wn, ws = _workspace(torch, _gated_ws(B, T, D, code), ws, dev)
         rc = lif_gated_scan(x.data_ptr(), f.data_ptr(), _ptr(length), _ptr(h_first), ctypes.byref(p), _ptr(h),
                             last.data_ptr(), _ptr(mk), wp, wn, _raw_stream(torch, dev, stream))
-    _check("lif_gated_scan", rc)
-    return GatedOut(h, last, mk)
+        _check("lif_gated_scan", rc)
+        return GatedOut(h, last, mk)
 
 
 def gated_scan_backward(x, f, marks, grad_h=None, grad_last=None, length=None, coupled: bool = True, stream=None,
@@ -945,17 +947,17 @@ def gated_scan_backward(x, f, marks, grad_h=None, grad_last=None, length=None, c
     """Run lif_gated_scan_backward with the forward's inputs and its marks;
     returns (grad_x, grad_f, grad_h_first)."""
     torch = _torch()
-    x, f, length, code, B, T, D = _gated_inputs(x, f, length)
-    dev = x.device
-    marks = _expect("marks", marks, (B, -(-T // LIF_GATED_MARK), D), torch.float32, dev)
-    if marks is None:
-        raise ValueError("the backward pass needs the forward's marks (gated_scan with marks=True)")
-    if grad_h is not None:
-        grad_h = _rows_of("grad_h", grad_h, x.shape, x.dtype, dev)
-    grad_last = _expect("grad_last", grad_last, (B, D), torch.float32, dev)
-    p = lif_gated_params(B, T, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), x.stride(1), f.stride(0),
-                         f.stride(1), *((0, 0) if grad_h is None else grad_h.stride()[:2]))
-    with _on(torch, dev, stream):
+    with _on(torch, x, stream):
+        x, f, length, code, B, T, D = _gated_inputs(x, f, length)
+        dev = x.device
+        marks = _expect("marks", marks, (B, -(-T // LIF_GATED_MARK), D), torch.float32, dev)
+        if marks is None:
+            raise ValueError("the backward pass needs the forward's marks (gated_scan with marks=True)")
+        if grad_h is not None:
+            grad_h = _rows_of("grad_h", grad_h, x.shape, x.dtype, dev)
+        grad_last = _expect("grad_last", grad_last, (B, D), torch.float32, dev)
+        p = lif_gated_params(B, T, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), x.stride(1),
+                             f.stride(0), f.stride(1), *((0, 0) if grad_h is None else grad_h.stride()[:2]))
         gx = torch.empty((B, T, D), dtype=x.dtype, device=dev)
         gf = torch.empty((B, T, D), dtype=x.dtype, device=dev)
         g0 = torch.empty((B, D), dtype=torch.float32, device=dev)
@@ -963,8 +965,8 @@ def gated_scan_backward(x, f, marks, grad_h=None, grad_last=None, length=None, c
         rc = lif_gated_scan_backward(x.data_ptr(), f.data_ptr(), _ptr(length), marks.data_ptr(), _ptr(grad_h),
                                      _ptr(grad_last), ctypes.byref(p), gx.data_ptr(), gf.data_ptr(), g0.data_ptr(),
                                      wp, wn, _raw_stream(torch, dev, stream))
-    _check("lif_gated_scan_backward", rc)
-    return gx, gf, g0
+        _check("lif_gated_scan_backward", rc)
+        return gx, gf, g0
 
 
 def gated_step(x, f, state, slot=None, coupled: bool = True, stream=None):
@@ -972,23 +974,24 @@ def gated_step(x, f, state, slot=None, coupled: bool = True, stream=None):
     are rows slot (int32 [B], distinct; None: rows 0 .. B - 1) of state
     (float32 [n_slots, D]), updated in place.  Returns h [B, D]."""
     torch = _torch()
-    if x.dim() != 2 or not x.is_cuda:
-        raise ValueError("x must be a CUDA tensor [B, D]")
-    code, dev = _dtype_code("x", x), x.device
-    x = _rows_of("x", x, x.shape, x.dtype, dev)
-    f = _rows_of("f", f, x.shape, x.dtype, dev)
-    B, D = x.shape
-    if state.dim() != 2 or state.shape[1] != D or state.dtype != torch.float32 or state.device != dev or \
-            not state.is_contiguous():
-        raise ValueError(f"state must be a contiguous float32 tensor [n_slots, {D}] on {dev}")
-    slot = _expect("slot", slot, (B,), torch.int32, dev)
-    p = lif_gated_params(B, 1, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), 0, f.stride(0), 0, 0, 0)
-    with _on(torch, dev, stream):
+    with _on(torch, x, stream):
+        if x.dim() != 2 or not x.is_cuda:
+            raise ValueError("x must be a CUDA tensor [B, D]")
+        code, dev = _dtype_code("x", x), x.device
+        x = _rows_of("x", x, x.shape, x.dtype, dev)
+        f = _rows_of("f", f, x.shape, x.dtype, dev)
+        B, D = x.shape
+        if state.dim() != 2 or state.shape[1] != D or state.dtype != torch.float32 or state.device != dev or \
+                not state.is_contiguous():
+            raise ValueError(f"state must be a contiguous float32 tensor [n_slots, {D}] on {dev}")
+        slot = _expect("slot", slot, (B,), torch.int32, dev)
+        p = lif_gated_params(B, 1, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), 0, f.stride(0), 0, 0,
+                             0)
         h = torch.empty((B, D), dtype=x.dtype, device=dev)
         rc = lif_gated_step(x.data_ptr(), f.data_ptr(), _ptr(slot), state.data_ptr(), state.shape[0], ctypes.byref(p),
                             h.data_ptr(), _raw_stream(torch, dev, stream))
-    _check("lif_gated_step", rc)
-    return h
+        _check("lif_gated_step", rc)
+        return h
 
 
 @dataclass
@@ -1019,12 +1022,12 @@ def token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 1.0, gr
     entropies, the k likeliest alternatives, and, when grad_logp or
     grad_entropy (float32 [R]) is given, the gradient to the logits."""
     torch = _torch()
-    logits, p, R, V = _row_params(logits, k, temperature, 0)
-    dev = logits.device
-    tokens = _expect("tokens", tokens, (R,), torch.int32, dev)
-    grad_logp = _expect("grad_logp", grad_logp, (R,), torch.float32, dev)
-    grad_entropy = _expect("grad_entropy", grad_entropy, (R,), torch.float32, dev)
-    with _on(torch, dev, stream):
+    with _on(torch, logits, stream):
+        logits, p, R, V = _row_params(logits, k, temperature, 0)
+        dev = logits.device
+        tokens = _expect("tokens", tokens, (R,), torch.int32, dev)
+        grad_logp = _expect("grad_logp", grad_logp, (R,), torch.float32, dev)
+        grad_entropy = _expect("grad_entropy", grad_entropy, (R,), torch.float32, dev)
         logp, ent, lse = torch.empty((3, R), dtype=torch.float32, device=dev).unbind(0)
         tv = ti = grad = None
         if k > 0:
@@ -1036,8 +1039,8 @@ def token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 1.0, gr
         rc = lif_token_logprobs(logits.data_ptr(), _ptr(tokens), ctypes.byref(p), logp.data_ptr(), ent.data_ptr(),
                                 lse.data_ptr(), _ptr(tv), _ptr(ti), _ptr(grad_logp), _ptr(grad_entropy), _ptr(grad),
                                 wp, wn, _raw_stream(torch, dev, stream))
-    _check("lif_token_logprobs", rc)
-    return LogprobOut(logp, ent, lse, tv, ti, grad)
+        _check("lif_token_logprobs", rc)
+        return LogprobOut(logp, ent, lse, tv, ti, grad)
 
 
 def distill_top(logits, teacher_logp, teacher_idx, temperature: float = 1.0, tail: bool = False, weight=None,
@@ -1046,18 +1049,18 @@ def distill_top(logits, teacher_logp, teacher_idx, temperature: float = 1.0, tai
     (float32 and int32 [R, k]); returns (loss float32 [R], grad [R, V] of the
     logits' type or None), the gradient of sum_r weight_r loss_r."""
     torch = _torch()
-    if teacher_idx.dim() != 2:
-        raise ValueError("teacher_idx must be [R, k]")
-    logits, p, R, V = _row_params(logits, teacher_idx.shape[1], temperature, LIF_DISTILL_TAIL if tail else 0)
-    dev = logits.device
-    teacher_logp = _expect("teacher_logp", teacher_logp, (R, p.k), torch.float32, dev)
-    teacher_idx = _expect("teacher_idx", teacher_idx, (R, p.k), torch.int32, dev)
-    weight = _expect("weight", weight, (R,), torch.float32, dev)
-    with _on(torch, dev, stream):
+    with _on(torch, logits, stream):
+        if teacher_idx.dim() != 2:
+            raise ValueError("teacher_idx must be [R, k]")
+        logits, p, R, V = _row_params(logits, teacher_idx.shape[1], temperature, LIF_DISTILL_TAIL if tail else 0)
+        dev = logits.device
+        teacher_logp = _expect("teacher_logp", teacher_logp, (R, p.k), torch.float32, dev)
+        teacher_idx = _expect("teacher_idx", teacher_idx, (R, p.k), torch.int32, dev)
+        weight = _expect("weight", weight, (R,), torch.float32, dev)
         loss = torch.empty(R, dtype=torch.float32, device=dev)
         grad = torch.empty((R, V), dtype=logits.dtype, device=dev) if want_grad else None
         wp, wn, ws = _workspace(torch, _rows_ws(R, V, p.k, p.dtype), ws, dev)
         rc = lif_distill_top(logits.data_ptr(), teacher_logp.data_ptr(), teacher_idx.data_ptr(), ctypes.byref(p),
                              _ptr(weight), loss.data_ptr(), _ptr(grad), wp, wn, _raw_stream(torch, dev, stream))
-    _check("lif_distill_top", rc)
-    return loss, grad
+        _check("lif_distill_top", rc)
+        return loss, grad

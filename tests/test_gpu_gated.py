@@ -291,6 +291,32 @@ def test_reproducible_and_on_another_stream(env):
         assert torch.equal(p, q) and torch.equal(p, r)
 
 
+def test_copies_run_on_the_given_stream(env):
+    """With a stream of its own, a call copies what it has to copy (inputs in
+    another order) on that stream: it does not wait for the current one, which
+    is busy here."""
+    torch, lif = env
+    x, f, gh, h0, gl = _inputs(env, 2, 300, 64, "f32", 51)
+    turned = lambda v: v.transpose(-1, -2).contiguous().transpose(-1, -2)         # noqa: E731
+    z, tok = x[0], torch.zeros(300, dtype=torch.int32, device="cuda:0")
+    lp, idx = lif.token_logprobs(z, k=4).top_logp, lif.token_logprobs(z, k=4).top_idx
+    args = [turned(v) for v in (x, f, gh, h0, gl, z, lp, idx)]
+
+    def go(x, f, gh, h0, gl, z, lp, idx, stream=None):
+        o = lif.gated_scan(x, f, h_first=h0, marks=True, stream=stream)
+        return (o.h, *lif.gated_scan_backward(x, f, o.marks, gh, grad_last=gl, stream=stream),
+                lif.token_logprobs(z, tok, stream=stream).logp, *lif.distill_top(z, lp, idx, stream=stream))
+    want = go(x, f, gh, h0, gl, z, lp, idx)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)
+    got = go(*args, stream=side)
+    side.synchronize()
+    for p, q in zip(want, got):
+        assert torch.equal(p, q.to(p.device))
+    torch.cuda.synchronize()
+
+
 def test_graph_replays(env):
     """Scan, backward and step captured once and replayed on new inputs."""
     torch, lif = env
