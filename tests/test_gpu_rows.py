@@ -249,6 +249,19 @@ def test_masks_ties_and_rows_that_are_not_finite(env, V, dtype):
             assert torch.isposinf(loss[0]) and not grad[0].any()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ties_over_many_segments(env, dtype):
+    """Constant rows, few distinct values and alternatives that all lie in one
+    segment, in rows that are cut into many."""
+    torch, _ = env
+    V = 300000
+    for v in (torch.zeros(1, V), torch.randn(1, V).round(), torch.arange(V).flip(0)[None] / 8.0,
+              torch.where(torch.arange(V) % 2999 == 7, 1.0, -float("inf"))[None]):
+        x = v.to(_dt(torch, dtype)).cuda()
+        for k in (128, 20, 1):
+            run_logprobs(env, x, dtype, np.array([5]), k, label="many segments")
+
+
 @pytest.mark.parametrize("V", [20, 64, 1000, 40009, 140001])
 def test_teacher_lists(env, V):
     """Unused entries, empty lists, entries of probability 0, repeated classes,
