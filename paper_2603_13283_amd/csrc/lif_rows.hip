@@ -227,14 +227,13 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_logprobs(
             if (lse) lse[r] = row_lse(st, a);
         }
     }
-    if (a.k > 0) {                              // the elements become their keys
-        int* key = reinterpret_cast<int*>(x);
-        for (int i = 0; i < n; ++i) key[L * i] = signed_key(x[L * i]);
+    if (a.k > 0) {                              // the elements become their keys' bits
+        for (int i = 0; i < n; ++i) x[L * i] = __int_as_float(signed_key(x[L * i]));
         for (int q = 0; q < a.k; ++q) {
             int best = kTaken, at = 0;          // equal ones by index
 #pragma unroll 4
             for (int i = 0; i < n; ++i) {
-                const int w = key[L * i];
+                const int w = __float_as_int(x[L * i]);
                 if (w > best) best = w, at = i;
             }
             int j = l + L * at;
@@ -246,7 +245,7 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_logprobs(
             if constexpr (L >= 8) better(dpp<0x141>(best), dpp<0x141>(j));
             if constexpr (L >= 16) better(dpp<0x140>(best), dpp<0x140>(j));
             if (rl < rows) {
-                if (j % L == l) key[j - l] = kTaken;
+                if (j % L == l) x[j - l] = __int_as_float(kTaken);
                 if (l == 0) {
                     top_idx[r * a.k + q] = j;
                     top_logp[r * a.k + q] = row_logp(st, a, signed_value(best));
