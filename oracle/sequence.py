@@ -124,18 +124,20 @@ def distill_top(logits, teacher_logp, teacher_idx, temperature=1.0, tail=False, 
     for r in range(R):
         use = [i for i in range(teacher_idx.shape[1]) if 0 <= int(teacher_idx[r, i]) < V]
         j = np.array([int(teacher_idx[r, i]) for i in use], np.int64)
-        q = np.exp(np.array([float(teacher_logp[r, i]) for i in use], np.float64))
-        total = q.sum()
-        if not total > 0 and not np.isnan(total):
+        lq = np.array([float(teacher_logp[r, i]) for i in use], np.float64)
+        if not (lq > -np.inf).any() and not np.isnan(lq).any():
             continue
-        if not tail:
-            q = q / total
+        if not tail:                                # relative to the largest: unlikely classes have a mass too
+            lq = lq - np.fmax.reduce(lq)
+            lq = lq - np.log(np.exp(lq).sum())
+        q = np.exp(lq)
+        total = q.sum()
         logp, _, mass = _row(x[r] / temperature)
         p = np.exp(logp)
         listed = np.zeros(V, bool)
         listed[j] = True
         with np.errstate(divide="ignore", invalid="ignore"):
-            loss[r] = sum(qi * (np.log(qi) - logp[ji]) for qi, ji in zip(q, j) if qi > 0 or np.isnan(qi))
+            loss[r] = sum(qi * (li - logp[ji]) for qi, li, ji in zip(q, lq, j) if qi > 0 or np.isnan(qi))
         q_rest, p_rest = 0.0, p[~listed].sum()
         if tail and 1.0 - total >= TAIL_MIN and not listed.all():
             q_rest = 1.0 - total

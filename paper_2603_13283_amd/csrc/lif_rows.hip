@@ -126,6 +126,10 @@ template <int Ctrl> __device__ __forceinline__ int dpp(int v)
 {
     return __builtin_amdgcn_update_dpp(v, v, Ctrl, 0xf, 0xf, false);
 }
+template <int Ctrl> __device__ __forceinline__ double dpp(double v)
+{
+    return __hiloint2double(dpp<Ctrl>(__double2hiint(v)), dpp<Ctrl>(__double2loint(v)));
+}
 // Combines with the lanes of a group of L <= 16 (aligned) lanes.
 template <int L, typename V, typename Op> __device__ __forceinline__ V over_lanes(V v, Op op)
 {
@@ -135,7 +139,7 @@ template <int L, typename V, typename Op> __device__ __forceinline__ V over_lane
     if constexpr (L >= 16) v = op(v, dpp<0x140>(v));        // mirrored in 16
     return v;
 }
-struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct Add { template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a + b; } };
 struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 struct Min { __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); } };
 
@@ -146,6 +150,15 @@ template <typename Op> __device__ __forceinline__ float over_wave(float v, Op op
     const float a = __int_as_float(__builtin_amdgcn_readlane(i, 0)), b = __int_as_float(__builtin_amdgcn_readlane(i, 16));
     const float c = __int_as_float(__builtin_amdgcn_readlane(i, 32)), d = __int_as_float(__builtin_amdgcn_readlane(i, 48));
     return op(op(a, b), op(c, d));
+}
+__device__ __forceinline__ double sum_over_wave(double v)
+{
+    v = over_lanes<16>(v, Add());
+    auto row = [&](int lane) {
+        return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane),
+                                __builtin_amdgcn_readlane(__double2loint(v), lane));
+    };
+    return (row(0) + row(16)) + (row(32) + row(48));
 }
 
 // ---------------------------------------------------------------------------
@@ -272,20 +285,31 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_logprobs(
     unstage_rows(grad + row0 * a.grad_stride, a.grad_stride, rows, a.V, pitch, sh);
 }
 
-// The teacher's side of a row: sums over its used entries.
+// The teacher's side of a row: sums over its used entries.  A list that is
+// made to sum to 1 is taken relative to its largest entry, so that unlikely
+// classes (a logp below -104 is 0 in float32) have a mass to divide by.  With
+// a tail q = e^logp; its sum is of float64 terms, since 1 - sum q is small for
+// a sure teacher.
 struct Teacher {
-    double sq;                          // sum of q
+    double sq;                          // sum of q as kept
     bool none;                          // no mass
     double q_rest, scale;               // the tail's share; what q is multiplied by
 };
-__device__ __forceinline__ Teacher teacher_of(double sq, bool tail, bool all_listed)
+// What is taken off the list's logps, of which the largest is m.
+__device__ __forceinline__ float list_shift(float m, bool tail) { return tail || m == kNegInf ? 0.0f : m; }
+__device__ __forceinline__ Teacher teacher_of(double sq, float m, bool tail, bool all_listed)
 {
     Teacher t;
     t.sq = sq;
-    t.none = sq == 0.0;
+    t.none = m == kNegInf && sq == 0.0;             // a NaN is kept
     t.q_rest = tail && 1.0 - sq >= LIF_DISTILL_TAIL_MIN && !all_listed ? 1.0 - sq : 0.0;
     t.scale = tail || t.none ? 1.0 : 1.0 / sq;
     return t;
+}
+// What is added to a logp for log q.
+__device__ __forceinline__ double log_scale(const Teacher& t, float m, bool tail)
+{
+    return tail ? 0.0 : -(double)list_shift(m, tail) - (double)logf((float)t.sq);
 }
 // One entry's share q (log q - log p) of the loss; lp the student's log p.
 __device__ __forceinline__ double entry_loss(double q, double log_q, double lp)
@@ -338,10 +362,24 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
         const int j = idx[i];
         if (j >= 0 && j < a.V && j % L == l) listed |= 1u << (j / L);
     }
+    float* q = sh + per_group * pitch + rl * a.k;               // of every entry
+    float m_list = kNegInf;
+    if (!a.tail) {
+        for (int i = l; i < k; i += L)
+            if (idx[i] >= 0 && idx[i] < a.V) m_list = fmaxf(m_list, lt[i]);
+        m_list = over_lanes<L>(m_list, Max());
+    }
+    const float shift = list_shift(m_list, a.tail);
     double sq = 0.0;
-    for (int i = l; i < k; i += L)
-        if (idx[i] >= 0 && idx[i] < a.V) sq += (double)expf(lt[i]);
-    for (int o = 1; o < L; o <<= 1) sq += __shfl_xor(sq, o);
+    for (int i = l; i < k; i += L) {
+        const bool used = idx[i] >= 0 && idx[i] < a.V;
+        const double e = used ? exp((double)lt[i] - (double)shift) : 0.0;
+        if (used) m_list = fmaxf(m_list, lt[i]);
+        q[i] = (float)e;
+        sq += e;
+    }
+    m_list = over_lanes<L>(m_list, Max());
+    sq = over_lanes<L>(sq, Add());
     float m = kNegInf, s_top = 0.0f, s_rest = 0.0f;
 #pragma unroll 4
     for (int i = 0; i < n; ++i) m = fmaxf(m, x[L * i]);
@@ -356,18 +394,18 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
     s_rest = over_lanes<L>(s_rest, Add());
     const int n_top = over_lanes<L>((int)__popc(listed), [](int p, int o) { return p + o; });
     const RowStat st = row_stat(ex, s_top + s_rest, 0.0f);
-    const Teacher t = teacher_of(sq, a.tail, n_top == a.V);
-    const double log_scale = t.scale == 1.0 ? 0.0 : (double)logf((float)t.scale);
+    const Teacher t = teacher_of(sq, m_list, a.tail, n_top == a.V);
     if (loss) {
+        const double add = log_scale(t, m_list, a.tail);
         double v = 0.0;
         for (int i = l; i < k; i += L) {
             const int j = idx[i];
             if (j < 0 || j >= a.V) continue;
             const double lp = st.empty ? (double)kNegInf
                                        : ((double)row[j] - (double)st.m) * a.inv_td - (double)st.ls;
-            v += entry_loss((double)expf(lt[i]) * t.scale, (double)lt[i] + log_scale, lp);
+            v += entry_loss((double)q[i] * t.scale, (double)lt[i] + add, lp);
         }
-        for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o);
+        v = over_lanes<L>(v, Add());
         if (l == 0 && rl < rows) loss[r] = t.none ? 0.0f : (float)(v + tail_loss(t, s_rest, st));
     }
     if (!grad) return;
@@ -381,10 +419,12 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
         const float e = pow2(ex.z(x[L * i]));
         x[L * i] = dead ? 0.0f : e * ((listed >> i & 1) ? c_top : c_rest);
     }
+    __syncthreads();
     // the lanes of a row hold its elements apart, so every element is changed by one lane
+    const float scale = (float)t.scale;
     for (int i = 0; i < k && !dead; ++i) {
         const int j = idx[i];
-        if (j >= 0 && j < a.V && j % L == l) row[j] -= (float)((double)expf(lt[i]) * t.scale) * w;
+        if (j >= 0 && j < a.V && j % L == l) row[j] -= q[i] * scale * w;
     }
     __syncthreads();
     unstage_rows(grad + row0 * a.grad_stride, a.grad_stride, rows, a.V, pitch, sh);
@@ -1080,41 +1120,57 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_logprobs(const E* __restr
 template <int NT> struct ListLds {
     int idx[LIF_TOP_MAX];               // -1: unused
     int first[LIF_TOP_MAX];             // the one entry of its class that counts there
-    float lt[LIF_TOP_MAX], q[LIF_TOP_MAX], x[LIF_TOP_MAX];
-    double sq;
+    float lt[LIF_TOP_MAX], x[LIF_TOP_MAX];
+    double q[LIF_TOP_MAX], sq;
+    float m;                            // the largest logp
     int used, distinct;
     float part[3][NT / 64];
 };
 
-// Entry i of the teacher's list and the student's logit there.
+// Entries lane and lane + 64 of the teacher's list (class -1: unused) and the
+// student's logits there, kept by one wave, with the sum of q.
+static_assert(LIF_TOP_MAX <= 128, "at most two entries a lane");
 template <int NT>
-__device__ __forceinline__ void keep_entry(ListLds<NT>& sh, int i, int j, float lt, float x)
+__device__ __forceinline__ void keep_list(ListLds<NT>& sh, const RowArgs& a, const int (&j)[2], const float (&lt)[2],
+                                          const float (&x)[2], int lane)
 {
-    const bool used = j >= 0;
-    sh.idx[i] = j;
-    sh.lt[i] = used ? lt : kNegInf;
-    sh.q[i] = used ? expf(lt) : 0.0f;
-    sh.x[i] = used ? x : kNegInf;
+    float m = kNegInf;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+        if (j[q] >= 0) m = fmaxf(m, lt[q]);
+    m = over_wave(m, Max());
+    const float shift = list_shift(m, a.tail);
+    double sq = 0.0;
+    int used = 0;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int i = lane + 64 * q;
+        const bool is = j[q] >= 0;
+        const double e = is ? exp((double)lt[q] - (double)shift) : 0.0;
+        sq += e;
+        used += __popcll(__ballot(is));
+        if (i >= a.k) continue;
+        sh.idx[i] = j[q];
+        sh.lt[i] = is ? lt[q] : kNegInf;
+        sh.q[i] = e;
+        sh.x[i] = is ? x[q] : kNegInf;
+    }
+    sq = sum_over_wave(sq);
+    if (lane == 0) sh.sq = sq, sh.m = m, sh.used = used;
 }
 
-// Sums over the list, by one wave: q, and the terms e of distinct classes.
+// The sum of the terms e of distinct classes, by one wave.
 template <int NT>
 __device__ __forceinline__ float sum_list(ListLds<NT>& sh, int k, const Exponent& ex, int lane)
 {
-    double sq = 0.0;
     float e = 0.0f;
-    int used = 0, distinct = 0;
-    for (int i = lane; i < k; i += 64) {
-        sq += (double)sh.q[i];
-        used += sh.idx[i] >= 0;
-        if (sh.first[i]) e += pow2(ex.z(sh.x[i])), ++distinct;
+    int distinct = 0;
+    for (int i = lane; i < 128; i += 64) {
+        const bool first = i < k && sh.first[i];
+        if (first) e += pow2(ex.z(sh.x[i]));
+        distinct += __popcll(__ballot(first));
     }
-    for (int o = 32; o; o >>= 1) {
-        sq += __shfl_xor(sq, o);
-        used += __shfl_xor(used, o);
-        distinct += __shfl_xor(distinct, o);
-    }
-    if (lane == 0) sh.sq = sq, sh.used = used, sh.distinct = distinct;
+    if (lane == 0) sh.distinct = distinct;
     return over_wave(e, Add());
 }
 
@@ -1123,14 +1179,14 @@ template <int NT>
 __device__ __forceinline__ double list_loss(const ListLds<NT>& sh, int k, const RowArgs& a, const RowStat& st,
                                             const Teacher& t, float s_rest, int lane)
 {
-    const double log_scale = t.scale == 1.0 ? 0.0 : (double)logf((float)t.scale);
+    const double add = log_scale(t, sh.m, a.tail);
     double v = 0.0;
     for (int i = lane; i < k; i += 64) {
         if (sh.idx[i] < 0) continue;
         const double lp = st.empty ? (double)kNegInf : ((double)sh.x[i] - (double)st.m) * a.inv_td - (double)st.ls;
-        v += entry_loss((double)sh.q[i] * t.scale, (double)sh.lt[i] + log_scale, lp);
+        v += entry_loss(sh.q[i] * t.scale, (double)sh.lt[i] + add, lp);
     }
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    v = sum_over_wave(v);
     return t.none ? 0.0 : v + tail_loss(t, s_rest, st);
 }
 
@@ -1144,14 +1200,14 @@ __device__ __forceinline__ void store_listed(const ListLds<NT>& sh, int k, const
     for (int i = threadIdx.x; i < k; i += NT) {
         const int j = sh.idx[i];
         if (j < j0 || j >= j1) continue;
-        double q = (double)sh.q[i];
+        double q = sh.q[i];
         if (sh.distinct < sh.used) {    // repeated entries write the same value
             q = 0.0;
             for (int p = 0; p < k; ++p)
-                if (sh.idx[p] == j) q += (double)sh.q[p];
+                if (sh.idx[p] == j) q += sh.q[p];
         }
-        const float v = dead ? 0.0f : fmaf(pow2(ex.z(sh.x[i])), c_top, -(float)(q * t.scale));
-        out[j] = from_f32<E>(dead ? 0.0f : v * w);
+        const double v = (double)pow2(ex.z(sh.x[i])) * (double)c_top - q * t.scale;     // one rounding at the end
+        out[j] = from_f32<E>(dead ? 0.0f : (float)(v * (double)w));
     }
 }
 
@@ -1168,40 +1224,40 @@ __global__ __launch_bounds__(NT, 4) void k_wide_distill(const E* __restrict__ lo
     const int r = blockIdx.x / a.nseg, sg = blockIdx.x - r * a.nseg;
     const int j0 = sg * a.seg;
     const E* row = logits + r * a.stride;
-    static_assert(NT >= 64 && LIF_TOP_MAX <= 128, "at most two entries a thread");
     // the list's loads first: they are short, and the logits that it names are
-    // on their way right behind the row
+    // on their way right behind the row; the first wave works on it meanwhile
     int ej[2] = {-1, -1};
-    float el[2], ex_[2];
+    float el[2] = {}, xl[2] = {};
+    if (w == 0)
 #pragma unroll
-    for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q) {
-        const int i = tid + q * NT;
-        if (i >= a.k) continue;
-        ej[q] = t_idx[(int64_t)r * a.k + i];
-        el[q] = t_logp[(int64_t)r * a.k + i];
-    }
+        for (int q = 0; q < 2; ++q)
+            if (lane + 64 * q < a.k) {
+                ej[q] = t_idx[(int64_t)r * a.k + lane + 64 * q];
+                el[q] = t_logp[(int64_t)r * a.k + lane + 64 * q];
+            }
     Held<E, NT, NV> h;
     h.load(row + j0, min(a.seg, a.V - j0));
+    if (w == 0) {
 #pragma unroll
-    for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q) {
-        if (ej[q] < 0 || ej[q] >= a.V) ej[q] = -1;
-        else ex_[q] = to_f32(row[ej[q]]);
+        for (int q = 0; q < 2; ++q) {
+            if (ej[q] < 0 || ej[q] >= a.V) ej[q] = -1;
+            else if (a.nseg == 1) xl[q] = to_f32(row[ej[q]]);
+        }
+        if (a.nseg == 1) keep_list(sh, a, ej, el, xl, lane);
     }
     for (int i = tid; i < (h.len + 31) / 32; i += NT) bits[i] = 0;
-#pragma unroll
-    for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q)
-        if (tid + q * NT < a.k) keep_entry(sh, tid + q * NT, ej[q], el[q], ex_[q]);
     __syncthreads();
+    if (w == 0)
 #pragma unroll
-    for (int q = 0; q < (NT < LIF_TOP_MAX ? 2 : 1); ++q) {
-        const int i = tid + q * NT, j = ej[q] - j0;
-        if (i >= a.k) continue;
-        bool first = false;
-        if (ej[q] >= 0 && j >= 0 && j < h.len) {
-            first = !(atomicOr(&bits[j >> 5], 1u << (j & 31)) >> (j & 31) & 1);
+        for (int q = 0; q < 2; ++q) {
+            const int i = lane + 64 * q, j = ej[q] - j0;
+            if (i >= a.k) continue;
+            bool first = false;
+            if (ej[q] >= 0 && j >= 0 && j < h.len) {
+                first = !(atomicOr(&bits[j >> 5], 1u << (j & 31)) >> (j & 31) & 1);
+            }
+            sh.first[i] = first;
         }
-        sh.first[i] = first;
-    }
     float vm[NV];
     float m = over_wave(h.maxima(vm), Max());
     if (lane == 0) sh.part[0][w] = m;
@@ -1230,7 +1286,7 @@ __global__ __launch_bounds__(NT, 4) void k_wide_distill(const E* __restrict__ lo
     __syncthreads();
     const float s_rest = join_parts<NT>(sh.part[1], Add()), s_top = sh.part[2][0];
     const RowStat st = row_stat(ex, s_top + s_rest, 0.0f);
-    const Teacher t = teacher_of(sh.sq, a.tail, sh.distinct == a.V);
+    const Teacher t = teacher_of(sh.sq, sh.m, a.tail, sh.distinct == a.V);
     if (grad) {
         float c_top, c_rest;
         grad_factors(t, st, s_rest, c_top, c_rest);
@@ -1261,10 +1317,18 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_distill(const E* __restri
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int r = blockIdx.x / pieces, pc = blockIdx.x - r * pieces;
     const E* row = logits + r * a.stride;
-    for (int i = tid; i < a.k; i += NT) {
-        const int j = t_idx[(int64_t)r * a.k + i];
-        const bool used = j >= 0 && j < a.V;
-        keep_entry(sh, i, used ? j : -1, t_logp[(int64_t)r * a.k + i], used ? to_f32(row[j]) : 0.0f);
+    if (w == 0) {
+        int ej[2] = {-1, -1};
+        float el[2] = {}, xl[2] = {};
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int64_t at = (int64_t)r * a.k + lane + 64 * q;
+            if (lane + 64 * q >= a.k || t_idx[at] < 0 || t_idx[at] >= a.V) continue;
+            ej[q] = t_idx[at];
+            el[q] = t_logp[at];
+            xl[q] = to_f32(row[ej[q]]);
+        }
+        keep_list(sh, a, ej, el, xl, lane);
     }
     __syncthreads();
     for (int i = tid; i < a.k; i += NT) {
@@ -1280,7 +1344,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_distill(const E* __restri
     }
     __syncthreads();
     const RowStat st = row_stat(ex, sh.part[2][0] + s_rest, 0.0f);
-    const Teacher t = teacher_of(sh.sq, a.tail, sh.distinct == a.V);
+    const Teacher t = teacher_of(sh.sq, sh.m, a.tail, sh.distinct == a.V);
     if (loss && pc == 0 && w == 0) {
         const double v = list_loss<NT>(sh, a.k, a, st, t, s_rest, lane);
         if (lane == 0) loss[r] = (float)v;
@@ -1402,7 +1466,11 @@ template <typename Fn> void with_lanes(int dtype, int V, Fn&& fn)
 }
 static_assert((kNarrow + 15) / 16 <= kNarrowPer && 16 <= kNarrowPer, "a lane's elements have a bit each");
 
-size_t narrow_lds(int V, int L) { return (size_t)(kNarrowThreads / L) * narrow_pitch(V, L) * sizeof(float); }
+// The staged rows, and behind them k more values a row.
+size_t narrow_lds(int V, int L, int k)
+{
+    return (size_t)(kNarrowThreads / L) * (narrow_pitch(V, L) + k) * sizeof(float);
+}
 
 // The pieces of a row that the second launch writes gradients of.
 void gradient_pieces(const RowArgs& a, bool grad, int elem, int& pieces, int& piece)
@@ -1451,7 +1519,7 @@ extern "C" int lif_token_logprobs(const void* logits, const int32_t* token, cons
             using E = decltype(e);
             constexpr int L = decltype(l)::value, per = kNarrowThreads / L;
             TIMED_LAUNCH("token_logprobs", (k_narrow_logprobs<E, L>), dim3((unsigned)(((int64_t)a.R + per - 1) / per)),
-                         dim3(kNarrowThreads), narrow_lds(a.V, L), s, (const E*)logits, token, a, logp, entropy, lse,
+                         dim3(kNarrowThreads), narrow_lds(a.V, L, 0), s, (const E*)logits, token, a, logp, entropy, lse,
                          top_logp, top_idx, grad_logp, grad_entropy, (E*)grad);
         });
         return check_launch();
@@ -1494,8 +1562,9 @@ extern "C" int lif_distill_top(const void* logits, const float* teacher_logp, co
         with_lanes(p->dtype, p->V, [&](auto e, auto l) {
             using E = decltype(e);
             constexpr int L = decltype(l)::value, per = kNarrowThreads / L;
-            TIMED_LAUNCH("distill_top", (k_narrow_distill<E, L>), dim3((unsigned)(((int64_t)a.R + per - 1) / per)), dim3(kNarrowThreads),
-                         narrow_lds(a.V, L), s, (const E*)logits, teacher_logp, teacher_idx, a, weight, loss, (E*)grad);
+            TIMED_LAUNCH("distill_top", (k_narrow_distill<E, L>), dim3((unsigned)(((int64_t)a.R + per - 1) / per)),
+                         dim3(kNarrowThreads), narrow_lds(a.V, L, a.k), s, (const E*)logits, teacher_logp, teacher_idx,
+                         a, weight, loss, (E*)grad);
         });
         return check_launch();
     }
