@@ -39,6 +39,14 @@ struct RowArgs {
     int nseg, seg;                      // segments of a row and their length
 };
 
+// m c rounded, wherever it is used: contracted into the difference of two
+// offsets it would not be the offset that the terms were taken by.
+__device__ __forceinline__ float rounded_product(float m, float c)
+{
+#pragma clang fp contract(off)
+    return m * c;
+}
+
 // The exponents of a row: z = x c - o, for the largest logit m.  The rounding
 // of o multiplies all terms by the same factor, below 2^64 while |m| c < 2^30.
 // From there on (rows masked by the type's lowest value, say) logits that
@@ -53,7 +61,7 @@ struct Exponent {
         m = largest == kNegInf ? 0.0f : largest;
         plain = fabsf(m * a.c) < 0x1p30f;
         c = plain ? a.c : fabsf(m) < 0x1p100f ? a.c_pow2 : 0x1p-60f;
-        o = m * c;
+        o = rounded_product(m, c);
     }
     __device__ __forceinline__ float z(float x) const { return fmaf(x, c, -o); }
 };

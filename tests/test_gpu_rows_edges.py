@@ -1,14 +1,14 @@
-"""Distillation from a teacher's list (lif_distill_top) where float32 would
-run out of range or depend on an order, against the float64 reference.  Every
-case runs on the three ways a row can take: staged in LDS (V <= 256), held by
+"""Rows of logits (lif_token_logprobs, lif_distill_top) where float32 would
+run out of range, lose an offset or depend on an order, against the float64
+reference.  Every case runs on the three ways a row can take: staged in LDS (V <= 256), held by
 one workgroup (many rows), and cut into segments (few rows).
 
-Tolerances are those of test_gpu_rows.run_distill unless a test says
-otherwise."""
+Tolerances are those of test_gpu_rows unless a test says otherwise."""
 import numpy as np
 import pytest
 
-from test_gpu_rows import _logits, env, run_distill       # noqa: F401
+import test_gpu_rows as rows
+from test_gpu_rows import _logits, env, run_distill, run_logprobs       # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +62,36 @@ def test_lists_of_unlikely_classes(env, R, V):
     for tail in (False, True):
         loss, grad = run_repeated(env, x, lp, idx, "f32", R, 1.0, tail, label="unlikely classes")
         assert (loss > 0).all() and grad.any(1).all()
+
+
+@pytest.mark.parametrize("R,V", PLACES)
+@pytest.mark.parametrize("offset,T", [(5000.0, 1.0), (-1e6, 1.0), (1e8, 8.0)])
+def test_rows_far_from_zero(env, monkeypatch, R, V, offset, T):
+    """A common offset of a row's logits cancels in everything but lse: the
+    bounds of test_gpu_rows without the term of the offset's rounding."""
+    torch, _ = env
+    terms = rows._terms
+    monkeypatch.setattr(rows, "_terms", lambda x, T: [0.0 * v if i == 5 else v for i, v in enumerate(terms(x, T))])
+    n = min(R, 3)
+    g = torch.Generator().manual_seed(V)
+    x = (torch.randn(n, V, generator=g, dtype=torch.float64) * 2.5 * T + offset).float().cuda()
+    big = _repeat(torch, x, R)
+    r = np.random.default_rng(V)
+    tok = np.resize(r.integers(0, V, n), R)
+    gl, ge = np.resize(r.standard_normal(n), R), np.resize(r.standard_normal(n), R)
+    first = lambda v: None if v is None else v[:n]                                # noqa: E731
+
+    class First:                                  # the first rows of the call with all of them
+        @staticmethod
+        def token_logprobs(_, tokens, **k):
+            dev = lambda a, t: None if a is None else torch.tensor(a, dtype=t, device="cuda:0")   # noqa: E731
+            if k["grad_logp"] is not None:
+                k["grad_logp"], k["grad_entropy"] = dev(gl, torch.float32), dev(ge, torch.float32)
+            o = env[1].token_logprobs(big, dev(tok, torch.int32), **k)
+            return type(o)(*(first(v) for v in (o.logp, o.entropy, o.lse, o.top_logp, o.top_idx, o.grad)))
+    run_logprobs((torch, First), x, "f32", tok[:n], min(V, 5), T, label="far")
+    run_logprobs((torch, First), x, "f32", tok[:n], 0, T, gl[:n], ge[:n], label="far")
+    idx = np.stack([r.permutation(V)[:6] for _ in range(n)]).astype(np.int32)
+    lp = np.log(r.random((n, 6)) / 6).astype(np.float32)
+    for tail in (False, True):
+        run_repeated(env, x, lp, idx, "f32", R, T, tail, label="far")
