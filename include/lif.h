@@ -595,6 +595,10 @@ int lif_gated_step(const void* x, const void* f, const int32_t* slot, float* sta
  * (q and q log q of each).  A row whose list has no mass (every entry unused
  * or of probability 0) has loss 0 and gradient 0.
  *
+ * Probabilities below 2^-126 of the row's largest count as 0 in sums and
+ * gradients; those of the classes outside a list, where they form the further
+ * class, by the largest among them, however far they lie below the listed ones.
+ *
  * Values that are not finite: a logit of -infinity has p = 0 and no part in
  * any sum (as a token its logp is -infinity, in a teacher's list with q > 0
  * the loss is +infinity).  A row with nothing above -infinity has lse and all

@@ -138,15 +138,17 @@ def distill_top(logits, teacher_logp, teacher_idx, temperature=1.0, tail=False, 
         listed[j] = True
         with np.errstate(divide="ignore", invalid="ignore"):
             loss[r] = sum(qi * (li - logp[ji]) for qi, li, ji in zip(q, lq, j) if qi > 0 or np.isnan(qi))
-        q_rest, p_rest = 0.0, p[~listed].sum()
+        q_rest, share = 0.0, None
         if tail and 1.0 - total >= TAIL_MIN and not listed.all():
             q_rest = 1.0 - total
-            with np.errstate(divide="ignore"):
-                loss[r] += q_rest * (np.log(q_rest) - np.log(p_rest))
+            # by their own largest logit: next to the row's they may all be 0
+            within, log_rest, some = _row(logp[~listed])
+            loss[r] += q_rest * (np.log(q_rest) - log_rest)
+            share = np.exp(within) if some else None
         if mass:
             v = p * ((total if tail else 1.0) + q_rest)
             np.subtract.at(v, j, q)
-            if q_rest > 0 and not p_rest == 0:
-                v[~listed] -= p[~listed] * (q_rest / p_rest)
+            if share is not None:
+                v[~listed] -= q_rest * share
             grad[r] = v * ((1.0 if weight is None else float(weight[r])) / temperature)
     return loss, grad

@@ -55,15 +55,24 @@ __device__ __forceinline__ float rounded_product(float m, float c)
 // 2^-64 for others, and 2^-60 one that does not overflow from |m| = 2^100 on.
 struct Exponent {
     float m, c, o;                      // m is 0 where nothing is above -infinity
-    bool plain;                         // c is the row's
+    bool plain, none;                   // c is the row's; nothing is above -infinity
     __device__ __forceinline__ Exponent(float largest, const RowArgs& a)
     {
-        m = largest == kNegInf ? 0.0f : largest;
+        none = largest == kNegInf;
+        m = none ? 0.0f : largest;
         plain = fabsf(m * a.c) < 0x1p30f;
         c = plain ? a.c : fabsf(m) < 0x1p100f ? a.c_pow2 : 0x1p-60f;
         o = rounded_product(m, c);
     }
     __device__ __forceinline__ float z(float x) const { return fmaf(x, c, -o); }
+    // The exponent of the factor that makes sums of a part's terms, by the
+    // part's own exponents, sums by these.  A part without anything above
+    // -infinity has sums of 0 (or a NaN).
+    __device__ __forceinline__ float from(const Exponent& part) const
+    {
+        if (part.none || part.m == m) return 0.0f;
+        return part.plain && plain ? part.o - o : -200.0f;
+    }
 };
 __device__ __forceinline__ float pow2(float z) { return __builtin_amdgcn_exp2f(z); }
 // z where it is multiplied by e: -infinity (e = 0) must not give a NaN.
@@ -324,22 +333,37 @@ __device__ __forceinline__ double entry_loss(double q, double log_q, double lp)
 {
     return q > 0.0 ? q * (log_q - lp) : q != q ? q : 0.0;
 }
-__device__ __forceinline__ double tail_loss(const Teacher& t, float s_rest, const RowStat& st)
+// The classes that are not listed.  Their terms are taken by their own largest
+// logit, not by the row's: next to a list that the student is sure of they
+// would all be 0 in float32 (from a distance of 87 temperatures on), where
+// their log probability and their shares of it are ordinary numbers.
+struct Rest {
+    Exponent own;
+    float s, f;                         // sum of the terms; s f is a part of the row's S
+    __device__ __forceinline__ Rest(const Exponent& own_, const Exponent& row, float sum)
+        : own(own_), s(sum), f(pow2(row.from(own_)))
+    {
+    }
+};
+__device__ __forceinline__ double tail_loss(const Teacher& t, const Rest& rest, const RowStat& st, const RowArgs& a)
 {
     if (!(t.q_rest > 0.0)) return 0.0;
-    const float lp = st.empty ? kNegInf : logf(s_rest) - st.lz;
-    return t.q_rest * (double)(logf((float)t.q_rest) - lp);
+    const RowStat r = row_stat(rest.own, rest.s, 0.0f);
+    const double lp = r.empty ? (double)kNegInf
+                              : ((double)r.m - (double)st.m) * a.inv_td + ((double)r.ls - (double)st.ls);
+    return t.q_rest * ((double)logf((float)t.q_rest) - lp);
 }
-// dloss/dz_j = e_j c_top - q_j for a listed class, e_j c_rest for another.
-__device__ __forceinline__ void grad_factors(const Teacher& t, const RowStat& st, float s_rest, float& c_top,
+// dloss/dz_j = e_j c_top - q_j for a listed class, e_j c_rest for another, by
+// the exponents of its kind.
+__device__ __forceinline__ void grad_factors(const Teacher& t, const RowStat& st, const Rest& rest, float& c_top,
                                              float& c_rest)
 {
     const double mass = t.scale == 1.0 && !t.none ? t.sq + t.q_rest : 1.0;
     c_top = t.none || st.empty ? 0.0f : (float)mass / st.s;
-    c_rest = c_top;
-    // mass / S - q_rest / s_rest: the difference, which may be small, in float64
-    if (!t.none && !st.empty && t.q_rest > 0.0 && s_rest > 0.0f)
-        c_rest = (float)(mass * (double)s_rest - t.q_rest * (double)st.s) / st.s / s_rest;
+    c_rest = c_top * rest.f;
+    // mass f / S - q_rest / s: the difference, which may be small, in float64
+    if (!t.none && !st.empty && t.q_rest > 0.0 && rest.s > 0.0f)
+        c_rest = (float)(mass * (double)rest.f * (double)rest.s - t.q_rest * (double)st.s) / st.s / rest.s;
 }
 
 template <typename E, int L>
@@ -388,20 +412,26 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
     }
     m_list = over_lanes<L>(m_list, Max());
     sq = over_lanes<L>(sq, Add());
-    float m = kNegInf, s_top = 0.0f, s_rest = 0.0f;
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) m = fmaxf(m, x[L * i]);
-    const Exponent ex(over_lanes<L>(m, Max()), a);
+    float m = kNegInf, m_rest = kNegInf, s_top = 0.0f, s_rest = 0.0f;
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
-        const float e = pow2(ex.z(x[L * i]));
-        if (listed >> i & 1) s_top += e;
+        const float v = x[L * i];
+        m = fmaxf(m, v);
+        m_rest = fmaxf(m_rest, listed >> i & 1 ? kNegInf : v);
+    }
+    const Exponent ex(over_lanes<L>(m, Max()), a), er(over_lanes<L>(m_rest, Max()), a);
+    auto term = [&](float v, bool top) { return pow2(fmaf(v, top ? ex.c : er.c, top ? -ex.o : -er.o)); };
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const bool top = listed >> i & 1;
+        const float e = term(x[L * i], top);
+        if (top) s_top += e;
         else s_rest += e;
     }
     s_top = over_lanes<L>(s_top, Add());
-    s_rest = over_lanes<L>(s_rest, Add());
     const int n_top = over_lanes<L>((int)__popc(listed), [](int p, int o) { return p + o; });
-    const RowStat st = row_stat(ex, s_top + s_rest, 0.0f);
+    const Rest rest(er, ex, over_lanes<L>(s_rest, Add()));
+    const RowStat st = row_stat(ex, fmaf(rest.s, rest.f, s_top), 0.0f);
     const Teacher t = teacher_of(sq, m_list, a.tail, n_top == a.V);
     if (loss) {
         const double add = log_scale(t, m_list, a.tail);
@@ -414,18 +444,18 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
             v += entry_loss((double)q[i] * t.scale, (double)lt[i] + add, lp);
         }
         v = over_lanes<L>(v, Add());
-        if (l == 0 && rl < rows) loss[r] = t.none ? 0.0f : (float)(v + tail_loss(t, s_rest, st));
+        if (l == 0 && rl < rows) loss[r] = t.none ? 0.0f : (float)(v + tail_loss(t, rest, st, a));
     }
     if (!grad) return;
     float c_top, c_rest;
-    grad_factors(t, st, s_rest, c_top, c_rest);
+    grad_factors(t, st, rest, c_top, c_rest);
     const float w = rl < rows ? (weight ? weight[r] : 1.0f) * a.inv_t : 0.0f;
     const bool dead = t.none || st.empty;
     c_top *= w;
     c_rest *= w;
     for (int i = 0; i < n; ++i) {
-        const float e = pow2(ex.z(x[L * i]));
-        x[L * i] = dead ? 0.0f : e * ((listed >> i & 1) ? c_top : c_rest);
+        const bool top = listed >> i & 1;
+        x[L * i] = dead ? 0.0f : term(x[L * i], top) * (top ? c_top : c_rest);
     }
     __syncthreads();
     // the lanes of a row hold its elements apart, so every element is changed by one lane
@@ -948,11 +978,7 @@ __device__ __forceinline__ Exponent join_row(const Part* __restrict__ parts, con
     for (int i = tid; i < a.nseg; i += NT) {
         const Part p = parts[i];
         const Exponent own(p.m, a);
-        // a segment without anything above -infinity has s = u = 0 (or a NaN)
-        float d = own.o - ex.o;
-        if (p.m == kNegInf || own.m == ex.m) d = 0.0f;
-        else if (!own.plain || !ex.plain) d = -200.0f;
-        const float f = pow2(d);
+        const float d = ex.from(own), f = pow2(d);
         s += p.s * f;
         u += f * fmaf(p.s, z_finite(d), p.u);
     }
@@ -1121,9 +1147,9 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_logprobs(const E* __restr
 
 // ---------------------------------------------------------------------------
 // Distillation of wide rows.  The listed classes are found with a bitmap in
-// LDS and taken out of the held elements (set to -infinity) before the sums,
-// so that the sum over the others is summed directly; the listed logits are
-// read one by one.  Their gradients are written last.
+// LDS and taken out of the held elements (set to -infinity) before the maximum
+// and the sums, which are then the others'; the listed logits are read one by
+// one.  Their gradients are written last.
 // ---------------------------------------------------------------------------
 template <int NT> struct ListLds {
     int idx[LIF_TOP_MAX];               // -1: unused
@@ -1167,6 +1193,12 @@ __device__ __forceinline__ void keep_list(ListLds<NT>& sh, const RowArgs& a, con
     if (lane == 0) sh.sq = sq, sh.m = m, sh.used = used;
 }
 
+// The student's largest logit in the list, the same in every lane.
+template <int NT> __device__ __forceinline__ float list_max(const ListLds<NT>& sh, int k, int lane)
+{
+    return over_wave(fmaxf(lane < k ? sh.x[lane] : kNegInf, lane + 64 < k ? sh.x[lane + 64] : kNegInf), Max());
+}
+
 // The sum of the terms e of distinct classes, by one wave.
 template <int NT>
 __device__ __forceinline__ float sum_list(ListLds<NT>& sh, int k, const Exponent& ex, int lane)
@@ -1185,7 +1217,7 @@ __device__ __forceinline__ float sum_list(ListLds<NT>& sh, int k, const Exponent
 // The loss of a row, by one wave.
 template <int NT>
 __device__ __forceinline__ double list_loss(const ListLds<NT>& sh, int k, const RowArgs& a, const RowStat& st,
-                                            const Teacher& t, float s_rest, int lane)
+                                            const Teacher& t, const Rest& rest, int lane)
 {
     const double add = log_scale(t, sh.m, a.tail);
     double v = 0.0;
@@ -1195,7 +1227,7 @@ __device__ __forceinline__ double list_loss(const ListLds<NT>& sh, int k, const 
         v += entry_loss(sh.q[i] * t.scale, (double)sh.lt[i] + add, lp);
     }
     v = sum_over_wave(v);
-    return t.none ? 0.0 : v + tail_loss(t, s_rest, st);
+    return t.none ? 0.0 : v + tail_loss(t, rest, st, a);
 }
 
 // The gradients at the listed classes in [j0, j1), after those of the others.
@@ -1266,20 +1298,22 @@ __global__ __launch_bounds__(NT, 4) void k_wide_distill(const E* __restrict__ lo
             }
             sh.first[i] = first;
         }
-    float vm[NV];
-    float m = over_wave(h.maxima(vm), Max());
-    if (lane == 0) sh.part[0][w] = m;
+    const float m_list = a.nseg == 1 ? list_max(sh, a.k, lane) : kNegInf;
     __syncthreads();
-    m = join_parts<NT>(sh.part[0], Max());
-    const Exponent ex(m, a);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         if (!h.any(i) || h.first(i) >= h.len) continue;
         const uint32_t b = bits[h.first(i) >> 5] >> (h.first(i) & 31) & ((1u << VEC) - 1u);
         if (b) h.drop(i, b);
     }
+    float vm[NV];
+    float m = over_wave(h.maxima(vm), Max());
+    if (lane == 0) sh.part[0][w] = m;
+    __syncthreads();
+    m = join_parts<NT>(sh.part[0], Max());
+    const Exponent er(m, a), ex(fmaxf(m, m_list), a);
     float s = 0.0f;
-    h.each([&](float v) { s += pow2(ex.z(v)); });
+    h.each([&](float v) { s += pow2(er.z(v)); });
     s = over_wave(s, Add());
     if (lane == 0) sh.part[1][w] = s;
     if (a.nseg > 1) {
@@ -1292,22 +1326,22 @@ __global__ __launch_bounds__(NT, 4) void k_wide_distill(const E* __restrict__ lo
         if (lane == 0) sh.part[2][0] = e;
     }
     __syncthreads();
-    const float s_rest = join_parts<NT>(sh.part[1], Add()), s_top = sh.part[2][0];
-    const RowStat st = row_stat(ex, s_top + s_rest, 0.0f);
+    const Rest rest(er, ex, join_parts<NT>(sh.part[1], Add()));
+    const RowStat st = row_stat(ex, fmaf(rest.s, rest.f, sh.part[2][0]), 0.0f);
     const Teacher t = teacher_of(sh.sq, sh.m, a.tail, sh.distinct == a.V);
     if (grad) {
         float c_top, c_rest;
-        grad_factors(t, st, s_rest, c_top, c_rest);
+        grad_factors(t, st, rest, c_top, c_rest);
         const float wt = (weight ? weight[r] : 1.0f) * a.inv_t, f = t.none || st.empty ? 0.0f : c_rest * wt;
         E* out = grad + r * a.grad_stride;
         // a row without a gradient may hold a NaN, which 0 f would keep
         if (t.none || st.empty) h.store(out, row, [&](float) { return 0.0f; });
-        else h.store(out, row, [&](float v) { return pow2(ex.z(v)) * f; });
+        else h.store(out, row, [&](float v) { return pow2(er.z(v)) * f; });
         __syncthreads();
         store_listed<E, NT>(sh, a.k, ex, st, t, c_top, wt, 0, a.V, out);
     }
     if (loss && w == 0) {
-        const double v = list_loss<NT>(sh, a.k, a, st, t, s_rest, lane);
+        const double v = list_loss<NT>(sh, a.k, a, st, t, rest, lane);
         if (lane == 0) loss[r] = (float)v;
     }
 }
@@ -1345,21 +1379,24 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_distill(const E* __restri
         sh.first[i] = first;
     }
     float s_rest, u;
-    const Exponent ex = join_row<NT>(parts + (int64_t)r * a.nseg, a, s_rest, u, sh.part);
+    const Exponent er = join_row<NT>(parts + (int64_t)r * a.nseg, a, s_rest, u, sh.part);
+    const float m_list = list_max(sh, a.k, lane);
+    const Exponent ex(er.none ? m_list : fmaxf(er.m, m_list), a);
     if (w == 0) {
         const float e = sum_list<NT>(sh, a.k, ex, lane);
         if (lane == 0) sh.part[2][0] = e;
     }
     __syncthreads();
-    const RowStat st = row_stat(ex, sh.part[2][0] + s_rest, 0.0f);
+    const Rest rest(er, ex, s_rest);
+    const RowStat st = row_stat(ex, fmaf(rest.s, rest.f, sh.part[2][0]), 0.0f);
     const Teacher t = teacher_of(sh.sq, sh.m, a.tail, sh.distinct == a.V);
     if (loss && pc == 0 && w == 0) {
-        const double v = list_loss<NT>(sh, a.k, a, st, t, s_rest, lane);
+        const double v = list_loss<NT>(sh, a.k, a, st, t, rest, lane);
         if (lane == 0) loss[r] = (float)v;
     }
     if (!grad) return;
     float c_top, c_rest;
-    grad_factors(t, st, s_rest, c_top, c_rest);
+    grad_factors(t, st, rest, c_top, c_rest);
     const float wt = (weight ? weight[r] : 1.0f) * a.inv_t, f = t.none || st.empty ? 0.0f : c_rest * wt;
     E* out = grad + r * a.grad_stride;
     const int j0 = pc * piece, j1 = min(j0 + piece, a.V);
@@ -1367,7 +1404,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_distill(const E* __restri
         Held<E, NT, 1> h;
         h.load(row + j, j1 - j);
         if (t.none || st.empty) h.store(out + j, row + j, [&](float) { return 0.0f; });
-        else h.store(out + j, row + j, [&](float v) { return pow2(ex.z(v)) * f; });
+        else h.store(out + j, row + j, [&](float v) { return pow2(er.z(v)) * f; });
     }
     __syncthreads();
     store_listed<E, NT>(sh, a.k, ex, st, t, c_top, wt, j0, j1, out);

@@ -8,7 +8,8 @@ import numpy as np
 import pytest
 
 import test_gpu_rows as rows
-from test_gpu_rows import _logits, env, run_distill, run_logprobs       # noqa: F401
+from oracle import sequence as S
+from test_gpu_rows import ROUND, _dt, _logits, _np, env, run_distill, run_logprobs       # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +96,78 @@ def test_rows_far_from_zero(env, monkeypatch, R, V, offset, T):
     lp = np.log(r.random((n, 6)) / 6).astype(np.float32)
     for tail in (False, True):
         run_repeated(env, x, lp, idx, "f32", R, T, tail, label="far")
+
+
+def _far_bounds(x, lp, idx, T, w):
+    """Bounds on the error of loss and gradient for a list with a tail whose
+    distance to the rest is anything: the terms of test_gpu_rows, those of the
+    rest by its own largest logit."""
+    R, V = x.shape
+    z = x / T
+    listed = np.zeros((R, V), bool)
+    np.put_along_axis(listed, idx.astype(np.int64), True, 1)
+    q = np.exp(lp.astype(np.float64))
+    eta_q = (2 * np.abs(lp.astype(np.float64)) + 6) * U
+    dq, q_rest = (q * eta_q).sum(1, keepdims=True), 1 - q.sum(1, keepdims=True)
+
+    def terms(z):
+        m = z.max(1, keepdims=True)
+        d = np.where(np.isinf(z), 0.0, z - m)
+        e = np.exp(z - m)
+        p = e / e.sum(1, keepdims=True)
+        eta = (4 * np.abs(d) + 4) * U
+        return d, p, eta, (p * eta).sum(1, keepdims=True) + 160 * U, m + np.log(e.sum(1, keepdims=True))
+    with np.errstate(over="ignore"):
+        d, p, eta, etaS, lse = terms(z)
+        _, share, eta_r, etaS_r, lse_r = terms(np.where(listed, -np.inf, z))
+        lp_rest, dl = np.abs(lse_r - lse), np.abs(np.take_along_axis(d, idx.astype(np.int64), 1))
+    off = 2 * U * np.abs(z.max(1, keepdims=True))
+    t_lp = etaS + off + 4 * U * (dl + 12)                                 # log S < 12
+    t_loss = (q * (t_lp + (eta_q + 8 * U) * (np.abs(lp) + dl + 14))).sum(1)
+    t_loss += (q_rest * (etaS + etaS_r + 2 * off + 8 * U * (24 + np.abs(np.log(q_rest))) + dq / q_rest)
+               + dq * (np.abs(np.log(q_rest)) + lp_rest + 1))[:, 0]
+    tol = 2.0 ** -126 * 4 + p * (eta + etaS + 8 * U + dq)
+    tol += share * q_rest * (eta_r + etaS_r + 8 * U + dq / q_rest)
+    np.add.at(tol, (np.arange(R)[:, None], idx), q * (eta_q + 8 * U))
+    return t_loss, tol * np.abs(w)[:, None] / T
+
+
+GAPS = [0.0, 20.0, 60.0, 84.0, 87.5, 90.0, 104.0, 150.0, 400.0, 700.0, 5000.0, None]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("R,V", PLACES)
+def test_the_tail_far_below_the_list(env, R, V, dtype):
+    """Unlisted logits far below the listed ones, up to the type's lowest value
+    (None): the loss is q_rest times the distance, the unlisted classes share
+    -q_rest, and the gradient of a row sums to 0.  Weights as a loss scale sets
+    them, temperatures that stretch a small distance."""
+    torch, lif = env
+    n, k = 3, 6
+    r = np.random.default_rng(V)
+    idx = np.stack([r.permutation(V)[:k] for _ in range(n)]).astype(np.int32)
+    q = r.random((n, k)) + 0.05
+    lp = np.log(q / q.sum(1, keepdims=True) * np.array([[0.9], [0.5], [0.99]])).astype(np.float32)
+    base = r.standard_normal((n, V))
+    for T in (1.0, 0.1):
+        for gap in GAPS:
+            x = torch.tensor(base, dtype=_dt(torch, dtype))
+            for i in range(n):
+                rest = np.setdiff1d(np.arange(V), idx[i])
+                x[i, rest] = torch.finfo(x.dtype).min if gap is None else (x[i, rest].double() - gap * T).to(x.dtype)
+            x[0, np.setdiff1d(np.arange(V), idx[0])[::3]] = -float("inf")
+            w = np.array([1.0, 0.25, 65536.0 if dtype != "f16" else 16.0])
+            at = np.arange(R) % n
+            dev = lambda a, t: torch.tensor(a[at], dtype=t, device="cuda:0")      # noqa: E731
+            print(f"[case] far tail R={R} V={V} {dtype} T={T} gap={gap}", flush=True)
+            loss, grad = lif.distill_top(x.cuda()[torch.tensor(at, device="cuda:0")], dev(lp, torch.float32),
+                                         dev(idx, torch.int32), temperature=T, tail=True,
+                                         weight=dev(w, torch.float32))
+            torch.cuda.synchronize()
+            for i in range(n, R):
+                assert torch.equal(grad[i], grad[i % n]) and loss[i] == loss[i % n]
+            X = x.double().numpy()
+            wl, wg = S.distill_top(X, lp, idx, T, True, w)
+            t_loss, t_grad = _far_bounds(X, lp, idx, T, w)
+            rows._check(loss[:n].cpu().numpy(), wl, t_loss, 2 * U, 0, f"gap {gap} loss")
+            rows._check(_np(grad[:n]), wg, t_grad, *ROUND[dtype], f"gap {gap} grad")
