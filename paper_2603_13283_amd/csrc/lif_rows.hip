@@ -1193,6 +1193,16 @@ __device__ __forceinline__ void keep_list(ListLds<NT>& sh, const RowArgs& a, con
     if (lane == 0) sh.sq = sq, sh.m = m, sh.used = used;
 }
 
+// Marks the first entry of each class.
+template <int NT> __device__ __forceinline__ void find_first(ListLds<NT>& sh, int k, int from, int step)
+{
+    for (int i = from; i < k; i += step) {
+        bool first = sh.idx[i] >= 0;
+        for (int p = 0; p < i; ++p) first &= sh.idx[p] != sh.idx[i];
+        sh.first[i] = first;
+    }
+}
+
 // The student's largest logit in the list, the same in every lane.
 template <int NT> __device__ __forceinline__ float list_max(const ListLds<NT>& sh, int k, int lane)
 {
@@ -1287,7 +1297,8 @@ __global__ __launch_bounds__(NT, 4) void k_wide_distill(const E* __restrict__ lo
     }
     for (int i = tid; i < (h.len + 31) / 32; i += NT) bits[i] = 0;
     __syncthreads();
-    if (w == 0)
+    if (w == 0) {
+        bool again = false;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             const int i = lane + 64 * q, j = ej[q] - j0;
@@ -1295,9 +1306,13 @@ __global__ __launch_bounds__(NT, 4) void k_wide_distill(const E* __restrict__ lo
             bool first = false;
             if (ej[q] >= 0 && j >= 0 && j < h.len) {
                 first = !(atomicOr(&bits[j >> 5], 1u << (j & 31)) >> (j & 31) & 1);
+                again |= !first;
             }
             sh.first[i] = first;
         }
+        // a class listed twice counts at the entry of the lowest index, whichever came first to its bit
+        if (a.nseg == 1 && __any(again)) find_first(sh, a.k, lane, 64);
+    }
     const float m_list = a.nseg == 1 ? list_max(sh, a.k, lane) : kNegInf;
     __syncthreads();
 #pragma unroll
@@ -1373,11 +1388,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_distill(const E* __restri
         keep_list(sh, a, ej, el, xl, lane);
     }
     __syncthreads();
-    for (int i = tid; i < a.k; i += NT) {
-        bool first = sh.idx[i] >= 0;
-        for (int p = 0; p < i; ++p) first &= sh.idx[p] != sh.idx[i];
-        sh.first[i] = first;
-    }
+    find_first(sh, a.k, tid, NT);
     float s_rest, u;
     const Exponent er = join_row<NT>(parts + (int64_t)r * a.nseg, a, s_rest, u, sh.part);
     const float m_list = list_max(sh, a.k, lane);

@@ -171,3 +171,26 @@ def test_the_tail_far_below_the_list(env, R, V, dtype):
             t_loss, t_grad = _far_bounds(X, lp, idx, T, w)
             rows._check(loss[:n].cpu().numpy(), wl, t_loss, 2 * U, 0, f"gap {gap} loss")
             rows._check(_np(grad[:n]), wg, t_grad, *ROUND[dtype], f"gap {gap} grad")
+
+
+@pytest.mark.parametrize("R,V", [(256, 300), (256, 4100), (1024, 20011), (512, 40009), (256, 70001), (3, 20011)])
+def test_a_class_listed_twice_counts_at_its_first_entry(env, R, V):
+    """Entries of probability 0 that repeat earlier ones' classes, in another
+    wave's part of the list or in the same, change nothing: not a bit, and not
+    from call to call."""
+    torch, lif = env
+    k = 128
+    x = _logits(env, R, V, "f32", V)
+    g = torch.Generator().manual_seed(1)
+    idx = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(R)]).to(torch.int32)
+    lp = torch.log(torch.rand(R, k, generator=g) / k)
+    lp[:, 90:], idx[:, 90:] = -float("inf"), -1
+    print(f"[case] repeated classes R={R} V={V}", flush=True)
+    lp = lp.cuda()
+    want = lif.distill_top(x, lp, idx.cuda(), tail=True)
+    for where in (slice(0, 38), slice(52, 90)):
+        twice = idx.clone()
+        twice[:, 90:] = idx[:, where]
+        for _ in range(3):
+            got = lif.distill_top(x, lp, twice.cuda(), tail=True)
+            assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
