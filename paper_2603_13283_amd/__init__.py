@@ -162,6 +162,9 @@ def load(path: Optional[str] = None):
     path = path or LIB_PATH
     if not os.path.exists(path):
         raise LibraryMissing(f"{path} not found: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
+    # torch brings a HIP runtime of its own: the library finds that one if it is
+    # there already, and otherwise brings a second one into the process
+    _torch()
     lib = ctypes.CDLL(path)
     lib.lif_version.restype = ctypes.c_char_p
     lib.lif_version.argtypes = []
