@@ -14,7 +14,8 @@ from test_gpu_rows import ROUND, _dt, _logits, _np, env, run_distill, run_logpro
 pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
-#         rows, logits: LDS with 2, 4 and 16 lanes a row; one workgroup of 256, 512, 512 and 1024 threads; segments
+# rows, logits: LDS with 2, 4 and 16 lanes a row; one workgroup of 512, 512 and
+# 1024 threads and segments (float32), of 256 to 1024 (16 bits); segments
 PLACES = [(5, 20), (6, 64), (4, 200), (256, 4100), (256, 20011), (256, 40009), (256, 70001), (3, 20011), (3, 300000)]
 
 
