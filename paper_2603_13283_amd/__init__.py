@@ -900,7 +900,7 @@ def _workspace(torch, need, ws, dev):
     """(pointer, bytes, the tensor that holds them) of a workspace."""
     if need == 0:
         return None, 0, None
-    if ws is None or ws.numel() * ws.element_size() < need or ws.device != dev:
+    if ws is None or ws.numel() * ws.element_size() < need or ws.device != dev or not ws.is_contiguous():
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
     return ws.data_ptr(), ws.numel() * ws.element_size(), ws
 

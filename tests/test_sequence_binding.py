@@ -1,0 +1,20 @@
+"""What the sequence and row bindings refuse or replace before anything is
+launched (no GPU needed: stand-ins for device tensors where one is asked
+for)."""
+import pytest
+
+import paper_2603_13283_amd as L
+
+torch = pytest.importorskip("torch")
+
+
+def test_a_workspace_that_is_not_one_block_is_not_written_to():
+    """A view with gaps, or one element repeated, has as many elements as are
+    needed but not as many bytes behind its pointer."""
+    dev = torch.device("cpu")
+    block = torch.empty(4096, dtype=torch.uint8)
+    ptr, n, kept = L._workspace(torch, 1024, block, dev)
+    assert ptr == block.data_ptr() and n == 4096 and kept is block
+    for ws in (block[:1].expand(4096), block[::2], torch.empty(64, 64, dtype=torch.uint8)[:, :32]):
+        ptr, n, kept = L._workspace(torch, 1024, ws, dev)
+        assert n >= 1024 and kept is not ws and kept.is_contiguous() and ptr == kept.data_ptr()
