@@ -853,6 +853,8 @@ def _on(torch, t, stream):
     if not t.is_cuda:
         raise ValueError(f"a CUDA tensor is needed, not one on {t.device}")
     if stream is not None:
+        if stream.device != t.device:
+            raise ValueError(f"the stream is one of {stream.device}, the input is on {t.device}")
         return torch.cuda.stream(stream)
     if t.device.index != torch._C._cuda_getDevice():
         return torch.cuda.device(t.device)

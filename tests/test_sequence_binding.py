@@ -18,3 +18,27 @@ def test_a_workspace_that_is_not_one_block_is_not_written_to():
     for ws in (block[:1].expand(4096), block[::2], torch.empty(64, 64, dtype=torch.uint8)[:, :32]):
         ptr, n, kept = L._workspace(torch, 1024, ws, dev)
         assert n >= 1024 and kept is not ws and kept.is_contiguous() and ptr == kept.data_ptr()
+
+
+class Stand:
+    """As much of a device tensor as the checks look at."""
+
+    def __init__(self, shape, strides=None, dtype=torch.bfloat16, device="cuda:0"):
+        self.shape, self.dtype, self.device, self.is_cuda = torch.Size(shape), dtype, torch.device(device), True
+        self.strides = strides or [0] * (len(shape) - 1) + [1]
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self, i=None):
+        return tuple(self.strides) if i is None else self.strides[i]
+
+
+class Stream:
+    def __init__(self, device):
+        self.device, self.cuda_stream = torch.device(device), 1
+
+
+def test_a_stream_of_another_device_is_refused():
+    with pytest.raises(ValueError, match="cuda:1"):
+        L._on(torch, Stand((2, 3)), Stream("cuda:1"))
