@@ -877,6 +877,12 @@ def _expect(name, t, shape, dtype, dev):
     return t.contiguous()
 
 
+def _int32(*sizes):
+    """The C structures hold 32-bit sizes."""
+    if max(sizes) > 0x7fffffff:
+        raise ValueError(f"sizes {sizes} do not fit 32 bits")
+
+
 def _rows_of(name, t, shape, dtype, dev):
     """A device tensor of this shape and type whose last axis is contiguous
     (a copy of one that is not)."""
@@ -921,6 +927,7 @@ def _gated_inputs(x, f, length):
     x = _rows_of("x", x, x.shape, x.dtype, x.device)
     f = _rows_of("f", f, x.shape, x.dtype, x.device)
     B, T, D = x.shape
+    _int32(B, T, D)
     return x, f, _expect("length", length, (B,), _torch().int32, x.device), code, B, T, D
 
 
@@ -989,6 +996,7 @@ def gated_step(x, f, state, slot=None, coupled: bool = True, stream=None):
         if state.dim() != 2 or state.shape[1] != D or state.dtype != torch.float32 or state.device != dev or \
                 not state.is_contiguous():
             raise ValueError(f"state must be a contiguous float32 tensor [n_slots, {D}] on {dev}")
+        _int32(B, D, state.shape[0])
         slot = _expect("slot", slot, (B,), torch.int32, dev)
         p = lif_gated_params(B, 1, D, code, LIF_GATED_COUPLED if coupled else 0, 0, x.stride(0), 0, f.stride(0), 0, 0,
                              0)
@@ -1014,6 +1022,7 @@ def _row_params(logits, k, temperature, flags):
         raise ValueError("logits must be a CUDA tensor [R, V]")
     code = _dtype_code("logits", logits)
     R, V = logits.shape
+    _int32(R, V, k)
     if (V > 1 and logits.stride(1) != 1) or (R > 1 and logits.stride(0) < V):
         logits = logits.contiguous()
     return logits, lif_rows_params(R, V, int(k), code, logits.stride(0) if R > 1 else V, V, float(temperature), flags,

@@ -42,3 +42,18 @@ class Stream:
 def test_a_stream_of_another_device_is_refused():
     with pytest.raises(ValueError, match="cuda:1"):
         L._on(torch, Stand((2, 3)), Stream("cuda:1"))
+
+
+def test_sizes_past_32_bits_are_refused():
+    """The C structures hold 32-bit sizes: a larger one would be taken modulo
+    2^32, and most of the output left unwritten."""
+    n = (1 << 32) + 5
+    for shape, k in (((n, 2), 1), ((3, n), 1), ((3, 4), n)):
+        with pytest.raises(ValueError, match="32 bits"):
+            L._row_params(Stand(shape, [shape[1], 1]), k, 1.0, 0)
+    for shape in ((n, 1, 1), (1, n, 1), (1, 1, n)):
+        with pytest.raises(ValueError, match="32 bits"):
+            L._gated_inputs(Stand(shape), Stand(shape), None)
+    with pytest.raises(ValueError, match="32 bits"):
+        L._int32((1 << 31))
+    L._int32((1 << 31) - 1, 0)
