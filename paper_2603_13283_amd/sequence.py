@@ -15,11 +15,12 @@ from .train import AdamParams
 
 def bin_spikes(fwd: ForwardOut, bins: int, dt: float, dtype=None):
     """Spike counts [B, bins, N] of a layer's output in bins of dt seconds
-    from t = 0; later spikes are left out."""
+    from t = 0; earlier and later spikes are left out."""
     torch = _torch()
     B, N, S = fwd.out_t.shape
-    there = torch.arange(S, device=fwd.out_t.device) < fwd.out_n[:, :, None]
-    at = torch.where(there, fwd.out_t / dt, float(bins)).clamp(max=float(bins)).long()
+    at = fwd.out_t / dt
+    there = (torch.arange(S, device=at.device) < fwd.out_n[:, :, None]) & (at >= 0) & (at < bins)
+    at = torch.where(there, at, float(bins)).long()
     counts = torch.zeros((B, N, bins + 1), dtype=torch.float32, device=fwd.out_t.device)
     counts.scatter_add_(2, at, there.float())
     return counts[:, :, :bins].transpose(1, 2).contiguous().to(dtype or torch.float32)
