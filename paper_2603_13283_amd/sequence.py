@@ -70,16 +70,20 @@ class SequenceHead:
         o = gated_scan(x, f, length=length, h_first=h_first, coupled=self.coupled, marks=train)
         return HeadOut(o.h, o.h.view(B * T, -1) @ self.params["Wo"], o.h_last, x, f, o.marks)
 
-    def backward(self, counts, out: HeadOut, grad_logits, length=None, h_first=None) -> dict:
+    def backward(self, counts, out: HeadOut, grad_logits, length=None, h_first=None, *, grad_last=None) -> dict:
         """Gradients of the parameters for dL/dlogits [B * T, K] of a forward
-        with train=True."""
+        with train=True, and dL/dh_last = grad_last (float32 [B, D]).  With
+        the forward's h_first, its gradient is there too: what a sequence that
+        goes on in pieces hands to the piece before as grad_last."""
         B, T, N = counts.shape
         flat = counts.reshape(B * T, N)
         gh = (grad_logits @ self.params["Wo"].t()).view(B, T, -1)
-        gx, gf, _ = gated_scan_backward(out.x, out.f, out.marks, gh, length=length, coupled=self.coupled)
+        gx, gf, g0 = gated_scan_backward(out.x, out.f, out.marks, gh, grad_last=grad_last, length=length,
+                                         coupled=self.coupled)
         gx, gf = gx.view(B * T, -1), gf.view(B * T, -1)
-        return {"Wx": flat.t() @ gx, "Wf": flat.t() @ gf, "bf": gf.sum(0),
-                "Wo": out.h.view(B * T, -1).t() @ grad_logits}
+        grads = {"Wx": flat.t() @ gx, "Wf": flat.t() @ gf, "bf": gf.sum(0),
+                 "Wo": out.h.view(B * T, -1).t() @ grad_logits}
+        return grads if h_first is None else {**grads, "h_first": g0}
 
     def update(self, grads: dict) -> None:
         self.t += 1
