@@ -59,11 +59,12 @@ class SequenceHead:
                    w(D, K), **kw)
 
     def _gates(self, counts):
-        p, flat = self.params, counts.reshape(-1, counts.shape[-1])
+        p = self.params
+        flat = counts.reshape(-1, counts.shape[-1]).to(p["Wx"].dtype)
         return flat @ p["Wx"], flat @ p["Wf"] + p["bf"]
 
     def forward(self, counts, length=None, h_first=None, train: bool = False) -> HeadOut:
-        """counts float32 [B, T, N], length int32 [B]: logits of every bin
+        """counts [B, T, N] of any type, length int32 [B]: logits of every bin
         (those of bins past a sample's length come from h = 0)."""
         B, T, _ = counts.shape
         x, f = (v.view(B, T, -1) for v in self._gates(counts))
@@ -76,7 +77,7 @@ class SequenceHead:
         the forward's h_first, its gradient is there too: what a sequence that
         goes on in pieces hands to the piece before as grad_last."""
         B, T, N = counts.shape
-        flat = counts.reshape(B * T, N)
+        flat = counts.reshape(B * T, N).to(self.params["Wx"].dtype)
         gh = (grad_logits @ self.params["Wo"].t()).view(B, T, -1)
         gx, gf, g0 = gated_scan_backward(out.x, out.f, out.marks, gh, grad_last=grad_last, length=length,
                                          coupled=self.coupled)

@@ -1,4 +1,5 @@
-"""The sequence head on sequences that go on in pieces."""
+"""The sequence head on sequences that go on in pieces and on counts of other
+types."""
 import pytest
 
 from test_gpu_sequence import GRAD_RTOL, env       # noqa: F401
@@ -35,3 +36,19 @@ def test_pieces_of_a_sequence_have_its_gradients(env):                          
     for k in want:
         got = ga[k] + gb[k]
         assert (got - want[k]).norm() <= GRAD_RTOL * want[k].norm(), k
+
+
+def test_counts_of_any_type(env):                                                  # noqa: F811
+    """Counts are small whole numbers, the same in any type that bin_spikes
+    makes: the same results, bit for bit."""
+    torch, _ = env
+    head, counts, gl = _head(env)
+    labels = torch.tensor([0, 5, 2], dtype=torch.int32, device="cuda:0")
+    want, wg = head.train_step(counts, labels, update=False)
+    state = torch.zeros(3, 14, device="cuda:0")
+    step = head.stream_step(counts[:, 0], state.clone(), k=2)
+    for dtype in (torch.bfloat16, torch.float16, torch.int32):
+        loss, g = head.train_step(counts.to(dtype), labels, update=False)
+        assert torch.equal(loss, want) and all(torch.equal(g[k], wg[k]) for k in wg)
+        got = head.stream_step(counts[:, 0].to(dtype), state.clone(), k=2)
+        assert torch.equal(got.top_idx, step.top_idx) and torch.equal(got.lse, step.lse)
