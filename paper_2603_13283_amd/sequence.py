@@ -67,9 +67,9 @@ class SequenceHead:
         """counts [B, T, N] of any type, length int32 [B]: logits of every bin
         (those of bins past a sample's length come from h = 0)."""
         B, T, _ = counts.shape
-        x, f = (v.view(B, T, -1) for v in self._gates(counts))
+        x, f = (v.view(B, T, v.shape[1]) for v in self._gates(counts))
         o = gated_scan(x, f, length=length, h_first=h_first, coupled=self.coupled, marks=train)
-        return HeadOut(o.h, o.h.view(B * T, -1) @ self.params["Wo"], o.h_last, x, f, o.marks)
+        return HeadOut(o.h, o.h.view(B * T, o.h.shape[2]) @ self.params["Wo"], o.h_last, x, f, o.marks)
 
     def backward(self, counts, out: HeadOut, grad_logits, length=None, h_first=None, *, grad_last=None) -> dict:
         """Gradients of the parameters for dL/dlogits [B * T, K] of a forward
@@ -78,12 +78,13 @@ class SequenceHead:
         goes on in pieces hands to the piece before as grad_last."""
         B, T, N = counts.shape
         flat = counts.reshape(B * T, N).to(self.params["Wx"].dtype)
-        gh = (grad_logits @ self.params["Wo"].t()).view(B, T, -1)
+        D = out.x.shape[2]
+        gh = (grad_logits @ self.params["Wo"].t()).view(B, T, D)
         gx, gf, g0 = gated_scan_backward(out.x, out.f, out.marks, gh, grad_last=grad_last, length=length,
                                          coupled=self.coupled)
-        gx, gf = gx.view(B * T, -1), gf.view(B * T, -1)
+        gx, gf = gx.view(B * T, D), gf.view(B * T, D)
         grads = {"Wx": flat.t() @ gx, "Wf": flat.t() @ gf, "bf": gf.sum(0),
-                 "Wo": out.h.view(B * T, -1).t() @ grad_logits}
+                 "Wo": out.h.view(B * T, D).t() @ grad_logits}
         return grads if h_first is None else {**grads, "h_first": g0}
 
     def update(self, grads: dict) -> None:

@@ -1,5 +1,5 @@
-"""The sequence head on sequences that go on in pieces and on counts of other
-types."""
+"""The sequence head on sequences that go on in pieces, on counts of other
+types and on sequences of nothing."""
 import pytest
 
 from test_gpu_sequence import GRAD_RTOL, env       # noqa: F401
@@ -52,3 +52,17 @@ def test_counts_of_any_type(env):                                               
         assert torch.equal(loss, want) and all(torch.equal(g[k], wg[k]) for k in wg)
         got = head.stream_step(counts[:, 0].to(dtype), state.clone(), k=2)
         assert torch.equal(got.top_idx, step.top_idx) and torch.equal(got.lse, step.lse)
+
+
+def test_sequences_of_nothing(env):                                                # noqa: F811
+    torch, _ = env
+    head, counts, _ = _head(env)
+    labels = torch.tensor([0, 5, 2], dtype=torch.int32, device="cuda:0")
+    for c, lab in ((counts[:, :0], labels), (counts[:0], labels[:0])):
+        loss, g = head.train_step(c, lab, update=False)
+        assert float(loss) == 0 and all(not v.any() for v in g.values())
+        lists = head.alternatives(c, 2)
+        assert lists.top_idx.shape == (0, 2)
+        assert float(head.distill_step(c, lists, update=False)[0]) == 0
+    h0 = torch.randn(3, 14, device="cuda:0")
+    assert torch.equal(head.forward(counts[:, :0], h_first=h0).h_last, h0)
