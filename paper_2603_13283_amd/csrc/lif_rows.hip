@@ -1437,6 +1437,7 @@ struct Shape {
     int nt, nv;
 };
 constexpr Shape kShapes[] = {{64, 4}, {256, 4}, {512, 8}, {512, 16}, {1024, 16}};
+constexpr int kFewRows = 64, kLongVectors = 4096;       // at most and more than
 constexpr int kNumShapes = sizeof(kShapes) / sizeof(kShapes[0]);
 
 struct RowPlan {
@@ -1466,8 +1467,19 @@ RowPlan plan_rows(const lif_rows_params& p)
     auto holds = [&](int s) { return kShapes[s].nt * kShapes[s].nv * vec; };
     int seg = p.V;
     if (seg > holds(kNumShapes - 1)) seg = holds(2);            // does not fit: segments of a middling size
-    // few rows: enough segments for two workgroups on every CU, of 512 vectors at least
-    if (p.R > 0 && p.R < 256 && seg > 512 * vec) {
+    // Few long rows: enough segments for two workgroups on every CU.  That costs
+    // a second launch and, for a gradient, a second read, which rows of more
+    // than 4096 vectors and up to 64 of them make up for (bf16, in segments and
+    // whole, us; 20 alternatives, gradient, distillation with gradient):
+    //    8 x  16384  12.2  7.7    7.6  7.1   10.6  8.9
+    //    8 x  50048  12.3 10.3    7.8 12.4   10.9 14.0
+    //    8 x 131072  12.8 16.5    8.1 23.4   11.0 22.5
+    //   64 x  50048  13.6 10.8   11.9 13.6   15.4 15.2
+    //   64 x 131072  16.6 18.3   17.3 26.6   20.3 25.5
+    //  128 x 131072  19.6 22.0   25.5 29.4   28.9 28.1
+    //  192 x 131072  26.5 24.9   36.6 32.1   40.5 31.0
+    //  255 x   4104  12.4  7.4    8.9  5.9   12.1  7.9
+    if (p.R > 0 && p.R <= kFewRows && seg > kLongVectors * vec) {
         const int want = (512 + p.R - 1) / p.R;
         int few = (p.V + want - 1) / want;
         few = few < 512 * vec ? 512 * vec : few;

@@ -19,7 +19,7 @@ def shape_of(R, V, dtype):
     vec = 16 // ELEM[dtype]
     holds = [t * n * vec for t, n in SHAPES]
     seg = V if V <= holds[-1] else holds[2]
-    if R < 256 and seg > 512 * vec:
+    if R <= 64 and seg > 4096 * vec:
         seg = min(seg, max(512 * vec, -(-V // -(-512 // R))))
     n = -(-V // seg)
     seg = -(-V // n)
@@ -33,11 +33,13 @@ def shape_of(R, V, dtype):
 CASES = [(256, 300, "f32", (64, 4, 1)), (256, 1024, "f32", (64, 4, 1)), (256, 1025, "f32", (256, 4, 1)),
          (256, 4096, "f32", (256, 4, 1)), (256, 4097, "f32", (512, 8, 1)), (257, 16383, "f32", (512, 8, 1)),
          (256, 16385, "f32", (512, 16, 1)), (256, 32768, "f32", (512, 16, 1)), (256, 32769, "f32", (1024, 16, 1)),
-         (256, 65533, "f32", (1024, 16, 1)), (256, 65537, "f32", (512, 8, 5)), (200, 60001, "f32", (512, 16, 3)),
+         (256, 65533, "f32", (1024, 16, 1)), (256, 65537, "f32", (512, 8, 5)), (64, 60001, "f32", (512, 8, 8)),
+         (65, 60001, "f32", (1024, 16, 1)), (10, 16385, "f32", (256, 4, 9)), (10, 16384, "f32", (512, 8, 1)),
          (256, 2049, "bf16", (256, 4, 1)), (256, 8192, "f16", (256, 4, 1)), (256, 8193, "bf16", (512, 8, 1)),
          (300, 32767, "f16", (512, 8, 1)), (256, 32769, "f16", (512, 16, 1)), (256, 50021, "bf16", (512, 16, 1)),
          (256, 65536, "bf16", (512, 16, 1)), (256, 65537, "f16", (1024, 16, 1)), (256, 131071, "bf16", (1024, 16, 1)),
-         (256, 131073, "f16", (512, 8, 5)), (200, 100003, "bf16", (512, 16, 3))]
+         (256, 131073, "f16", (512, 8, 5)), (64, 100003, "bf16", (512, 8, 8)), (65, 100003, "bf16", (1024, 16, 1)),
+         (10, 32769, "f16", (256, 4, 9)), (10, 32768, "f16", (512, 8, 1))]
 
 
 def test_cases_reach_every_shape():
