@@ -507,7 +507,8 @@ int lif_softplus_grad(const float* x, const float* grad_d, float* grad_x, size_t
  *            t = 0, LIF_GATED_MARK, 2 LIF_GATED_MARK, ... (where t >= n the
  *            last state); the backward pass needs them; may be NULL
  * Values of x and f at steps t >= n have no effect.  A NaN or infinity at an
- * earlier step reaches that channel's later states only.
+ * earlier step reaches that channel's later states only (an infinite state may
+ * come out as a NaN where gates below 2^-149 in all have decayed it since).
  *
  * lif_gated_scan_backward: for L with dL/dh = grad_h ([B][T][D] of p->dtype,
  * rows contiguous, strides g_batch and g_time; NULL: 0) and dL/dh_last =

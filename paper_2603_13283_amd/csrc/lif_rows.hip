@@ -25,7 +25,10 @@ namespace {
 
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kNegInf = -INFINITY;
-constexpr int kNarrow = 256;            // longest row of the narrow kernels
+// Longest row of the narrow kernels.  50000 x 256 bf16, narrow and wide, us: 8
+// alternatives 40 45, gradient 31 33, distillation 42 57 (x 160: 34 48, 23 33, 35
+// 58); 30000 x 320: 36 30, 30 22, 39 38 (x 257, an odd row: 29 37, 22 29, 30 43).
+constexpr int kNarrow = 256;
 constexpr int kNarrowThreads = 128;
 constexpr int kMaxV = 1 << 24;
 constexpr int kCand = 512;              // candidates of a top-k selection held in LDS
@@ -183,8 +186,10 @@ __device__ __forceinline__ double sum_over_wave(double v)
 // l of a row holds its elements j = l + L i.  The rows pass through LDS, with
 // a row length of an odd multiple of L words, so that the lanes of a wave read
 // different banks.  Bound by instructions (vector units busy for two thirds of
-// the time): 128000 x 20 f32 with 5 alternatives 12 us, 17 MB; with a wave a
-// row it would be 128000 waves of one element a lane.
+// the time; 95 a logit with 5 alternatives, 138 in distillation, most of them
+// for the alternatives, the list and the staging): 128000 x 20 f32 with 5
+// alternatives 12 us, 17 MB, distillation 18 us, 27 MB; with a wave a row it
+// would be 128000 waves of one element a lane.
 // ---------------------------------------------------------------------------
 constexpr int kNarrowPer = 32;          // at most this many elements a lane: one bit each in a mask
 
@@ -470,12 +475,13 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
 
 // ---------------------------------------------------------------------------
 // Wide rows, read once.  At 2 bytes a logit the vector units take nearly as
-// long as the memory (about 11 instructions a logit, one of them an
-// exponential, against 14 that fit the time of its load), so two workgroups
-// share a CU and one computes while the other loads: rows of 65536 16-bit
-// logits take 64 of 128 registers.  4096 x 50048 bf16 with 5 alternatives
-// 96 us, 410 MB at 4.3 TB/s; gradient of 4096 x 32768 f32 200 us, 1.07 GB at
-// 5.4 TB/s; distillation 4096 x 50048 bf16 165 us, 820 MB at 5.0 TB/s.
+// long as the memory (15 instructions a logit with 64 alternatives, 19 with the
+// gradient, 22 in distillation, against about 15 that fit the time of its load
+// and as many that of its store), so two workgroups share a CU and one computes
+// while the other loads: rows of 65536 16-bit logits take 64 of 128 registers.
+// 4096 x 50048 bf16 with 5 alternatives 102 us, 410 MB at 4.0 TB/s; gradient of
+// 4096 x 32768 f32 200 us, 1.07 GB at 5.4 TB/s; distillation 4096 x 50048 bf16
+// with 64 entries 170 us, 820 MB at 4.8 TB/s.
 //
 // A workgroup of NT threads holds a segment in registers: NV
 // vectors of 16 bytes a thread, vector i of thread t at element
@@ -1432,7 +1438,14 @@ int check_rows(const lif_rows_params* p)
     return LIF_OK;
 }
 
-// Workgroup shapes of the wide kernels: threads and vectors a thread.
+// Workgroup shapes of the wide kernels: threads and vectors a thread.  us, 20
+// alternatives, (gradient,) distillation, with the shape and with another:
+//   20000 x   700 bf16  30 35         {128, 2}   37 42
+//    8000 x  4096       33 42         {512, 2}   56 57
+//    4000 x 12000       50 54 51      {256, 16}  36 43 53
+//    4000 x 30000       70 115 98     {256, 16}  55 101 101
+//    2000 x 40000       49 80 80      {1024, 8}  72 100 75
+// (The third suits distillation; the other two would gain by 256 threads.)
 struct Shape {
     int nt, nv;
 };
