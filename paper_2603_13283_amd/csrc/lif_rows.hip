@@ -333,6 +333,7 @@ __device__ __forceinline__ double log_scale(const Teacher& t, float m, bool tail
 {
     return tail ? 0.0 : -(double)list_shift(m, tail) - (double)logf((float)t.sq);
 }
+constexpr float kLogTiny = -745.13f;    // e to this is float64's smallest number
 // One entry's share q (log q - log p) of the loss; lp the student's log p.
 __device__ __forceinline__ double entry_loss(double q, double log_q, double lp)
 {
@@ -447,6 +448,8 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
             const double lp = st.empty ? (double)kNegInf
                                        : ((double)row[j] - (double)st.m) * a.inv_td - (double)st.ls;
             v += entry_loss((double)q[i] * t.scale, (double)lt[i] + add, lp);
+            // next to a class of probability 0 it matters whether q is 0 or only its float32
+            if (q[i] == 0.0f && lp == (double)kNegInf && lt[i] - shift > kLogTiny) v += INFINITY;
         }
         v = over_lanes<L>(v, Add());
         if (l == 0 && rl < rows) loss[r] = t.none ? 0.0f : (float)(v + tail_loss(t, rest, st, a));

@@ -195,3 +195,21 @@ def test_a_class_listed_twice_counts_at_its_first_entry(env, R, V):
         for _ in range(3):
             got = lif.distill_top(x, lp, twice.cuda(), tail=True)
             assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+@pytest.mark.parametrize("R,V", PLACES)
+def test_an_unlikely_class_that_the_student_rules_out(env, R, V):
+    """However small its q, a listed class of the student's probability 0 makes
+    the loss infinite; one of q = 0 does not."""
+    torch, _ = env
+    n, k = min(R, 3), 4
+    x = _logits(env, n, V, "f32", V)
+    r = np.random.default_rng(V)
+    idx = np.stack([r.permutation(V)[:k] for _ in range(n)]).astype(np.int32)
+    lp = np.log(np.array([[0.5, 0.2, 0.1, 0.1]] * n)).astype(np.float32)
+    for i, v in enumerate((-90.0, -200.0, -np.inf)):
+        lp[i, 2] = v
+        x[i, int(idx[i, 2])] = -float("inf")
+    for tail in (False, True):
+        loss, _ = run_repeated(env, x, lp, idx, "f32", R, 1.0, tail, label="ruled out")
+        assert torch.isposinf(loss[:2]).all() and torch.isfinite(loss[2])
