@@ -448,8 +448,8 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_distill(const E* __re
             const double lp = st.empty ? (double)kNegInf
                                        : ((double)row[j] - (double)st.m) * a.inv_td - (double)st.ls;
             v += entry_loss((double)q[i] * t.scale, (double)lt[i] + add, lp);
-            // next to a class of probability 0 it matters whether q is 0 or only its float32
-            if (q[i] == 0.0f && lp == (double)kNegInf && lt[i] - shift > kLogTiny) v += INFINITY;
+            // where log p is -infinity or a NaN it matters whether q is 0 or only its float32
+            if (q[i] == 0.0f && !(lp > (double)kNegInf) && lt[i] - shift > kLogTiny) v -= lp;
         }
         v = over_lanes<L>(v, Add());
         if (l == 0 && rl < rows) loss[r] = t.none ? 0.0f : (float)(v + tail_loss(t, rest, st, a));

@@ -213,3 +213,21 @@ def test_an_unlikely_class_that_the_student_rules_out(env, R, V):
     for tail in (False, True):
         loss, _ = run_repeated(env, x, lp, idx, "f32", R, 1.0, tail, label="ruled out")
         assert torch.isposinf(loss[:2]).all() and torch.isfinite(loss[2])
+
+
+@pytest.mark.parametrize("R,V", PLACES)
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_row_that_is_not_finite_next_to_unlikely_classes(env, R, V, value):
+    """A NaN or +infinity is in every result of its row, however small the q of
+    the listed classes."""
+    torch, _ = env
+    n, k = min(R, 3), min(V, 128)
+    x = _logits(env, n, V, "f32", V)
+    r = np.random.default_rng(V)
+    idx = np.stack([r.permutation(V)[:k] for _ in range(n)]).astype(np.int32)
+    lp = np.full((n, k), -200.0, np.float32)
+    for i in range(n):
+        x[i, int(idx[i, k - 1] if i else r.integers(0, V))] = value
+    for tail in (False, True):
+        loss, grad = run_repeated(env, x, lp, idx, "f32", R, 1.0, tail, label="not finite")
+        assert torch.isnan(loss).all() and torch.isnan(grad).all()
