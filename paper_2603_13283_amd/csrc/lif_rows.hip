@@ -186,7 +186,7 @@ __device__ __forceinline__ double sum_over_wave(double v)
 // l of a row holds its elements j = l + L i.  The rows pass through LDS, with
 // a row length of an odd multiple of L words, so that the lanes of a wave read
 // different banks.  Bound by instructions (vector units busy for two thirds of
-// the time; 95 a logit with 5 alternatives, 138 in distillation, most of them
+// the time; 95 a logit with 5 alternatives, 140 in distillation, most of them
 // for the alternatives, the list and the staging): 128000 x 20 f32 with 5
 // alternatives 12 us, 17 MB, distillation 18 us, 27 MB; with a wave a row it
 // would be 128000 waves of one element a lane.
