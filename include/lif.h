@@ -638,6 +638,180 @@ int lif_distill_top(const void* logits, const float* teacher_logp, const int32_t
                     size_t ws_bytes, lif_stream_t stream);
 
 /* --------------------------------------------------------------------- */
+/* Models over tokens.                                                     */
+/*                                                                         */
+/* The events of a queue, taken in their order, are a sequence of tokens   */
+/* (their source channels), as words are.  The calls below look up one     */
+/* learned row per token (lif_embed), mix each channel with its last few   */
+/* inputs (lif_causal_conv) and run a state space whose step, input and    */
+/* output depend on the token (lif_selective_scan), each with its          */
+/* gradient; the last two also one step at a time for running streams.     */
+/* Activations have one of the types above, states, parameters and their   */
+/* gradients are float32, and a result in a 16-bit type is rounded once.   */
+/* length (int32 [B], NULL: T everywhere) is clamped into [0, T]; inputs   */
+/* at steps t >= n = length[b] are not read, outputs there are 0.  No      */
+/* output may overlap an input or another output (the steps' states,       */
+/* updated in place, are the exception).  A workspace holds nothing between */
+/* calls and serves one call at a time.  All are bitwise reproducible.     */
+/* --------------------------------------------------------------------- */
+
+/* Rows of a table: out[b][t] = scale W[token[b][t]], and 0 where t >= n or the
+ * token lies outside [0, V) (padding).
+ *   token    int32 [B][T] contiguous
+ *   W        [V][D] of p->table, rows contiguous, p->w_row elements apart
+ *   out      [B][T][D] contiguous, of p->dtype
+ *
+ * lif_embed_backward: for dL/dout = grad ([B][T][D] of p->dtype, rows
+ * contiguous, strides g_batch and g_time >= 0),
+ *   grad_W   float [V][D] contiguous: scale times the sum of grad over the
+ *            places of each token, in their order; 0 for a row without one
+ * ws: lif_embed_backward_workspace_size(p) bytes, 16-byte aligned.
+ * Errors: LIF_ERR_ARG (null pointers, sizes, types, strides, w_row < D, a scale
+ * that is not finite), LIF_ERR_SIZE (V > 2^24, D > 2^20 or B * T >= 2^31),
+ * LIF_ERR_WORKSPACE. */
+typedef struct lif_embed_params {
+    int32_t  B, T;               /* samples and places; either may be 0             */
+    int32_t  V, D;               /* rows of the table (>= 1) and their width (>= 1) */
+    int32_t  dtype;              /* of out and grad                                 */
+    int32_t  table;              /* of W (forward only)                             */
+    int64_t  w_row;              /* elements between rows of W, >= D (forward only) */
+    int64_t  g_batch, g_time;    /* strides of grad (backward only)                 */
+    double   scale;
+    uint32_t flags;              /* must be 0                                       */
+    int32_t  reserved;           /* must be 0                                       */
+} lif_embed_params;
+
+int lif_embed(const int32_t* token, const void* W, const int32_t* length, const lif_embed_params* p, void* out,
+              lif_stream_t stream);
+size_t lif_embed_backward_workspace_size(const lif_embed_params* p);
+int lif_embed_backward(const int32_t* token, const void* grad, const int32_t* length, const lif_embed_params* p,
+                       float* grad_W, void* ws, size_t ws_bytes, lif_stream_t stream);
+
+/* Short causal convolution of each channel along time, K = p->K taps:
+ *   c_t[d] = bias[d] + sum_{j < K} w[d][j] x_{t - K + 1 + j}[d]
+ *   y_t = c_t / (1 + e^{-c_t})  (LIF_CONV_SILU), or c_t without the flag
+ *   x        [B][T][D] of p->dtype, rows contiguous, strides >= 0
+ *   w        float [D][K]; bias float [D] (NULL: 0)
+ *   x_first  [B][K - 1][D] of p->dtype, contiguous: the inputs before t = 0
+ *            (NULL: 0)
+ *   y        [B][T][D] contiguous, of p->dtype; may be NULL
+ *   x_last   [B][K - 1][D] of p->dtype: the last K - 1 inputs before t = n
+ *            (x_first's among them where n < K - 1); may be NULL
+ *
+ * lif_causal_conv_backward: for dL/dy = grad_y ([B][T][D] of p->dtype, rows
+ * contiguous, strides g_batch, g_time; NULL: 0) and dL/dx_last = grad_last
+ * (float [B][K - 1][D]; NULL: 0),
+ *   grad_x       [B][T][D] contiguous, of p->dtype; 0 at t >= n
+ *   grad_w       float [D][K], grad_bias float [D] (either may be NULL)
+ *   grad_x_first float [B][K - 1][D]; may be NULL
+ * ws: lif_causal_conv_workspace_size(p) bytes, 16-byte aligned (backward only).
+ *
+ * lif_causal_conv_step: one step of B streams whose last K - 1 inputs are
+ * state[slot[b]] ([n_slots][K - 1][D] of p->dtype, oldest first; slot NULL: row
+ * b), updated in place.  p->T is 1; x [B][D] with stride x_batch; y [B][D]
+ * contiguous.  The slots of one call must be distinct; a stream whose slot lies
+ * outside [0, n_slots) is left out (its y is 0).
+ * Errors: LIF_ERR_ARG (null pointers, sizes, flags, dtype, strides),
+ * LIF_ERR_SIZE (K > LIF_CONV_MAX, B * D >= 2^28, T > 2^30 or B * T * D >=
+ * 2^40), LIF_ERR_WORKSPACE. */
+#define LIF_CONV_MAX 8
+#define LIF_CONV_SILU 1u
+typedef struct lif_conv_params {
+    int32_t  B, T, D, K;         /* samples, steps, channels, taps (>= 2); T or B may be 0 */
+    int32_t  dtype;
+    uint32_t flags;              /* LIF_CONV_SILU                                   */
+    int64_t  x_batch, x_time;    /* strides of x in elements                        */
+    int64_t  g_batch, g_time;    /* strides of grad_y (backward pass)               */
+} lif_conv_params;
+
+size_t lif_causal_conv_workspace_size(const lif_conv_params* p);
+int lif_causal_conv(const void* x, const float* w, const float* bias, const int32_t* length, const void* x_first,
+                    const lif_conv_params* p, void* y, void* x_last, lif_stream_t stream);
+int lif_causal_conv_backward(const void* x, const float* w, const float* bias, const int32_t* length,
+                             const void* x_first, const void* grad_y, const float* grad_last,
+                             const lif_conv_params* p, void* grad_x, float* grad_w, float* grad_bias,
+                             float* grad_x_first, void* ws, size_t ws_bytes, lif_stream_t stream);
+int lif_causal_conv_step(const void* x, const float* w, const float* bias, const int32_t* slot, void* state,
+                         int n_slots, const lif_conv_params* p, void* y, lif_stream_t stream);
+
+/* Selective state space scan: D channels in G = p->G groups of D / G, each
+ * channel with N states.  With g the group of channel d,
+ *   r = dt_t[d] + dt_bias[d]
+ *   delta = log(1 + e^r)  (LIF_SELECT_SOFTPLUS), or r without the flag
+ *   h_t[d][i] = e^{delta A[d][i]} h_{t-1}[d][i] + delta x_t[d] B_t[g][i]
+ *   y_t[d] = (sum_i C_t[g][i] h_t[d][i] + skip[d] x_t[d]) s(z_t[d])
+ * with s(z) = z / (1 + e^{-z}) (z NULL: 1), from h_{-1} = h_first (NULL: 0).
+ * With A < 0 this is a bank of leaky integrators whose step lengths, inputs and
+ * readouts depend on the token.
+ *   x, dt, z  [B][T][D] of p->dtype, rows contiguous, strides >= 0
+ *   Bm, C     [B][T][G][N] of p->dtype, the G * N values of a step contiguous
+ *   A         float [D][N]; skip, dt_bias float [D] (NULL: 0)
+ *   h_first   float [B][D][N]
+ *   y         [B][T][D] contiguous, of p->dtype; may be NULL
+ *   h_last    float [B][D][N], the state after step n - 1; may be NULL
+ *   marks     float [B][ceil(T / LIF_SELECT_MARK)][N][D]: the states entering
+ *             steps 0, LIF_SELECT_MARK, 2 LIF_SELECT_MARK, ... < n (later ones
+ *             are not written); the backward pass needs them; may be NULL
+ * Decays e^{delta A} below 2^-126 count as 0.
+ *
+ * lif_selective_scan_backward: for dL/dy = grad_y ([B][T][D] of p->dtype, rows
+ * contiguous, strides g_batch, g_time; NULL: 0) and dL/dh_last = grad_last
+ * (float [B][D][N]; NULL: 0), from the forward's marks, the gradients of every
+ * input:
+ *   grad_x, grad_dt, grad_z  [B][T][D] contiguous, of p->dtype; 0 at t >= n
+ *            (grad_z with z only)
+ *   grad_B, grad_C  [B][T][G][N] contiguous, of p->dtype; 0 at t >= n
+ *   grad_A   float [D][N]; grad_skip, grad_dt_bias float [D] (may be NULL)
+ *   grad_h_first  float [B][D][N]; may be NULL
+ * Where one row of an input serves several steps or samples (stride 0), the
+ * caller sums their gradients.
+ *
+ * lif_selective_step: one step of B streams whose states are rows slot[b] of
+ * state (float [n_slots][D][N], updated in place; slot NULL: row b).  p->T is
+ * 1; x, dt, z [B][D] and Bm, C [B][G][N] with their batch strides; y [B][D]
+ * contiguous.  The slots of one call must be distinct; a stream whose slot lies
+ * outside [0, n_slots) is left out (its y is 0).
+ *
+ * ws: lif_selective_scan_workspace_size(p) bytes for the forward pass (0 for
+ * many shapes; ws may then be NULL), lif_selective_scan_backward_workspace_size
+ * for the backward pass, 16-byte aligned.
+ * Errors: LIF_ERR_ARG (null pointers, sizes, flags, dtype, strides, D not a
+ * multiple of G), LIF_ERR_SIZE (N > LIF_SELECT_MAX_STATES, B * D >= 2^26, T >
+ * 2^30, B * T * D * N >= 2^44 or B * G * ceil(D / G / 64) >= 2^23),
+ * LIF_ERR_WORKSPACE. */
+#define LIF_SELECT_MARK 16
+#define LIF_SELECT_MAX_STATES 64
+#define LIF_SELECT_SOFTPLUS 1u
+typedef struct lif_select_params {
+    int32_t  B, T, D, N, G;      /* samples, steps, channels, states, groups; T or B may be 0 */
+    int32_t  dtype;
+    uint32_t flags;              /* LIF_SELECT_SOFTPLUS                             */
+    int32_t  reserved;           /* must be 0                                       */
+    int64_t  x_batch, x_time;    /* strides in elements                             */
+    int64_t  dt_batch, dt_time;
+    int64_t  z_batch, z_time;
+    int64_t  b_batch, b_time;    /* of Bm                                           */
+    int64_t  c_batch, c_time;
+    int64_t  g_batch, g_time;    /* of grad_y (backward pass)                       */
+} lif_select_params;
+
+size_t lif_selective_scan_workspace_size(const lif_select_params* p);
+int lif_selective_scan(const void* x, const void* dt, const float* A, const void* Bm, const void* C,
+                       const float* skip, const void* z, const float* dt_bias, const int32_t* length,
+                       const float* h_first, const lif_select_params* p, void* y, float* h_last, float* marks,
+                       void* ws, size_t ws_bytes, lif_stream_t stream);
+size_t lif_selective_scan_backward_workspace_size(const lif_select_params* p);
+int lif_selective_scan_backward(const void* x, const void* dt, const float* A, const void* Bm, const void* C,
+                                const float* skip, const void* z, const float* dt_bias, const int32_t* length,
+                                const float* marks, const void* grad_y, const float* grad_last,
+                                const lif_select_params* p, void* grad_x, void* grad_dt, float* grad_A, void* grad_B,
+                                void* grad_C, float* grad_skip, void* grad_z, float* grad_dt_bias,
+                                float* grad_h_first, void* ws, size_t ws_bytes, lif_stream_t stream);
+int lif_selective_step(const void* x, const void* dt, const float* A, const void* Bm, const void* C,
+                       const float* skip, const void* z, const float* dt_bias, const int32_t* slot, float* state,
+                       int n_slots, const lif_select_params* p, void* y, lif_stream_t stream);
+
+/* --------------------------------------------------------------------- */
 /* Optional kernel timer (host-side state, off by default).  When enabled, */
 /* every kernel launched by this library is launched with a pair of HIP    */
 /* events that its own dispatch records (hipExtLaunchKernel), so each      */

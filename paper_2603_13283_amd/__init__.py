@@ -5,10 +5,12 @@ in the library's HIP kernels.  PyTorch supplies device memory and the current
 HIP stream.  The entry points carry the C names of ``include/lif.h``
 (``lif_layer_forward``, ``lif_layer_forward_sequential``,
 ``lif_layer_backward``, ``lif_merge_spikes``, ``lif_first_spike_ce``,
-``lif_gated_scan``, ``lif_token_logprobs``, ``lif_distill_top``, the
+``lif_gated_scan``, ``lif_token_logprobs``, ``lif_distill_top``,
+``lif_embed``, ``lif_causal_conv``, ``lif_selective_scan``, the
 workspace-size queries, ``lif_version``); ``forward``/``backward``/``merge``/
-``gated_scan``/``token_logprobs``/``distill_top`` are conveniences that
-allocate outputs and workspace as torch tensors and call them.
+``gated_scan``/``token_logprobs``/``distill_top``/``embed``/``causal_conv``/
+``selective_scan`` are conveniences that allocate outputs and workspace as
+torch tensors and call them.
 
 Importing this module does not touch the GPU.  Loading the library fails
 loudly (``LibraryMissing``) if ``liblif.so`` has not been built: there is no
@@ -61,6 +63,10 @@ EXPORTED = ["lif_version", "lif_layer_forward_workspace_size", "lif_layer_forwar
             "lif_add", "lif_softplus", "lif_softplus_grad",
             "lif_gated_scan_workspace_size", "lif_gated_scan", "lif_gated_scan_backward", "lif_gated_step",
             "lif_rows_workspace_size", "lif_token_logprobs", "lif_distill_top",
+            "lif_embed", "lif_embed_backward_workspace_size", "lif_embed_backward",
+            "lif_causal_conv_workspace_size", "lif_causal_conv", "lif_causal_conv_backward", "lif_causal_conv_step",
+            "lif_selective_scan_workspace_size", "lif_selective_scan",
+            "lif_selective_scan_backward_workspace_size", "lif_selective_scan_backward", "lif_selective_step",
             "lif_timer_enable", "lif_timer_read"]
 LIF_LI_MAX_CLASSES = 64
 LIF_F32, LIF_BF16, LIF_F16 = 0, 1, 2
@@ -69,6 +75,11 @@ LIF_GATED_COUPLED = 1
 LIF_TOP_MAX = 128
 LIF_DISTILL_TAIL = 1
 LIF_DISTILL_TAIL_MIN = 2.0 ** -20
+LIF_CONV_MAX = 8
+LIF_CONV_SILU = 1
+LIF_SELECT_MARK = 16
+LIF_SELECT_MAX_STATES = 64
+LIF_SELECT_SOFTPLUS = 1
 
 
 class LibraryMissing(RuntimeError):
@@ -145,6 +156,29 @@ class lif_rows_params(ctypes.Structure):
     _fields_ = [("R", ctypes.c_int32), ("V", ctypes.c_int32), ("k", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("stride", ctypes.c_int64), ("grad_stride", ctypes.c_int64), ("temperature", ctypes.c_double),
                 ("flags", ctypes.c_uint32), ("reserved", ctypes.c_int32)]
+
+
+class lif_embed_params(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("table", ctypes.c_int32), ("w_row", ctypes.c_int64),
+                ("g_batch", ctypes.c_int64), ("g_time", ctypes.c_int64), ("scale", ctypes.c_double),
+                ("flags", ctypes.c_uint32), ("reserved", ctypes.c_int32)]
+
+
+class lif_conv_params(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("D", ctypes.c_int32), ("K", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("x_batch", ctypes.c_int64),
+                ("x_time", ctypes.c_int64), ("g_batch", ctypes.c_int64), ("g_time", ctypes.c_int64)]
+
+
+class lif_select_params(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("D", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("G", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("reserved", ctypes.c_int32), ("x_batch", ctypes.c_int64), ("x_time", ctypes.c_int64),
+                ("dt_batch", ctypes.c_int64), ("dt_time", ctypes.c_int64), ("z_batch", ctypes.c_int64),
+                ("z_time", ctypes.c_int64), ("b_batch", ctypes.c_int64), ("b_time", ctypes.c_int64),
+                ("c_batch", ctypes.c_int64), ("c_time", ctypes.c_int64), ("g_batch", ctypes.c_int64),
+                ("g_time", ctypes.c_int64)]
 
 
 _lib = None
@@ -255,6 +289,23 @@ def load(path: Optional[str] = None):
     lib.lif_token_logprobs.argtypes = [_P, _P, rp, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
     lib.lif_distill_top.restype = _I
     lib.lif_distill_top.argtypes = [_P, _P, _P, rp, _P, _P, _P, _P, _SZ, _P]
+    ep, cp, sp = (ctypes.POINTER(s) for s in (lif_embed_params, lif_conv_params, lif_select_params))
+    for name, params in (("lif_embed_backward", ep), ("lif_causal_conv", cp), ("lif_selective_scan", sp),
+                         ("lif_selective_scan_backward", sp)):
+        f = getattr(lib, name + "_workspace_size")
+        f.restype = _SZ
+        f.argtypes = [params]
+    for name, args in (("lif_embed", [_P, _P, _P, ep, _P, _P]),
+                       ("lif_embed_backward", [_P, _P, _P, ep, _P, _P, _SZ, _P]),
+                       ("lif_causal_conv", [_P, _P, _P, _P, _P, cp, _P, _P, _P]),
+                       ("lif_causal_conv_backward", [_P] * 7 + [cp] + [_P] * 5 + [_SZ, _P]),
+                       ("lif_causal_conv_step", [_P, _P, _P, _P, _P, _I, cp, _P, _P]),
+                       ("lif_selective_scan", [_P] * 10 + [sp] + [_P] * 4 + [_SZ, _P]),
+                       ("lif_selective_scan_backward", [_P] * 12 + [sp] + [_P] * 10 + [_SZ, _P]),
+                       ("lif_selective_step", [_P] * 10 + [_I, sp, _P, _P])):
+        f = getattr(lib, name)
+        f.restype = _I
+        f.argtypes = args
     lib.lif_timer_enable.restype = None
     lib.lif_timer_enable.argtypes = [_I]
     lib.lif_timer_read.restype = _I
@@ -422,6 +473,54 @@ def lif_token_logprobs(*args) -> int:
 
 def lif_distill_top(*args) -> int:
     return load().lif_distill_top(*args)
+
+
+def lif_embed(*args) -> int:
+    return load().lif_embed(*args)
+
+
+def lif_embed_backward_workspace_size(p: lif_embed_params) -> int:
+    return int(load().lif_embed_backward_workspace_size(ctypes.byref(p)))
+
+
+def lif_embed_backward(*args) -> int:
+    return load().lif_embed_backward(*args)
+
+
+def lif_causal_conv_workspace_size(p: lif_conv_params) -> int:
+    return int(load().lif_causal_conv_workspace_size(ctypes.byref(p)))
+
+
+def lif_causal_conv(*args) -> int:
+    return load().lif_causal_conv(*args)
+
+
+def lif_causal_conv_backward(*args) -> int:
+    return load().lif_causal_conv_backward(*args)
+
+
+def lif_causal_conv_step(*args) -> int:
+    return load().lif_causal_conv_step(*args)
+
+
+def lif_selective_scan_workspace_size(p: lif_select_params) -> int:
+    return int(load().lif_selective_scan_workspace_size(ctypes.byref(p)))
+
+
+def lif_selective_scan(*args) -> int:
+    return load().lif_selective_scan(*args)
+
+
+def lif_selective_scan_backward_workspace_size(p: lif_select_params) -> int:
+    return int(load().lif_selective_scan_backward_workspace_size(ctypes.byref(p)))
+
+
+def lif_selective_scan_backward(*args) -> int:
+    return load().lif_selective_scan_backward(*args)
+
+
+def lif_selective_step(*args) -> int:
+    return load().lif_selective_step(*args)
 
 
 def lif_timer_enable(on: bool) -> None:
@@ -1078,3 +1177,325 @@ def distill_top(logits, teacher_logp, teacher_idx, temperature: float = 1.0, tai
                              _ptr(weight), loss.data_ptr(), _ptr(grad), wp, wn, _raw_stream(torch, dev, stream))
         _check("lif_distill_top", rc)
         return loss, grad
+
+
+# ---------------------------------------------------------------------------
+# models over tokens
+# ---------------------------------------------------------------------------
+
+@functools.lru_cache(maxsize=256)
+def _embed_ws(B, T, V, D) -> int:
+    """lif_embed_backward_workspace_size: it depends on sizes only."""
+    return lif_embed_backward_workspace_size(lif_embed_params(B, T, V, D, LIF_F32, LIF_F32, D, 0, 0, 1.0, 0, 0))
+
+
+@functools.lru_cache(maxsize=256)
+def _conv_ws(B, T, D, K, dtype) -> int:
+    """lif_causal_conv_workspace_size: it depends on sizes and type only."""
+    return lif_causal_conv_workspace_size(lif_conv_params(B, T, D, K, dtype, 0, 0, 0, 0, 0))
+
+
+@functools.lru_cache(maxsize=256)
+def _select_ws(B, T, D, N, G, dtype, back) -> int:
+    """The scan's workspace sizes: they depend on sizes and type only."""
+    p = lif_select_params(B, T, D, N, G, dtype, *([0] * 14))
+    return (lif_selective_scan_backward_workspace_size if back else lif_selective_scan_workspace_size)(p)
+
+
+def _tokens(torch, tokens, length):
+    """(tokens, length, B, T): tokens [B] are one place of each sample."""
+    if tokens.dim() not in (1, 2):
+        raise ValueError("tokens must be [B] or [B, T]")
+    tokens = _expect("tokens", tokens, tokens.shape, torch.int32, tokens.device)
+    B, T = tokens.shape if tokens.dim() == 2 else (tokens.shape[0], 1)
+    return tokens, _expect("length", length, (B,), torch.int32, tokens.device), B, T
+
+
+def embed(tokens, W, scale: float = 1.0, length=None, dtype=None, stream=None):
+    """Run lif_embed: scale times the rows of W [V, D] (any row stride) that
+    tokens (int32 [B, T], or [B]) name, 0 for a token outside the table and at
+    places from length (int32 [B]) on.  Returns [B, T, D] (or [B, D]) of dtype
+    (default: W's)."""
+    torch = _torch()
+    with _on(torch, tokens, stream):
+        tokens, length, B, T = _tokens(torch, tokens, length)
+        dev = tokens.device
+        if W.dim() != 2:
+            raise ValueError("W must be [V, D]")
+        table, (V, D) = _dtype_code("W", W), W.shape
+        W = _rows_of("W", W, W.shape, W.dtype, dev)
+        _int32(B, T, V, D)
+        if V > 1 and W.stride(0) < D:
+            W = W.contiguous()
+        out = torch.empty((*tokens.shape, D), dtype=dtype or W.dtype, device=dev)
+        p = lif_embed_params(B, T, V, D, _dtype_code("dtype", out), table, W.stride(0) if V > 1 else D, 0, 0,
+                             float(scale), 0, 0)
+        rc = lif_embed(tokens.data_ptr(), W.data_ptr(), _ptr(length), ctypes.byref(p), out.data_ptr(),
+                       _raw_stream(torch, dev, stream))
+        _check("lif_embed", rc)
+        return out
+
+
+def embed_backward(tokens, grad, rows: int, scale: float = 1.0, length=None, stream=None, ws=None):
+    """Run lif_embed_backward: the gradient (float32 [rows, D]) of embed's
+    table of that many rows, for dL/dout = grad [B, T, D] (any batch and time
+    strides; [B, D] for tokens [B])."""
+    torch = _torch()
+    with _on(torch, tokens, stream):
+        tokens, length, B, T = _tokens(torch, tokens, length)
+        dev = tokens.device
+        if grad.dim() != tokens.dim() + 1:
+            raise ValueError("grad must have the shape of tokens and one axis more")
+        D, code = grad.shape[-1], _dtype_code("grad", grad)
+        grad = _rows_of("grad", grad, (*tokens.shape, D), grad.dtype, dev)
+        _int32(B, T, rows, D)
+        p = lif_embed_params(B, T, int(rows), D, code, code, D, grad.stride(0),
+                             grad.stride(1) if tokens.dim() == 2 else 0, float(scale), 0, 0)
+        gW = torch.empty((int(rows), D), dtype=torch.float32, device=dev)
+        wp, wn, ws = _workspace(torch, _embed_ws(B, T, int(rows), D), ws, dev)
+        rc = lif_embed_backward(tokens.data_ptr(), grad.data_ptr(), _ptr(length), ctypes.byref(p), gW.data_ptr(), wp,
+                                wn, _raw_stream(torch, dev, stream))
+        _check("lif_embed_backward", rc)
+        return gW
+
+
+@dataclass
+class ConvOut:
+    y: "object"              # [B, T, D], the input's type
+    x_last: "object"         # [B, K - 1, D], the input's type: x_first of the piece that follows
+
+
+@dataclass
+class ConvGrads:
+    x: "object"              # [B, T, D], the input's type
+    w: "object"              # float32 [D, K]
+    bias: "object"           # float32 [D]; None without a bias
+    x_first: "object"        # float32 [B, K - 1, D]: grad_last of the piece before
+
+
+def _conv_inputs(torch, x, w, bias, dims):
+    if x.dim() != dims or not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor " + ("[B, T, D]" if dims == 3 else "[B, D]"))
+    code, dev, D = _dtype_code("x", x), x.device, x.shape[-1]
+    x = _rows_of("x", x, x.shape, x.dtype, dev)
+    if w.dim() != 2:
+        raise ValueError("w must be [D, K]")
+    K = w.shape[1]
+    w = _expect("w", w, (D, K), torch.float32, dev)
+    _int32(*x.shape)
+    return x, w, _expect("bias", bias, (D,), torch.float32, dev), code, dev, D, K
+
+
+def causal_conv(x, w, bias=None, length=None, x_first=None, silu: bool = True, stream=None) -> ConvOut:
+    """Run lif_causal_conv on x [B, T, D] (any batch and time strides): each
+    channel's short convolution along time with taps w (float32 [D, K], the
+    last one for the present step) and its activation.  x_first [B, K - 1, D]
+    holds the inputs before the first step."""
+    torch = _torch()
+    with _on(torch, x, stream):
+        x, w, bias, code, dev, D, K = _conv_inputs(torch, x, w, bias, 3)
+        B, T = x.shape[:2]
+        length = _expect("length", length, (B,), torch.int32, dev)
+        x_first = _expect("x_first", x_first, (B, K - 1, D), x.dtype, dev)
+        p = lif_conv_params(B, T, D, K, code, LIF_CONV_SILU if silu else 0, x.stride(0), x.stride(1), 0, 0)
+        y = torch.empty((B, T, D), dtype=x.dtype, device=dev)
+        last = torch.empty((B, max(K - 1, 0), D), dtype=x.dtype, device=dev)
+        rc = lif_causal_conv(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(length), _ptr(x_first), ctypes.byref(p),
+                             y.data_ptr(), last.data_ptr(), _raw_stream(torch, dev, stream))
+        _check("lif_causal_conv", rc)
+        return ConvOut(y, last)
+
+
+def causal_conv_backward(x, w, grad_y, bias=None, length=None, x_first=None, grad_last=None, silu: bool = True,
+                         stream=None, ws=None) -> ConvGrads:
+    """Run lif_causal_conv_backward with the forward's inputs, dL/dy = grad_y
+    (None: 0) and dL/dx_last = grad_last (float32 [B, K - 1, D])."""
+    torch = _torch()
+    with _on(torch, x, stream):
+        x, w, bias, code, dev, D, K = _conv_inputs(torch, x, w, bias, 3)
+        B, T = x.shape[:2]
+        length = _expect("length", length, (B,), torch.int32, dev)
+        x_first = _expect("x_first", x_first, (B, K - 1, D), x.dtype, dev)
+        grad_last = _expect("grad_last", grad_last, (B, K - 1, D), torch.float32, dev)
+        if grad_y is not None:
+            grad_y = _rows_of("grad_y", grad_y, x.shape, x.dtype, dev)
+        p = lif_conv_params(B, T, D, K, code, LIF_CONV_SILU if silu else 0, x.stride(0), x.stride(1),
+                            *((0, 0) if grad_y is None else grad_y.stride()[:2]))
+        gx = torch.empty((B, T, D), dtype=x.dtype, device=dev)
+        gw = torch.empty((D, K), dtype=torch.float32, device=dev)
+        gb = None if bias is None else torch.empty(D, dtype=torch.float32, device=dev)
+        g0 = torch.empty((B, max(K - 1, 0), D), dtype=torch.float32, device=dev)
+        wp, wn, ws = _workspace(torch, _conv_ws(B, T, D, K, code), ws, dev)
+        rc = lif_causal_conv_backward(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(length), _ptr(x_first),
+                                      _ptr(grad_y), _ptr(grad_last), ctypes.byref(p), gx.data_ptr(), gw.data_ptr(),
+                                      _ptr(gb), g0.data_ptr(), wp, wn, _raw_stream(torch, dev, stream))
+        _check("lif_causal_conv_backward", rc)
+        return ConvGrads(gx, gw, gb, g0)
+
+
+def _pool(torch, state, shape, dtype, dev):
+    """A contiguous pool of states [n_slots, *shape], updated in place."""
+    if state.shape[1:] != shape or state.dim() != len(shape) + 1 or state.dtype != dtype or state.device != dev or \
+            not state.is_contiguous():
+        raise ValueError(f"state must be a contiguous {dtype} tensor [n_slots, {', '.join(map(str, shape))}] on {dev}")
+    _int32(state.shape[0])
+    return state
+
+
+def causal_conv_step(x, w, state, slot=None, bias=None, silu: bool = True, stream=None):
+    """Run lif_causal_conv_step: one step of B streams, x [B, D]; their last
+    K - 1 inputs are rows slot (int32 [B], distinct; None: rows 0 .. B - 1) of
+    state ([n_slots, K - 1, D] of x's type), updated in place.  Returns y
+    [B, D]."""
+    torch = _torch()
+    with _on(torch, x, stream):
+        x, w, bias, code, dev, D, K = _conv_inputs(torch, x, w, bias, 2)
+        B = x.shape[0]
+        state = _pool(torch, state, (K - 1, D), x.dtype, dev)
+        slot = _expect("slot", slot, (B,), torch.int32, dev)
+        p = lif_conv_params(B, 1, D, K, code, LIF_CONV_SILU if silu else 0, x.stride(0), 0, 0, 0)
+        y = torch.empty((B, D), dtype=x.dtype, device=dev)
+        rc = lif_causal_conv_step(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(slot), state.data_ptr(),
+                                  state.shape[0], ctypes.byref(p), y.data_ptr(), _raw_stream(torch, dev, stream))
+        _check("lif_causal_conv_step", rc)
+        return y
+
+
+@dataclass
+class SelectiveOut:
+    y: "object"              # [B, T, D], the inputs' type; None when not asked for
+    h_last: "object"         # float32 [B, D, N]: h_first of the piece that follows
+    marks: "object" = None   # float32 [B, ceil(T / 16), N, D]: the states that the backward pass starts from
+
+
+@dataclass
+class SelectiveGrads:
+    x: "object"              # [B, T, D], as dt and z
+    dt: "object"
+    A: "object"              # float32 [D, N]
+    B: "object"              # of B's shape and type, as C
+    C: "object"
+    D: "object"              # float32 [D]; None without it, as z and dt_bias
+    z: "object"
+    dt_bias: "object"
+    h_first: "object"        # float32 [B, D, N]: grad_last of the piece before
+
+
+class _Selective:
+    """The inputs of the selective scan and of its step, checked."""
+
+    def __init__(self, torch, x, dt, A, B, C, D, z, dt_bias, dims):
+        lead = dims - 1                                  # axes before the channels
+        if x.dim() != dims or not x.is_cuda:
+            raise ValueError("x must be a CUDA tensor " + ("[B, T, D]" if dims == 3 else "[B, D]"))
+        self.dev, self.code, self.type = x.device, _dtype_code("x", x), x.dtype
+        self.steps, self.width = x.shape[:lead], x.shape[-1]
+        self.x = _rows_of("x", x, x.shape, x.dtype, self.dev)
+        self.dt = _rows_of("dt", dt, x.shape, x.dtype, self.dev)
+        self.z = None if z is None else _rows_of("z", z, x.shape, x.dtype, self.dev)
+        if A.dim() != 2:
+            raise ValueError("A must be [D, N]")
+        self.N = A.shape[1]
+        self.A = _expect("A", A, (self.width, self.N), torch.float32, self.dev)
+        self.G = B.shape[lead] if B.dim() == dims + 1 else 1
+        shape = (*self.steps, self.G, self.N) if B.dim() == dims + 1 else (*self.steps, self.N)
+        self.B, self.C = self._states("B", B, shape), self._states("C", C, shape)
+        self.D = _expect("D", D, (self.width,), torch.float32, self.dev)
+        self.dt_bias = _expect("dt_bias", dt_bias, (self.width,), torch.float32, self.dev)
+        _int32(*x.shape, self.N, self.G)
+
+    def _states(self, name, t, shape):
+        """B or C: the last two axes (groups, states) contiguous."""
+        t = _rows_of(name, t, shape, self.type, self.dev)
+        if len(shape) > len(self.steps) + 1 and shape[-2] > 1 and t.stride(-2) != shape[-1]:
+            t = t.contiguous()
+        return t
+
+    def params(self, softplus, grad=None):
+        def strides(t):
+            if t is None:
+                return 0, 0
+            return t.stride()[:2] if len(self.steps) == 2 else (t.stride(0), 0)
+        B, T = self.steps if len(self.steps) == 2 else (self.steps[0], 1)
+        pairs = (s for t in (self.x, self.dt, self.z, self.B, self.C, grad) for s in strides(t))
+        return lif_select_params(B, T, self.width, self.N, self.G, self.code, LIF_SELECT_SOFTPLUS if softplus else 0,
+                                 0, *pairs)
+
+    def pointers(self):
+        return (self.x.data_ptr(), self.dt.data_ptr(), self.A.data_ptr(), self.B.data_ptr(), self.C.data_ptr(),
+                _ptr(self.D), _ptr(self.z), _ptr(self.dt_bias))
+
+
+def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, length=None, h_first=None, softplus: bool = True,
+                   marks: bool = False, outputs: bool = True, stream=None, ws=None) -> SelectiveOut:
+    """Run lif_selective_scan: x, dt, z [B, T, D] and B, C [B, T, N] or
+    [B, T, G, N] (any batch and time strides), A float32 [D, N], D and dt_bias
+    float32 [D], length int32 [B], h_first float32 [B, D, N].  marks=True keeps
+    what selective_scan_backward needs; outputs=False returns the last state
+    only."""
+    torch = _torch()
+    with _on(torch, x, stream):
+        a = _Selective(torch, x, dt, A, B, C, D, z, dt_bias, 3)
+        (nb, T), W, N, dev = a.steps, a.width, a.N, a.dev
+        length = _expect("length", length, (nb,), torch.int32, dev)
+        h_first = _expect("h_first", h_first, (nb, W, N), torch.float32, dev)
+        p = a.params(softplus)
+        y = torch.empty((nb, T, W), dtype=a.type, device=dev) if outputs else None
+        last = torch.empty((nb, W, N), dtype=torch.float32, device=dev)
+        mk = torch.empty((nb, -(-T // LIF_SELECT_MARK), N, W), dtype=torch.float32, device=dev) if marks else None
+        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, a.G, a.code, False), ws, dev)
+        rc = lif_selective_scan(*a.pointers(), _ptr(length), _ptr(h_first), ctypes.byref(p), _ptr(y), last.data_ptr(),
+                                _ptr(mk), wp, wn, _raw_stream(torch, dev, stream))
+        _check("lif_selective_scan", rc)
+        return SelectiveOut(y, last, mk)
+
+
+def selective_scan_backward(x, dt, A, B, C, marks, grad_y=None, D=None, z=None, dt_bias=None, grad_last=None,
+                            length=None, softplus: bool = True, stream=None, ws=None) -> SelectiveGrads:
+    """Run lif_selective_scan_backward with the forward's inputs and its
+    marks, dL/dy = grad_y (None: 0) and dL/dh_last = grad_last (float32
+    [B, D, N])."""
+    torch = _torch()
+    with _on(torch, x, stream):
+        a = _Selective(torch, x, dt, A, B, C, D, z, dt_bias, 3)
+        (nb, T), W, N, dev = a.steps, a.width, a.N, a.dev
+        length = _expect("length", length, (nb,), torch.int32, dev)
+        marks = _expect("marks", marks, (nb, -(-T // LIF_SELECT_MARK), N, W), torch.float32, dev)
+        if marks is None:
+            raise ValueError("the backward pass needs the forward's marks (selective_scan with marks=True)")
+        if grad_y is not None:
+            grad_y = _rows_of("grad_y", grad_y, x.shape, a.type, dev)
+        grad_last = _expect("grad_last", grad_last, (nb, W, N), torch.float32, dev)
+        p = a.params(softplus, grad_y)
+        full = lambda t, like, kind: None if like is None else torch.empty(t, dtype=kind, device=dev)   # noqa: E731
+        g = SelectiveGrads(*(full((nb, T, W), x, a.type) for _ in range(2)), full((W, N), A, torch.float32),
+                           full(B.shape, B, a.type), full(C.shape, C, a.type), full((W,), D, torch.float32),
+                           full((nb, T, W), z, a.type), full((W,), dt_bias, torch.float32),
+                           full((nb, W, N), x, torch.float32))
+        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, a.G, a.code, True), ws, dev)
+        rc = lif_selective_scan_backward(*a.pointers(), _ptr(length), marks.data_ptr(), _ptr(grad_y), _ptr(grad_last),
+                                         ctypes.byref(p), g.x.data_ptr(), g.dt.data_ptr(), g.A.data_ptr(),
+                                         g.B.data_ptr(), g.C.data_ptr(), _ptr(g.D), _ptr(g.z), _ptr(g.dt_bias),
+                                         g.h_first.data_ptr(), wp, wn, _raw_stream(torch, dev, stream))
+        _check("lif_selective_scan_backward", rc)
+        return g
+
+
+def selective_step(x, dt, A, B, C, state, slot=None, D=None, z=None, dt_bias=None, softplus: bool = True,
+                   stream=None):
+    """Run lif_selective_step: one step of B streams, x, dt, z [B, D] and B, C
+    [B, N] or [B, G, N]; their states are rows slot (int32 [B], distinct; None:
+    rows 0 .. B - 1) of state (float32 [n_slots, D, N]), updated in place.
+    Returns y [B, D]."""
+    torch = _torch()
+    with _on(torch, x, stream):
+        a = _Selective(torch, x, dt, A, B, C, D, z, dt_bias, 2)
+        nb, dev = a.steps[0], a.dev
+        state = _pool(torch, state, (a.width, a.N), torch.float32, dev)
+        slot = _expect("slot", slot, (nb,), torch.int32, dev)
+        p = a.params(softplus)
+        y = torch.empty((nb, a.width), dtype=a.type, device=dev)
+        rc = lif_selective_step(*a.pointers(), _ptr(slot), state.data_ptr(), state.shape[0], ctypes.byref(p),
+                                y.data_ptr(), _raw_stream(torch, dev, stream))
+        _check("lif_selective_step", rc)
+        return y

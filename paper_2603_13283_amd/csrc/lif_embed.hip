@@ -1,0 +1,445 @@
+// lif_embed.hip -- rows of a table by token (lif_embed), and the gradient of
+// the table (lif_embed_backward).
+//
+// The gradient sorts the places of the tokens, stably and by counting: a digit
+// at a time, each of a few hundred waves counts the digits of its chunk of
+// places, the counts are summed over chunks, and every wave hands out the
+// places of its chunk in order.  Then each row of the table has its places in
+// one run; the list is cut into pieces of equal length that waves sum up, and
+// runs that cross pieces are joined in the order of the pieces.  The order of
+// all sums follows from tokens and sizes alone.
+#include "lif_host.hpp"
+#include "lif_types.hpp"
+#include "lif_walk.hpp"
+
+namespace lif {
+namespace {
+
+constexpr int kMaxBits = 10;          // of a digit
+constexpr int kChunks = 256;          // waves that count and hand out
+constexpr int kAhead = 8;             // rows whose loads are in flight at once
+constexpr int kJoinWaves = 8;
+constexpr int kZeroRows = 16;         // rows of the table that a wave looks up
+
+// The row of place i, V where it has none.
+__device__ __forceinline__ uint32_t key_of(const int32_t* __restrict__ token, const int32_t* __restrict__ length,
+                                           int T, int V, int i)
+{
+    const int v = token[i];
+    bool on = v >= 0 && v < V;
+    if (length && on) {
+        const int b = i / T;
+        on = i - b * T < length[b];
+    }
+    return on ? (uint32_t)v : (uint32_t)V;
+}
+
+// Vectors of VEC elements; where VEC does not divide D, a row's last one starts
+// at D - VEC and repeats some of the one before.
+template <typename E, typename F, int VEC>
+__global__ __launch_bounds__(256) void k_embed(const int32_t* __restrict__ token, const E* __restrict__ W,
+                                               const int32_t* __restrict__ length, int T, int V, int D, int groups,
+                                               int rows, int64_t w_row, float scale, int R, F* __restrict__ out)
+{
+    const int64_t r0 = (int64_t)blockIdx.x * rows, items = (int64_t)min((int64_t)rows, R - r0) * groups;
+    for (int64_t j = threadIdx.x; j < items; j += 256) {
+        const int64_t r = r0 + j / groups;
+        const int d = min((int)(j % groups) * VEC, D - VEC);
+        const uint32_t v = key_of(token, length, T, V, (int)r);
+        E e[VEC];
+        F o[VEC];
+        if (v < (uint32_t)V) load_elems<E, VEC>(W + (int64_t)v * w_row + d, e);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) o[k] = from_f32<F>(v < (uint32_t)V ? to_f32(e[k]) * scale : 0.0f);
+        store_elems<F, VEC>(out + r * D + d, o);
+    }
+}
+
+struct Sort {
+    int R, T, V, chunk, chunks, bits, shift;
+};
+
+// Counts of a chunk's digits.
+__global__ __launch_bounds__(kWave) void k_count(const int32_t* __restrict__ token,
+                                                 const int32_t* __restrict__ length,
+                                                 const uint32_t* __restrict__ keys, Sort q,
+                                                 uint32_t* __restrict__ count)
+{
+    __shared__ uint32_t sh[1 << kMaxBits];
+    const int lane = threadIdx.x, bins = 1 << q.bits, c = blockIdx.x;
+    for (int i = lane; i < bins; i += kWave) sh[i] = 0;
+    __syncthreads();
+    const int end = min((int64_t)(c + 1) * q.chunk, (int64_t)q.R);
+    for (int64_t i = (int64_t)c * q.chunk + lane; i < end; i += kWave) {
+        const uint32_t k = keys ? keys[i] : key_of(token, length, q.T, q.V, (int)i);
+        atomicAdd(&sh[(k >> q.shift) & (bins - 1)], 1u);
+    }
+    __syncthreads();
+    for (int i = lane; i < bins; i += kWave) count[(int64_t)c * bins + i] = sh[i];
+}
+
+// Per digit: the counts become sums over the chunks before, total the whole.
+__global__ __launch_bounds__(kWave) void k_chunk_sums(uint32_t* __restrict__ count, int chunks, int bins,
+                                                      uint32_t* __restrict__ total)
+{
+    const int d = blockIdx.x * kWave + threadIdx.x;
+    if (d >= bins) return;
+    uint32_t s = 0;
+#pragma unroll 16
+    for (int c = 0; c < chunks; ++c) {
+        const uint32_t v = count[(int64_t)c * bins + d];
+        count[(int64_t)c * bins + d] = s;
+        s += v;
+    }
+    total[d] = s;
+}
+
+// Hands out a chunk's places in order: 64 at a time, lanes of the same digit
+// find each other by ballots over its bits.
+__global__ __launch_bounds__(kWave) void k_hand_out(const int32_t* __restrict__ token,
+                                                    const int32_t* __restrict__ length,
+                                                    const uint32_t* __restrict__ keys,
+                                                    const uint32_t* __restrict__ places, Sort q,
+                                                    const uint32_t* __restrict__ count,
+                                                    const uint32_t* __restrict__ total, uint32_t* __restrict__ keys_out,
+                                                    uint32_t* __restrict__ places_out)
+{
+    __shared__ uint32_t next[1 << kMaxBits];
+    const int lane = threadIdx.x, bins = 1 << q.bits, c = blockIdx.x;
+    // where each digit begins, and this chunk's part of it
+    const int per = (bins + kWave - 1) / kWave;
+    uint32_t sum = 0;
+    for (int i = 0; i < per; ++i)
+        if (lane * per + i < bins) sum += total[lane * per + i];
+    uint32_t before = sum;
+    for (int o = 1; o < kWave; o <<= 1) {
+        const uint32_t v = __shfl_up(before, o);
+        if (lane >= o) before += v;
+    }
+    before -= sum;
+    for (int i = 0; i < per; ++i) {
+        const int d = lane * per + i;
+        if (d < bins) {
+            next[d] = before + count[(int64_t)c * bins + d];
+            before += total[d];
+        }
+    }
+    __syncthreads();
+    const int64_t first = (int64_t)c * q.chunk;
+    const int n = (int)min((int64_t)q.chunk, (int64_t)q.R - first);
+    for (int i0 = 0; i0 < n; i0 += kWave) {
+        const bool on = i0 + lane < n;
+        const int64_t i = first + (on ? i0 + lane : 0);
+        const uint32_t k = keys ? keys[i] : key_of(token, length, q.T, q.V, (int)i);
+        const uint32_t digit = (k >> q.shift) & (bins - 1);
+        uint64_t same = __ballot(on);
+        for (int b = 0; b < q.bits; ++b) {
+            const uint64_t set = __ballot((digit >> b) & 1);
+            same &= (digit >> b) & 1 ? set : ~set;
+        }
+        const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+        uint32_t at = 0;
+        if (on) at = next[digit] + rank;
+        __syncthreads();
+        if (on && rank == 0) next[digit] = at + __popcll(same);
+        __syncthreads();
+        if (on) {
+            keys_out[at] = k;
+            places_out[at] = places ? places[i] : (uint32_t)i;
+        }
+    }
+}
+
+struct Sums {
+    int R, T, V, D, piece, pieces, columns;
+    int64_t g_batch, g_time;
+    float scale;
+};
+
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// A wave sums the rows of a piece of the sorted list for 64 VEC columns.  A run
+// that lies within the piece goes to the table's gradient, one that comes from
+// the piece before to part[piece][0], one that begins here and goes on to
+// part[piece][1].
+template <typename E, int VEC>
+__global__ __launch_bounds__(256) void k_embed_sums(const E* __restrict__ grad, const uint32_t* __restrict__ keys,
+                                                    const uint32_t* __restrict__ places, Sums q,
+                                                    float* __restrict__ gW, float* __restrict__ part)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int piece = __builtin_amdgcn_readfirstlane((int)(item / q.columns));
+    const int column = __builtin_amdgcn_readfirstlane((int)(item - (int64_t)piece * q.columns));
+    if (piece >= q.pieces) return;
+    const int first = piece * q.piece, end = min((int64_t)first + q.piece, (int64_t)q.R);
+    const int at = (column * kWave + lane) * VEC, d = min(at, q.D - VEC);
+    const bool live = at < q.D;
+    float acc[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
+    uint32_t run = uniform(keys[first]);
+    bool open = first > 0 && uniform(keys[first - 1]) == run;      // the run comes from the piece before
+    auto put = [&](float* to, float by) {
+        float o[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) o[k] = acc[k] * by;
+        if (live) store_elems<float, VEC>(to + d, o);
+    };
+    for (int i0 = first; i0 < end; i0 += kAhead) {
+        E row[kAhead][VEC];
+        uint32_t key[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int i = min(i0 + j, end - 1);
+            key[j] = uniform(keys[i]);
+            const int r = (int)uniform(places[i]), b = r / q.T;
+            if (key[j] < (uint32_t)q.V)
+                load_elems<E, VEC>(grad + b * q.g_batch + (r - b * q.T) * q.g_time + d, row[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (i0 + j >= end) break;
+            if (key[j] != run) {
+                if (open) put(part + (int64_t)piece * 2 * q.D, 1.0f);
+                else put(gW + (int64_t)run * q.D, q.scale);
+                run = key[j];
+                open = false;
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
+            }
+            if (run >= (uint32_t)q.V) return;                       // padding comes last
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) acc[k] += to_f32(row[j][k]);
+        }
+    }
+    const bool on = end < q.R && uniform(keys[end]) == run;        // it goes on in the next piece
+    if (open) put(part + (int64_t)piece * 2 * q.D, 1.0f);
+    else if (on) put(part + ((int64_t)piece * 2 + 1) * q.D, 1.0f);
+    else put(gW + (int64_t)run * q.D, q.scale);
+}
+
+// The first place in the sorted list whose key is at least v.
+__device__ __forceinline__ int lower_bound(const uint32_t* __restrict__ keys, int R, uint32_t v)
+{
+    int lo = 0, hi = R;
+    while (lo < hi) {
+        const int mid = lo + (hi - lo) / 2;
+        if (keys[mid] < v) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Workgroups below join_blocks: a piece and 64 VEC columns; if a run begins in
+// the piece and goes on, its parts are added up.  The others clear the rows of
+// the table that no token names.
+template <int VEC>
+__global__ __launch_bounds__(kJoinWaves* kWave) void k_embed_join(const uint32_t* __restrict__ keys, Sums q,
+                                                                  const float* __restrict__ part, int64_t join_blocks,
+                                                                  float* __restrict__ gW)
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (blockIdx.x >= join_blocks) {
+        const int64_t v0 = ((int64_t)(blockIdx.x - join_blocks) * kJoinWaves + w) * kZeroRows;
+        bool missing = false;
+        if (lane < kZeroRows && v0 + lane < q.V) {
+            const int at = lower_bound(keys, q.R, (uint32_t)(v0 + lane));
+            missing = at >= q.R || keys[at] != (uint32_t)(v0 + lane);
+        }
+        uint64_t rows = __ballot(missing);
+        const float zero[VEC] = {};
+        while (rows) {
+            const int i = __builtin_ctzll(rows);
+            rows &= rows - 1;
+            float* to = gW + (v0 + i) * q.D;
+            for (int d = lane * VEC; d < q.D; d += kWave * VEC) store_elems<float, VEC>(to + min(d, q.D - VEC), zero);
+        }
+        return;
+    }
+    __shared__ float sh[kJoinWaves][kWave * VEC];
+    const int piece = blockIdx.x / q.columns, column = blockIdx.x % q.columns;
+    const int64_t first = (int64_t)piece * q.piece, end = first + q.piece;
+    if (end >= q.R) return;
+    const uint32_t run = keys[end];
+    if (run >= (uint32_t)q.V || keys[end - 1] != run || (first > 0 && keys[first - 1] == run)) return;
+    const int last = (lower_bound(keys, q.R, run + 1) - 1) / q.piece, n = last - piece + 1;
+    const int at = (column * kWave + lane) * VEC, d = min(at, q.D - VEC);
+    float acc[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
+    const int to = (int)((int64_t)n * (w + 1) / kJoinWaves);
+#pragma unroll 4
+    for (int j = (int)((int64_t)n * w / kJoinWaves); j < to; ++j) {
+        float v[VEC];
+        load_elems<float, VEC>(part + ((int64_t)(piece + j) * 2 + (j == 0)) * q.D + d, v);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) acc[k] += v[k];
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) sh[w][lane * VEC + k] = acc[k];
+    __syncthreads();
+    if (w != 0 || at >= q.D) return;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        acc[k] = 0.0f;
+        for (int j = 0; j < kJoinWaves; ++j) acc[k] += sh[j][lane * VEC + k];
+        acc[k] *= q.scale;
+    }
+    store_elems<float, VEC>(gW + (int64_t)run * q.D + d, acc);
+}
+
+// No token at all: the gradient is 0.
+__global__ __launch_bounds__(256) void k_clear(float* __restrict__ to, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = 0.0f;
+}
+
+int check_embed(const lif_embed_params* p)
+{
+    if (!p || p->B < 0 || p->T < 0 || p->V < 1 || p->D < 1 || p->flags != 0 || p->reserved != 0) return LIF_ERR_ARG;
+    for (int t : {p->dtype, p->table})
+        if (t != LIF_F32 && t != LIF_BF16 && t != LIF_F16) return LIF_ERR_ARG;
+    if (p->w_row < p->D || p->g_batch < 0 || p->g_time < 0 || !isfinite(p->scale) || !isfinite((float)p->scale))
+        return LIF_ERR_ARG;
+    if (p->V > (1 << 24) || p->D > (1 << 20) || (int64_t)p->B * p->T >= ((int64_t)1 << 31)) return LIF_ERR_SIZE;
+    return LIF_OK;
+}
+
+int vec_of(int D) { return D >= 4 ? 4 : 1; }
+
+template <int V> struct Int { static constexpr int value = V; };
+
+struct Plan {
+    int passes, bits, chunk, chunks;
+    Sums s;
+    size_t keys[2], places[2], count, total, part, end;
+};
+
+Plan plan_of(const lif_embed_params& p)
+{
+    Plan q;
+    const int R = p.B * p.T;
+    int bits = 1;
+    while (((int64_t)1 << bits) <= p.V) ++bits;                     // keys are 0 .. V
+    q.passes = (bits + kMaxBits - 1) / kMaxBits;
+    q.bits = (bits + q.passes - 1) / q.passes;
+    const int64_t least = ((int64_t)R + kChunks - 1) / kChunks;
+    q.chunk = (int)((least + kWave - 1) / kWave * kWave);
+    q.chunks = q.chunk ? (int)(((int64_t)R + q.chunk - 1) / q.chunk) : 0;
+    Sums& s = q.s;
+    s.R = R, s.T = p.T, s.V = p.V, s.D = p.D;
+    s.columns = (p.D + kWave * vec_of(p.D) - 1) / (kWave * vec_of(p.D));
+    s.g_batch = p.g_batch, s.g_time = p.g_time;
+    s.scale = (float)p.scale;
+    int64_t piece = ((int64_t)R * s.columns + 4095) / 4096;
+    if (piece < 16) piece = 16;
+    if (piece > 1 << 30) piece = 1 << 30;
+    s.piece = (int)piece;
+    s.pieces = (int)(((int64_t)R + piece - 1) / piece);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 15) & ~(size_t)15;
+        return here;
+    };
+    for (int i = 0; i < 2; ++i) {
+        q.keys[i] = take(sizeof(uint32_t) * (size_t)R);
+        q.places[i] = take(sizeof(uint32_t) * (size_t)R);
+        if (q.passes == 1) q.keys[1] = q.keys[0], q.places[1] = q.places[0], i = 2;
+    }
+    q.count = take(sizeof(uint32_t) * ((size_t)q.chunks << q.bits));
+    q.total = take(sizeof(uint32_t) << q.bits);
+    q.part = take(sizeof(float) * 2 * (size_t)s.pieces * p.D);
+    q.end = R > 0 ? at : 0;
+    return q;
+}
+
+}  // namespace
+}  // namespace lif
+
+extern "C" int lif_embed(const int32_t* token, const void* W, const int32_t* length, const lif_embed_params* p,
+                         void* out, lif_stream_t stream)
+{
+    using namespace lif;
+    const int rc = check_embed(p);
+    if (rc) return rc;
+    const int64_t R = (int64_t)p->B * p->T;
+    if (R == 0) return LIF_OK;
+    if (!token || !W || !out) return LIF_ERR_ARG;
+    const int vec = vec_of(p->D), groups = (p->D + vec - 1) / vec;
+    // a workgroup's rows: about 1024 vectors, and no more than 2^22 workgroups
+    int rows = groups >= 1024 ? 1 : 1024 / groups;
+    while ((R + rows - 1) / rows > (1 << 22)) rows *= 2;
+    with_dtype(p->table, [&](auto e) {
+        with_dtype(p->dtype, [&](auto f) {
+            using E = decltype(e);
+            using F = decltype(f);
+            const dim3 grid((unsigned)((R + rows - 1) / rows));
+            if (vec == 4)
+                TIMED_LAUNCH("embed", (k_embed<E, F, 4>), grid, dim3(256), 0, (hipStream_t)stream, token, (const E*)W,
+                             length, p->T, p->V, p->D, groups, rows, p->w_row, (float)p->scale, (int)R, (F*)out);
+            else
+                TIMED_LAUNCH("embed", (k_embed<E, F, 1>), grid, dim3(256), 0, (hipStream_t)stream, token, (const E*)W,
+                             length, p->T, p->V, p->D, groups, rows, p->w_row, (float)p->scale, (int)R, (F*)out);
+        });
+    });
+    return check_launch();
+}
+
+extern "C" size_t lif_embed_backward_workspace_size(const lif_embed_params* p)
+{
+    using namespace lif;
+    if (check_embed(p) != LIF_OK) return 0;
+    return plan_of(*p).end;
+}
+
+extern "C" int lif_embed_backward(const int32_t* token, const void* grad, const int32_t* length,
+                                  const lif_embed_params* p, float* grad_W, void* ws, size_t ws_bytes,
+                                  lif_stream_t stream)
+{
+    using namespace lif;
+    const int rc = check_embed(p);
+    if (rc) return rc;
+    const int64_t R = (int64_t)p->B * p->T;
+    if (!grad_W || (R > 0 && (!token || !grad))) return LIF_ERR_ARG;
+    const Plan q = plan_of(*p);
+    if (q.end > 0 && (!ws || (uintptr_t)ws % 16)) return LIF_ERR_ARG;
+    if (ws_bytes < q.end) return LIF_ERR_WORKSPACE;
+    const hipStream_t s = (hipStream_t)stream;
+    if (R == 0) {
+        TIMED_LAUNCH("embed_clear", k_clear, dim3(1024), dim3(256), 0, s, grad_W, (int64_t)p->V * p->D);
+        return check_launch();
+    }
+    char* base = (char*)ws;
+    uint32_t *count = (uint32_t*)(base + q.count), *total = (uint32_t*)(base + q.total);
+    const uint32_t *keys = nullptr, *places = nullptr;
+    for (int i = 0; i < q.passes; ++i) {
+        const Sort o = {(int)R, p->T, p->V, q.chunk, q.chunks, q.bits, i * q.bits};
+        uint32_t *ko = (uint32_t*)(base + q.keys[i & 1]), *po = (uint32_t*)(base + q.places[i & 1]);
+        const int bins = 1 << q.bits;
+        TIMED_LAUNCH("embed_count", k_count, dim3(q.chunks), dim3(kWave), 0, s, token, length, keys, o, count);
+        TIMED_LAUNCH("embed_chunks", k_chunk_sums, dim3((bins + kWave - 1) / kWave), dim3(kWave), 0, s, count,
+                     q.chunks, bins, total);
+        TIMED_LAUNCH("embed_sort", k_hand_out, dim3(q.chunks), dim3(kWave), 0, s, token, length, keys, places, o,
+                     count, total, ko, po);
+        keys = ko, places = po;
+    }
+    const int64_t items = (int64_t)q.s.pieces * q.s.columns;
+    const int64_t zero = ((int64_t)p->V + kJoinWaves * kZeroRows - 1) / (kJoinWaves * kZeroRows);
+    const dim3 sums((unsigned)((items + 3) / 4)), join((unsigned)(items + zero));
+    float* part = (float*)(base + q.part);
+    with_dtype(p->dtype, [&](auto e) {
+        using E = decltype(e);
+        auto with = [&](auto vec) {
+            constexpr int VEC = decltype(vec)::value;
+            TIMED_LAUNCH("embed_sums", (k_embed_sums<E, VEC>), sums, dim3(256), 0, s, (const E*)grad, keys, places,
+                         q.s, grad_W, part);
+            TIMED_LAUNCH("embed_join", (k_embed_join<VEC>), join, dim3(kJoinWaves * kWave), 0, s, keys, q.s, part,
+                         items, grad_W);
+        };
+        if (vec_of(p->D) == 4) with(Int<4>());
+        else with(Int<1>());
+    });
+    return check_launch();
+}
