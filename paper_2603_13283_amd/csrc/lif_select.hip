@@ -17,6 +17,9 @@
 #include "lif_types.hpp"
 #include "lif_walk.hpp"
 
+#include <type_traits>
+#include <utility>
+
 namespace lif {
 namespace {
 
@@ -62,42 +65,34 @@ __device__ __forceinline__ Place place_of(const Geometry& q, const int32_t* __re
     return p;
 }
 
-// e^{-|r|}, to a few units of 2^-24: the power of two of the rounded product,
-// and to first order what the rounding left out.
-__device__ __forceinline__ float exp_neg(float r)
-{
-    const float q = -fabsf(r), p = q * kLog2e;
-    const float left = fmaf(q, kLog2e, -p) + q * 1.92596299e-8f;       // log2 e - kLog2e
-    const float e = __builtin_amdgcn_exp2f(p);
-    return fmaf(e, left * 0.693147181f, e);
-}
-
-// log(1 + e^r) = max(r, 0) + log1p(e^{-|r|}), and its derivative.  With
-// s = e / (2 + e) <= 1/3, log1p(e) = 2 atanh(s) = 2 (s + s^3/3 + s^5/5 + ...):
-// relative to the value to a few units of 2^-24 however small e is (the ninth
-// term is 9^-8 / 17 of the first).
+// log(1 + e^r) = max(r, 0) + log1p(e^{-|r|}), and its derivative, to a few
+// units of 2^-24 relative to the value.  e^{-|r|} is the power of two of the
+// rounded product, corrected to first order by what the rounding left out.
+// With s = 2 e / (2 + e) <= 2/3, log1p(e) = 2 atanh(s / 2) = s v(s^2), v a power
+// series with v(0) = 1; its polynomial of degree 4 that is best over [0, 4/9]
+// relative to the value is off by 0.8 10^-8.
 __device__ __forceinline__ float softplus(float r, float& slope)
 {
-    const float e = exp_neg(r);
-    const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
-    float v = 1.0f / 15.0f;
-    v = fmaf(v, q, 1.0f / 13.0f);
-    v = fmaf(v, q, 1.0f / 11.0f);
-    v = fmaf(v, q, 1.0f / 9.0f);
-    v = fmaf(v, q, 1.0f / 7.0f);
-    v = fmaf(v, q, 1.0f / 5.0f);
-    v = fmaf(v, q, 1.0f / 3.0f);
+    const float m = fminf(fabsf(r), 128.0f), p = -kLog2e * m;         // e is 0 from |r| = 104 on
+    const float left = fmaf(m, -1.92596299e-8f, fmaf(m, -kLog2e, -p));       // log2 e - kLog2e = 1.9 10^-8
+    float e = __builtin_amdgcn_exp2f(p);
+    e = fmaf(e, left * 0.693147181f, e);
+    const float s = e * __builtin_amdgcn_rcpf(fmaf(e, 0.5f, 1.0f)), q = s * s;
+    float v = fmaf(q, 5.50358106e-4f, 2.18442209e-3f);
+    v = fmaf(v, q, 1.25077845e-2f);
+    v = fmaf(v, q, 8.33328934e-2f);
     v = fmaf(v, q, 1.0f);
     const float k = __builtin_amdgcn_rcpf(1.0f + e);
     slope = r >= 0.0f ? k : e * k;
-    return (r != r) ? r : fmaf(2.0f * s, v, fmaxf(r, 0.0f));
+    return fmaf(0.5f, r + fabsf(r), s * v);                           // a NaN stays one
 }
 
 __device__ __forceinline__ float step_length(const Geometry& q, float r, float& slope)
 {
-    if (q.flags & LIF_SELECT_SOFTPLUS) return softplus(r, slope);
-    slope = 1.0f;
-    return r;
+    const bool soft = q.flags & LIF_SELECT_SOFTPLUS;
+    const float v = softplus(r, slope);
+    slope = soft ? slope : 1.0f;
+    return soft ? v : r;
 }
 
 // s(z) = z / (1 + e^-z) and its derivative.
@@ -116,153 +111,283 @@ __device__ __forceinline__ float rate_of(float a)
     return fabsf(v) > 3.0e38f ? copysignf(3.0e38f, v) : v;
 }
 
-// The raw elements of a tile that one thread loads: the steps w, w + W, ... of
-// its wave for its lane's channel, and a share of B and C.
-template <typename E, int NS, int W, int IN>
-struct Raw {
-    static constexpr int kSteps = kTile / W;
-    static constexpr int kShare = kTile * NS / kWave > 0 ? kTile * NS / kWave : 1;
-    E v[IN][kSteps];
-    E bc[2][kShare];
-};
-
-// Which share of a tile's B and C a thread brings: element j is step t[j],
-// state n[j] (on[j] false: none, or past N).
-template <int NS, int W> struct Share {
-    static constexpr int kShare = kTile * NS / kWave > 0 ? kTile * NS / kWave : 1;
-    int t[kShare], n[kShare];
-    bool there[kShare], on[kShare];
-    __device__ __forceinline__ Share(int N)
-    {
-#pragma unroll
-        for (int j = 0; j < kShare; ++j) {
-            const int i = threadIdx.x + j * W * kWave;
-            n[j] = i % (W * NS);
-            t[j] = i / (W * NS);
-            there[j] = t[j] < kTile;
-            on[j] = there[j] && n[j] < N;
-        }
-    }
-};
-
-template <typename E, int NS, int W, int IN>
-__device__ __forceinline__ void load_bc(Raw<E, NS, W, IN>& r, const Share<NS, W>& s, const E* __restrict__ Bm,
-                                        const E* __restrict__ C, const Geometry& q, const Place& p, int t0)
+template <int CTRL> __device__ __forceinline__ float dpp(float v)
 {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+
+// B_t[i] (or C_t[i]) of 16 steps lie in the lanes of each row of 16, step l % 16
+// in lane l.  An instruction of the vector unit reads the value of step I for
+// all lanes through its first operand.
+template <int I> __device__ __forceinline__ float of_step(float v) { return dpp<0x150 | I>(v); }
+
+// acc[j] += v of step I + j times x[j], for four steps.  The compiler has no
+// such sum; the wait lets a write of v by the instruction before arrive.
+template <int I> __device__ __forceinline__ void add_steps(float* acc, float v, float x0, float x1, float x2, float x3)
+{
+    asm("s_nop 1\n\t"
+        "v_fmac_f32_dpp %0, %4, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %1, %4, %6 row_newbcast:%10 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %2, %4, %7 row_newbcast:%11 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %3, %4, %8 row_newbcast:%12 row_mask:0xf bank_mask:0xf"
+        : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3])
+        : "v"(v), "v"(x0), "v"(x1), "v"(x2), "v"(x3), "n"(I), "n"(I + 1), "n"(I + 2), "n"(I + 3));
+}
+
+template <int I> using Step = std::integral_constant<int, I>;
+// fn(Step<0>()) .. fn(Step<15>()), or in reverse.
+template <typename Fn, int... I>
+__device__ __forceinline__ void each_of(Fn&& fn, std::integer_sequence<int, I...>)
+{
+    (fn(Step<I>()), ...);
+}
+template <typename Fn> __device__ __forceinline__ void each_step(Fn&& fn)
+{
+    each_of(fn, std::make_integer_sequence<int, kTile>());
+}
+template <typename Fn> __device__ __forceinline__ void each_step_back(Fn&& fn)
+{
+    each_of([&](auto i) { fn(Step<kTile - 1 - decltype(i)::value>()); }, std::make_integer_sequence<int, kTile>());
+}
+
+// A row stride that the compiler takes for a new value each time: otherwise it
+// keeps the multiples of every stride for a tile's steps in scalar registers,
+// and spills them.
+__device__ __forceinline__ int64_t fresh(int64_t stride)
+{
+    asm volatile("" : "+s"(stride));
+    return stride;
+}
+
+// An element on its way from memory, in a register of its own: the compiler
+// packs pairs of 16-bit ones into one register, and waits for the loads to do
+// so.
+template <typename E> struct Bits {
+    using type = std::conditional_t<sizeof(E) == 2, uint16_t, uint32_t>;
+    uint32_t v;
+    __device__ __forceinline__ void load(const E* at) { v = *reinterpret_cast<const type*>(at); }
+    __device__ __forceinline__ float f32() const { return to_f32(__builtin_bit_cast(E, (type)v)); }
+};
+
+// The raw elements of a tile that one lane loads: IN inputs of its channel for
+// the steps that its wave makes ready, w STEPS .. (w + 1) STEPS - 1, and B and
+// C of step lane % 16 for the wave's states.
+template <typename E, int NS, int STEPS, int IN, int NB = 1> struct Raw {
+    Bits<E> v[IN][STEPS];
+    Bits<E> bc[2][NB][NS];
+};
+
+// One input along time: the scalar address of a step's row, and bytes from one
+// row to the next; a lane's channel is an offset to it.
+struct Rows {
+    const char* at;
+    int64_t step;
+};
+template <typename E> __device__ __forceinline__ Rows rows_of(const void* in, int64_t batch, int64_t time, int b, int t)
+{
+    return {(const char*)((const E*)in + b * batch + t * time), time * (int64_t)sizeof(E)};
+}
+// STEPS steps, of which `there` are before the end; the last of those is
+// repeated in place of the others.
+template <typename E, int STEPS>
+__device__ __forceinline__ void load_rows(Bits<E> (&v)[STEPS], const Rows& r, uint32_t offset, int there = STEPS)
+{
+    const char* at = r.at;
 #pragma unroll
-    for (int j = 0; j < Raw<E, NS, W, IN>::kShare; ++j) {
-        r.bc[0][j] = r.bc[1][j] = from_f32<E>(0.0f);
-        const int t = t0 + s.t[j];
-        if (s.on[j] && t < p.n) {
-            r.bc[0][j] = Bm[p.b * q.b_batch + t * q.b_time + p.g * q.N + s.n[j]];
-            r.bc[1][j] = C[p.b * q.c_batch + t * q.c_time + p.g * q.N + s.n[j]];
-        }
+    for (int i = 0; i < STEPS; ++i) {
+        v[i].load((const E*)(at + offset));
+        if (i + 1 < there) at += r.step;
     }
 }
 
-// Puts B and C of a tile into LDS: per step and wave, NS of B and then NS of C.
-template <typename E, int NS, int W, int IN>
-__device__ __forceinline__ void store_bc(const Raw<E, NS, W, IN>& r, const Share<NS, W>& s, float* sh)
-{
-#pragma unroll
-    for (int j = 0; j < Raw<E, NS, W, IN>::kShare; ++j)
-        if (s.there[j]) {
-            float* at = sh + (s.t[j] * W + s.n[j] / NS) * 2 * NS + s.n[j] % NS;
-            at[0] = to_f32(r.bc[0][j]);
-            at[NS] = to_f32(r.bc[1][j]);
-        }
-}
-
+// A scan is bound by the vector unit and by the rate at which a wave issues
+// instructions (5.5 a state and step: a product and 2^x for the decay, three
+// and a half for state and readout; 60 a channel and step in phases A and C).
+// The phases of three tiles run in one stretch between two barriers (B of a
+// tile, C of the one before, A of the one after), so that the waits of one are
+// filled by the others.  Only whole tiles go through that loop: it has no
+// branches but for the stores.
 template <typename E, int NS, int W>
 __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q, const float* __restrict__ h_first,
                                                           E* __restrict__ y, float* __restrict__ h_last,
                                                           float* __restrict__ marks)
 {
-    constexpr int kSteps = kTile / W;
-    __shared__ float2 shD[kTile][kWave];
-    __shared__ float4 shBC[kTile * W * 2 * NS / 4];
-    __shared__ float shY[W][kTile][kWave];
+    constexpr int STEPS = kTile / W;
+    __shared__ float4 shD[2][kTile / 2][kWave];               // delta, delta x of two steps
+    __shared__ float4 shY[2][W][kTile / 4][kWave];            // the waves' parts of y of four
     const int lane = threadIdx.x & 63, w = wave_index();
     const Place p = place_of(q, in.length, lane);
-    const Share<NS, W> share(q.N);
-    const int n0 = w * NS, used = (q.N + NS - 1) / NS;
-    const E *x = (const E*)in.x, *dt = (const E*)in.dt, *z = (const E*)in.z;
+    const int n0 = w * NS, s0 = w * STEPS;
+    const bool gated = in.z != nullptr;
     float h[NS], rate[NS];
+    int at[NS];                                               // places past N repeat the last state, with B = C = 0
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
         const bool on = p.live && n0 + k < q.N;
         rate[k] = on ? rate_of(in.A[(int64_t)p.d * q.N + n0 + k]) : 0.0f;
         h[k] = on && h_first ? h_first[((int64_t)p.b * q.D + p.d) * q.N + n0 + k] : 0.0f;
+        at[k] = min(n0 + k, q.N - 1);
     }
     const float bias = in.bias ? in.bias[p.d] : 0.0f, skip = in.skip ? in.skip[p.d] : 0.0f;
+    const uint32_t offset = p.d * (uint32_t)sizeof(E), offset4 = p.d * 4u;
 
-    Raw<E, NS, W, 3> cur, nxt;
-    auto load = [&](Raw<E, NS, W, 3>& r, int t0) {
+    // From step t0 on: the rows of the wave's steps, and B and C of the lane's.
+    const int64_t bt = q.b_time, ct = q.c_time;
+    auto states_at = [&](const E* (&to)[2][NS], int t) {
+        const E* Bt = (const E*)in.Bm + p.b * q.b_batch + t * bt + (int64_t)p.g * q.N;
+        const E* Ct = (const E*)in.C + p.b * q.c_batch + t * ct + (int64_t)p.g * q.N;
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int t = t0 + w + W * i;
-            r.v[0][i] = r.v[1][i] = r.v[2][i] = from_f32<E>(0.0f);
-            if (t < p.n) {
-                r.v[0][i] = x[p.b * q.x_batch + t * q.x_time + p.d];
-                r.v[1][i] = dt[p.b * q.dt_batch + t * q.dt_time + p.d];
-                if (z && y) r.v[2][i] = z[p.b * q.z_batch + t * q.z_time + p.d];
-            }
-        }
-        load_bc(r, share, (const E*)in.Bm, (const E*)in.C, q, p, t0);
+        for (int k = 0; k < NS; ++k) to[0][k] = Bt + at[k], to[1][k] = Ct + at[k];
     };
-    if (p.n > 0) load(cur, 0);
-    for (int t0 = 0; t0 < p.n; t0 += kTile) {
-        const int cnt = min(kTile, p.n - t0);
+    auto rows_at = [&](Rows (&to)[3], int t) {
+        to[0] = rows_of<E>(in.x, q.x_batch, q.x_time, p.b, t);
+        to[1] = rows_of<E>(in.dt, q.dt_batch, q.dt_time, p.b, t);
+        to[2] = gated ? rows_of<E>(in.z, q.z_batch, q.z_time, p.b, t) : to[0];
+    };
+    auto load_states = [&](Raw<E, NS, STEPS, 3>& r, const E* const (&from)[2][NS]) {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
+        for (int k = 0; k < NS; ++k) r.bc[0][0][k].load(from[0][k]), r.bc[1][0][k].load(from[1][k]);
+    };
+    auto ready = [&](const Raw<E, NS, STEPS, 3>& r, float4 (*to)[kWave]) {
+#pragma unroll
+        for (int i = 0; i < STEPS; i += 2) {
+            float slope, dl[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) dl[j] = step_length(q, r.v[1][i + j].f32() + bias, slope);
+            to[(s0 + i) / 2][lane] = make_float4(dl[0], dl[0] * r.v[0][i].f32(), dl[1], dl[1] * r.v[0][i + 1].f32());
+        }
+    };
+    // A tile's delta and delta x, read ahead of what comes between.
+    auto fetch = [&](float4 (&to)[kTile / 2], const float4 (*from)[kWave]) {
+#pragma unroll
+        for (int i = 0; i < kTile / 2; ++i) to[i] = from[i][lane];
+    };
+    auto walk = [&](const Raw<E, NS, STEPS, 3>& r, const float4 (&at_step)[kTile / 2], float4 (*to)[kWave], auto whole,
+                    int cnt) {
+        float B[NS], Cv[NS], sum[kTile], hs[kTile][NS], a[kTile][NS];
+#pragma unroll
+        for (int k = 0; k < NS; ++k) {
+            B[k] = n0 + k < q.N ? r.bc[0][0][k].f32() : 0.0f;
+            Cv[k] = n0 + k < q.N ? r.bc[1][0][k].f32() : 0.0f;
+        }
+        auto decays = [&](int i) {
+            const float dl = i % 2 ? at_step[i / 2].z : at_step[i / 2].x;
+#pragma unroll
+            for (int k = 0; k < NS; ++k) a[i][k] = __builtin_amdgcn_exp2f(dl * rate[k]);
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) decays(i);
+        each_step([&](auto step) {
+            constexpr int i = decltype(step)::value;
+            if constexpr (i + 4 < kTile) decays(i + 4);
+            if (decltype(whole)::value || i < cnt) {
+                const float u = i % 2 ? at_step[i / 2].w : at_step[i / 2].y;
+#pragma unroll
+                for (int k = 0; k < NS; ++k) h[k] = fmaf(a[i][k], h[k], u * of_step<i>(B[k]));
+            }
+#pragma unroll
+            for (int k = 0; k < NS; ++k) hs[i][k] = h[k];
+            sum[i] = of_step<i>(Cv[0]) * h[0];
+            if constexpr (i % 4 == 3) {
+#pragma unroll
+                for (int k = 1; k < NS; ++k)
+                    add_steps<i - 3>(sum + i - 3, Cv[k], hs[i - 3][k], hs[i - 2][k], hs[i - 1][k], hs[i][k]);
+                to[i / 4][lane] = make_float4(sum[i - 3], sum[i - 2], sum[i - 1], sum[i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+    };
+    auto put_marks = [&](int t0) {
+        if (marks && p.live) {
+            char* to = (char*)(marks + (((int64_t)p.b * ((q.T + kTile - 1) / kTile) + t0 / kTile) * q.N + n0) * q.D);
+#pragma unroll
+            for (int k = 0; k < NS; ++k, to += q.D * (int64_t)4)
+                if (n0 + k < q.N) *(float*)(to + offset4) = h[k];
+        }
+    };
+    auto read_out = [&](const Raw<E, NS, STEPS, 3>& r, const float4 (*from)[kTile / 4][kWave], int t0, int cnt) {
+        if (!y) return;
+        float v[STEPS];
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) v[i] = skip * r.v[0][i].f32();
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) v[i] += ((const float*)&from[j][(s0 + i) / 4][lane])[(s0 + i) % 4];
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
             float slope;
-            const float d = step_length(q, to_f32(cur.v[1][i]) + bias, slope);
-            shD[w + W * i][lane] = p.live ? make_float2(d, d * to_f32(cur.v[0][i])) : make_float2(0.0f, 0.0f);
+            const float s = silu(r.v[2][i].f32(), slope);
+            v[i] = gated ? v[i] * s : v[i];
         }
-        store_bc(cur, share, (float*)shBC);
-        if (t0 + kTile < p.n) load(nxt, t0 + kTile);
-        __syncthreads();
-        if (n0 < q.N) {
-            if (marks && p.live)
+        char* to = (char*)(y + ((int64_t)p.b * q.T + t0 + s0) * q.D);
+        if (p.live)
 #pragma unroll
-                for (int k = 0; k < NS; ++k)
-                    if (n0 + k < q.N)
-                        marks[(((int64_t)p.b * ((q.T + kTile - 1) / kTile) + t0 / kTile) * q.N + n0 + k) * q.D + p.d] =
-                            h[k];
-            auto step = [&](int i) {
-                const float2 v = shD[i][lane];
-                const float* bc = (const float*)shBC + (i * W + w) * 2 * NS;
-                float sum = 0.0f;
+            for (int i = 0; i < STEPS; ++i, to += q.D * (int64_t)sizeof(E))
+                if (s0 + i < cnt) *(E*)(to + offset) = from_f32<E>(v[i]);
+    };
+
+    // Four tiles' raw elements in turn: copies from one to the next would wait
+    // for loads that are still on their way.
+    const int whole = p.n / kTile;
+    Raw<E, NS, STEPS, 3> r0, r1, r2, r3;
+    if (whole > 0) {
+        Rows rows[3];
+        const E* states[2][NS];
+        int j = -2;                                           // the tile that is loaded is j + 2
+        auto load = [&](Raw<E, NS, STEPS, 3>& r) {
 #pragma unroll
-                for (int k = 0; k < NS; ++k) {
-                    const float a = __builtin_amdgcn_exp2f(v.x * rate[k]);
-                    h[k] = fmaf(a, h[k], v.y * bc[k]);
-                    sum = fmaf(bc[NS + k], h[k], sum);
-                }
-                shY[w][i][lane] = sum;
-            };
-            if (cnt == kTile) {
+            for (int i = 0; i < 3; ++i) load_rows(r.v[i], rows[i], offset);
+            load_states(r, states);
+            if (j + 3 < whole) {                              // the last tile is loaded again where there are no more
 #pragma unroll
-                for (int i = 0; i < kTile; ++i) step(i);
-            } else {
-                for (int i = 0; i < cnt; ++i) step(i);
+                for (int i = 0; i < 3; ++i) rows[i].at += kTile * rows[i].step;
+#pragma unroll
+                for (int k = 0; k < NS; ++k) states[0][k] += kTile * bt, states[1][k] += kTile * ct;
             }
+        };
+        auto turn = [&](const auto& before, const auto& cur, const auto& next, auto& far) {
+            load(far);
+            put_marks(j * kTile);
+            float4 steps[kTile / 2];
+            fetch(steps, shD[j & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+            ready(next, shD[(j + 1) & 1]);
+            walk(cur, steps, shY[j & 1][w], std::true_type(), kTile);
+            if (j > 0) read_out(before, shY[(j - 1) & 1], (j - 1) * kTile, kTile);
+            __syncthreads();
+            if (++j < whole) return true;
+            read_out(cur, shY[(j - 1) & 1], (j - 1) * kTile, kTile);
+            return false;
+        };
+        rows_at(rows, s0);
+        states_at(states, lane & 15);
+        load(r0), ++j;
+        load(r1), ++j;
+        ready(r0, shD[0]);
+        __syncthreads();
+        while (turn(r3, r0, r1, r2) && turn(r0, r1, r2, r3) && turn(r1, r2, r3, r0) && turn(r2, r3, r0, r1)) {
         }
         __syncthreads();
-        if (y) {
+    }
+    const int left = p.n - whole * kTile;
+    if (left > 0) {
+        const int t0 = whole * kTile;
+        Rows rows[3];
+        const E* states[2][NS];
+        rows_at(rows, min(t0 + s0, p.n - 1));
+        states_at(states, min(t0 + (lane & 15), p.n - 1));
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const int t = t0 + w + W * i;
-                if (t < p.n) {
-                    float v = skip * to_f32(cur.v[0][i]);
-                    for (int j = 0; j < used; ++j) v += shY[j][w + W * i][lane];
-                    float slope;
-                    if (z) v *= silu(to_f32(cur.v[2][i]), slope);
-                    if (p.live) y[((int64_t)p.b * q.T + t) * q.D + p.d] = from_f32<E>(v);
-                }
-            }
-        }
-        cur = nxt;
+        for (int i = 0; i < 3; ++i) load_rows(r0.v[i], rows[i], offset, left - s0);
+        load_states(r0, states);
+        put_marks(t0);
+        ready(r0, shD[0]);
+        __syncthreads();
+        float4 steps[kTile / 2];
+        fetch(steps, shD[0]);
+        walk(r0, steps, shY[0][w], std::false_type(), left);
+        __syncthreads();
+        read_out(r0, shY[0], t0, left);
     }
     if (!p.live) return;
     if (y)
@@ -278,11 +403,6 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
 // runs backwards through the tiles; a tile's states are run forward again from
 // its mark and kept in registers.
 // ---------------------------------------------------------------------------
-
-template <int CTRL> __device__ __forceinline__ float dpp(float v)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
-}
 
 // Sums over the lanes of several values at once: each merge takes two values
 // and leaves the sum of the first over pairs of lanes in one half of them and
@@ -305,11 +425,12 @@ template <int CTRL> __device__ __forceinline__ float merge_in_row(float a, float
     return (second ? b : a) + dpp<CTRL>(second ? a : b);
 }
 
-// Four values of a step: rows 0 .. 3 of the wave get the sums of v[0], v[2],
-// v[1], v[3] over the four rows.
-__device__ __forceinline__ float merge_states(const float (&v)[4])
+// Two values each of two states (or of one) of a step: rows 0 .. 3 of the wave
+// get the sums over the four rows of the first state's b and c, and of the
+// second's.
+__device__ __forceinline__ float merge_states(float b0, float b1, float c0, float c1)
 {
-    return merge_rows(merge_halves(v[0], v[1]), merge_halves(v[2], v[3]));
+    return merge_rows(merge_halves(b0, b1), merge_halves(c0, c1));
 }
 
 // 16 steps: lane l gets its row's sum of step l % 16.
@@ -333,159 +454,188 @@ template <typename E> struct BackOut {
     float *g_first;
 };
 
-template <typename E, int W, int NB>
+template <typename E, int NS, int W, int NB>
 __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q, const float* __restrict__ marks,
                                                           const float* __restrict__ grad_last, BackOut<E> out)
 {
-    constexpr int kSteps = kTile / W, NS = 4;
-    __shared__ float shD[3][kTile][kWave];                    // delta, delta x, g
-    __shared__ float4 shBC[NB][kTile * W * 2 * NS / 4];
-    __shared__ float shP[W][kTile][kWave], shQ[W][kTile][kWave], shY[W][kTile][kWave];
+    constexpr int STEPS = kTile / W;
+    __shared__ float4 shD[kTile / 2][kWave];                  // delta, delta x of two steps
+    __shared__ float shG[kTile / 4][kWave][4];                // g of four
+    __shared__ float shP[3][W][kTile / 4][kWave][4];          // the waves' parts of P, Q and y
     const int lane = threadIdx.x & 63, w = wave_index();
     const Place p = place_of(q, in.length, lane);
-    const Share<NS * NB, W> share(q.N);
-    const int used = min(W, (q.N + NS - 1) / NS);
-    const E *x = (const E*)in.x, *dt = (const E*)in.dt, *z = (const E*)in.z, *gy = (const E*)in.gy;
-    float mu[NB][NS], A[NB][NS], rate[NB][NS], gA[NB][NS];
-    auto state = [&](int nb, int k) { return (nb * W + w) * NS + k; };
+    const int used = min(W, (q.N + NS - 1) / NS), s0 = w * STEPS;
+    const E* Bm = (const E*)in.Bm + p.b * q.b_batch + (int64_t)p.g * q.N;
+    const E* C = (const E*)in.C + p.b * q.c_batch + (int64_t)p.g * q.N;
+    float mu[NB][NS], A[NB][NS], gA[NB][NS];
+    auto first = [&](int nb) { return (nb * W + w) * NS; };
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int k = 0; k < NS; ++k) {
-            const int n = state(nb, k);
+            const int n = first(nb) + k;
             const bool on = p.live && n < q.N;
             A[nb][k] = on ? in.A[(int64_t)p.d * q.N + n] : 0.0f;
-            rate[nb][k] = rate_of(A[nb][k]);
             mu[nb][k] = on && grad_last ? grad_last[((int64_t)p.b * q.D + p.d) * q.N + n] : 0.0f;
             gA[nb][k] = 0.0f;
         }
     const float bias = in.bias ? in.bias[p.d] : 0.0f, skip = in.skip ? in.skip[p.d] : 0.0f;
     float g_skip = 0.0f, g_bias = 0.0f;
+    const uint32_t d = p.d, offset = d * (uint32_t)sizeof(E);
+    const int64_t mark_row = (int64_t)p.b * ((q.T + kTile - 1) / kTile) * q.N;
 
-    Raw<E, NS * NB, W, 4> cur, nxt;
-    auto load = [&](Raw<E, NS * NB, W, 4>& r, int t0) {
+    Raw<E, NS, STEPS, 4, NB> cur, nxt;
+    auto load = [&](Raw<E, NS, STEPS, 4, NB>& r, int t0, auto all) {
+        constexpr bool kAll = decltype(all)::value;
+        const int64_t tb = kAll ? t0 + (lane & 15) : min(t0 + (lane & 15), p.n - 1);
+        const int t = kAll ? t0 + s0 : min(t0 + s0, p.n - 1), there = kAll ? STEPS : p.n - t0 - s0;
+        const Rows x = rows_of<E>(in.x, q.x_batch, q.x_time, p.b, t);
+        load_rows(r.v[0], x, offset, there);
+        load_rows(r.v[1], rows_of<E>(in.dt, q.dt_batch, q.dt_time, p.b, t), offset, there);
+        load_rows(r.v[2], in.z ? rows_of<E>(in.z, q.z_batch, q.z_time, p.b, t) : x, offset, there);
+        load_rows(r.v[3], in.gy ? rows_of<E>(in.gy, q.g_batch, q.g_time, p.b, t) : x, offset, there);
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int t = t0 + w + W * i;
-            r.v[0][i] = r.v[1][i] = r.v[2][i] = r.v[3][i] = from_f32<E>(0.0f);
-            if (t < p.n) {
-                r.v[0][i] = x[p.b * q.x_batch + t * q.x_time + p.d];
-                r.v[1][i] = dt[p.b * q.dt_batch + t * q.dt_time + p.d];
-                if (z) r.v[2][i] = z[p.b * q.z_batch + t * q.z_time + p.d];
-                if (gy) r.v[3][i] = gy[p.b * q.g_batch + t * q.g_time + p.d];
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int k = 0; k < NS; ++k) {
+                const int at = min(first(nb) + k, q.N - 1);
+                r.bc[0][nb][k].load(Bm + tb * q.b_time + at);
+                r.bc[1][nb][k].load(C + tb * q.c_time + at);
             }
-        }
-        load_bc(r, share, (const E*)in.Bm, (const E*)in.C, q, p, t0);
     };
     const int64_t column = blockIdx.x;
     const int last = (p.n - 1) / kTile * kTile;
-    if (p.n > 0) load(cur, last);
+    if (p.n > 0) load(cur, last, std::false_type());
     for (int t0 = last; t0 >= 0 && p.n > 0; t0 -= kTile) {
         const int cnt = min(kTile, p.n - t0);
-        float delta[kSteps], g[kSteps];
+        float delta[STEPS], d_slope[STEPS], g[STEPS], z_slope[STEPS];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            float slope;
-            delta[i] = step_length(q, to_f32(cur.v[1][i]) + bias, slope);
-            g[i] = to_f32(cur.v[3][i]);
-            if (z) g[i] *= silu(to_f32(cur.v[2][i]), slope);
-            const bool on = p.live && w + W * i < cnt;
-            shD[0][w + W * i][lane] = on ? delta[i] : 0.0f;
-            shD[1][w + W * i][lane] = on ? delta[i] * to_f32(cur.v[0][i]) : 0.0f;
-            shD[2][w + W * i][lane] = on ? g[i] : 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < Share<NS * NB, W>::kShare; ++j)
-            if (share.there[j]) {
-                const int n = share.n[j], slice = n / NS;            // slice nb * W + w
-                float* at = (float*)shBC[slice / W] + (share.t[j] * W + slice % W) * 2 * NS + n % NS;
-                at[0] = to_f32(cur.bc[0][j]);
-                at[NS] = to_f32(cur.bc[1][j]);
+        for (int i = 0; i < STEPS; ++i) {
+            delta[i] = step_length(q, cur.v[1][i].f32() + bias, d_slope[i]);
+            g[i] = in.gy ? cur.v[3][i].f32() : 0.0f;
+            z_slope[i] = 0.0f;
+            if (in.z) {
+                const float gate = silu(cur.v[2][i].f32(), z_slope[i]);
+                z_slope[i] *= g[i];
+                g[i] *= gate;
             }
-        if (t0 > 0) load(nxt, t0 - kTile);
+            const bool on = p.live && s0 + i < cnt;
+            float* to = (float*)&shD[(s0 + i) / 2][lane] + (s0 + i) % 2 * 2;
+            to[0] = on ? delta[i] : 0.0f;
+            to[1] = on ? delta[i] * cur.v[0][i].f32() : 0.0f;
+            shG[(s0 + i) / 4][lane][(s0 + i) % 4] = on ? g[i] : 0.0f;
+        }
+        float B[NB][NS], Cv[NB][NS], h0[NB][NS];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int k = 0; k < NS; ++k) {
+                const bool on = first(nb) + k < q.N;
+                B[nb][k] = on ? cur.bc[0][nb][k].f32() : 0.0f, Cv[nb][k] = on ? cur.bc[1][nb][k].f32() : 0.0f;
+                h0[nb][k] = p.live && first(nb) + k < q.N
+                                ? (marks + (mark_row + t0 / kTile * (int64_t)q.N + first(nb) + k) * q.D)[d]
+                                : 0.0f;
+            }
+        if (t0 > 0) load(nxt, t0 - kTile, std::true_type());
         __syncthreads();
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            if (state(nb, 0) >= q.N) continue;
-            float h0[NS];
-#pragma unroll
-            for (int k = 0; k < NS; ++k)
-                h0[k] = p.live && state(nb, k) < q.N
-                            ? marks[(((int64_t)p.b * ((q.T + kTile - 1) / kTile) + t0 / kTile) * q.N + state(nb, k)) *
-                                        q.D + p.d]
-                            : 0.0f;
+            if (first(nb) >= q.N) continue;
             auto walk = [&](auto whole) {
                 constexpr bool kWhole = decltype(whole)::value;
-                float h[kTile][NS], a[kTile][NS], vb[kTile], vc[kTile];
-#pragma unroll
-                for (int i = 0; i < kTile; ++i) {
-                    if (!kWhole && i >= cnt) continue;
-                    const float* bc = (const float*)shBC[nb] + (i * W + w) * 2 * NS;
-                    const float d = shD[0][i][lane], u = shD[1][i][lane];
-                    float sum = 0.0f;
+                float h[kTile][NS], a[kTile][NS], sum[kTile], P[kTile], Q[kTile], part[NS / 2][kTile], lams[kTile][NS];
+                each_step([&](auto step) {
+                    constexpr int i = decltype(step)::value;
+                    const float4 v = shD[i / 2][lane];
+                    const float dl = i % 2 ? v.z : v.x, u = i % 2 ? v.w : v.y;
 #pragma unroll
                     for (int k = 0; k < NS; ++k) {
-                        a[i][k] = __builtin_amdgcn_exp2f(d * rate[nb][k]);
-                        h[i][k] = fmaf(a[i][k], i ? h[i - 1][k] : h0[k], u * bc[k]);
-                        sum = fmaf(bc[NS + k], h[i][k], sum);
+                        const float prev = i ? h[i ? i - 1 : 0][k] : h0[nb][k];
+                        const bool on = kWhole || i < cnt;
+                        a[i][k] = on ? __builtin_amdgcn_exp2f(dl * rate_of(A[nb][k])) : 1.0f;
+                        h[i][k] = on ? fmaf(a[i][k], prev, u * of_step<i>(B[nb][k])) : prev;
                     }
-                    shY[w][i][lane] = nb ? shY[w][i][lane] + sum : sum;
-                }
+                    sum[i] = of_step<i>(Cv[nb][0]) * h[i][0];
+                    if constexpr (i % 4 == 3)
 #pragma unroll
-                for (int i = kTile - 1; i >= 0; --i) {
-                    vb[i] = vc[i] = 0.0f;
-                    if (!kWhole && i >= cnt) continue;
-                    const float* bc = (const float*)shBC[nb] + (i * W + w) * 2 * NS;
-                    const float d = shD[0][i][lane], u = shD[1][i][lane], gg = shD[2][i][lane];
-                    float P = 0.0f, Q = 0.0f, pb[NS], pc[NS];
+                        for (int k = 1; k < NS; ++k)
+                            add_steps<i - 3>(sum + i - 3, Cv[nb][k], h[i - 3][k], h[i - 2][k], h[i - 1][k], h[i][k]);
+                });
+                each_step_back([&](auto step) {
+                    constexpr int i = decltype(step)::value;
+                    const float4 v = shD[i / 2][lane];
+                    const float dl = i % 2 ? v.z : v.x, u = i % 2 ? v.w : v.y, gg = shG[i / 4][lane][i % 4];
+                    const bool on = kWhole || i < cnt;
+                    float pb[NS], pc[NS];
+                    P[i] = 0.0f;
 #pragma unroll
                     for (int k = 0; k < NS; ++k) {
-                        const float lam = fmaf(gg, bc[NS + k], mu[nb][k]);
-                        pc[k] = gg * h[i][k];
+                        const float lam = on ? fmaf(gg, of_step<i>(Cv[nb][k]), mu[nb][k]) : 0.0f;
+                        lams[i][k] = lam;
+                        pc[k] = on ? gg * h[i][k] : 0.0f;
                         pb[k] = lam * u;
-                        Q = fmaf(lam, bc[k], Q);
-                        mu[nb][k] = a[i][k] * lam;
-                        const float f = mu[nb][k] * (i ? h[i - 1][k] : h0[k]);
-                        P = fmaf(A[nb][k], f, P);
-                        gA[nb][k] = fmaf(d, f, gA[nb][k]);
+                        if (on) {
+                            mu[nb][k] = a[i][k] * lam;
+                            const float f = mu[nb][k] * (i ? h[i ? i - 1 : 0][k] : h0[nb][k]);
+                            P[i] = fmaf(A[nb][k], f, P[i]);
+                            gA[nb][k] = fmaf(dl, f, gA[nb][k]);
+                        }
                     }
-                    shP[w][i][lane] = nb ? shP[w][i][lane] + P : P;
-                    shQ[w][i][lane] = nb ? shQ[w][i][lane] + Q : Q;
-                    vb[i] = merge_states(pb);
-                    vc[i] = merge_states(pc);
+                    Q[i] = of_step<i>(B[nb][0]) * lams[i][0];
+                    if constexpr (i % 4 == 0)
+#pragma unroll
+                        for (int k = 1; k < NS; ++k)
+                            add_steps<i>(Q + i, B[nb][k], lams[i][k], lams[i + 1][k], lams[i + 2][k], lams[i + 3][k]);
+#pragma unroll
+                    for (int k = 0; k < NS; k += 2) part[k / 2][i] = merge_states(pb[k], pb[k + 1], pc[k], pc[k + 1]);
+                });
+                // rows 0 .. 3 hold b and c of the first state, b and c of the second
+                const int row = lane >> 4, i = lane & 15;
+#pragma unroll
+                for (int k = 0; k < NS; k += 2) {
+                    const float s = merge_steps(part[k / 2], lane);
+                    const int n = first(nb) + k + (row >> 1);
+                    if (i < cnt && n < q.N)
+                        (row & 1 ? out.partC : out.partB)[(column * q.T + t0 + i) * q.N + n] = s;
                 }
-                const float sb = merge_steps(vb, lane), sc = merge_steps(vc, lane);
-                const int row = lane >> 4, n = state(nb, (row & 1) * 2 + (row >> 1)), i = lane & 15;
-                if (i < cnt && n < q.N) {
-                    const int64_t at = (column * q.T + t0 + i) * q.N + n;
-                    out.partB[at] = sb;
-                    out.partC[at] = sc;
+#pragma unroll
+                for (int j = 0; j < 3; ++j) {
+                    float(&v)[kTile] = j == 0 ? P : j == 1 ? Q : sum;
+#pragma unroll
+                    for (int s = 0; s < kTile; s += 4) {
+                        float4* to = (float4*)shP[j][w][s / 4][lane];
+                        float4 o = nb ? *to : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        o.x += v[s], o.y += v[s + 1], o.z += v[s + 2], o.w += v[s + 3];
+                        *to = o;
+                    }
                 }
             };
             if (cnt == kTile) walk(std::true_type());
             else walk(std::false_type());
         }
         __syncthreads();
+        float P[STEPS], Q[STEPS], Y[STEPS];
+        int64_t row = ((int64_t)p.b * q.T + t0 + s0) * q.D;
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int s = w + W * i, t = t0 + s;
-            if (t < p.n) {
-                float P = 0.0f, Q = 0.0f, Y = 0.0f;
-                for (int j = 0; j < used; ++j) P += shP[j][s][lane], Q += shQ[j][s][lane], Y += shY[j][s][lane];
-                const float xv = to_f32(cur.v[0][i]);
-                float slope;
-                step_length(q, to_f32(cur.v[1][i]) + bias, slope);
-                const float g_r = fmaf(xv, Q, P) * slope;
+        for (int i = 0; i < STEPS; ++i) P[i] = Q[i] = Y[i] = 0.0f;
+        for (int j = 0; j < used; ++j)
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                P[i] += shP[0][j][(s0 + i) / 4][lane][(s0 + i) % 4];
+                Q[i] += shP[1][j][(s0 + i) / 4][lane][(s0 + i) % 4];
+                Y[i] += shP[2][j][(s0 + i) / 4][lane][(s0 + i) % 4];
+            }
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i, row += q.D) {
+            if (s0 + i < cnt) {
+                const float xv = cur.v[0][i].f32();
+                const float g_r = fmaf(xv, Q[i], P[i]) * d_slope[i];
                 g_skip = fmaf(g[i], xv, g_skip);
                 g_bias += g_r;
                 if (p.live) {
-                    const int64_t at = ((int64_t)p.b * q.T + t) * q.D + p.d;
-                    out.gx[at] = from_f32<E>(fmaf(delta[i], Q, skip * g[i]));
-                    out.gdt[at] = from_f32<E>(g_r);
-                    if (z) {
-                        silu(to_f32(cur.v[2][i]), slope);
-                        out.gz[at] = from_f32<E>(to_f32(cur.v[3][i]) * fmaf(skip, xv, Y) * slope);
-                    }
+                    (out.gx + row)[d] = from_f32<E>(fmaf(delta[i], Q[i], skip * g[i]));
+                    (out.gdt + row)[d] = from_f32<E>(g_r);
+                    if (in.z) (out.gz + row)[d] = from_f32<E>(fmaf(skip, xv, Y[i]) * z_slope[i]);
                 }
             }
         }
@@ -495,26 +645,26 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         for (int t = p.n + w; t < q.T; t += W) {
             const int64_t at = ((int64_t)p.b * q.T + t) * q.D + p.d;
             out.gx[at] = out.gdt[at] = from_f32<E>(0.0f);
-            if (z) out.gz[at] = from_f32<E>(0.0f);
+            if (in.z) out.gz[at] = from_f32<E>(0.0f);
         }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int k = 0; k < NS; ++k)
-                if (state(nb, k) < q.N) {
-                    const int64_t at = ((int64_t)p.b * q.D + p.d) * q.N + state(nb, k);
+                if (first(nb) + k < q.N) {
+                    const int64_t at = ((int64_t)p.b * q.D + p.d) * q.N + first(nb) + k;
                     out.partA[at] = gA[nb][k];
                     if (out.g_first) out.g_first[at] = mu[nb][k];
                 }
     }
     __syncthreads();
-    shP[w][0][lane] = g_skip;
-    shP[w][1][lane] = g_bias;
+    shP[0][w][0][lane][0] = g_skip;
+    shP[0][w][0][lane][1] = g_bias;
     __syncthreads();
     if (w == 0 && p.live) {
-        float s0 = 0.0f, s1 = 0.0f;
-        for (int j = 0; j < W; ++j) s0 += shP[j][0][lane], s1 += shP[j][1][lane];
-        out.partS[(int64_t)p.b * 2 * q.D + p.d] = s0;
+        float s0_ = 0.0f, s1 = 0.0f;
+        for (int j = 0; j < W; ++j) s0_ += shP[0][j][0][lane][0], s1 += shP[0][j][0][lane][1];
+        out.partS[(int64_t)p.b * 2 * q.D + p.d] = s0_;
         out.partS[((int64_t)p.b * 2 + 1) * q.D + p.d] = s1;
     }
 }
@@ -661,9 +811,10 @@ template <int V> struct Int { static constexpr int value = V; };
 // waves that hold N states.
 template <typename Fn> void with_waves(int N, Fn&& fn)
 {
-    if (N <= 4) fn(Int<4>(), Int<1>());
-    else if (N <= 8) fn(Int<4>(), Int<2>());
-    else if (N <= 16) fn(Int<4>(), Int<4>());
+    if (N <= 2) fn(Int<2>(), Int<1>());
+    else if (N <= 4) fn(Int<2>(), Int<2>());
+    else if (N <= 8) fn(Int<2>(), Int<4>());
+    else if (N <= 16) fn(Int<2>(), Int<8>());
     else if (N <= 32) fn(Int<4>(), Int<8>());
     else fn(Int<8>(), Int<8>());
 }
@@ -758,17 +909,18 @@ extern "C" int lif_selective_scan_backward(const void* x, const void* dt, const 
         const BackOut<E> out = {(E*)grad_x, (E*)grad_dt, (E*)grad_z, (float*)(base + l.partB),
                                 (float*)(base + l.partC), (float*)(base + l.partA), (float*)(base + l.partS),
                                 grad_h_first};
-        auto launch = [&](auto waves, auto nb) {
-            constexpr int W = decltype(waves)::value, NB = decltype(nb)::value;
-            TIMED_LAUNCH("select_back", (k_select_back<E, W, NB>), dim3((unsigned)(q.B * q.G * q.cols)),
+        auto launch = [&](auto ns, auto waves, auto nb) {
+            constexpr int NS = decltype(ns)::value, W = decltype(waves)::value, NB = decltype(nb)::value;
+            TIMED_LAUNCH("select_back", (k_select_back<E, NS, W, NB>), dim3((unsigned)(q.B * q.G * q.cols)),
                          dim3(W * kWave), 0, (hipStream_t)stream, in, q, marks, grad_last, out);
         };
         if (q.B > 0) {
-            if (q.N <= 4) launch(Int<1>(), Int<1>());
-            else if (q.N <= 8) launch(Int<2>(), Int<1>());
-            else if (q.N <= 16) launch(Int<4>(), Int<1>());
-            else if (q.N <= 32) launch(Int<8>(), Int<1>());
-            else launch(Int<8>(), Int<2>());
+            if (q.N <= 2) launch(Int<2>(), Int<1>(), Int<1>());
+            else if (q.N <= 4) launch(Int<2>(), Int<2>(), Int<1>());
+            else if (q.N <= 8) launch(Int<2>(), Int<4>(), Int<1>());
+            else if (q.N <= 16) launch(Int<2>(), Int<8>(), Int<1>());
+            else if (q.N <= 32) launch(Int<2>(), Int<8>(), Int<2>());
+            else launch(Int<2>(), Int<8>(), Int<4>());
         }
         TIMED_LAUNCH("select_sums", (k_select_sums<E>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, q,
                      length, out.partB, out.partC, out.partA, out.partS, (E*)grad_B, (E*)grad_C, grad_A, grad_skip,
