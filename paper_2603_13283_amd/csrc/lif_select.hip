@@ -25,12 +25,14 @@ namespace {
 
 constexpr int kTile = LIF_SELECT_MARK;
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kMaxSegments = 256, kSplitColumns = 128, kSplitGroups = 1024, kSplitTiles = 4, kSplitLeast = 4;
 static_assert(kTile == 16, "the sums over lanes below put 16 steps x 4 states into the lanes of a wave");
 
 // What a call works on.  Columns of 64 channels: column c is sample
 // c / (G cols), group c / cols % G, channels 64 (c % cols) .. of that group.
+// S segments of seg_len steps (whole tiles) of the time axis.
 struct Geometry {
-    int B, T, D, N, G, Dg, cols;
+    int B, T, D, N, G, Dg, cols, columns, S, seg_len;
     uint32_t flags;
     int64_t x_batch, x_time, dt_batch, dt_time, z_batch, z_time, b_batch, b_time, c_batch, c_time, g_batch, g_time;
 };
@@ -43,25 +45,29 @@ struct Inputs {
 
 __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
-// A workgroup's column, and a lane's channel in it.  Lanes past the group's
-// last channel repeat it, with inputs of 0, and store nothing.
+// A workgroup's column and segment, and a lane's channel in it.  Lanes past the
+// group's last channel repeat it and store nothing.  The segment is steps t0 ..
+// t1 - 1, of which the first n lie before the sample's length.
 struct Place {
-    int b, g, col, d, n;
+    int b, g, d, column, seg, t0, t1, n, length;
     bool live;
 };
 
 __device__ __forceinline__ Place place_of(const Geometry& q, const int32_t* __restrict__ length, int lane)
 {
     Place p;
-    const int c = blockIdx.x;
-    p.col = c % q.cols;
-    p.g = c / q.cols % q.G;
-    p.b = c / q.cols / q.G;
-    const int at = p.col * kWave + lane;
+    p.seg = blockIdx.x / q.columns;
+    p.column = blockIdx.x - p.seg * q.columns;
+    p.g = p.column / q.cols % q.G;
+    p.b = p.column / q.cols / q.G;
+    const int at = p.column % q.cols * kWave + lane;
     p.live = at < q.Dg;
     p.d = p.g * q.Dg + (p.live ? at : q.Dg - 1);
-    p.n = length ? min(max(length[p.b], 0), q.T) : q.T;
-    p.n = __builtin_amdgcn_readfirstlane(p.n);
+    p.length = length ? min(max(length[p.b], 0), q.T) : q.T;
+    p.length = __builtin_amdgcn_readfirstlane(p.length);
+    p.t0 = p.seg * q.seg_len;
+    p.t1 = min(p.t0 + q.seg_len, q.T);
+    p.n = max(min(p.length, p.t1) - p.t0, 0);
     return p;
 }
 
@@ -200,6 +206,139 @@ __device__ __forceinline__ void load_rows(Bits<E> (&v)[STEPS], const Rows& r, ui
     }
 }
 
+// Where there are few columns, the time axis is cut into segments that
+// workgroups share out.  A segment's map of the state that enters it is
+//   h -> e^{A sum delta} h + H,
+// one sum of delta per channel and one H per state: a first launch makes them,
+// and every segment then starts from the maps before it.  The adjoint's maps
+// (REVERSE: mu -> e^{A sum delta} mu + M) go the other way.
+//   sums [S][B][D], ends [S][B][N][D]
+template <typename E, int NS, int W, bool REVERSE>
+__global__ __launch_bounds__(W* kWave) void k_select_maps(Inputs in, Geometry q, float* __restrict__ sums,
+                                                          float* __restrict__ ends)
+{
+    constexpr int STEPS = kTile / W, IN = REVERSE ? 3 : 2;
+    __shared__ float4 shD[2][kTile / 2][kWave];               // delta and delta x (delta and g) of two steps
+    const int lane = threadIdx.x & 63, w = wave_index();
+    Place p = place_of(q, in.length, lane);
+    if (REVERSE) {                                            // the first segment needs no map
+        p.t0 += q.seg_len, p.t1 = min(p.t1 + q.seg_len, q.T), ++p.seg;
+        p.n = max(min(p.length, p.t1) - p.t0, 0);
+    }
+    const int n0 = w * NS, s0 = w * STEPS;
+    float h[NS], rate[NS], total = 0.0f;
+    int at[NS];
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+        rate[k] = n0 + k < q.N ? rate_of(in.A[(int64_t)p.d * q.N + n0 + k]) : 0.0f;
+        h[k] = 0.0f;
+        at[k] = min(n0 + k, q.N - 1);
+    }
+    const float bias = in.bias ? in.bias[p.d] : 0.0f;
+    const uint32_t offset = p.d * (uint32_t)sizeof(E);
+    const bool gated = in.z != nullptr, driven = in.gy != nullptr;
+
+    Raw<E, NS, STEPS, IN> r0, r1, r2;
+    auto load = [&](Raw<E, NS, STEPS, IN>& r, int from) {
+        const int left = p.n - from, t = p.t0 + from + min(s0, left - 1);
+        const Rows dt = rows_of<E>(in.dt, q.dt_batch, q.dt_time, p.b, t);
+        load_rows(r.v[0], dt, offset, left - s0);
+        if constexpr (REVERSE) {
+            load_rows(r.v[1], driven ? rows_of<E>(in.gy, q.g_batch, q.g_time, p.b, t) : dt, offset, left - s0);
+            load_rows(r.v[2], gated ? rows_of<E>(in.z, q.z_batch, q.z_time, p.b, t) : dt, offset, left - s0);
+        } else {
+            load_rows(r.v[1], rows_of<E>(in.x, q.x_batch, q.x_time, p.b, t), offset, left - s0);
+        }
+        const int64_t tb = p.t0 + from + min(lane & 15, left - 1);
+        const E* bc = REVERSE ? (const E*)in.C + p.b * q.c_batch + tb * q.c_time
+                              : (const E*)in.Bm + p.b * q.b_batch + tb * q.b_time;
+#pragma unroll
+        for (int k = 0; k < NS; ++k) r.bc[0][0][k].load(bc + (int64_t)p.g * q.N + at[k]);
+    };
+    // steps past the end have delta = 0: the identity
+    auto ready = [&](const Raw<E, NS, STEPS, IN>& r, float4 (*to)[kWave], int left) {
+#pragma unroll
+        for (int i = 0; i < STEPS; i += 2) {
+            float slope, dl[2], u[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bool on = s0 + i + j < left;
+                dl[j] = step_length(q, r.v[0][i + j].f32() + bias, slope);
+                u[j] = r.v[1][i + j].f32();
+                if constexpr (REVERSE) {
+                    const float s = silu(r.v[2][i + j].f32(), slope);
+                    u[j] = !driven ? 0.0f : gated ? u[j] * s : u[j];
+                } else {
+                    u[j] *= dl[j];
+                }
+                dl[j] = on ? dl[j] : 0.0f, u[j] = on ? u[j] : 0.0f;
+            }
+            to[(s0 + i) / 2][lane] = make_float4(dl[0], u[0], dl[1], u[1]);
+        }
+    };
+    auto walk = [&](const Raw<E, NS, STEPS, IN>& r, const float4 (*from)[kWave]) {
+        float B[NS];
+        float4 v[kTile / 2];
+#pragma unroll
+        for (int i = 0; i < kTile / 2; ++i) v[i] = from[i][lane];
+#pragma unroll
+        for (int k = 0; k < NS; ++k) B[k] = n0 + k < q.N ? r.bc[0][0][k].f32() : 0.0f;
+        auto step = [&](auto at_step) {
+            constexpr int i = decltype(at_step)::value;
+            const float dl = i % 2 ? v[i / 2].z : v[i / 2].x, u = i % 2 ? v[i / 2].w : v[i / 2].y;
+            total += dl;
+#pragma unroll
+            for (int k = 0; k < NS; ++k) {
+                const float a = __builtin_amdgcn_exp2f(dl * rate[k]), b = u * of_step<i>(B[k]);
+                h[k] = REVERSE ? a * (h[k] + b) : fmaf(a, h[k], b);
+            }
+        };
+        if constexpr (REVERSE) each_step_back(step);
+        else each_step(step);
+    };
+    const int tiles = (p.n + kTile - 1) / kTile;
+    if (tiles > 0) {
+        int j = 0;
+        auto from = [&](int i) { return (REVERSE ? tiles - 1 - i : i) * kTile; };
+        auto turn = [&](const auto& cur, const auto& next, auto& far) {
+            if (j + 2 < tiles) load(far, from(j + 2));
+            if (j + 1 < tiles) ready(next, shD[(j + 1) & 1], p.n - from(j + 1));
+            walk(cur, shD[j & 1]);
+            __syncthreads();
+            return ++j < tiles;
+        };
+        load(r0, from(0));
+        if (tiles > 1) load(r1, from(1));
+        ready(r0, shD[0], p.n - from(0));
+        __syncthreads();
+        while (turn(r0, r1, r2) && turn(r1, r2, r0) && turn(r2, r0, r1)) {
+        }
+    }
+    if (!p.live) return;
+    const int64_t row = (int64_t)p.seg * q.B + p.b;
+    if (w == 0) sums[row * q.D + p.d] = total;
+#pragma unroll
+    for (int k = 0; k < NS; ++k)
+        if (n0 + k < q.N) ends[(row * q.N + n0 + k) * q.D + p.d] = h[k];
+}
+
+// c carried through the maps of segments from, from + by, ... (count of them).
+template <int NS>
+__device__ __forceinline__ void carry(float (&c)[NS], const float (&rate)[NS], const float* __restrict__ sums,
+                                      const float* __restrict__ ends, const Geometry& q, const Place& p, int n0,
+                                      int from, int count, int by)
+{
+#pragma unroll 4
+    for (int i = 0; i < count; ++i) {
+        const int64_t row = (int64_t)(from + i * by) * q.B + p.b;
+        const float sum = sums[row * q.D + p.d];
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+            c[k] = fmaf(__builtin_amdgcn_exp2f(sum * rate[k]), c[k],
+                        ends[(row * q.N + min(n0 + k, q.N - 1)) * q.D + p.d]);
+    }
+}
+
 // A scan is bound by the vector unit and by the rate at which a wave issues
 // instructions (5.5 a state and step: a product and 2^x for the decay, three
 // and a half for state and readout; 60 a channel and step in phases A and C).
@@ -209,6 +348,8 @@ __device__ __forceinline__ void load_rows(Bits<E> (&v)[STEPS], const Rows& r, ui
 // branches but for the stores.
 template <typename E, int NS, int W>
 __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q, const float* __restrict__ h_first,
+                                                          const float* __restrict__ sums,
+                                                          const float* __restrict__ ends,
                                                           E* __restrict__ y, float* __restrict__ h_last,
                                                           float* __restrict__ marks)
 {
@@ -228,6 +369,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
         h[k] = on && h_first ? h_first[((int64_t)p.b * q.D + p.d) * q.N + n0 + k] : 0.0f;
         at[k] = min(n0 + k, q.N - 1);
     }
+    if (p.n > 0) carry(h, rate, sums, ends, q, p, n0, 0, p.seg, 1);
     const float bias = in.bias ? in.bias[p.d] : 0.0f, skip = in.skip ? in.skip[p.d] : 0.0f;
     const uint32_t offset = p.d * (uint32_t)sizeof(E), offset4 = p.d * 4u;
 
@@ -299,7 +441,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
     };
     auto put_marks = [&](int t0) {
         if (marks && p.live) {
-            char* to = (char*)(marks + (((int64_t)p.b * ((q.T + kTile - 1) / kTile) + t0 / kTile) * q.N + n0) * q.D);
+            char* to = (char*)(marks + (((int64_t)p.b * ((q.T + kTile - 1) / kTile) + (p.t0 + t0) / kTile) * q.N + n0) * q.D);
 #pragma unroll
             for (int k = 0; k < NS; ++k, to += q.D * (int64_t)4)
                 if (n0 + k < q.N) *(float*)(to + offset4) = h[k];
@@ -320,7 +462,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
             const float s = silu(r.v[2][i].f32(), slope);
             v[i] = gated ? v[i] * s : v[i];
         }
-        char* to = (char*)(y + ((int64_t)p.b * q.T + t0 + s0) * q.D);
+        char* to = (char*)(y + ((int64_t)p.b * q.T + p.t0 + t0 + s0) * q.D);
         if (p.live)
 #pragma unroll
             for (int i = 0; i < STEPS; ++i, to += q.D * (int64_t)sizeof(E))
@@ -360,8 +502,8 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
             read_out(cur, shY[(j - 1) & 1], (j - 1) * kTile, kTile);
             return false;
         };
-        rows_at(rows, s0);
-        states_at(states, lane & 15);
+        rows_at(rows, p.t0 + s0);
+        states_at(states, p.t0 + (lane & 15));
         load(r0), ++j;
         load(r1), ++j;
         ready(r0, shD[0]);
@@ -375,8 +517,8 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
         const int t0 = whole * kTile;
         Rows rows[3];
         const E* states[2][NS];
-        rows_at(rows, min(t0 + s0, p.n - 1));
-        states_at(states, min(t0 + (lane & 15), p.n - 1));
+        rows_at(rows, p.t0 + min(t0 + s0, p.n - 1));
+        states_at(states, p.t0 + min(t0 + (lane & 15), p.n - 1));
 #pragma unroll
         for (int i = 0; i < 3; ++i) load_rows(r0.v[i], rows[i], offset, left - s0);
         load_states(r0, states);
@@ -391,8 +533,9 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
     }
     if (!p.live) return;
     if (y)
-        for (int t = p.n + w; t < q.T; t += W) y[((int64_t)p.b * q.T + t) * q.D + p.d] = from_f32<E>(0.0f);
-    if (h_last)
+        for (int t = p.t0 + p.n + w; t < p.t1; t += W) y[((int64_t)p.b * q.T + t) * q.D + p.d] = from_f32<E>(0.0f);
+    // the segment that the sample ends in has the last state
+    if (h_last && (p.n > 0 ? p.t0 + p.n == p.length : p.seg == 0 && p.length == 0))
 #pragma unroll
         for (int k = 0; k < NS; ++k)
             if (n0 + k < q.N) h_last[((int64_t)p.b * q.D + p.d) * q.N + n0 + k] = h[k];
@@ -449,228 +592,260 @@ __device__ __forceinline__ float merge_steps(const float (&v)[16], int lane)
 template <typename E> struct BackOut {
     E *gx, *gdt, *gz;
     float *partB, *partC;         // [B G cols][T][N] sums over a column's channels
-    float *partA;                 // [B][D][N]
+    float *partA;                 // [S B][D][N]
     float *partS;                 // [B][2][D]: of skip, of dt_bias
     float *g_first;
 };
 
-template <typename E, int NS, int W, int NB>
+// Bound by instructions: 14 a state and step, 4 more for the sums over channels
+// that grad_B and grad_C are, 100 a channel and step in phases A and C.  A wave
+// holds two states at a time, NB times over, so that a tile's states and decays
+// fit its registers.  Between two barriers a tile is walked; then its results
+// are written while the tile before it is made ready and the one before that is
+// on its way.
+template <typename E, int W, int NB>
 __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q, const float* __restrict__ marks,
-                                                          const float* __restrict__ grad_last, BackOut<E> out)
+                                                          const float* __restrict__ grad_last,
+                                                          const float* __restrict__ sums,
+                                                          const float* __restrict__ ends, BackOut<E> out)
 {
-    constexpr int STEPS = kTile / W;
+    constexpr int STEPS = kTile / W, NS = 2;
     __shared__ float4 shD[kTile / 2][kWave];                  // delta, delta x of two steps
-    __shared__ float shG[kTile / 4][kWave][4];                // g of four
-    __shared__ float shP[3][W][kTile / 4][kWave][4];          // the waves' parts of P, Q and y
+    __shared__ float4 shG[kTile / 4][kWave];                  // g of four
+    __shared__ float4 shP[3][W][kTile / 4][kWave];            // the waves' parts of P, Q and y of four
     const int lane = threadIdx.x & 63, w = wave_index();
     const Place p = place_of(q, in.length, lane);
-    const int used = min(W, (q.N + NS - 1) / NS), s0 = w * STEPS;
-    const E* Bm = (const E*)in.Bm + p.b * q.b_batch + (int64_t)p.g * q.N;
-    const E* C = (const E*)in.C + p.b * q.c_batch + (int64_t)p.g * q.N;
-    float mu[NB][NS], A[NB][NS], gA[NB][NS];
+    const int s0 = w * STEPS;
+    const bool gated = in.z != nullptr, driven = in.gy != nullptr;
     auto first = [&](int nb) { return (nb * W + w) * NS; };
+    float mu[NB][NS], A[NB][NS], rate[NB][NS], gA[NB][NS];
+    int at[NB][NS];                                           // places past N repeat the last state, with B = C = 0
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int k = 0; k < NS; ++k) {
             const int n = first(nb) + k;
+            at[nb][k] = min(n, q.N - 1);
             const bool on = p.live && n < q.N;
             A[nb][k] = on ? in.A[(int64_t)p.d * q.N + n] : 0.0f;
+            rate[nb][k] = rate_of(A[nb][k]);
             mu[nb][k] = on && grad_last ? grad_last[((int64_t)p.b * q.D + p.d) * q.N + n] : 0.0f;
             gA[nb][k] = 0.0f;
         }
+    const int segments = (p.length + q.seg_len - 1) / q.seg_len;       // that have steps
+    if (p.seg + 1 < segments)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+            carry(mu[nb], rate[nb], sums, ends, q, p, first(nb), segments - 1, segments - 1 - p.seg, -1);
     const float bias = in.bias ? in.bias[p.d] : 0.0f, skip = in.skip ? in.skip[p.d] : 0.0f;
+    const uint32_t offset = p.d * (uint32_t)sizeof(E), offset4 = p.d * 4u;
     float g_skip = 0.0f, g_bias = 0.0f;
-    const uint32_t d = p.d, offset = d * (uint32_t)sizeof(E);
-    const int64_t mark_row = (int64_t)p.b * ((q.T + kTile - 1) / kTile) * q.N;
 
-    Raw<E, NS, STEPS, 4, NB> cur, nxt;
-    auto load = [&](Raw<E, NS, STEPS, 4, NB>& r, int t0, auto all) {
-        constexpr bool kAll = decltype(all)::value;
-        const int64_t tb = kAll ? t0 + (lane & 15) : min(t0 + (lane & 15), p.n - 1);
-        const int t = kAll ? t0 + s0 : min(t0 + s0, p.n - 1), there = kAll ? STEPS : p.n - t0 - s0;
+    // A tile's raw elements and marks on their way, and what phase A makes of
+    // the steps of this wave.
+    Raw<E, NS, STEPS, 4, NB> raw;
+    float mark[NB][NS];
+    struct Made {
+        float x[STEPS], delta[STEPS], slope[STEPS], g[STEPS], z_slope[STEPS];
+        float B[NB][NS], C[NB][NS], h0[NB][NS];
+    } made;
+    auto load = [&](int t0, int left) {
+        const int t = p.t0 + t0 + min(s0, left - 1), tb = p.t0 + t0 + min(lane & 15, left - 1);
         const Rows x = rows_of<E>(in.x, q.x_batch, q.x_time, p.b, t);
-        load_rows(r.v[0], x, offset, there);
-        load_rows(r.v[1], rows_of<E>(in.dt, q.dt_batch, q.dt_time, p.b, t), offset, there);
-        load_rows(r.v[2], in.z ? rows_of<E>(in.z, q.z_batch, q.z_time, p.b, t) : x, offset, there);
-        load_rows(r.v[3], in.gy ? rows_of<E>(in.gy, q.g_batch, q.g_time, p.b, t) : x, offset, there);
+        load_rows(raw.v[0], x, offset, left - s0);
+        load_rows(raw.v[1], rows_of<E>(in.dt, q.dt_batch, q.dt_time, p.b, t), offset, left - s0);
+        load_rows(raw.v[2], gated ? rows_of<E>(in.z, q.z_batch, q.z_time, p.b, t) : x, offset, left - s0);
+        load_rows(raw.v[3], driven ? rows_of<E>(in.gy, q.g_batch, q.g_time, p.b, t) : x, offset, left - s0);
+        const E* Bt = (const E*)in.Bm + p.b * q.b_batch + tb * q.b_time + (int64_t)p.g * q.N;
+        const E* Ct = (const E*)in.C + p.b * q.c_batch + tb * q.c_time + (int64_t)p.g * q.N;
+        const char* m = (const char*)(marks + ((int64_t)p.b * ((q.T + kTile - 1) / kTile) + (p.t0 + t0) / kTile) * q.N *
+                                                  q.D);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
-                const int at = min(first(nb) + k, q.N - 1);
-                r.bc[0][nb][k].load(Bm + tb * q.b_time + at);
-                r.bc[1][nb][k].load(C + tb * q.c_time + at);
+                raw.bc[0][nb][k].load(Bt + at[nb][k]);
+                raw.bc[1][nb][k].load(Ct + at[nb][k]);
+                mark[nb][k] = *(const float*)(m + (int64_t)at[nb][k] * q.D * 4 + offset4);
             }
     };
-    const int64_t column = blockIdx.x;
-    const int last = (p.n - 1) / kTile * kTile;
-    if (p.n > 0) load(cur, last, std::false_type());
-    for (int t0 = last; t0 >= 0 && p.n > 0; t0 -= kTile) {
-        const int cnt = min(kTile, p.n - t0);
-        float delta[STEPS], d_slope[STEPS], g[STEPS], z_slope[STEPS];
+    auto ready = [&](int left) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
-            delta[i] = step_length(q, cur.v[1][i].f32() + bias, d_slope[i]);
-            g[i] = in.gy ? cur.v[3][i].f32() : 0.0f;
-            z_slope[i] = 0.0f;
-            if (in.z) {
-                const float gate = silu(cur.v[2][i].f32(), z_slope[i]);
-                z_slope[i] *= g[i];
-                g[i] *= gate;
-            }
-            const bool on = p.live && s0 + i < cnt;
+            made.x[i] = raw.v[0][i].f32();
+            made.delta[i] = step_length(q, raw.v[1][i].f32() + bias, made.slope[i]);
+            made.g[i] = driven ? raw.v[3][i].f32() : 0.0f;
+            const float gate = silu(raw.v[2][i].f32(), made.z_slope[i]);
+            made.z_slope[i] *= made.g[i];
+            made.g[i] = gated ? made.g[i] * gate : made.g[i];
+            // a channel past the group's last has no part in the sums over channels
+            const bool on = p.live && s0 + i < left;
             float* to = (float*)&shD[(s0 + i) / 2][lane] + (s0 + i) % 2 * 2;
-            to[0] = on ? delta[i] : 0.0f;
-            to[1] = on ? delta[i] * cur.v[0][i].f32() : 0.0f;
-            shG[(s0 + i) / 4][lane][(s0 + i) % 4] = on ? g[i] : 0.0f;
+            to[0] = on ? made.delta[i] : 0.0f;
+            to[1] = on ? made.delta[i] * made.x[i] : 0.0f;
+            ((float*)&shG[(s0 + i) / 4][lane])[(s0 + i) % 4] = on ? made.g[i] : 0.0f;
         }
-        float B[NB][NS], Cv[NB][NS], h0[NB][NS];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
                 const bool on = first(nb) + k < q.N;
-                B[nb][k] = on ? cur.bc[0][nb][k].f32() : 0.0f, Cv[nb][k] = on ? cur.bc[1][nb][k].f32() : 0.0f;
-                h0[nb][k] = p.live && first(nb) + k < q.N
-                                ? (marks + (mark_row + t0 / kTile * (int64_t)q.N + first(nb) + k) * q.D)[d]
-                                : 0.0f;
+                made.B[nb][k] = on ? raw.bc[0][nb][k].f32() : 0.0f;
+                made.C[nb][k] = on ? raw.bc[1][nb][k].f32() : 0.0f;
+                made.h0[nb][k] = on ? mark[nb][k] : 0.0f;
             }
-        if (t0 > 0) load(nxt, t0 - kTile, std::true_type());
-        __syncthreads();
+    };
+    auto walk = [&](auto whole, int t0, int cnt) {
+        constexpr bool kWhole = decltype(whole)::value;
+        float4 D[kTile / 2], G[kTile / 4];
+#pragma unroll
+        for (int i = 0; i < kTile / 2; ++i) D[i] = shD[i][lane];
+#pragma unroll
+        for (int i = 0; i < kTile / 4; ++i) G[i] = shG[i][lane];
+        auto delta = [&](int i) { return i % 2 ? D[i / 2].z : D[i / 2].x; };
+        auto input = [&](int i) { return i % 2 ? D[i / 2].w : D[i / 2].y; };
+        auto grad = [&](int i) { return ((const float*)&G[i / 4])[i % 4]; };
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            if (first(nb) >= q.N) continue;
-            auto walk = [&](auto whole) {
-                constexpr bool kWhole = decltype(whole)::value;
-                float h[kTile][NS], a[kTile][NS], sum[kTile], P[kTile], Q[kTile], part[NS / 2][kTile], lams[kTile][NS];
-                each_step([&](auto step) {
-                    constexpr int i = decltype(step)::value;
-                    const float4 v = shD[i / 2][lane];
-                    const float dl = i % 2 ? v.z : v.x, u = i % 2 ? v.w : v.y;
+            float h[kTile][NS], a[kTile][NS], sum[kTile], P[kTile], Q[kTile], lam[kTile][NS], part[kTile];
+            const float(&B)[NS] = made.B[nb], (&C)[NS] = made.C[nb], (&h0)[NS] = made.h0[nb];
+            each_step([&](auto step) {
+                constexpr int i = decltype(step)::value;
 #pragma unroll
-                    for (int k = 0; k < NS; ++k) {
-                        const float prev = i ? h[i ? i - 1 : 0][k] : h0[nb][k];
-                        const bool on = kWhole || i < cnt;
-                        a[i][k] = on ? __builtin_amdgcn_exp2f(dl * rate_of(A[nb][k])) : 1.0f;
-                        h[i][k] = on ? fmaf(a[i][k], prev, u * of_step<i>(B[nb][k])) : prev;
-                    }
-                    sum[i] = of_step<i>(Cv[nb][0]) * h[i][0];
-                    if constexpr (i % 4 == 3)
-#pragma unroll
-                        for (int k = 1; k < NS; ++k)
-                            add_steps<i - 3>(sum + i - 3, Cv[nb][k], h[i - 3][k], h[i - 2][k], h[i - 1][k], h[i][k]);
-                });
-                each_step_back([&](auto step) {
-                    constexpr int i = decltype(step)::value;
-                    const float4 v = shD[i / 2][lane];
-                    const float dl = i % 2 ? v.z : v.x, u = i % 2 ? v.w : v.y, gg = shG[i / 4][lane][i % 4];
-                    const bool on = kWhole || i < cnt;
-                    float pb[NS], pc[NS];
-                    P[i] = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < NS; ++k) {
-                        const float lam = on ? fmaf(gg, of_step<i>(Cv[nb][k]), mu[nb][k]) : 0.0f;
-                        lams[i][k] = lam;
-                        pc[k] = on ? gg * h[i][k] : 0.0f;
-                        pb[k] = lam * u;
-                        if (on) {
-                            mu[nb][k] = a[i][k] * lam;
-                            const float f = mu[nb][k] * (i ? h[i ? i - 1 : 0][k] : h0[nb][k]);
-                            P[i] = fmaf(A[nb][k], f, P[i]);
-                            gA[nb][k] = fmaf(dl, f, gA[nb][k]);
-                        }
-                    }
-                    Q[i] = of_step<i>(B[nb][0]) * lams[i][0];
-                    if constexpr (i % 4 == 0)
-#pragma unroll
-                        for (int k = 1; k < NS; ++k)
-                            add_steps<i>(Q + i, B[nb][k], lams[i][k], lams[i + 1][k], lams[i + 2][k], lams[i + 3][k]);
-#pragma unroll
-                    for (int k = 0; k < NS; k += 2) part[k / 2][i] = merge_states(pb[k], pb[k + 1], pc[k], pc[k + 1]);
-                });
-                // rows 0 .. 3 hold b and c of the first state, b and c of the second
-                const int row = lane >> 4, i = lane & 15;
-#pragma unroll
-                for (int k = 0; k < NS; k += 2) {
-                    const float s = merge_steps(part[k / 2], lane);
-                    const int n = first(nb) + k + (row >> 1);
-                    if (i < cnt && n < q.N)
-                        (row & 1 ? out.partC : out.partB)[(column * q.T + t0 + i) * q.N + n] = s;
+                for (int k = 0; k < NS; ++k) {
+                    a[i][k] = __builtin_amdgcn_exp2f(delta(i) * rate[nb][k]);
+                    h[i][k] = fmaf(a[i][k], i ? h[i ? i - 1 : 0][k] : h0[k], input(i) * of_step<i>(B[k]));
                 }
-#pragma unroll
-                for (int j = 0; j < 3; ++j) {
-                    float(&v)[kTile] = j == 0 ? P : j == 1 ? Q : sum;
-#pragma unroll
-                    for (int s = 0; s < kTile; s += 4) {
-                        float4* to = (float4*)shP[j][w][s / 4][lane];
-                        float4 o = nb ? *to : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        o.x += v[s], o.y += v[s + 1], o.z += v[s + 2], o.w += v[s + 3];
-                        *to = o;
-                    }
+                sum[i] = of_step<i>(C[0]) * h[i][0];
+                if constexpr (i % 4 == 3) {
+                    add_steps<i - 3>(sum + i - 3, C[1], h[i - 3][1], h[i - 2][1], h[i - 1][1], h[i][1]);
+                    float4* to = &shP[2][w][i / 4][lane];
+                    float4 o = make_float4(sum[i - 3], sum[i - 2], sum[i - 1], sum[i]);
+                    if (nb) o.x += to->x, o.y += to->y, o.z += to->z, o.w += to->w;
+                    *to = o;
                 }
-            };
-            if (cnt == kTile) walk(std::true_type());
-            else walk(std::false_type());
+            });
+            each_step_back([&](auto step) {
+                constexpr int i = decltype(step)::value;
+                float pb[NS], pc[NS];
+#pragma unroll
+                for (int k = 0; k < NS; ++k) {
+                    lam[i][k] = mu[nb][k] + grad(i) * of_step<i>(C[k]);
+                    pc[k] = grad(i) * h[i][k];
+                    pb[k] = lam[i][k] * input(i);
+                    mu[nb][k] = a[i][k] * lam[i][k];
+                    float f = mu[nb][k] * (i ? h[i ? i - 1 : 0][k] : h0[k]);
+                    if (!kWhole) f = i < cnt ? f : 0.0f;
+                    P[i] = k ? fmaf(A[nb][k], f, P[i]) : A[nb][k] * f;
+                    gA[nb][k] = fmaf(delta(i), f, gA[nb][k]);
+                }
+                Q[i] = of_step<i>(B[0]) * lam[i][0];
+                part[i] = merge_states(pb[0], pb[1], pc[0], pc[1]);
+                if constexpr (i % 4 == 0) {
+                    add_steps<i>(Q + i, B[1], lam[i][1], lam[i + 1][1], lam[i + 2][1], lam[i + 3][1]);
+                    float4 *tp = &shP[0][w][i / 4][lane], *tq = &shP[1][w][i / 4][lane];
+                    float4 op = make_float4(P[i], P[i + 1], P[i + 2], P[i + 3]);
+                    float4 oq = make_float4(Q[i], Q[i + 1], Q[i + 2], Q[i + 3]);
+                    if (nb) {
+                        op.x += tp->x, op.y += tp->y, op.z += tp->z, op.w += tp->w;
+                        oq.x += tq->x, oq.y += tq->y, oq.z += tq->z, oq.w += tq->w;
+                    }
+                    *tp = op, *tq = oq;
+                }
+            });
+            // rows 0 .. 3 hold b and c of the first state, b and c of the second
+            const float s = merge_steps(part, lane);
+            const int row = lane >> 4, i = lane & 15, n = first(nb) + (row >> 1);
+            if (i < cnt && n < q.N)
+                (row & 1 ? out.partC : out.partB)[((int64_t)p.column * q.T + p.t0 + t0 + i) * q.N + n] = s;
         }
-        __syncthreads();
+    };
+    auto write = [&](int t0, int cnt) {
         float P[STEPS], Q[STEPS], Y[STEPS];
-        int64_t row = ((int64_t)p.b * q.T + t0 + s0) * q.D;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) P[i] = Q[i] = Y[i] = 0.0f;
-        for (int j = 0; j < used; ++j)
+        for (int i = 0; i < STEPS; ++i) P[i] = Q[i] = 0.0f, Y[i] = skip * made.x[i];
+#pragma unroll
+        for (int j = 0; j < W; ++j)
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                P[i] += shP[0][j][(s0 + i) / 4][lane][(s0 + i) % 4];
-                Q[i] += shP[1][j][(s0 + i) / 4][lane][(s0 + i) % 4];
-                Y[i] += shP[2][j][(s0 + i) / 4][lane][(s0 + i) % 4];
+                P[i] += ((const float*)&shP[0][j][(s0 + i) / 4][lane])[(s0 + i) % 4];
+                Q[i] += ((const float*)&shP[1][j][(s0 + i) / 4][lane])[(s0 + i) % 4];
+                Y[i] += ((const float*)&shP[2][j][(s0 + i) / 4][lane])[(s0 + i) % 4];
             }
+        const int64_t row = (((int64_t)p.b * q.T + p.t0 + t0 + s0) * q.D) * (int64_t)sizeof(E);
+        char *gx = (char*)out.gx + row, *gdt = (char*)out.gdt + row, *gz = (char*)out.gz + row;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i, row += q.D) {
-            if (s0 + i < cnt) {
-                const float xv = cur.v[0][i].f32();
-                const float g_r = fmaf(xv, Q[i], P[i]) * d_slope[i];
-                g_skip = fmaf(g[i], xv, g_skip);
-                g_bias += g_r;
-                if (p.live) {
-                    (out.gx + row)[d] = from_f32<E>(fmaf(delta[i], Q[i], skip * g[i]));
-                    (out.gdt + row)[d] = from_f32<E>(g_r);
-                    if (in.z) (out.gz + row)[d] = from_f32<E>(fmaf(skip, xv, Y[i]) * z_slope[i]);
-                }
+        for (int i = 0; i < STEPS; ++i) {
+            if (s0 + i >= cnt) break;
+            const float g_r = fmaf(made.x[i], Q[i], P[i]) * made.slope[i];
+            g_skip = fmaf(made.g[i], made.x[i], g_skip);
+            g_bias += g_r;
+            if (p.live) {
+                *(E*)(gx + offset) = from_f32<E>(fmaf(made.delta[i], Q[i], skip * made.g[i]));
+                *(E*)(gdt + offset) = from_f32<E>(g_r);
+                if (gated) *(E*)(gz + offset) = from_f32<E>(Y[i] * made.z_slope[i]);
             }
+            const int64_t next = q.D * (int64_t)sizeof(E);
+            gx += next, gdt += next, gz += next;
         }
-        cur = nxt;
+    };
+
+    int t0 = p.n / kTile * kTile;                             // after the last whole tile
+    if (t0 < p.n) {
+        load(t0, p.n - t0);
+        ready(p.n - t0);
+        __syncthreads();
+        walk(std::false_type(), t0, p.n - t0);
+        __syncthreads();
+        write(t0, p.n - t0);
+    }
+    if (t0 > 0) {
+        t0 -= kTile;
+        load(t0, kTile);
+        ready(kTile);
+        load(max(t0 - kTile, 0), kTile);
+        for (;;) {
+            __syncthreads();
+            walk(std::true_type(), t0, kTile);
+            __syncthreads();
+            write(t0, kTile);
+            if (t0 == 0) break;
+            t0 -= kTile;
+            ready(kTile);
+            load(max(t0 - kTile, 0), kTile);
+        }
     }
     if (p.live) {
-        for (int t = p.n + w; t < q.T; t += W) {
-            const int64_t at = ((int64_t)p.b * q.T + t) * q.D + p.d;
-            out.gx[at] = out.gdt[at] = from_f32<E>(0.0f);
-            if (in.z) out.gz[at] = from_f32<E>(0.0f);
+        for (int t = p.t0 + p.n + w; t < p.t1; t += W) {
+            const int64_t to = ((int64_t)p.b * q.T + t) * q.D + p.d;
+            out.gx[to] = out.gdt[to] = from_f32<E>(0.0f);
+            if (gated) out.gz[to] = from_f32<E>(0.0f);
         }
+        const int64_t states = (int64_t)q.D * q.N;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int k = 0; k < NS; ++k)
                 if (first(nb) + k < q.N) {
-                    const int64_t at = ((int64_t)p.b * q.D + p.d) * q.N + first(nb) + k;
-                    out.partA[at] = gA[nb][k];
-                    if (out.g_first) out.g_first[at] = mu[nb][k];
+                    const int64_t to = (int64_t)p.d * q.N + first(nb) + k;
+                    out.partA[((int64_t)p.seg * q.B + p.b) * states + to] = gA[nb][k];
+                    if (out.g_first && p.seg == 0) out.g_first[p.b * states + to] = mu[nb][k];
                 }
     }
     __syncthreads();
-    shP[0][w][0][lane][0] = g_skip;
-    shP[0][w][0][lane][1] = g_bias;
+    shP[0][w][0][lane] = make_float4(g_skip, g_bias, 0.0f, 0.0f);
     __syncthreads();
     if (w == 0 && p.live) {
-        float s0_ = 0.0f, s1 = 0.0f;
-        for (int j = 0; j < W; ++j) s0_ += shP[0][j][0][lane][0], s1 += shP[0][j][0][lane][1];
-        out.partS[(int64_t)p.b * 2 * q.D + p.d] = s0_;
-        out.partS[((int64_t)p.b * 2 + 1) * q.D + p.d] = s1;
+        float skips = 0.0f, biases = 0.0f;
+        for (int j = 0; j < W; ++j) skips += shP[0][j][0][lane].x, biases += shP[0][j][0][lane].y;
+        float* to = out.partS + ((int64_t)p.seg * q.B + p.b) * 2 * q.D + p.d;
+        to[0] = skips;
+        to[q.D] = biases;
     }
 }
 
 // Adds up the columns' parts of grad_B and grad_C, and the samples' parts of
-// the parameters' gradients, in the order of columns and samples.
+// the parameters' gradients, in the order of columns, segments and samples.
 template <typename E>
 __global__ __launch_bounds__(256) void k_select_sums(Geometry q, const int32_t* __restrict__ length,
                                                      const float* __restrict__ partB, const float* __restrict__ partC,
@@ -703,13 +878,13 @@ __global__ __launch_bounds__(256) void k_select_sums(Geometry q, const int32_t* 
     if (at < states) {
         float s = 0.0f;
 #pragma unroll 8
-        for (int b = 0; b < q.B; ++b) s += partA[b * states + at];
+        for (int64_t i = 0; i < (int64_t)q.S * q.B; ++i) s += partA[i * states + at];
         gA[at] = s;
     } else if (at < states + 2 * q.D) {
         const int64_t i = at - states;                        // skip's, then dt_bias'
         float s = 0.0f;
 #pragma unroll 8
-        for (int b = 0; b < q.B; ++b) s += partS[(int64_t)b * 2 * q.D + i];
+        for (int64_t j = 0; j < (int64_t)q.S * q.B; ++j) s += partS[j * 2 * q.D + i];
         float* to = i < q.D ? g_skip : g_bias;
         if (to) to[i < q.D ? i : i - q.D] = s;
     }
@@ -792,12 +967,27 @@ int check_select(const lif_select_params* p)
     return LIF_OK;
 }
 
-Geometry geometry_of(const lif_select_params& p)
+// Segments of the time axis: see the rule.
+int segments_of(const lif_select_params& p, int columns, bool back)
+{
+    const int tiles = (p.T + kTile - 1) / kTile;
+    if (columns > kSplitColumns) return 1;
+    int S = 1;
+    while (S < kMaxSegments && columns * S * 2 <= kSplitGroups && tiles >= S * 2 * kSplitTiles) S *= 2;
+    return S < kSplitLeast ? 1 : S;
+}
+
+Geometry geometry_of(const lif_select_params& p, bool back)
 {
     Geometry q;
     q.B = p.B, q.T = p.T, q.D = p.D, q.N = p.N, q.G = p.G;
     q.Dg = p.D / p.G;
     q.cols = (q.Dg + kWave - 1) / kWave;
+    q.columns = q.B * q.G * q.cols;
+    const int tiles = (q.T + kTile - 1) / kTile, S = segments_of(p, q.columns, back);
+    const int per = tiles > 0 ? (tiles + S - 1) / S : 1;
+    q.seg_len = per * kTile;
+    q.S = tiles > 0 ? (tiles + per - 1) / per : 1;
     q.flags = p.flags;
     q.x_batch = p.x_batch, q.x_time = p.x_time, q.dt_batch = p.dt_batch, q.dt_time = p.dt_time;
     q.z_batch = p.z_batch, q.z_time = p.z_time, q.b_batch = p.b_batch, q.b_time = p.b_time;
@@ -821,20 +1011,26 @@ template <typename Fn> void with_waves(int N, Fn&& fn)
 
 size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
 
+// Segments' sums and ends (none where there is one segment).
+size_t sums_size(const Geometry& q) { return q.S > 1 ? align16(sizeof(float) * q.S * (size_t)q.B * q.D) : 0; }
+size_t ends_size(const Geometry& q) { return q.S > 1 ? align16(sizeof(float) * q.S * (size_t)q.B * q.D * q.N) : 0; }
+
 struct BackLayout {
-    size_t partB, partC, partA, partS, total;
+    size_t partB, partC, partA, partS, sums, ends, total;
 };
 
 BackLayout back_layout(const lif_select_params& p)
 {
-    const Geometry q = geometry_of(p);
+    const Geometry q = geometry_of(p, true);
     BackLayout l;
     const size_t bc = align16(sizeof(float) * q.B * q.G * q.cols * (size_t)q.T * q.N);
     l.partB = 0;
     l.partC = bc;
     l.partA = 2 * bc;
-    l.partS = l.partA + align16(sizeof(float) * q.B * (size_t)q.D * q.N);
-    l.total = l.partS + align16(sizeof(float) * 2 * q.B * (size_t)q.D);
+    l.partS = l.partA + align16(sizeof(float) * q.S * (size_t)q.B * q.D * q.N);
+    l.sums = l.partS + align16(sizeof(float) * 2 * q.S * (size_t)q.B * q.D);
+    l.ends = l.sums + sums_size(q);
+    l.total = l.ends + ends_size(q);
     return l;
 }
 
@@ -845,7 +1041,8 @@ extern "C" size_t lif_selective_scan_workspace_size(const lif_select_params* p)
 {
     using namespace lif;
     if (check_select(p) != LIF_OK) return 0;
-    return 0;
+    const Geometry q = geometry_of(*p, false);
+    return sums_size(q) + ends_size(q);
 }
 
 extern "C" int lif_selective_scan(const void* x, const void* dt, const float* A, const void* Bm, const void* C,
@@ -858,16 +1055,22 @@ extern "C" int lif_selective_scan(const void* x, const void* dt, const float* A,
     if (rc) return rc;
     if (p->B > 0 && p->T > 0 && (!x || !dt || !Bm || !C)) return LIF_ERR_ARG;
     if (p->B > 0 && (!A || (!y && !h_last && !marks))) return LIF_ERR_ARG;
+    const size_t need = lif_selective_scan_workspace_size(p);
+    if (need > 0 && (!ws || (uintptr_t)ws % 16)) return LIF_ERR_ARG;
+    if (ws_bytes < need) return LIF_ERR_WORKSPACE;
     if (p->B == 0) return LIF_OK;
-    const Geometry q = geometry_of(*p);
+    const Geometry q = geometry_of(*p, false);
     const Inputs in = {x, dt, Bm, C, z, nullptr, A, skip, dt_bias, length};
-    const dim3 grid((unsigned)(q.B * q.G * q.cols));
+    float *sums = (float*)ws, *ends = (float*)((char*)ws + sums_size(q));
     with_dtype(p->dtype, [&](auto e) {
         using E = decltype(e);
         with_waves(q.N, [&](auto ns, auto waves) {
             constexpr int NS = decltype(ns)::value, W = decltype(waves)::value;
-            TIMED_LAUNCH("select_scan", (k_select_scan<E, NS, W>), grid, dim3(W * kWave), 0, (hipStream_t)stream, in, q,
-                         h_first, (E*)y, h_last, marks);
+            if (q.S > 1)
+                TIMED_LAUNCH("select_maps", (k_select_maps<E, NS, W, false>), dim3((unsigned)(q.columns * (q.S - 1))),
+                             dim3(W * kWave), 0, (hipStream_t)stream, in, q, sums, ends);
+            TIMED_LAUNCH("select_scan", (k_select_scan<E, NS, W>), dim3((unsigned)(q.columns * q.S)), dim3(W * kWave),
+                         0, (hipStream_t)stream, in, q, h_first, sums, ends, (E*)y, h_last, marks);
         });
     });
     return check_launch();
@@ -898,7 +1101,7 @@ extern "C" int lif_selective_scan_backward(const void* x, const void* dt, const 
     const BackLayout l = back_layout(*p);
     if (l.total > 0 && (!ws || (uintptr_t)ws % 16)) return LIF_ERR_ARG;
     if (ws_bytes < l.total) return LIF_ERR_WORKSPACE;
-    const Geometry q = geometry_of(*p);
+    const Geometry q = geometry_of(*p, true);
     const Inputs in = {x, dt, Bm, C, z, grad_y, A, skip, dt_bias, length};
     const int64_t bc = (int64_t)q.B * q.G * q.T * q.N;
     const int64_t bc_blocks = bc > ((int64_t)1 << 30) ? 1 << 22 : (bc + 255) / 256;
@@ -909,18 +1112,26 @@ extern "C" int lif_selective_scan_backward(const void* x, const void* dt, const 
         const BackOut<E> out = {(E*)grad_x, (E*)grad_dt, (E*)grad_z, (float*)(base + l.partB),
                                 (float*)(base + l.partC), (float*)(base + l.partA), (float*)(base + l.partS),
                                 grad_h_first};
-        auto launch = [&](auto ns, auto waves, auto nb) {
-            constexpr int NS = decltype(ns)::value, W = decltype(waves)::value, NB = decltype(nb)::value;
-            TIMED_LAUNCH("select_back", (k_select_back<E, NS, W, NB>), dim3((unsigned)(q.B * q.G * q.cols)),
-                         dim3(W * kWave), 0, (hipStream_t)stream, in, q, marks, grad_last, out);
+        float *sums = (float*)(base + l.sums), *ends = (float*)(base + l.ends);
+        auto launch = [&](auto waves, auto nb) {
+            constexpr int W = decltype(waves)::value, NB = decltype(nb)::value;
+            TIMED_LAUNCH("select_back", (k_select_back<E, W, NB>), dim3((unsigned)(q.columns * q.S)),
+                         dim3(W * kWave), 0, (hipStream_t)stream, in, q, marks, grad_last, sums, ends, out);
         };
+        if (q.S > 1)
+            with_waves(q.N, [&](auto ns, auto waves) {
+                constexpr int NS = decltype(ns)::value, W = decltype(waves)::value;
+                TIMED_LAUNCH("select_maps_back", (k_select_maps<E, NS, W, true>),
+                             dim3((unsigned)(q.columns * (q.S - 1))), dim3(W * kWave), 0, (hipStream_t)stream, in, q,
+                             sums, ends);
+            });
         if (q.B > 0) {
-            if (q.N <= 2) launch(Int<2>(), Int<1>(), Int<1>());
-            else if (q.N <= 4) launch(Int<2>(), Int<2>(), Int<1>());
-            else if (q.N <= 8) launch(Int<2>(), Int<4>(), Int<1>());
-            else if (q.N <= 16) launch(Int<2>(), Int<8>(), Int<1>());
-            else if (q.N <= 32) launch(Int<2>(), Int<8>(), Int<2>());
-            else launch(Int<2>(), Int<8>(), Int<4>());
+            if (q.N <= 2) launch(Int<1>(), Int<1>());
+            else if (q.N <= 4) launch(Int<2>(), Int<1>());
+            else if (q.N <= 8) launch(Int<4>(), Int<1>());
+            else if (q.N <= 16) launch(Int<8>(), Int<1>());
+            else if (q.N <= 32) launch(Int<8>(), Int<2>());
+            else launch(Int<8>(), Int<4>());
         }
         TIMED_LAUNCH("select_sums", (k_select_sums<E>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, q,
                      length, out.partB, out.partC, out.partA, out.partS, (E*)grad_B, (E*)grad_C, grad_A, grad_skip,
@@ -939,7 +1150,7 @@ extern "C" int lif_selective_step(const void* x, const void* dt, const float* A,
     if (p->T != 1 || n_slots < 0 || (!slot && n_slots < p->B)) return LIF_ERR_ARG;
     if (p->B == 0) return LIF_OK;
     if (!x || !dt || !A || !Bm || !C || !y || (n_slots > 0 && !state)) return LIF_ERR_ARG;
-    const Geometry q = geometry_of(*p);
+    const Geometry q = geometry_of(*p, false);
     const Inputs in = {x, dt, Bm, C, z, nullptr, A, skip, dt_bias, nullptr};
     int L = 1;
     while (4 * L < q.N) L *= 2;

@@ -14,7 +14,7 @@ TYPES = ("f32", "bf16", "f16")
 # (samples, steps, channels, states, groups)
 SHAPES = [(1, 1, 1, 1, 1), (2, 1, 5, 3, 1), (1, 2, 64, 4, 1), (3, 15, 7, 5, 1), (2, 16, 65, 8, 1), (2, 17, 130, 16, 2),
           (1, 33, 63, 17, 3), (2, 48, 40, 32, 2), (1, 50, 20, 33, 1), (2, 35, 66, 64, 3), (1, 700, 24, 16, 1),
-          (40, 20, 20, 16, 1), (1, 3000, 6, 4, 1)]
+          (40, 20, 20, 16, 1), (1, 3000, 6, 4, 1), (2, 1111, 130, 16, 2), (1, 2005, 40, 33, 1)]
 
 
 @pytest.fixture(scope="module")
