@@ -140,6 +140,16 @@ template <int I> __device__ __forceinline__ void add_steps(float* acc, float v, 
         : "v"(v), "v"(x0), "v"(x1), "v"(x2), "v"(x3), "n"(I), "n"(I + 1), "n"(I + 2), "n"(I + 3));
 }
 
+// a += u of step I times x, b += v of step I times x.
+template <int I> __device__ __forceinline__ void add_step(float& a, float& b, float u, float v, float x)
+{
+    asm("s_nop 1\n\t"
+        "v_fmac_f32_dpp %0, %2, %4 row_newbcast:%5 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %1, %3, %4 row_newbcast:%5 row_mask:0xf bank_mask:0xf"
+        : "+v"(a), "+v"(b)
+        : "v"(u), "v"(v), "v"(x), "n"(I));
+}
+
 template <int I> using Step = std::integral_constant<int, I>;
 // fn(Step<0>()) .. fn(Step<15>()), or in reverse.
 template <typename Fn, int... I>
@@ -611,8 +621,8 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
 {
     constexpr int STEPS = kTile / W, NS = 2;
     __shared__ float4 shD[kTile / 2][kWave];                  // delta, delta x of two steps
-    __shared__ float4 shG[kTile / 4][kWave];                  // g of four
-    __shared__ float4 shP[3][W][kTile / 4][kWave];            // the waves' parts of P, Q and y of four
+    __shared__ float2 shG[kTile / 2][kWave];                  // g of two
+    __shared__ float2 shP[3][W][kTile / 2][kWave];            // the waves' parts of P, Q and y of two
     const int lane = threadIdx.x & 63, w = wave_index();
     const Place p = place_of(q, in.length, lane);
     const int s0 = w * STEPS;
@@ -649,25 +659,37 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         float x[STEPS], delta[STEPS], slope[STEPS], g[STEPS], z_slope[STEPS];
         float B[NB][NS], C[NB][NS], h0[NB][NS];
     } made;
-    auto load = [&](int t0, int left) {
+    // Where the tile that is loaded next lies.
+    Rows rows[4];
+    const E *Bt, *Ct;
+    const char* mark_at;
+    auto find = [&](int t0, int left) {
         const int t = p.t0 + t0 + min(s0, left - 1), tb = p.t0 + t0 + min(lane & 15, left - 1);
-        const Rows x = rows_of<E>(in.x, q.x_batch, q.x_time, p.b, t);
-        load_rows(raw.v[0], x, offset, left - s0);
-        load_rows(raw.v[1], rows_of<E>(in.dt, q.dt_batch, q.dt_time, p.b, t), offset, left - s0);
-        load_rows(raw.v[2], gated ? rows_of<E>(in.z, q.z_batch, q.z_time, p.b, t) : x, offset, left - s0);
-        load_rows(raw.v[3], driven ? rows_of<E>(in.gy, q.g_batch, q.g_time, p.b, t) : x, offset, left - s0);
-        const E* Bt = (const E*)in.Bm + p.b * q.b_batch + tb * q.b_time + (int64_t)p.g * q.N;
-        const E* Ct = (const E*)in.C + p.b * q.c_batch + tb * q.c_time + (int64_t)p.g * q.N;
-        const char* m = (const char*)(marks + ((int64_t)p.b * ((q.T + kTile - 1) / kTile) + (p.t0 + t0) / kTile) * q.N *
-                                                  q.D);
+        rows[0] = rows_of<E>(in.x, q.x_batch, q.x_time, p.b, t);
+        rows[1] = rows_of<E>(in.dt, q.dt_batch, q.dt_time, p.b, t);
+        rows[2] = gated ? rows_of<E>(in.z, q.z_batch, q.z_time, p.b, t) : rows[0];
+        rows[3] = driven ? rows_of<E>(in.gy, q.g_batch, q.g_time, p.b, t) : rows[0];
+        Bt = (const E*)in.Bm + p.b * q.b_batch + tb * q.b_time + (int64_t)p.g * q.N;
+        Ct = (const E*)in.C + p.b * q.c_batch + tb * q.c_time + (int64_t)p.g * q.N;
+        mark_at = (const char*)(marks + ((int64_t)p.b * ((q.T + kTile - 1) / kTile) + (p.t0 + t0) / kTile) * q.N * q.D);
+    };
+    auto load = [&](int left) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_rows(raw.v[i], rows[i], offset, left - s0);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
                 raw.bc[0][nb][k].load(Bt + at[nb][k]);
                 raw.bc[1][nb][k].load(Ct + at[nb][k]);
-                mark[nb][k] = *(const float*)(m + (int64_t)at[nb][k] * q.D * 4 + offset4);
+                mark[nb][k] = *(const float*)(mark_at + at[nb][k] * (q.D * (int64_t)4) + offset4);
             }
+    };
+    auto back = [&] {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rows[i].at -= kTile * rows[i].step;
+        Bt -= kTile * q.b_time, Ct -= kTile * q.c_time;
+        mark_at -= q.N * (q.D * (int64_t)4);
     };
     auto ready = [&](int left) {
 #pragma unroll
@@ -678,12 +700,21 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
             const float gate = silu(raw.v[2][i].f32(), made.z_slope[i]);
             made.z_slope[i] *= made.g[i];
             made.g[i] = gated ? made.g[i] * gate : made.g[i];
-            // a channel past the group's last has no part in the sums over channels
-            const bool on = p.live && s0 + i < left;
-            float* to = (float*)&shD[(s0 + i) / 2][lane] + (s0 + i) % 2 * 2;
-            to[0] = on ? made.delta[i] : 0.0f;
-            to[1] = on ? made.delta[i] * made.x[i] : 0.0f;
-            ((float*)&shG[(s0 + i) / 4][lane])[(s0 + i) % 4] = on ? made.g[i] : 0.0f;
+        }
+        // a channel past the group's last has no part in the sums over channels,
+        // steps past the end are the identity
+#pragma unroll
+        for (int i = 0; i < STEPS; i += 2) {
+            float v[2][3];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bool on = p.live && s0 + i + j < left;
+                v[j][0] = on ? made.delta[i + j] : 0.0f;
+                v[j][1] = on ? made.delta[i + j] * made.x[i + j] : 0.0f;
+                v[j][2] = on ? made.g[i + j] : 0.0f;
+            }
+            shD[(s0 + i) / 2][lane] = make_float4(v[0][0], v[0][1], v[1][0], v[1][1]);
+            shG[(s0 + i) / 2][lane] = make_float2(v[0][2], v[1][2]);
         }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
@@ -695,16 +726,19 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                 made.h0[nb][k] = on ? mark[nb][k] : 0.0f;
             }
     };
+    auto put = [&](int what, int i, int nb, float a, float b) {
+        float2* to = &shP[what][w][i / 2][lane];
+        *to = nb ? make_float2(to->x + a, to->y + b) : make_float2(a, b);
+    };
     auto walk = [&](auto whole, int t0, int cnt) {
         constexpr bool kWhole = decltype(whole)::value;
-        float4 D[kTile / 2], G[kTile / 4];
+        float4 D[kTile / 2];
+        float2 G[kTile / 2];
 #pragma unroll
-        for (int i = 0; i < kTile / 2; ++i) D[i] = shD[i][lane];
-#pragma unroll
-        for (int i = 0; i < kTile / 4; ++i) G[i] = shG[i][lane];
+        for (int i = 0; i < kTile / 2; ++i) D[i] = shD[i][lane], G[i] = shG[i][lane];
         auto delta = [&](int i) { return i % 2 ? D[i / 2].z : D[i / 2].x; };
         auto input = [&](int i) { return i % 2 ? D[i / 2].w : D[i / 2].y; };
-        auto grad = [&](int i) { return ((const float*)&G[i / 4])[i % 4]; };
+        auto grad = [&](int i) { return i % 2 ? G[i / 2].y : G[i / 2].x; };
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             float h[kTile][NS], a[kTile][NS], sum[kTile], P[kTile], Q[kTile], lam[kTile][NS], part[kTile];
@@ -719,18 +753,17 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                 sum[i] = of_step<i>(C[0]) * h[i][0];
                 if constexpr (i % 4 == 3) {
                     add_steps<i - 3>(sum + i - 3, C[1], h[i - 3][1], h[i - 2][1], h[i - 1][1], h[i][1]);
-                    float4* to = &shP[2][w][i / 4][lane];
-                    float4 o = make_float4(sum[i - 3], sum[i - 2], sum[i - 1], sum[i]);
-                    if (nb) o.x += to->x, o.y += to->y, o.z += to->z, o.w += to->w;
-                    *to = o;
+                    put(2, i - 3, nb, sum[i - 3], sum[i - 2]);
+                    put(2, i - 1, nb, sum[i - 1], sum[i]);
                 }
             });
             each_step_back([&](auto step) {
                 constexpr int i = decltype(step)::value;
                 float pb[NS], pc[NS];
+                lam[i][0] = mu[nb][0], lam[i][1] = mu[nb][1];
+                add_step<i>(lam[i][0], lam[i][1], C[0], C[1], grad(i));
 #pragma unroll
                 for (int k = 0; k < NS; ++k) {
-                    lam[i][k] = mu[nb][k] + grad(i) * of_step<i>(C[k]);
                     pc[k] = grad(i) * h[i][k];
                     pb[k] = lam[i][k] * input(i);
                     mu[nb][k] = a[i][k] * lam[i][k];
@@ -743,14 +776,11 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                 part[i] = merge_states(pb[0], pb[1], pc[0], pc[1]);
                 if constexpr (i % 4 == 0) {
                     add_steps<i>(Q + i, B[1], lam[i][1], lam[i + 1][1], lam[i + 2][1], lam[i + 3][1]);
-                    float4 *tp = &shP[0][w][i / 4][lane], *tq = &shP[1][w][i / 4][lane];
-                    float4 op = make_float4(P[i], P[i + 1], P[i + 2], P[i + 3]);
-                    float4 oq = make_float4(Q[i], Q[i + 1], Q[i + 2], Q[i + 3]);
-                    if (nb) {
-                        op.x += tp->x, op.y += tp->y, op.z += tp->z, op.w += tp->w;
-                        oq.x += tq->x, oq.y += tq->y, oq.z += tq->z, oq.w += tq->w;
+#pragma unroll
+                    for (int j = 0; j < 4; j += 2) {
+                        put(0, i + j, nb, P[i + j], P[i + j + 1]);
+                        put(1, i + j, nb, Q[i + j], Q[i + j + 1]);
                     }
-                    *tp = op, *tq = oq;
                 }
             });
             // rows 0 .. 3 hold b and c of the first state, b and c of the second
@@ -767,32 +797,36 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
 #pragma unroll
         for (int j = 0; j < W; ++j)
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                P[i] += ((const float*)&shP[0][j][(s0 + i) / 4][lane])[(s0 + i) % 4];
-                Q[i] += ((const float*)&shP[1][j][(s0 + i) / 4][lane])[(s0 + i) % 4];
-                Y[i] += ((const float*)&shP[2][j][(s0 + i) / 4][lane])[(s0 + i) % 4];
+            for (int i = 0; i < STEPS; i += 2) {
+                const float2 a = shP[0][j][(s0 + i) / 2][lane], b = shP[1][j][(s0 + i) / 2][lane];
+                const float2 c = shP[2][j][(s0 + i) / 2][lane];
+                P[i] += a.x, P[i + 1] += a.y, Q[i] += b.x, Q[i + 1] += b.y, Y[i] += c.x, Y[i + 1] += c.y;
             }
         const int64_t row = (((int64_t)p.b * q.T + p.t0 + t0 + s0) * q.D) * (int64_t)sizeof(E);
         char *gx = (char*)out.gx + row, *gdt = (char*)out.gdt + row, *gz = (char*)out.gz + row;
+        const int64_t next = q.D * (int64_t)sizeof(E);
+        float g_r[STEPS];
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
-            if (s0 + i >= cnt) break;
-            const float g_r = fmaf(made.x[i], Q[i], P[i]) * made.slope[i];
-            g_skip = fmaf(made.g[i], made.x[i], g_skip);
-            g_bias += g_r;
-            if (p.live) {
-                *(E*)(gx + offset) = from_f32<E>(fmaf(made.delta[i], Q[i], skip * made.g[i]));
-                *(E*)(gdt + offset) = from_f32<E>(g_r);
-                if (gated) *(E*)(gz + offset) = from_f32<E>(Y[i] * made.z_slope[i]);
-            }
-            const int64_t next = q.D * (int64_t)sizeof(E);
-            gx += next, gdt += next, gz += next;
+            g_r[i] = fmaf(made.x[i], Q[i], P[i]) * made.slope[i];
+            const bool on = s0 + i < cnt;
+            g_skip = on ? fmaf(made.g[i], made.x[i], g_skip) : g_skip;
+            g_bias = on ? g_bias + g_r[i] : g_bias;
         }
+        if (!p.live) return;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+            if (s0 + i < cnt) {
+                *(E*)(gx + i * next + offset) = from_f32<E>(fmaf(made.delta[i], Q[i], skip * made.g[i]));
+                *(E*)(gdt + i * next + offset) = from_f32<E>(g_r[i]);
+                if (gated) *(E*)(gz + i * next + offset) = from_f32<E>(Y[i] * made.z_slope[i]);
+            }
     };
 
     int t0 = p.n / kTile * kTile;                             // after the last whole tile
     if (t0 < p.n) {
-        load(t0, p.n - t0);
+        find(t0, p.n - t0);
+        load(p.n - t0);
         ready(p.n - t0);
         __syncthreads();
         walk(std::false_type(), t0, p.n - t0);
@@ -801,9 +835,11 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
     }
     if (t0 > 0) {
         t0 -= kTile;
-        load(t0, kTile);
+        find(t0, kTile);
+        load(kTile);
         ready(kTile);
-        load(max(t0 - kTile, 0), kTile);
+        if (t0 > 0) back();
+        load(kTile);                                          // (the first tile again where there is none before it)
         for (;;) {
             __syncthreads();
             walk(std::true_type(), t0, kTile);
@@ -812,7 +848,8 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
             if (t0 == 0) break;
             t0 -= kTile;
             ready(kTile);
-            load(max(t0 - kTile, 0), kTile);
+            if (t0 > 0) back();
+            load(kTile);
         }
     }
     if (p.live) {
@@ -833,7 +870,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                 }
     }
     __syncthreads();
-    shP[0][w][0][lane] = make_float4(g_skip, g_bias, 0.0f, 0.0f);
+    shP[0][w][0][lane] = make_float2(g_skip, g_bias);
     __syncthreads();
     if (w == 0 && p.live) {
         float skips = 0.0f, biases = 0.0f;
