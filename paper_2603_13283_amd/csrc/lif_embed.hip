@@ -2,8 +2,8 @@
 // the table (lif_embed_backward).
 //
 // The gradient sorts the places of the tokens, stably and by counting: a digit
-// at a time, each of a few hundred waves counts the digits of its chunk of
-// places, the counts are summed over chunks, and every wave hands out the
+// at a time, each of up to 256 workgroups counts the digits of its chunk of
+// places, the counts are summed over chunks, and every workgroup hands out the
 // places of its chunk in order.  Then each row of the table has its places in
 // one run; the list is cut into pieces of equal length that waves sum up, and
 // runs that cross pieces are joined in the order of the pieces.  The order of
@@ -16,10 +16,11 @@ namespace lif {
 namespace {
 
 constexpr int kMaxBits = 10;          // of a digit
-constexpr int kChunks = 256;          // waves that count and hand out
+constexpr int kChunks = 256;          // workgroups that count and hand out
+constexpr int kSortWaves = 4;
 constexpr int kAhead = 8;             // rows whose loads are in flight at once
 constexpr int kJoinWaves = 8;
-constexpr int kZeroRows = 16;         // rows of the table that a wave looks up
+constexpr int kSeek = 16;             // lanes that look for a row of the table together
 
 // The row of place i, V where it has none.
 __device__ __forceinline__ uint32_t key_of(const int32_t* __restrict__ token, const int32_t* __restrict__ length,
@@ -60,77 +61,118 @@ struct Sort {
 };
 
 // Counts of a chunk's digits.
-__global__ __launch_bounds__(kWave) void k_count(const int32_t* __restrict__ token,
-                                                 const int32_t* __restrict__ length,
-                                                 const uint32_t* __restrict__ keys, Sort q,
-                                                 uint32_t* __restrict__ count)
+__global__ __launch_bounds__(kSortWaves* kWave) void k_count(const int32_t* __restrict__ token,
+                                                             const int32_t* __restrict__ length,
+                                                             const uint32_t* __restrict__ keys, Sort q,
+                                                             uint32_t* __restrict__ count)
 {
     __shared__ uint32_t sh[1 << kMaxBits];
-    const int lane = threadIdx.x, bins = 1 << q.bits, c = blockIdx.x;
-    for (int i = lane; i < bins; i += kWave) sh[i] = 0;
+    const int bins = 1 << q.bits, c = blockIdx.x;
+    for (int i = threadIdx.x; i < bins; i += kSortWaves * kWave) sh[i] = 0;
     __syncthreads();
-    const int end = min((int64_t)(c + 1) * q.chunk, (int64_t)q.R);
-    for (int64_t i = (int64_t)c * q.chunk + lane; i < end; i += kWave) {
+    const int64_t end = min((int64_t)(c + 1) * q.chunk, (int64_t)q.R);
+    for (int64_t i = (int64_t)c * q.chunk + threadIdx.x; i < end; i += kSortWaves * kWave) {
         const uint32_t k = keys ? keys[i] : key_of(token, length, q.T, q.V, (int)i);
         atomicAdd(&sh[(k >> q.shift) & (bins - 1)], 1u);
     }
     __syncthreads();
-    for (int i = lane; i < bins; i += kWave) count[(int64_t)c * bins + i] = sh[i];
+    for (int i = threadIdx.x; i < bins; i += kSortWaves * kWave) count[(int64_t)c * bins + i] = sh[i];
 }
 
 // Per digit: the counts become sums over the chunks before, total the whole.
-__global__ __launch_bounds__(kWave) void k_chunk_sums(uint32_t* __restrict__ count, int chunks, int bins,
-                                                      uint32_t* __restrict__ total)
+// A workgroup takes 64 digits, its 16 waves 16 chunks each, all their loads in
+// flight at once (one wave over all chunks: 30 us, this 3).
+__global__ __launch_bounds__(16 * kWave) void k_chunk_sums(uint32_t* __restrict__ count, int chunks, int bins,
+                                                           uint32_t* __restrict__ total)
 {
-    const int d = blockIdx.x * kWave + threadIdx.x;
-    if (d >= bins) return;
-    uint32_t s = 0;
-#pragma unroll 16
-    for (int c = 0; c < chunks; ++c) {
-        const uint32_t v = count[(int64_t)c * bins + d];
-        count[(int64_t)c * bins + d] = s;
-        s += v;
+    constexpr int kEach = kChunks / 16;
+    __shared__ uint32_t sh[16][kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, d = blockIdx.x * kWave + lane;
+    uint32_t v[kEach], s = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int c = w * kEach + i;
+        v[i] = d < bins && c < chunks ? count[(int64_t)c * bins + d] : 0;
     }
-    total[d] = s;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) s += v[i];
+    sh[w][lane] = s;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+    for (int i = 0; i < 16; ++i) {
+        before += i < w ? sh[i][lane] : 0;
+        all += sh[i][lane];
+    }
+    if (d >= bins) return;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int c = w * kEach + i;
+        if (c < chunks) count[(int64_t)c * bins + d] = before;
+        before += v[i];
+    }
+    if (w == 0) total[d] = all;
 }
 
-// Hands out a chunk's places in order: 64 at a time, lanes of the same digit
-// find each other by ballots over its bits.
-__global__ __launch_bounds__(kWave) void k_hand_out(const int32_t* __restrict__ token,
-                                                    const int32_t* __restrict__ length,
-                                                    const uint32_t* __restrict__ keys,
-                                                    const uint32_t* __restrict__ places, Sort q,
-                                                    const uint32_t* __restrict__ count,
-                                                    const uint32_t* __restrict__ total, uint32_t* __restrict__ keys_out,
-                                                    uint32_t* __restrict__ places_out)
+// Hands out a chunk's places in order.  Each wave takes a contiguous part of
+// the chunk, 64 places at a time: lanes of the same digit find each other by
+// ballots over its bits.
+__global__ __launch_bounds__(kSortWaves* kWave) void k_hand_out(const int32_t* __restrict__ token,
+                                                                const int32_t* __restrict__ length,
+                                                                const uint32_t* __restrict__ keys,
+                                                                const uint32_t* __restrict__ places, Sort q,
+                                                                const uint32_t* __restrict__ count,
+                                                                const uint32_t* __restrict__ total,
+                                                                uint32_t* __restrict__ keys_out,
+                                                                uint32_t* __restrict__ places_out)
 {
-    __shared__ uint32_t next[1 << kMaxBits];
-    const int lane = threadIdx.x, bins = 1 << q.bits, c = blockIdx.x;
-    // where each digit begins, and this chunk's part of it
-    const int per = (bins + kWave - 1) / kWave;
-    uint32_t sum = 0;
-    for (int i = 0; i < per; ++i)
-        if (lane * per + i < bins) sum += total[lane * per + i];
+    constexpr int kThreads = kSortWaves * kWave, kPer = (1 << kMaxBits) / kThreads;
+    __shared__ uint32_t next[kSortWaves][1 << kMaxBits], waves[kSortWaves];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, bins = 1 << q.bits, c = blockIdx.x;
+    for (int i = threadIdx.x; i < bins; i += kThreads)
+        for (int j = 0; j < kSortWaves; ++j) next[j][i] = 0;
+    // where each digit begins: a scan of the totals, kPer adjacent ones a thread
+    uint32_t mine[kPer], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int d = threadIdx.x * kPer + i;
+        mine[i] = d < bins ? total[d] : 0;
+        sum += mine[i];
+    }
     uint32_t before = sum;
     for (int o = 1; o < kWave; o <<= 1) {
         const uint32_t v = __shfl_up(before, o);
         if (lane >= o) before += v;
     }
+    if (lane == kWave - 1) waves[w] = before;
+    __syncthreads();
     before -= sum;
-    for (int i = 0; i < per; ++i) {
-        const int d = lane * per + i;
+    for (int i = 0; i < w; ++i) before += waves[i];
+    // the waves' counts, then where each wave's places of a digit begin
+    const int64_t first = (int64_t)c * q.chunk;
+    const int n = (int)min((int64_t)q.chunk, (int64_t)q.R - first), part = q.chunk / kSortWaves;
+    const int from = min(w * part, n), end = min(from + part, n);
+    auto key_at = [&](int64_t i) { return keys ? keys[i] : key_of(token, length, q.T, q.V, (int)i); };
+    for (int i = from + lane; i < end; i += kWave)
+        atomicAdd(&next[w][(key_at(first + i) >> q.shift) & (bins - 1)], 1u);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int d = threadIdx.x * kPer + i;
         if (d < bins) {
-            next[d] = before + count[(int64_t)c * bins + d];
-            before += total[d];
+            uint32_t at = before + count[(int64_t)c * bins + d];
+            for (int j = 0; j < kSortWaves; ++j) {
+                const uint32_t v = next[j][d];
+                next[j][d] = at;
+                at += v;
+            }
+            before += mine[i];
         }
     }
     __syncthreads();
-    const int64_t first = (int64_t)c * q.chunk;
-    const int n = (int)min((int64_t)q.chunk, (int64_t)q.R - first);
-    for (int i0 = 0; i0 < n; i0 += kWave) {
-        const bool on = i0 + lane < n;
-        const int64_t i = first + (on ? i0 + lane : 0);
-        const uint32_t k = keys ? keys[i] : key_of(token, length, q.T, q.V, (int)i);
+    for (int i0 = 0; i0 < part; i0 += kWave) {
+        const bool on = from + i0 + lane < end;
+        const int64_t i = first + (on ? from + i0 + lane : 0);
+        const uint32_t k = key_at(i);
         const uint32_t digit = (k >> q.shift) & (bins - 1);
         uint64_t same = __ballot(on);
         for (int b = 0; b < q.bits; ++b) {
@@ -139,9 +181,9 @@ __global__ __launch_bounds__(kWave) void k_hand_out(const int32_t* __restrict__ 
         }
         const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
         uint32_t at = 0;
-        if (on) at = next[digit] + rank;
+        if (on) at = next[w][digit] + rank;
         __syncthreads();
-        if (on && rank == 0) next[digit] = at + __popcll(same);
+        if (on && rank == 0) next[w][digit] = at + __popcll(same);
         __syncthreads();
         if (on) {
             keys_out[at] = k;
@@ -158,16 +200,50 @@ struct Sums {
 
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// Whether row v of the table is named, looked for by kSeek lanes at once: each
+// step leaves one of kSeek + 1 parts of the list.
+__device__ __forceinline__ bool named(const uint32_t* __restrict__ keys, int R, uint32_t v, int lane)
+{
+    int lo = 0, hi = R;                                             // the first key of at least v is in [lo, hi]
+    const int sub = lane & (kSeek - 1), shift = lane & ~(kSeek - 1);
+    while (__any(lo < hi)) {
+        const int at = lo + (int)((int64_t)(hi - lo) * (sub + 1) / (kSeek + 1));
+        const bool less = lo < hi && keys[at] < v;
+        const int below = __popcll((__ballot(less) >> shift) & ((1u << kSeek) - 1));
+        const int from = __shfl(at, shift + max(below - 1, 0)), to = __shfl(at, shift + min(below, kSeek - 1));
+        if (lo < hi) {
+            const int l = below > 0 ? from + 1 : lo;
+            hi = below < kSeek ? to : hi;
+            lo = l;
+        }
+    }
+    return lo < R && keys[lo] == v;
+}
+
 // A wave sums the rows of a piece of the sorted list for 64 VEC columns.  A run
 // that lies within the piece goes to the table's gradient, one that comes from
 // the piece before to part[piece][0], one that begins here and goes on to
-// part[piece][1].
+// part[piece][1].  The workgroups from sum_blocks on clear the rows that no
+// token names.
 template <typename E, int VEC>
 __global__ __launch_bounds__(256) void k_embed_sums(const E* __restrict__ grad, const uint32_t* __restrict__ keys,
-                                                    const uint32_t* __restrict__ places, Sums q,
+                                                    const uint32_t* __restrict__ places, Sums q, int64_t sum_blocks,
                                                     float* __restrict__ gW, float* __restrict__ part)
 {
     const int lane = threadIdx.x & 63;
+    if (blockIdx.x >= sum_blocks) {
+        const int64_t v0 = ((blockIdx.x - sum_blocks) * 4 + (threadIdx.x >> 6)) * (kWave / kSeek);
+        const int64_t v = v0 + lane / kSeek;
+        const bool missing = !named(keys, q.R, (uint32_t)min(v, (int64_t)q.V - 1), lane) && v < q.V;
+        uint64_t rows = __ballot(missing && (lane & (kSeek - 1)) == 0);
+        const float zero[VEC] = {};
+        while (rows) {
+            float* to = gW + (v0 + __builtin_ctzll(rows) / kSeek) * q.D;
+            rows &= rows - 1;
+            for (int d = lane * VEC; d < q.D; d += kWave * VEC) store_elems<float, VEC>(to + min(d, q.D - VEC), zero);
+        }
+        return;
+    }
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int piece = __builtin_amdgcn_readfirstlane((int)(item / q.columns));
     const int column = __builtin_amdgcn_readfirstlane((int)(item - (int64_t)piece * q.columns));
@@ -219,51 +295,28 @@ __global__ __launch_bounds__(256) void k_embed_sums(const E* __restrict__ grad, 
     else put(gW + (int64_t)run * q.D, q.scale);
 }
 
-// The first place in the sorted list whose key is at least v.
-__device__ __forceinline__ int lower_bound(const uint32_t* __restrict__ keys, int R, uint32_t v)
-{
-    int lo = 0, hi = R;
-    while (lo < hi) {
-        const int mid = lo + (hi - lo) / 2;
-        if (keys[mid] < v) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
-}
-
-// Workgroups below join_blocks: a piece and 64 VEC columns; if a run begins in
-// the piece and goes on, its parts are added up.  The others clear the rows of
-// the table that no token names.
+// A workgroup takes a piece and 64 VEC columns: if a run begins in the piece and
+// goes on, its parts are added up, each wave's share of the pieces in order.
 template <int VEC>
 __global__ __launch_bounds__(kJoinWaves* kWave) void k_embed_join(const uint32_t* __restrict__ keys, Sums q,
-                                                                  const float* __restrict__ part, int64_t join_blocks,
+                                                                  const float* __restrict__ part,
                                                                   float* __restrict__ gW)
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if (blockIdx.x >= join_blocks) {
-        const int64_t v0 = ((int64_t)(blockIdx.x - join_blocks) * kJoinWaves + w) * kZeroRows;
-        bool missing = false;
-        if (lane < kZeroRows && v0 + lane < q.V) {
-            const int at = lower_bound(keys, q.R, (uint32_t)(v0 + lane));
-            missing = at >= q.R || keys[at] != (uint32_t)(v0 + lane);
-        }
-        uint64_t rows = __ballot(missing);
-        const float zero[VEC] = {};
-        while (rows) {
-            const int i = __builtin_ctzll(rows);
-            rows &= rows - 1;
-            float* to = gW + (v0 + i) * q.D;
-            for (int d = lane * VEC; d < q.D; d += kWave * VEC) store_elems<float, VEC>(to + min(d, q.D - VEC), zero);
-        }
-        return;
-    }
     __shared__ float sh[kJoinWaves][kWave * VEC];
     const int piece = blockIdx.x / q.columns, column = blockIdx.x % q.columns;
     const int64_t first = (int64_t)piece * q.piece, end = first + q.piece;
     if (end >= q.R) return;
     const uint32_t run = keys[end];
     if (run >= (uint32_t)q.V || keys[end - 1] != run || (first > 0 && keys[first - 1] == run)) return;
-    const int last = (lower_bound(keys, q.R, run + 1) - 1) / q.piece, n = last - piece + 1;
+    int n = 2;                                                      // pieces that the run lies in
+    for (;;) {
+        const int64_t next = ((int64_t)piece + n + lane) * q.piece;
+        const uint64_t on = __ballot(next < q.R && keys[min(next, (int64_t)q.R - 1)] == run);
+        const int more = ~on ? __builtin_ctzll(~on) : kWave;
+        n += more;
+        if (more < kWave) break;
+    }
     const int at = (column * kWave + lane) * VEC, d = min(at, q.D - VEC);
     float acc[VEC];
 #pragma unroll
@@ -324,8 +377,8 @@ Plan plan_of(const lif_embed_params& p)
     while (((int64_t)1 << bits) <= p.V) ++bits;                     // keys are 0 .. V
     q.passes = (bits + kMaxBits - 1) / kMaxBits;
     q.bits = (bits + q.passes - 1) / q.passes;
-    const int64_t least = ((int64_t)R + kChunks - 1) / kChunks;
-    q.chunk = (int)((least + kWave - 1) / kWave * kWave);
+    const int64_t least = ((int64_t)R + kChunks - 1) / kChunks, unit = kSortWaves * kWave;
+    q.chunk = (int)((least + unit - 1) / unit * unit);
     q.chunks = q.chunk ? (int)(((int64_t)R + q.chunk - 1) / q.chunk) : 0;
     Sums& s = q.s;
     s.R = R, s.T = p.T, s.V = p.V, s.D = p.D;
@@ -418,25 +471,25 @@ extern "C" int lif_embed_backward(const int32_t* token, const void* grad, const 
         const Sort o = {(int)R, p->T, p->V, q.chunk, q.chunks, q.bits, i * q.bits};
         uint32_t *ko = (uint32_t*)(base + q.keys[i & 1]), *po = (uint32_t*)(base + q.places[i & 1]);
         const int bins = 1 << q.bits;
-        TIMED_LAUNCH("embed_count", k_count, dim3(q.chunks), dim3(kWave), 0, s, token, length, keys, o, count);
-        TIMED_LAUNCH("embed_chunks", k_chunk_sums, dim3((bins + kWave - 1) / kWave), dim3(kWave), 0, s, count,
+        TIMED_LAUNCH("embed_count", k_count, dim3(q.chunks), dim3(kSortWaves * kWave), 0, s, token, length, keys, o,
+                     count);
+        TIMED_LAUNCH("embed_chunks", k_chunk_sums, dim3((bins + kWave - 1) / kWave), dim3(16 * kWave), 0, s, count,
                      q.chunks, bins, total);
-        TIMED_LAUNCH("embed_sort", k_hand_out, dim3(q.chunks), dim3(kWave), 0, s, token, length, keys, places, o,
-                     count, total, ko, po);
+        TIMED_LAUNCH("embed_sort", k_hand_out, dim3(q.chunks), dim3(kSortWaves * kWave), 0, s, token, length, keys,
+                     places, o, count, total, ko, po);
         keys = ko, places = po;
     }
-    const int64_t items = (int64_t)q.s.pieces * q.s.columns;
-    const int64_t zero = ((int64_t)p->V + kJoinWaves * kZeroRows - 1) / (kJoinWaves * kZeroRows);
-    const dim3 sums((unsigned)((items + 3) / 4)), join((unsigned)(items + zero));
+    const int64_t items = (int64_t)q.s.pieces * q.s.columns, sum_blocks = (items + 3) / 4;
+    const int64_t rows = 4 * kWave / kSeek, zero_blocks = ((int64_t)p->V + rows - 1) / rows;
     float* part = (float*)(base + q.part);
     with_dtype(p->dtype, [&](auto e) {
         using E = decltype(e);
         auto with = [&](auto vec) {
             constexpr int VEC = decltype(vec)::value;
-            TIMED_LAUNCH("embed_sums", (k_embed_sums<E, VEC>), sums, dim3(256), 0, s, (const E*)grad, keys, places,
-                         q.s, grad_W, part);
-            TIMED_LAUNCH("embed_join", (k_embed_join<VEC>), join, dim3(kJoinWaves * kWave), 0, s, keys, q.s, part,
-                         items, grad_W);
+            TIMED_LAUNCH("embed_sums", (k_embed_sums<E, VEC>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256),
+                         0, s, (const E*)grad, keys, places, q.s, sum_blocks, grad_W, part);
+            TIMED_LAUNCH("embed_join", (k_embed_join<VEC>), dim3((unsigned)items), dim3(kJoinWaves * kWave), 0, s,
+                         keys, q.s, part, grad_W);
         };
         if (vec_of(p->D) == 4) with(Int<4>());
         else with(Int<1>());
