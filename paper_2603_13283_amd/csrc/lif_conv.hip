@@ -14,7 +14,8 @@ namespace lif {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kAhead = 8;             // steps whose loads are in flight at once
+constexpr int kAhead = 8;             // steps of a batch, whose loads are in flight at once
+constexpr int kMaxStrip = 64, kMinStrip = 16, kStripLanes = 1 << 16;
 
 struct Geometry {
     int B, T, D, groups, S, strip;    // channel groups, strips of the time axis and their steps
@@ -44,26 +45,50 @@ __device__ __forceinline__ bool place_of(const Geometry& q, const int32_t* __res
     return true;
 }
 
-template <typename E, int VEC> __device__ __forceinline__ void load_f32(const E* at, float (&v)[VEC])
+template <typename E, int VEC> struct Vec {
+    E v[VEC];
+};
+
+// STEPS steps of x or grad_y from t on; those outside the sample as 0.  The
+// loads of a batch are issued together; `first` serves x before t = 0.
+template <typename E, int VEC, int STEPS>
+__device__ __forceinline__ void load_batch(Vec<E, VEC> (&to)[STEPS], const E* __restrict__ in, int64_t time, int t,
+                                           int n)
 {
-    E raw[VEC];
-    load_elems<E, VEC>(at, raw);
+    const E* at = in + t * time;
+    if (t >= 0 && t + STEPS <= n) {
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) v[k] = to_f32(raw[k]);
+        for (int i = 0; i < STEPS; ++i, at += time) load_elems<E, VEC>(at, to[i].v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i, at += time) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) to[i].v[k] = from_f32<E>(0.0f);
+            if (t + i >= 0 && t + i < n) load_elems<E, VEC>(at, to[i].v);
+        }
+    }
 }
 
 // The input at step t < n, from x_first (or 0) where t < 0.
 template <typename E, int K, int VEC>
-__device__ __forceinline__ void input_at(const E* __restrict__ x, const E* __restrict__ first, const Geometry& q,
-                                         const Place& p, int t, float (&v)[VEC])
+__device__ __forceinline__ Vec<E, VEC> input_at(const E* __restrict__ x, const E* __restrict__ first,
+                                                const Geometry& q, const Place& p, int t)
+{
+    Vec<E, VEC> v;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) v.v[k] = from_f32<E>(0.0f);
+    if (t >= 0) {
+        if (t < p.n) load_elems<E, VEC>(x + p.b * q.x_batch + t * q.x_time + p.d, v.v);
+    } else if (first) {
+        load_elems<E, VEC>(first + ((int64_t)p.b * (K - 1) + t + K - 1) * q.D + p.d, v.v);
+    }
+    return v;
+}
+
+template <typename E, int VEC> __device__ __forceinline__ void to_floats(const Vec<E, VEC>& r, float (&v)[VEC])
 {
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) v[k] = 0.0f;
-    if (t >= 0) {
-        if (t < p.n) load_f32<E, VEC>(x + p.b * q.x_batch + t * q.x_time + p.d, v);
-    } else if (first) {
-        load_f32<E, VEC>(first + ((int64_t)p.b * (K - 1) + t + K - 1) * q.D + p.d, v);
-    }
+    for (int k = 0; k < VEC; ++k) v[k] = to_f32(r.v[k]);
 }
 
 template <int K, int VEC>
@@ -96,25 +121,25 @@ __global__ __launch_bounds__(256) void k_conv(const E* __restrict__ x, const flo
     if (!place_of<VEC>(q, length, p)) return;
     if (last && p.s == 0)
         for (int j = 0; j < K - 1; ++j) {
-            float v[VEC];
-            input_at<E, K, VEC>(x, first, q, p, p.n - (K - 1) + j, v);
-            E o[VEC];
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) o[k] = from_f32<E>(v[k]);
-            store_elems<E, VEC>(last + ((int64_t)p.b * (K - 1) + j) * q.D + p.d, o);
+            const Vec<E, VEC> v = input_at<E, K, VEC>(x, first, q, p, p.n - (K - 1) + j);
+            store_elems<E, VEC>(last + ((int64_t)p.b * (K - 1) + j) * q.D + p.d, v.v);
         }
     if (!y) return;
     float tap[K][VEC], b[VEC], win[K - 1 + kAhead][VEC];
+    Vec<E, VEC> raw[kAhead];
+    const E* in = x + p.b * q.x_batch + p.d;
+    load_batch<E, VEC, kAhead>(raw, in, q.x_time, p.t0, p.n);
     load_taps<K, VEC>(w, bias, p.d, tap, b);
 #pragma unroll
-    for (int j = 0; j < K - 1; ++j) input_at<E, K, VEC>(x, first, q, p, p.t0 - (K - 1) + j, win[j]);
+    for (int j = 0; j < K - 1; ++j) to_floats(input_at<E, K, VEC>(x, first, q, p, p.t0 - (K - 1) + j), win[j]);
     E* out = y + ((int64_t)p.b * q.T + p.t0) * q.D + p.d;
     for (int t = p.t0; t < p.t1; t += kAhead) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) input_at<E, K, VEC>(x, first, q, p, t + i, win[K - 1 + i]);
+        for (int i = 0; i < kAhead; ++i) to_floats(raw[i], win[K - 1 + i]);
+        if (t + kAhead < p.t1) load_batch<E, VEC, kAhead>(raw, in, q.x_time, t + kAhead, p.n);
+        const bool whole = t + kAhead <= min(p.n, p.t1);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i, out += q.D) {
-            if (t + i >= p.t1) break;
             E o[VEC];
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
@@ -122,9 +147,9 @@ __global__ __launch_bounds__(256) void k_conv(const E* __restrict__ x, const flo
 #pragma unroll
                 for (int j = 0; j < K; ++j) c = fmaf(tap[j][k], win[i + j][k], c);
                 if (q.flags & LIF_CONV_SILU) c = silu(c, slope);
-                o[k] = from_f32<E>(t + i < p.n ? c : 0.0f);
+                o[k] = from_f32<E>(whole || t + i < p.n ? c : 0.0f);
             }
-            store_elems<E, VEC>(out, o);
+            if (whole || t + i < p.t1) store_elems<E, VEC>(out, o);
         }
 #pragma unroll
         for (int j = 0; j < K - 1; ++j)
@@ -133,9 +158,9 @@ __global__ __launch_bounds__(256) void k_conv(const E* __restrict__ x, const flo
     }
 }
 
-// At step t the window of gradients gc_{t-K+1} .. gc_t gives that of the input
-// K - 1 steps before, sum_j w[j] gc_{t-j}: a strip walks K - 1 steps past its
-// end.  The sums for w and bias go over the strip's own steps.
+// At step t the gradients gc_{t-K+1} .. gc_t give that of the input K - 1 steps
+// before, sum_j w[j] gc_{t-j}: a strip walks K - 1 steps past its end.  The sums
+// for w and bias go over the strip's own steps.
 template <typename E, int K, int VEC>
 __global__ __launch_bounds__(256) void k_conv_back(const E* __restrict__ x, const float* __restrict__ w,
                                                    const float* __restrict__ bias, const int32_t* __restrict__ length,
@@ -144,53 +169,68 @@ __global__ __launch_bounds__(256) void k_conv_back(const E* __restrict__ x, cons
                                                    E* __restrict__ gx, float* __restrict__ g_first,
                                                    float* __restrict__ part)
 {
+    constexpr int U = K <= 4 ? 8 : 4;
     Place p;
     if (!place_of<VEC>(q, length, p)) return;
-    float tap[K][VEC], b[VEC], win[K][VEC], gc[K][VEC], gw[K][VEC], gb[VEC];
+    float tap[K][VEC], b[VEC], win[K - 1 + U][VEC], gc[K - 1 + U][VEC], gw[K][VEC], gb[VEC];
+    Vec<E, VEC> rx[U], rg[U];
+    const E* in = x + p.b * q.x_batch + p.d;
+    const E* gin = gy ? gy + p.b * q.g_batch + p.d : nullptr;
+    const int gn = gy ? p.n : 0;                              // steps that have a gradient
+    load_batch<E, VEC, U>(rx, in, q.x_time, p.t0, p.n);
+    load_batch<E, VEC, U>(rg, gin, q.g_time, p.t0, gn);
     load_taps<K, VEC>(w, bias, p.d, tap, b);
 #pragma unroll
-    for (int j = 0; j < K; ++j)
+    for (int k = 0; k < VEC; ++k) {
+        gb[k] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) win[j][k] = gc[j][k] = gw[j][k] = 0.0f;
+        for (int j = 0; j < K; ++j) gw[j][k] = 0.0f;
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) gb[k] = 0.0f;
+        for (int j = 0; j < K - 1; ++j) gc[j][k] = 0.0f;
+    }
 #pragma unroll
-    for (int j = 0; j < K - 1; ++j) input_at<E, K, VEC>(x, first, q, p, p.t0 - (K - 1) + j, win[j]);
+    for (int j = 0; j < K - 1; ++j) to_floats(input_at<E, K, VEC>(x, first, q, p, p.t0 - (K - 1) + j), win[j]);
     const int from = p.s == 0 ? -(K - 1) : p.t0, end = p.t1 + K - 1;
-    for (int t = p.t0; t < end; ++t) {
-        float g[VEC];
-        input_at<E, K, VEC>(x, first, q, p, t, win[K - 1]);
+    for (int t = p.t0; t < end; t += U) {
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) g[k] = 0.0f;
-        if (gy && t < p.n) load_f32<E, VEC>(gy + p.b * q.g_batch + t * q.g_time + p.d, g);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            float c = b[k], slope = 1.0f;
-#pragma unroll
-            for (int j = 0; j < K; ++j) c = fmaf(tap[j][k], win[j][k], c);
-            if (q.flags & LIF_CONV_SILU) silu(c, slope);
-            gc[K - 1][k] = t < p.n ? g[k] * slope : 0.0f;
+        for (int i = 0; i < U; ++i) {
+            to_floats(rx[i], win[K - 1 + i]);
+            to_floats(rg[i], gc[K - 1 + i]);
         }
-        if (t < p.t1 && t < p.n)
+        if (t + U < end) {
+            load_batch<E, VEC, U>(rx, in, q.x_time, t + U, p.n);
+            load_batch<E, VEC, U>(rg, gin, q.g_time, t + U, gn);
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const bool on = t + i < p.n, own = on && t + i < p.t1;
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
+                float c = b[k], slope = 1.0f;
 #pragma unroll
-                for (int j = 0; j < K; ++j) gw[j][k] = fmaf(gc[K - 1][k], win[j][k], gw[j][k]);
-                gb[k] += gc[K - 1][k];
+                for (int j = 0; j < K; ++j) c = fmaf(tap[j][k], win[i + j][k], c);
+                if (q.flags & LIF_CONV_SILU) silu(c, slope);
+                const float g = on ? gc[K - 1 + i][k] * slope : 0.0f;
+                gc[K - 1 + i][k] = g;
+                if (own) {
+#pragma unroll
+                    for (int j = 0; j < K; ++j) gw[j][k] = fmaf(g, win[i + j][k], gw[j][k]);
+                    gb[k] += g;
+                }
             }
-        const int at = t - (K - 1);
-        if (at >= from) {
+            const int at = t + i - (K - 1);
+            if (at < from || at >= p.t1) continue;
             float v[VEC];
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
                 v[k] = 0.0f;
 #pragma unroll
-                for (int j = 0; j < K; ++j) v[k] = fmaf(tap[j][k], gc[K - 1 - j][k], v[k]);
+                for (int j = 0; j < K; ++j) v[k] = fmaf(tap[j][k], gc[K - 1 + i - j][k], v[k]);
             }
             const int j = at - (p.n - (K - 1));
             if (grad_last && j >= 0 && j < K - 1) {
                 float l[VEC];
-                load_f32<float, VEC>(grad_last + ((int64_t)p.b * (K - 1) + j) * q.D + p.d, l);
+                load_elems<float, VEC>(grad_last + ((int64_t)p.b * (K - 1) + j) * q.D + p.d, l);
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) v[k] += l[k];
             }
@@ -206,7 +246,7 @@ __global__ __launch_bounds__(256) void k_conv_back(const E* __restrict__ x, cons
 #pragma unroll
         for (int j = 0; j < K - 1; ++j)
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) win[j][k] = win[j + 1][k], gc[j][k] = gc[j + 1][k];
+            for (int k = 0; k < VEC; ++k) win[j][k] = win[U + j][k], gc[j][k] = gc[U + j][k];
     }
     if (part) {
         float* to = part + ((int64_t)p.b * q.S + p.s) * (K + 1) * q.D + p.d;
@@ -299,11 +339,13 @@ Geometry geometry_of(const lif_conv_params& p, int strip)
     return q;
 }
 
-// Steps of a strip.  A launch has fewer than 2^32 threads.
+// Steps of a strip: shorter ones where there would be few lanes.  A launch has
+// fewer than 2^32 threads.
 int strip_of(const lif_conv_params& p)
 {
     const int64_t lanes = (int64_t)p.B * ((p.D + vec_of(p) - 1) / vec_of(p));
-    int strip = 64;
+    int strip = kMaxStrip;
+    while (strip > kMinStrip && lanes * ((p.T + strip - 1) / strip) < kStripLanes) strip /= 2;
     while (lanes * ((p.T + strip - 1) / strip) >= ((int64_t)1 << 31)) strip *= 2;
     return strip;
 }
