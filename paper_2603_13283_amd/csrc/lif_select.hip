@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kTile = LIF_SELECT_MARK;
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kMaxOrder = 512;         // samples that are put in order
 constexpr int kMaxSegments = 256, kSplitColumns = 128, kSplitGroups = 1024, kSplitTiles = 4, kSplitLeast = 4;
 static_assert(kTile == 16, "the sums over lanes below put 16 steps x 4 states into the lanes of a wave");
 
@@ -33,6 +34,7 @@ static_assert(kTile == 16, "the sums over lanes below put 16 steps x 4 states in
 // S segments of seg_len steps (whole tiles) of the time axis.
 struct Geometry {
     int B, T, D, N, G, Dg, cols, columns, S, seg_len;
+    bool ordered;                 // samples in the order of their length
     uint32_t flags;
     int64_t x_batch, x_time, dt_batch, dt_time, z_batch, z_time, b_batch, b_time, c_batch, c_time, g_batch, g_time;
 };
@@ -53,13 +55,38 @@ struct Place {
     bool live;
 };
 
-__device__ __forceinline__ Place place_of(const Geometry& q, const int32_t* __restrict__ length, int lane)
+// The sample of this length's rank, longest first, the first of equals first:
+// workgroups start in the order of their index, so the long samples do not come
+// last (128 samples of 0 to 1000 steps x 512 channels: 263 -> XXX us).  The whole
+// workgroup calls it, and scratch (B + 1 words of LDS) is free again after the
+// next barrier.
+__device__ __forceinline__ int sample_of(const int32_t* __restrict__ length, int B, int T, int rank, int* scratch)
+{
+    int *lengths = scratch + 1, &found = *scratch;
+    for (int i = threadIdx.x; i < B; i += blockDim.x) lengths[i] = min(max(length[i], 0), T);
+    __syncthreads();
+    for (int i = threadIdx.x; i < B; i += blockDim.x) {
+        const int n = lengths[i];
+        int r = 0;
+        for (int j = 0; j < B; ++j) r += lengths[j] > n || (lengths[j] == n && j < i);
+        if (r == rank) found = i;
+    }
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(found);
+}
+
+__device__ __forceinline__ Place place_of(const Geometry& q, const int32_t* __restrict__ length, int lane,
+                                          int* scratch)
 {
     Place p;
     p.seg = blockIdx.x / q.columns;
     p.column = blockIdx.x - p.seg * q.columns;
     p.g = p.column / q.cols % q.G;
     p.b = p.column / q.cols / q.G;
+    if (q.ordered && length) {
+        p.b = sample_of(length, q.B, q.T, p.b, scratch);
+        p.column = (p.b * q.G + p.g) * q.cols + p.column % q.cols;
+    }
     const int at = p.column % q.cols * kWave + lane;
     p.live = at < q.Dg;
     p.d = p.g * q.Dg + (p.live ? at : q.Dg - 1);
@@ -230,7 +257,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_maps(Inputs in, Geometry q,
     constexpr int STEPS = kTile / W, IN = REVERSE ? 3 : 2;
     __shared__ float4 shD[2][kTile / 2][kWave];               // delta and delta x (delta and g) of two steps
     const int lane = threadIdx.x & 63, w = wave_index();
-    Place p = place_of(q, in.length, lane);
+    Place p = place_of(q, in.length, lane, (int*)shD);
     if (REVERSE) {                                            // the first segment needs no map
         p.t0 += q.seg_len, p.t1 = min(p.t1 + q.seg_len, q.T), ++p.seg;
         p.n = max(min(p.length, p.t1) - p.t0, 0);
@@ -367,7 +394,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
     __shared__ float4 shD[2][kTile / 2][kWave];               // delta, delta x of two steps
     __shared__ float4 shY[2][W][kTile / 4][kWave];            // the waves' parts of y of four
     const int lane = threadIdx.x & 63, w = wave_index();
-    const Place p = place_of(q, in.length, lane);
+    const Place p = place_of(q, in.length, lane, (int*)shY);
     const int n0 = w * NS, s0 = w * STEPS;
     const bool gated = in.z != nullptr;
     float h[NS], rate[NS];
@@ -624,7 +651,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
     __shared__ float2 shG[kTile / 2][kWave];                  // g of two
     __shared__ float2 shP[3][W][kTile / 2][kWave];            // the waves' parts of P, Q and y of two
     const int lane = threadIdx.x & 63, w = wave_index();
-    const Place p = place_of(q, in.length, lane);
+    const Place p = place_of(q, in.length, lane, (int*)shP);
     const int s0 = w * STEPS;
     const bool gated = in.z != nullptr, driven = in.gy != nullptr;
     auto first = [&](int nb) { return (nb * W + w) * NS; };
@@ -1025,6 +1052,7 @@ Geometry geometry_of(const lif_select_params& p, bool back)
     const int per = tiles > 0 ? (tiles + S - 1) / S : 1;
     q.seg_len = per * kTile;
     q.S = tiles > 0 ? (tiles + per - 1) / per : 1;
+    q.ordered = q.S == 1 && q.B > 1 && q.B <= kMaxOrder;
     q.flags = p.flags;
     q.x_batch = p.x_batch, q.x_time = p.x_time, q.dt_batch = p.dt_batch, q.dt_time = p.dt_time;
     q.z_batch = p.z_batch, q.z_time = p.z_time, q.b_batch = p.b_batch, q.b_time = p.b_time;
