@@ -26,7 +26,13 @@ namespace {
 constexpr int kTile = LIF_SELECT_MARK;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kMaxOrder = 512;         // samples that are put in order
-constexpr int kMaxSegments = 256, kSplitColumns = 128, kSplitGroups = 1024, kSplitTiles = 4, kSplitLeast = 4;
+// The time axis is cut into segments where there are at most kSplitColumns
+// columns, into as many as give kSplitWaves waves and at least kSplitTiles tiles
+// each; kSplitLeast segments pay for reading the inputs twice.  In us, cut and
+// not: 8 columns of 65521 steps 302 and 5700, 128 of 1000 (training, 8 states)
+// 185 and 370, 32 of 1000 33 and 118; 192 of 2048 220 and 190.  2 x 4096 x 1024
+// x 16, training: 287 us with 4096 waves, 329 with 8192.
+constexpr int kMaxSegments = 256, kSplitColumns = 128, kSplitWaves = 4096, kSplitTiles = 4, kSplitLeast = 4;
 static_assert(kTile == 16, "the sums over lanes below put 16 steps x 4 states into the lanes of a wave");
 
 // What a call works on.  Columns of 64 channels: column c is sample
@@ -57,7 +63,7 @@ struct Place {
 
 // The sample of this length's rank, longest first, the first of equals first:
 // workgroups start in the order of their index, so the long samples do not come
-// last (128 samples of 0 to 1000 steps x 512 channels: 263 -> XXX us).  The whole
+// last (128 samples of 0 to 1000 steps x 512 channels: 263 -> 200 us).  The whole
 // workgroup calls it, and scratch (B + 1 words of LDS) is free again after the
 // next barrier.
 __device__ __forceinline__ int sample_of(const int32_t* __restrict__ length, int B, int T, int rank, int* scratch)
@@ -938,20 +944,23 @@ __global__ __launch_bounds__(256) void k_select_sums(Geometry q, const int32_t* 
         }
         return;
     }
-    const int64_t at = (int64_t)(blockIdx.x - bc_blocks) * 256 + threadIdx.x;
-    if (at < states) {
-        float s = 0.0f;
+    // 64 of the sums to a workgroup, a contiguous quarter of the rows to a wave
+    __shared__ float sh[4][kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t at = (int64_t)(blockIdx.x - bc_blocks) * kWave + lane, rows = (int64_t)q.S * q.B;
+    const float* from = at < states ? partA + at : partS + (at - states);
+    const int64_t per = at < states ? states : 2 * (int64_t)q.D;
+    float s = 0.0f;
+    if (at < states + 2 * q.D)
 #pragma unroll 8
-        for (int64_t i = 0; i < (int64_t)q.S * q.B; ++i) s += partA[i * states + at];
-        gA[at] = s;
-    } else if (at < states + 2 * q.D) {
-        const int64_t i = at - states;                        // skip's, then dt_bias'
-        float s = 0.0f;
-#pragma unroll 8
-        for (int64_t j = 0; j < (int64_t)q.S * q.B; ++j) s += partS[j * 2 * q.D + i];
-        float* to = i < q.D ? g_skip : g_bias;
-        if (to) to[i < q.D ? i : i - q.D] = s;
-    }
+        for (int64_t i = rows * w / 4; i < rows * (w + 1) / 4; ++i) s += from[i * per];
+    sh[w][lane] = s;
+    __syncthreads();
+    if (w != 0 || at >= states + 2 * q.D) return;
+    s = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
+    const int64_t i = at - states;                            // skip's, then dt_bias'
+    float* to = at < states ? gA : i < q.D ? g_skip : g_bias;
+    if (to) to[at < states ? at : i < q.D ? i : i - q.D] = s;
 }
 
 // ---------------------------------------------------------------------------
@@ -1031,35 +1040,6 @@ int check_select(const lif_select_params* p)
     return LIF_OK;
 }
 
-// Segments of the time axis: see the rule.
-int segments_of(const lif_select_params& p, int columns, bool back)
-{
-    const int tiles = (p.T + kTile - 1) / kTile;
-    if (columns > kSplitColumns) return 1;
-    int S = 1;
-    while (S < kMaxSegments && columns * S * 2 <= kSplitGroups && tiles >= S * 2 * kSplitTiles) S *= 2;
-    return S < kSplitLeast ? 1 : S;
-}
-
-Geometry geometry_of(const lif_select_params& p, bool back)
-{
-    Geometry q;
-    q.B = p.B, q.T = p.T, q.D = p.D, q.N = p.N, q.G = p.G;
-    q.Dg = p.D / p.G;
-    q.cols = (q.Dg + kWave - 1) / kWave;
-    q.columns = q.B * q.G * q.cols;
-    const int tiles = (q.T + kTile - 1) / kTile, S = segments_of(p, q.columns, back);
-    const int per = tiles > 0 ? (tiles + S - 1) / S : 1;
-    q.seg_len = per * kTile;
-    q.S = tiles > 0 ? (tiles + per - 1) / per : 1;
-    q.ordered = q.S == 1 && q.B > 1 && q.B <= kMaxOrder;
-    q.flags = p.flags;
-    q.x_batch = p.x_batch, q.x_time = p.x_time, q.dt_batch = p.dt_batch, q.dt_time = p.dt_time;
-    q.z_batch = p.z_batch, q.z_time = p.z_time, q.b_batch = p.b_batch, q.b_time = p.b_time;
-    q.c_batch = p.c_batch, q.c_time = p.c_time, q.g_batch = p.g_batch, q.g_time = p.g_time;
-    return q;
-}
-
 template <int V> struct Int { static constexpr int value = V; };
 
 // Calls fn(states of a wave, waves) with types that carry them: the fewest
@@ -1074,6 +1054,43 @@ template <typename Fn> void with_waves(int N, Fn&& fn)
     else fn(Int<8>(), Int<8>());
 }
 
+int waves_of(int N)
+{
+    int waves = 0;
+    with_waves(N, [&](auto, auto w) { waves = decltype(w)::value; });
+    return waves;
+}
+
+// Segments of the time axis, by the rule above.
+int segments_of(const lif_select_params& p, int columns)
+{
+    const int tiles = (p.T + kTile - 1) / kTile;
+    if (columns > kSplitColumns) return 1;
+    int S = 1;
+    const int waves = waves_of(p.N);
+    while (S < kMaxSegments && columns * S * 2 * waves <= kSplitWaves && tiles >= S * 2 * kSplitTiles) S *= 2;
+    return S < kSplitLeast ? 1 : S;
+}
+
+Geometry geometry_of(const lif_select_params& p)
+{
+    Geometry q;
+    q.B = p.B, q.T = p.T, q.D = p.D, q.N = p.N, q.G = p.G;
+    q.Dg = p.D / p.G;
+    q.cols = (q.Dg + kWave - 1) / kWave;
+    q.columns = q.B * q.G * q.cols;
+    const int tiles = (q.T + kTile - 1) / kTile, S = segments_of(p, q.columns);
+    const int per = tiles > 0 ? (tiles + S - 1) / S : 1;
+    q.seg_len = per * kTile;
+    q.S = tiles > 0 ? (tiles + per - 1) / per : 1;
+    q.ordered = q.S == 1 && q.B > 1 && q.B <= kMaxOrder;
+    q.flags = p.flags;
+    q.x_batch = p.x_batch, q.x_time = p.x_time, q.dt_batch = p.dt_batch, q.dt_time = p.dt_time;
+    q.z_batch = p.z_batch, q.z_time = p.z_time, q.b_batch = p.b_batch, q.b_time = p.b_time;
+    q.c_batch = p.c_batch, q.c_time = p.c_time, q.g_batch = p.g_batch, q.g_time = p.g_time;
+    return q;
+}
+
 size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
 
 // Segments' sums and ends (none where there is one segment).
@@ -1086,7 +1103,7 @@ struct BackLayout {
 
 BackLayout back_layout(const lif_select_params& p)
 {
-    const Geometry q = geometry_of(p, true);
+    const Geometry q = geometry_of(p);
     BackLayout l;
     const size_t bc = align16(sizeof(float) * q.B * q.G * q.cols * (size_t)q.T * q.N);
     l.partB = 0;
@@ -1106,7 +1123,7 @@ extern "C" size_t lif_selective_scan_workspace_size(const lif_select_params* p)
 {
     using namespace lif;
     if (check_select(p) != LIF_OK) return 0;
-    const Geometry q = geometry_of(*p, false);
+    const Geometry q = geometry_of(*p);
     return sums_size(q) + ends_size(q);
 }
 
@@ -1124,7 +1141,7 @@ extern "C" int lif_selective_scan(const void* x, const void* dt, const float* A,
     if (need > 0 && (!ws || (uintptr_t)ws % 16)) return LIF_ERR_ARG;
     if (ws_bytes < need) return LIF_ERR_WORKSPACE;
     if (p->B == 0) return LIF_OK;
-    const Geometry q = geometry_of(*p, false);
+    const Geometry q = geometry_of(*p);
     const Inputs in = {x, dt, Bm, C, z, nullptr, A, skip, dt_bias, length};
     float *sums = (float*)ws, *ends = (float*)((char*)ws + sums_size(q));
     with_dtype(p->dtype, [&](auto e) {
@@ -1166,11 +1183,11 @@ extern "C" int lif_selective_scan_backward(const void* x, const void* dt, const 
     const BackLayout l = back_layout(*p);
     if (l.total > 0 && (!ws || (uintptr_t)ws % 16)) return LIF_ERR_ARG;
     if (ws_bytes < l.total) return LIF_ERR_WORKSPACE;
-    const Geometry q = geometry_of(*p, true);
+    const Geometry q = geometry_of(*p);
     const Inputs in = {x, dt, Bm, C, z, grad_y, A, skip, dt_bias, length};
     const int64_t bc = (int64_t)q.B * q.G * q.T * q.N;
     const int64_t bc_blocks = bc > ((int64_t)1 << 30) ? 1 << 22 : (bc + 255) / 256;
-    const int64_t blocks = bc_blocks + ((int64_t)q.D * (q.N + 2) + 255) / 256;
+    const int64_t blocks = bc_blocks + ((int64_t)q.D * (q.N + 2) + kWave - 1) / kWave;
     with_dtype(p->dtype, [&](auto e) {
         using E = decltype(e);
         char* base = (char*)ws;
@@ -1215,7 +1232,7 @@ extern "C" int lif_selective_step(const void* x, const void* dt, const float* A,
     if (p->T != 1 || n_slots < 0 || (!slot && n_slots < p->B)) return LIF_ERR_ARG;
     if (p->B == 0) return LIF_OK;
     if (!x || !dt || !A || !Bm || !C || !y || (n_slots > 0 && !state)) return LIF_ERR_ARG;
-    const Geometry q = geometry_of(*p, false);
+    const Geometry q = geometry_of(*p);
     const Inputs in = {x, dt, Bm, C, z, nullptr, A, skip, dt_bias, nullptr};
     int L = 1;
     while (4 * L < q.N) L *= 2;
