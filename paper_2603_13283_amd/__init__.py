@@ -1381,49 +1381,42 @@ class SelectiveGrads:
     h_first: "object"        # float32 [B, D, N]: grad_last of the piece before
 
 
-class _Selective:
-    """The inputs of the selective scan and of its step, checked."""
-
-    def __init__(self, torch, x, dt, A, B, C, D, z, dt_bias, dims):
-        lead = dims - 1                                  # axes before the channels
-        if x.dim() != dims or not x.is_cuda:
-            raise ValueError("x must be a CUDA tensor " + ("[B, T, D]" if dims == 3 else "[B, D]"))
-        self.dev, self.code, self.type = x.device, _dtype_code("x", x), x.dtype
-        self.steps, self.width = x.shape[:lead], x.shape[-1]
-        self.x = _rows_of("x", x, x.shape, x.dtype, self.dev)
-        self.dt = _rows_of("dt", dt, x.shape, x.dtype, self.dev)
-        self.z = None if z is None else _rows_of("z", z, x.shape, x.dtype, self.dev)
-        if A.dim() != 2:
-            raise ValueError("A must be [D, N]")
-        self.N = A.shape[1]
-        self.A = _expect("A", A, (self.width, self.N), torch.float32, self.dev)
-        self.G = B.shape[lead] if B.dim() == dims + 1 else 1
-        shape = (*self.steps, self.G, self.N) if B.dim() == dims + 1 else (*self.steps, self.N)
-        self.B, self.C = self._states("B", B, shape), self._states("C", C, shape)
-        self.D = _expect("D", D, (self.width,), torch.float32, self.dev)
-        self.dt_bias = _expect("dt_bias", dt_bias, (self.width,), torch.float32, self.dev)
-        _int32(*x.shape, self.N, self.G)
-
-    def _states(self, name, t, shape):
-        """B or C: the last two axes (groups, states) contiguous."""
-        t = _rows_of(name, t, shape, self.type, self.dev)
-        if len(shape) > len(self.steps) + 1 and shape[-2] > 1 and t.stride(-2) != shape[-1]:
-            t = t.contiguous()
-        return t
-
-    def params(self, softplus, grad=None):
-        def strides(t):
-            if t is None:
-                return 0, 0
-            return t.stride()[:2] if len(self.steps) == 2 else (t.stride(0), 0)
-        B, T = self.steps if len(self.steps) == 2 else (self.steps[0], 1)
-        pairs = (s for t in (self.x, self.dt, self.z, self.B, self.C, grad) for s in strides(t))
-        return lif_select_params(B, T, self.width, self.N, self.G, self.code, LIF_SELECT_SOFTPLUS if softplus else 0,
-                                 0, *pairs)
-
-    def pointers(self):
-        return (self.x.data_ptr(), self.dt.data_ptr(), self.A.data_ptr(), self.B.data_ptr(), self.C.data_ptr(),
-                _ptr(self.D), _ptr(self.z), _ptr(self.dt_bias))
+def _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, dims, grad_y=None):
+    """The checked inputs of the selective scan (dims 3) or its step (dims 2):
+    (pointers of x, dt, A, B, C, D, z, dt_bias and grad_y, the parameters, what
+    has to live until the call is made).  Written out, for these calls are
+    short."""
+    if x.dim() != dims or not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor " + ("[B, T, D]" if dims == 3 else "[B, D]"))
+    code, shape, kind, dev = _dtype_code("x", x), x.shape, x.dtype, x.device
+    W, lead = shape[-1], shape[:-1]
+    x, dt = _rows_of("x", x, shape, kind, dev), _rows_of("dt", dt, shape, kind, dev)
+    if z is not None:
+        z = _rows_of("z", z, shape, kind, dev)
+    if grad_y is not None:
+        grad_y = _rows_of("grad_y", grad_y, shape, kind, dev)
+    if A.dim() != 2:
+        raise ValueError("A must be [D, N]")
+    N = A.shape[1]
+    A = _expect("A", A, (W, N), torch.float32, dev)
+    G = B.shape[-2] if B.dim() == dims + 1 else 1
+    states = (*lead, G, N) if B.dim() == dims + 1 else (*lead, N)
+    B, C = _rows_of("B", B, states, kind, dev), _rows_of("C", C, states, kind, dev)
+    if G > 1:                                            # the last two axes (groups, states) contiguous
+        B = B if B.stride(-2) == N else B.contiguous()
+        C = C if C.stride(-2) == N else C.contiguous()
+    D = _expect("D", D, (W,), torch.float32, dev)
+    dt_bias = _expect("dt_bias", dt_bias, (W,), torch.float32, dev)
+    if max(*shape, N, G) > 0x7fffffff:
+        _int32(*shape, N, G)
+    nb, T = lead if dims == 3 else (lead[0], 1)
+    second = (lambda s: s[1]) if dims == 3 else (lambda s: 0)
+    sx, sd, sb, sc = x.stride(), dt.stride(), B.stride(), C.stride()
+    sz, sg = (0, 0) if z is None else z.stride(), (0, 0) if grad_y is None else grad_y.stride()
+    p = lif_select_params(nb, T, W, N, G, code, LIF_SELECT_SOFTPLUS if softplus else 0, 0, sx[0], second(sx), sd[0],
+                          second(sd), sz[0], second(sz), sb[0], second(sb), sc[0], second(sc), sg[0], second(sg))
+    return (x.data_ptr(), dt.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(D), _ptr(z), _ptr(dt_bias),
+            _ptr(grad_y)), p, (x, dt, A, B, C, D, z, dt_bias, grad_y)
 
 
 def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, length=None, h_first=None, softplus: bool = True,
@@ -1435,16 +1428,15 @@ def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, length=None, h_
     only."""
     torch = _torch()
     with _on(torch, x, stream):
-        a = _Selective(torch, x, dt, A, B, C, D, z, dt_bias, 3)
-        (nb, T), W, N, dev = a.steps, a.width, a.N, a.dev
+        ptrs, p, held = _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, 3)
+        nb, T, W, N, dev = p.B, p.T, p.D, p.N, x.device
         length = _expect("length", length, (nb,), torch.int32, dev)
         h_first = _expect("h_first", h_first, (nb, W, N), torch.float32, dev)
-        p = a.params(softplus)
-        y = torch.empty((nb, T, W), dtype=a.type, device=dev) if outputs else None
+        y = torch.empty((nb, T, W), dtype=x.dtype, device=dev) if outputs else None
         last = torch.empty((nb, W, N), dtype=torch.float32, device=dev)
         mk = torch.empty((nb, -(-T // LIF_SELECT_MARK), N, W), dtype=torch.float32, device=dev) if marks else None
-        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, a.G, a.code, False), ws, dev)
-        rc = lif_selective_scan(*a.pointers(), _ptr(length), _ptr(h_first), ctypes.byref(p), _ptr(y), last.data_ptr(),
+        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, p.G, p.dtype, False), ws, dev)
+        rc = lif_selective_scan(*ptrs[:8], _ptr(length), _ptr(h_first), ctypes.byref(p), _ptr(y), last.data_ptr(),
                                 _ptr(mk), wp, wn, _raw_stream(torch, dev, stream))
         _check("lif_selective_scan", rc)
         return SelectiveOut(y, last, mk)
@@ -1457,23 +1449,23 @@ def selective_scan_backward(x, dt, A, B, C, marks, grad_y=None, D=None, z=None, 
     [B, D, N])."""
     torch = _torch()
     with _on(torch, x, stream):
-        a = _Selective(torch, x, dt, A, B, C, D, z, dt_bias, 3)
-        (nb, T), W, N, dev = a.steps, a.width, a.N, a.dev
+        ptrs, p, held = _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, 3, grad_y)
+        nb, T, W, N, dev = p.B, p.T, p.D, p.N, x.device
         length = _expect("length", length, (nb,), torch.int32, dev)
         marks = _expect("marks", marks, (nb, -(-T // LIF_SELECT_MARK), N, W), torch.float32, dev)
         if marks is None:
             raise ValueError("the backward pass needs the forward's marks (selective_scan with marks=True)")
-        if grad_y is not None:
-            grad_y = _rows_of("grad_y", grad_y, x.shape, a.type, dev)
         grad_last = _expect("grad_last", grad_last, (nb, W, N), torch.float32, dev)
-        p = a.params(softplus, grad_y)
-        full = lambda t, like, kind: None if like is None else torch.empty(t, dtype=kind, device=dev)   # noqa: E731
-        g = SelectiveGrads(*(full((nb, T, W), x, a.type) for _ in range(2)), full((W, N), A, torch.float32),
-                           full(B.shape, B, a.type), full(C.shape, C, a.type), full((W,), D, torch.float32),
-                           full((nb, T, W), z, a.type), full((W,), dt_bias, torch.float32),
-                           full((nb, W, N), x, torch.float32))
-        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, a.G, a.code, True), ws, dev)
-        rc = lif_selective_scan_backward(*a.pointers(), _ptr(length), marks.data_ptr(), _ptr(grad_y), _ptr(grad_last),
+        f32, kind, empty = torch.float32, x.dtype, torch.empty
+        g = SelectiveGrads(empty((nb, T, W), dtype=kind, device=dev), empty((nb, T, W), dtype=kind, device=dev),
+                           empty((W, N), dtype=f32, device=dev), empty(B.shape, dtype=kind, device=dev),
+                           empty(C.shape, dtype=kind, device=dev),
+                           None if D is None else empty((W,), dtype=f32, device=dev),
+                           None if z is None else empty((nb, T, W), dtype=kind, device=dev),
+                           None if dt_bias is None else empty((W,), dtype=f32, device=dev),
+                           empty((nb, W, N), dtype=f32, device=dev))
+        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, p.G, p.dtype, True), ws, dev)
+        rc = lif_selective_scan_backward(*ptrs[:8], _ptr(length), marks.data_ptr(), ptrs[8], _ptr(grad_last),
                                          ctypes.byref(p), g.x.data_ptr(), g.dt.data_ptr(), g.A.data_ptr(),
                                          g.B.data_ptr(), g.C.data_ptr(), _ptr(g.D), _ptr(g.z), _ptr(g.dt_bias),
                                          g.h_first.data_ptr(), wp, wn, _raw_stream(torch, dev, stream))
@@ -1489,13 +1481,12 @@ def selective_step(x, dt, A, B, C, state, slot=None, D=None, z=None, dt_bias=Non
     Returns y [B, D]."""
     torch = _torch()
     with _on(torch, x, stream):
-        a = _Selective(torch, x, dt, A, B, C, D, z, dt_bias, 2)
-        nb, dev = a.steps[0], a.dev
-        state = _pool(torch, state, (a.width, a.N), torch.float32, dev)
+        ptrs, p, held = _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, 2)
+        nb, dev = p.B, x.device
+        state = _pool(torch, state, (p.D, p.N), torch.float32, dev)
         slot = _expect("slot", slot, (nb,), torch.int32, dev)
-        p = a.params(softplus)
-        y = torch.empty((nb, a.width), dtype=a.type, device=dev)
-        rc = lif_selective_step(*a.pointers(), _ptr(slot), state.data_ptr(), state.shape[0], ctypes.byref(p),
+        y = torch.empty((nb, p.D), dtype=x.dtype, device=dev)
+        rc = lif_selective_step(*ptrs[:8], _ptr(slot), state.data_ptr(), state.shape[0], ctypes.byref(p),
                                 y.data_ptr(), _raw_stream(torch, dev, stream))
         _check("lif_selective_step", rc)
         return y

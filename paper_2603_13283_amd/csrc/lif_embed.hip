@@ -18,6 +18,7 @@ namespace {
 constexpr int kMaxBits = 10;          // of a digit
 constexpr int kChunks = 256;          // workgroups that count and hand out
 constexpr int kSortWaves = 4;
+constexpr int kFew = 4096, kSmallWaves = 16;      // places that one workgroup sorts
 constexpr int kAhead = 8;             // rows whose loads are in flight at once
 constexpr int kJoinWaves = 8;
 constexpr int kSeek = 16;             // lanes that look for a row of the table together
@@ -189,6 +190,73 @@ __global__ __launch_bounds__(kSortWaves* kWave) void k_hand_out(const int32_t* _
             keys_out[at] = k;
             places_out[at] = places ? places[i] : (uint32_t)i;
         }
+    }
+}
+
+// Few places: one workgroup sorts them in LDS, 8 bits of the key at a time, in
+// the same way (1000 places, 200 rows of the table 23.5 -> 17.7 us a call, 50000 rows
+// 31.7 -> 18.5; at 8000 places no gain).
+__global__ __launch_bounds__(kSmallWaves* kWave) void k_sort_few(const int32_t* __restrict__ token,
+                                                                 const int32_t* __restrict__ length, Sort q,
+                                                                 uint32_t* __restrict__ keys_out,
+                                                                 uint32_t* __restrict__ places_out)
+{
+    constexpr int kThreads = kSmallWaves * kWave, kBins = 256;
+    __shared__ uint32_t key[2][kFew], next[kSmallWaves][kBins], waves[kBins / kWave];
+    __shared__ uint16_t place[2][kFew];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (int i = threadIdx.x; i < q.R; i += kThreads) {
+        key[0][i] = key_of(token, length, q.T, q.V, i);
+        place[0][i] = (uint16_t)i;
+    }
+    const int part = (q.R + kThreads - 1) / kThreads * kWave, from = min(w * part, q.R), end = min(from + part, q.R);
+    int now = 0;
+    for (int shift = 0; shift < q.bits; shift += 8, now ^= 1) {
+        for (int i = threadIdx.x; i < kSmallWaves * kBins; i += kThreads) (&next[0][0])[i] = 0;
+        __syncthreads();
+        for (int i = from + lane; i < end; i += kWave) atomicAdd(&next[w][(key[now][i] >> shift) & (kBins - 1)], 1u);
+        __syncthreads();
+        uint32_t count = 0, before = 0;
+        if (threadIdx.x < kBins) {
+            for (int j = 0; j < kSmallWaves; ++j) count += next[j][threadIdx.x];
+            before = count;
+            for (int o = 1; o < kWave; o <<= 1) {
+                const uint32_t v = __shfl_up(before, o);
+                if (lane >= o) before += v;
+            }
+            if (lane == kWave - 1) waves[w] = before;
+        }
+        __syncthreads();
+        if (threadIdx.x < kBins) {
+            before -= count;
+            for (int j = 0; j < w; ++j) before += waves[j];
+            for (int j = 0; j < kSmallWaves; ++j) {
+                const uint32_t v = next[j][threadIdx.x];
+                next[j][threadIdx.x] = before;
+                before += v;
+            }
+        }
+        __syncthreads();
+        const bool last = shift + 8 >= q.bits;
+        for (int i0 = 0; i0 < part; i0 += kWave) {
+            const bool on = from + i0 + lane < end;
+            const int i = on ? from + i0 + lane : 0;
+            const uint32_t k = key[now][i], digit = (k >> shift) & (kBins - 1);
+            uint64_t same = __ballot(on);
+            for (int b = 0; b < 8; ++b) {
+                const uint64_t set = __ballot((digit >> b) & 1);
+                same &= (digit >> b) & 1 ? set : ~set;
+            }
+            const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+            uint32_t at = 0;
+            if (on) at = next[w][digit] + rank;
+            __syncthreads();
+            if (on && rank == 0) next[w][digit] = at + __popcll(same);
+            __syncthreads();
+            if (on && last) keys_out[at] = k, places_out[at] = place[now][i];
+            if (on && !last) key[now ^ 1][at] = k, place[now ^ 1][at] = place[now][i];
+        }
+        __syncthreads();
     }
 }
 
@@ -387,6 +455,7 @@ Plan plan_of(const lif_embed_params& p)
     s.scale = (float)p.scale;
     int64_t piece = ((int64_t)R * s.columns + 4095) / 4096;
     if (piece < 16) piece = 16;
+    if (R <= 64) piece = 64;                                        // one piece: no join
     if (piece > 1 << 30) piece = 1 << 30;
     s.piece = (int)piece;
     s.pieces = (int)(((int64_t)R + piece - 1) / piece);
@@ -467,7 +536,15 @@ extern "C" int lif_embed_backward(const int32_t* token, const void* grad, const 
     char* base = (char*)ws;
     uint32_t *count = (uint32_t*)(base + q.count), *total = (uint32_t*)(base + q.total);
     const uint32_t *keys = nullptr, *places = nullptr;
-    for (int i = 0; i < q.passes; ++i) {
+    if (R <= kFew) {
+        int bits = 1;
+        while ((1 << bits) <= p->V) ++bits;
+        const Sort o = {(int)R, p->T, p->V, 0, 0, bits, 0};
+        uint32_t *ko = (uint32_t*)(base + q.keys[0]), *po = (uint32_t*)(base + q.places[0]);
+        TIMED_LAUNCH("embed_sort_few", k_sort_few, dim3(1), dim3(kSmallWaves * kWave), 0, s, token, length, o, ko, po);
+        keys = ko, places = po;
+    }
+    for (int i = 0; i < q.passes && R > kFew; ++i) {
         const Sort o = {(int)R, p->T, p->V, q.chunk, q.chunks, q.bits, i * q.bits};
         uint32_t *ko = (uint32_t*)(base + q.keys[i & 1]), *po = (uint32_t*)(base + q.places[i & 1]);
         const int bins = 1 << q.bits;
@@ -488,7 +565,8 @@ extern "C" int lif_embed_backward(const int32_t* token, const void* grad, const 
             constexpr int VEC = decltype(vec)::value;
             TIMED_LAUNCH("embed_sums", (k_embed_sums<E, VEC>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256),
                          0, s, (const E*)grad, keys, places, q.s, sum_blocks, grad_W, part);
-            TIMED_LAUNCH("embed_join", (k_embed_join<VEC>), dim3((unsigned)items), dim3(kJoinWaves * kWave), 0, s,
+            if (q.s.pieces > 1)
+                TIMED_LAUNCH("embed_join", (k_embed_join<VEC>), dim3((unsigned)items), dim3(kJoinWaves * kWave), 0, s,
                          keys, q.s, part, grad_W);
         };
         if (vec_of(p->D) == 4) with(Int<4>());

@@ -13,7 +13,8 @@ pytestmark = pytest.mark.gpu
 TYPES = ("f32", "bf16", "f16")
 # (samples, places, rows, width)
 SHAPES = [(1, 1, 1, 1), (2, 3, 2, 3), (3, 70, 5, 4), (1, 65, 700, 20), (4, 333, 50, 33), (2, 1500, 1023, 7),
-          (2, 900, 1024, 130), (1, 4000, 5000, 9), (5, 200, 300, 257), (1, 20000, 2, 5), (1, 300, 1 << 21, 1)]
+          (2, 900, 1024, 130), (1, 4000, 5000, 9), (5, 200, 300, 257), (1, 20000, 2, 5), (1, 300, 1 << 21, 1),
+          (1, 64, 9, 4), (1, 4096, 70000, 6), (2, 2048, 3, 8), (1, 4097, 255, 3)]
 
 
 @pytest.fixture(scope="module")

@@ -169,6 +169,9 @@ class Stand:
     def contiguous(self):
         return self
 
+    def data_ptr(self):
+        return 0x1000
+
     def is_contiguous(self):
         return self.whole
 
