@@ -390,7 +390,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void k_embed_join(const uint32_t
 #pragma unroll
     for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
     const int to = (int)((int64_t)n * (w + 1) / kJoinWaves);
-#pragma unroll 4
+#pragma unroll 8
     for (int j = (int)((int64_t)n * w / kJoinWaves); j < to; ++j) {
         float v[VEC];
         load_elems<float, VEC>(part + ((int64_t)(piece + j) * 2 + (j == 0)) * q.D + d, v);
@@ -453,7 +453,7 @@ Plan plan_of(const lif_embed_params& p)
     s.columns = (p.D + kWave * vec_of(p.D) - 1) / (kWave * vec_of(p.D));
     s.g_batch = p.g_batch, s.g_time = p.g_time;
     s.scale = (float)p.scale;
-    int64_t piece = ((int64_t)R * s.columns + 4095) / 4096;
+    int64_t piece = ((int64_t)R * s.columns + 8191) / 8192;
     if (piece < 16) piece = 16;
     if (R <= 64) piece = 64;                                        // one piece: no join
     if (piece > 1 << 30) piece = 1 << 30;
