@@ -226,6 +226,15 @@ template <typename E, int NS, int STEPS, int IN, int NB = 1> struct Raw {
     Bits<E> bc[2][NB][NS];
 };
 
+// A lane's offset as a value of the place where it is used: otherwise its
+// widening to 64 bits moves out of the loop, and every address is added up by
+// the vector unit instead of in the access.
+__device__ __forceinline__ uint32_t here(uint32_t offset)
+{
+    asm volatile("" : "+v"(offset));
+    return offset;
+}
+
 // One input along time: the scalar address of a step's row, and bytes from one
 // row to the next; a lane's channel is an offset to it.
 struct Rows {
@@ -242,6 +251,7 @@ template <typename E, int STEPS>
 __device__ __forceinline__ void load_rows(Bits<E> (&v)[STEPS], const Rows& r, uint32_t offset, int there = STEPS)
 {
     const char* at = r.at;
+    offset = here(offset);
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
         v[i].load((const E*)(at + offset));
@@ -485,9 +495,10 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
     auto put_marks = [&](int t0) {
         if (marks && p.live) {
             char* to = (char*)(marks + (((int64_t)p.b * ((q.T + kTile - 1) / kTile) + (p.t0 + t0) / kTile) * q.N + n0) * q.D);
+            const uint32_t o = here(offset4);
 #pragma unroll
             for (int k = 0; k < NS; ++k, to += q.D * (int64_t)4)
-                if (n0 + k < q.N) *(float*)(to + offset4) = h[k];
+                if (n0 + k < q.N) *(float*)(to + o) = h[k];
         }
     };
     auto read_out = [&](const Raw<E, NS, STEPS, 3>& r, const float4 (*from)[kTile / 4][kWave], int t0, int cnt) {
@@ -506,10 +517,12 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
             v[i] = gated ? v[i] * s : v[i];
         }
         char* to = (char*)(y + ((int64_t)p.b * q.T + p.t0 + t0 + s0) * q.D);
-        if (p.live)
+        if (p.live) {
+            const uint32_t o = here(offset);
 #pragma unroll
             for (int i = 0; i < STEPS; ++i, to += q.D * (int64_t)sizeof(E))
-                if (s0 + i < cnt) *(E*)(to + offset) = from_f32<E>(v[i]);
+                if (s0 + i < cnt) *(E*)(to + o) = from_f32<E>(v[i]);
+        }
     };
 
     __syncthreads();
@@ -687,7 +700,6 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         for (int nb = 0; nb < NB; ++nb)
             carry(mu[nb], rate[nb], sums, ends, q, p, first(nb), segments - 1, segments - 1 - p.seg, -1);
     const float bias = in.bias ? in.bias[p.d] : 0.0f, skip = in.skip ? in.skip[p.d] : 0.0f;
-    const uint32_t offset = p.d * (uint32_t)sizeof(E), offset4 = p.d * 4u;
     float g_skip = 0.0f, g_bias = 0.0f;
 
     // A tile's raw elements and marks on their way, and what phase A makes of
@@ -698,37 +710,56 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         float x[STEPS], delta[STEPS], slope[STEPS], g[STEPS], z_slope[STEPS];
         float B[NB][NS], C[NB][NS], h0[NB][NS];
     } made;
-    // Where the tile that is loaded next lies.
-    Rows rows[4];
+    // Where the lane's steps of the tile that is loaded next lie, and where their
+    // gradients go: addresses of the lanes, for as scalars they spill the scalar
+    // registers (training, 8 x 2048 x 2048 x 16 bf16: 738 us, this 710).
+    const char *in_at[4], *mark_at;
     const E *Bt, *Ct;
-    const char* mark_at;
+    char* out_at[3];
+    const int64_t steps[4] = {q.x_time * (int64_t)sizeof(E), q.dt_time * (int64_t)sizeof(E),
+                              (gated ? q.z_time : q.x_time) * (int64_t)sizeof(E),
+                              (driven ? q.g_time : q.x_time) * (int64_t)sizeof(E)};
+    const int64_t out_step = q.D * (int64_t)sizeof(E), mark_step = q.D * (int64_t)4;
     auto find = [&](int t0, int left) {
         const int t = p.t0 + t0 + min(s0, left - 1), tb = p.t0 + t0 + min(lane & 15, left - 1);
-        rows[0] = rows_of<E>(in.x, q.x_batch, q.x_time, p.b, t);
-        rows[1] = rows_of<E>(in.dt, q.dt_batch, q.dt_time, p.b, t);
-        rows[2] = gated ? rows_of<E>(in.z, q.z_batch, q.z_time, p.b, t) : rows[0];
-        rows[3] = driven ? rows_of<E>(in.gy, q.g_batch, q.g_time, p.b, t) : rows[0];
+        auto lane_at = [&](const void* v, int64_t batch, int64_t time) {
+            return (const char*)((const E*)v + p.b * batch + t * time + p.d);
+        };
+        in_at[0] = lane_at(in.x, q.x_batch, q.x_time);
+        in_at[1] = lane_at(in.dt, q.dt_batch, q.dt_time);
+        in_at[2] = gated ? lane_at(in.z, q.z_batch, q.z_time) : in_at[0];
+        in_at[3] = driven ? lane_at(in.gy, q.g_batch, q.g_time) : in_at[0];
         Bt = (const E*)in.Bm + p.b * q.b_batch + tb * q.b_time + (int64_t)p.g * q.N;
         Ct = (const E*)in.C + p.b * q.c_batch + tb * q.c_time + (int64_t)p.g * q.N;
-        mark_at = (const char*)(marks + ((int64_t)p.b * ((q.T + kTile - 1) / kTile) + (p.t0 + t0) / kTile) * q.N * q.D);
+        mark_at = (const char*)(marks + ((int64_t)p.b * ((q.T + kTile - 1) / kTile) + (p.t0 + t0) / kTile) * q.N * q.D +
+                                p.d);
+        const int64_t row = ((int64_t)p.b * q.T + p.t0 + t0 + s0) * q.D + p.d;
+        out_at[0] = (char*)(out.gx + row), out_at[1] = (char*)(out.gdt + row), out_at[2] = (char*)(out.gz + row);
     };
-    auto load = [&](int left) {
+    auto load = [&](auto whole, int left) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_rows(raw.v[i], rows[i], offset, left - s0);
+        for (int j = 0; j < 4; ++j) {
+            const char* from = in_at[j];
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                raw.v[j][i].load((const E*)from);
+                if (decltype(whole)::value || s0 + i + 1 < left) from += steps[j];     // the last one again past the end
+            }
+        }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
                 raw.bc[0][nb][k].load(Bt + at[nb][k]);
                 raw.bc[1][nb][k].load(Ct + at[nb][k]);
-                mark[nb][k] = *(const float*)(mark_at + at[nb][k] * (q.D * (int64_t)4) + offset4);
+                mark[nb][k] = *(const float*)(mark_at + at[nb][k] * mark_step);
             }
     };
     auto back = [&] {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) rows[i].at -= kTile * rows[i].step;
+        for (int j = 0; j < 4; ++j) in_at[j] -= kTile * steps[j];
         Bt -= kTile * q.b_time, Ct -= kTile * q.c_time;
-        mark_at -= q.N * (q.D * (int64_t)4);
+        mark_at -= q.N * mark_step;
     };
     auto ready = [&](int left) {
 #pragma unroll
@@ -830,7 +861,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                 (row & 1 ? out.partC : out.partB)[((int64_t)p.column * q.T + p.t0 + t0 + i) * q.N + n] = s;
         }
     };
-    auto write = [&](int t0, int cnt) {
+    auto write = [&](int cnt) {
         float P[STEPS], Q[STEPS], Y[STEPS];
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) P[i] = Q[i] = 0.0f, Y[i] = skip * made.x[i];
@@ -842,9 +873,6 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                 const float2 c = shP[2][j][(s0 + i) / 2][lane];
                 P[i] += a.x, P[i + 1] += a.y, Q[i] += b.x, Q[i + 1] += b.y, Y[i] += c.x, Y[i + 1] += c.y;
             }
-        const int64_t row = (((int64_t)p.b * q.T + p.t0 + t0 + s0) * q.D) * (int64_t)sizeof(E);
-        char *gx = (char*)out.gx + row, *gdt = (char*)out.gdt + row, *gz = (char*)out.gz + row;
-        const int64_t next = q.D * (int64_t)sizeof(E);
         float g_r[STEPS];
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
@@ -853,14 +881,16 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
             g_skip = on ? fmaf(made.g[i], made.x[i], g_skip) : g_skip;
             g_bias = on ? g_bias + g_r[i] : g_bias;
         }
-        if (!p.live) return;
+        if (p.live)
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-            if (s0 + i < cnt) {
-                *(E*)(gx + i * next + offset) = from_f32<E>(fmaf(made.delta[i], Q[i], skip * made.g[i]));
-                *(E*)(gdt + i * next + offset) = from_f32<E>(g_r[i]);
-                if (gated) *(E*)(gz + i * next + offset) = from_f32<E>(Y[i] * made.z_slope[i]);
-            }
+            for (int i = 0; i < STEPS; ++i)
+                if (s0 + i < cnt) {
+                    *(E*)(out_at[0] + i * out_step) = from_f32<E>(fmaf(made.delta[i], Q[i], skip * made.g[i]));
+                    *(E*)(out_at[1] + i * out_step) = from_f32<E>(g_r[i]);
+                    if (gated) *(E*)(out_at[2] + i * out_step) = from_f32<E>(Y[i] * made.z_slope[i]);
+                }
+#pragma unroll
+        for (int j = 0; j < 3; ++j) out_at[j] -= kTile * out_step;
     };
 
     __syncthreads();
@@ -873,30 +903,30 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
     int t0 = p.n / kTile * kTile;                             // after the last whole tile
     if (t0 < p.n) {
         find(t0, p.n - t0);
-        load(p.n - t0);
+        load(std::false_type(), p.n - t0);
         ready(p.n - t0);
         __syncthreads();
         walk(std::false_type(), t0, p.n - t0);
         __syncthreads();
-        write(t0, p.n - t0);
+        write(p.n - t0);
     }
     if (t0 > 0) {
         t0 -= kTile;
         find(t0, kTile);
-        load(kTile);
+        load(std::true_type(), kTile);
         ready(kTile);
         if (t0 > 0) back();
-        load(kTile);                                          // (the first tile again where there is none before it)
+        load(std::true_type(), kTile);                                          // (the first tile again where there is none before it)
         for (;;) {
             __syncthreads();
             walk(std::true_type(), t0, kTile);
             __syncthreads();
-            write(t0, kTile);
+            write(kTile);
             if (t0 == 0) break;
             t0 -= kTile;
             ready(kTile);
             if (t0 > 0) back();
-            load(kTile);
+            load(std::true_type(), kTile);
         }
     }
     if (p.live) {
