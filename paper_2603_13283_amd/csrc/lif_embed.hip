@@ -124,8 +124,10 @@ __global__ __launch_bounds__(kSortWaves* kWave) void k_hand_out(const int32_t* _
                                                                 const uint32_t* __restrict__ count,
                                                                 const uint32_t* __restrict__ total,
                                                                 uint32_t* __restrict__ keys_out,
-                                                                uint32_t* __restrict__ places_out)
+                                                                uint32_t* __restrict__ places_out,
+                                                                uint32_t* __restrict__ list)
 {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *list = 0;
     constexpr int kThreads = kSortWaves * kWave, kPer = (1 << kMaxBits) / kThreads;
     __shared__ uint32_t next[kSortWaves][1 << kMaxBits], waves[kSortWaves];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, bins = 1 << q.bits, c = blockIdx.x;
@@ -199,8 +201,10 @@ __global__ __launch_bounds__(kSortWaves* kWave) void k_hand_out(const int32_t* _
 __global__ __launch_bounds__(kSmallWaves* kWave) void k_sort_few(const int32_t* __restrict__ token,
                                                                  const int32_t* __restrict__ length, Sort q,
                                                                  uint32_t* __restrict__ keys_out,
-                                                                 uint32_t* __restrict__ places_out)
+                                                                 uint32_t* __restrict__ places_out,
+                                                                 uint32_t* __restrict__ list)
 {
+    if (threadIdx.x == 0) *list = 0;
     constexpr int kThreads = kSmallWaves * kWave, kBins = 256;
     __shared__ uint32_t key[2][kFew], next[kSmallWaves][kBins], waves[kBins / kWave];
     __shared__ uint16_t place[2][kFew];
@@ -291,12 +295,14 @@ __device__ __forceinline__ bool named(const uint32_t* __restrict__ keys, int R, 
 // A wave sums the rows of a piece of the sorted list for 64 VEC columns.  A run
 // that lies within the piece goes to the table's gradient, one that comes from
 // the piece before to part[piece][0], one that begins here and goes on to
-// part[piece][1].  The workgroups from sum_blocks on clear the rows that no
-// token names.
+// part[piece][1], and the piece to the list of those whose run is joined later
+// (list[0] counts them; their order there is open, and without effect).  The
+// workgroups from sum_blocks on clear the rows that no token names.
 template <typename E, int VEC>
 __global__ __launch_bounds__(256) void k_embed_sums(const E* __restrict__ grad, const uint32_t* __restrict__ keys,
                                                     const uint32_t* __restrict__ places, Sums q, int64_t sum_blocks,
-                                                    float* __restrict__ gW, float* __restrict__ part)
+                                                    float* __restrict__ gW, float* __restrict__ part,
+                                                    uint32_t* __restrict__ list)
 {
     const int lane = threadIdx.x & 63;
     if (blockIdx.x >= sum_blocks) {
@@ -358,56 +364,64 @@ __global__ __launch_bounds__(256) void k_embed_sums(const E* __restrict__ grad, 
         }
     }
     const bool on = end < q.R && uniform(keys[end]) == run;        // it goes on in the next piece
-    if (open) put(part + (int64_t)piece * 2 * q.D, 1.0f);
-    else if (on) put(part + ((int64_t)piece * 2 + 1) * q.D, 1.0f);
-    else put(gW + (int64_t)run * q.D, q.scale);
+    if (open) {
+        put(part + (int64_t)piece * 2 * q.D, 1.0f);
+    } else if (on) {
+        put(part + ((int64_t)piece * 2 + 1) * q.D, 1.0f);
+        if (column == 0 && lane == 0) list[1 + atomicAdd(list, 1u)] = piece;
+    } else {
+        put(gW + (int64_t)run * q.D, q.scale);
+    }
 }
 
-// A workgroup takes a piece and 64 VEC columns: if a run begins in the piece and
-// goes on, its parts are added up, each wave's share of the pieces in order.
+// A workgroup takes 64 VEC columns of a listed piece: the parts of the run that
+// begins there are added up, each wave's share of the pieces in order.
 template <int VEC>
 __global__ __launch_bounds__(kJoinWaves* kWave) void k_embed_join(const uint32_t* __restrict__ keys, Sums q,
                                                                   const float* __restrict__ part,
+                                                                  const uint32_t* __restrict__ list,
                                                                   float* __restrict__ gW)
 {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     __shared__ float sh[kJoinWaves][kWave * VEC];
-    const int piece = blockIdx.x / q.columns, column = blockIdx.x % q.columns;
-    const int64_t first = (int64_t)piece * q.piece, end = first + q.piece;
-    if (end >= q.R) return;
-    const uint32_t run = keys[end];
-    if (run >= (uint32_t)q.V || keys[end - 1] != run || (first > 0 && keys[first - 1] == run)) return;
-    int n = 2;                                                      // pieces that the run lies in
-    for (;;) {
-        const int64_t next = ((int64_t)piece + n + lane) * q.piece;
-        const uint64_t on = __ballot(next < q.R && keys[min(next, (int64_t)q.R - 1)] == run);
-        const int more = ~on ? __builtin_ctzll(~on) : kWave;
-        n += more;
-        if (more < kWave) break;
-    }
-    const int at = (column * kWave + lane) * VEC, d = min(at, q.D - VEC);
-    float acc[VEC];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t items = (int64_t)*list * q.columns;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int piece = (int)list[1 + item / q.columns], column = (int)(item % q.columns);
+        const uint32_t run = keys[(int64_t)(piece + 1) * q.piece];
+        int n = 2;                                                  // pieces that the run lies in
+        for (;;) {
+            const int64_t next = ((int64_t)piece + n + lane) * q.piece;
+            const uint64_t on = __ballot(next < q.R && keys[min(next, (int64_t)q.R - 1)] == run);
+            const int more = ~on ? __builtin_ctzll(~on) : kWave;
+            n += more;
+            if (more < kWave) break;
+        }
+        const int at = (column * kWave + lane) * VEC, d = min(at, q.D - VEC);
+        float acc[VEC];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
-    const int to = (int)((int64_t)n * (w + 1) / kJoinWaves);
+        for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
+        const int to = (int)((int64_t)n * (w + 1) / kJoinWaves);
 #pragma unroll 8
-    for (int j = (int)((int64_t)n * w / kJoinWaves); j < to; ++j) {
-        float v[VEC];
-        load_elems<float, VEC>(part + ((int64_t)(piece + j) * 2 + (j == 0)) * q.D + d, v);
+        for (int j = (int)((int64_t)n * w / kJoinWaves); j < to; ++j) {
+            float v[VEC];
+            load_elems<float, VEC>(part + ((int64_t)(piece + j) * 2 + (j == 0)) * q.D + d, v);
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) acc[k] += v[k];
+            for (int k = 0; k < VEC; ++k) acc[k] += v[k];
+        }
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) sh[w][lane * VEC + k] = acc[k];
+        __syncthreads();
+        if (w == 0 && at < q.D) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                acc[k] = 0.0f;
+                for (int j = 0; j < kJoinWaves; ++j) acc[k] += sh[j][lane * VEC + k];
+                acc[k] *= q.scale;
+            }
+            store_elems<float, VEC>(gW + (int64_t)run * q.D + d, acc);
+        }
+        __syncthreads();
     }
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) sh[w][lane * VEC + k] = acc[k];
-    __syncthreads();
-    if (w != 0 || at >= q.D) return;
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-        acc[k] = 0.0f;
-        for (int j = 0; j < kJoinWaves; ++j) acc[k] += sh[j][lane * VEC + k];
-        acc[k] *= q.scale;
-    }
-    store_elems<float, VEC>(gW + (int64_t)run * q.D + d, acc);
 }
 
 // No token at all: the gradient is 0.
@@ -434,7 +448,7 @@ template <int V> struct Int { static constexpr int value = V; };
 struct Plan {
     int passes, bits, chunk, chunks;
     Sums s;
-    size_t keys[2], places[2], count, total, part, end;
+    size_t keys[2], places[2], count, total, part, list, end;
 };
 
 Plan plan_of(const lif_embed_params& p)
@@ -473,6 +487,7 @@ Plan plan_of(const lif_embed_params& p)
     q.count = take(sizeof(uint32_t) * ((size_t)q.chunks << q.bits));
     q.total = take(sizeof(uint32_t) << q.bits);
     q.part = take(sizeof(float) * 2 * (size_t)s.pieces * p.D);
+    q.list = take(sizeof(uint32_t) * (1 + (size_t)s.pieces));
     q.end = R > 0 ? at : 0;
     return q;
 }
@@ -536,12 +551,14 @@ extern "C" int lif_embed_backward(const int32_t* token, const void* grad, const 
     char* base = (char*)ws;
     uint32_t *count = (uint32_t*)(base + q.count), *total = (uint32_t*)(base + q.total);
     const uint32_t *keys = nullptr, *places = nullptr;
+    uint32_t* list = (uint32_t*)(base + q.list);
     if (R <= kFew) {
         int bits = 1;
         while ((1 << bits) <= p->V) ++bits;
         const Sort o = {(int)R, p->T, p->V, 0, 0, bits, 0};
         uint32_t *ko = (uint32_t*)(base + q.keys[0]), *po = (uint32_t*)(base + q.places[0]);
-        TIMED_LAUNCH("embed_sort_few", k_sort_few, dim3(1), dim3(kSmallWaves * kWave), 0, s, token, length, o, ko, po);
+        TIMED_LAUNCH("embed_sort_few", k_sort_few, dim3(1), dim3(kSmallWaves * kWave), 0, s, token, length, o, ko, po,
+                     list);
         keys = ko, places = po;
     }
     for (int i = 0; i < q.passes && R > kFew; ++i) {
@@ -553,7 +570,7 @@ extern "C" int lif_embed_backward(const int32_t* token, const void* grad, const 
         TIMED_LAUNCH("embed_chunks", k_chunk_sums, dim3((bins + kWave - 1) / kWave), dim3(16 * kWave), 0, s, count,
                      q.chunks, bins, total);
         TIMED_LAUNCH("embed_sort", k_hand_out, dim3(q.chunks), dim3(kSortWaves * kWave), 0, s, token, length, keys,
-                     places, o, count, total, ko, po);
+                     places, o, count, total, ko, po, list);
         keys = ko, places = po;
     }
     const int64_t items = (int64_t)q.s.pieces * q.s.columns, sum_blocks = (items + 3) / 4;
@@ -564,10 +581,10 @@ extern "C" int lif_embed_backward(const int32_t* token, const void* grad, const 
         auto with = [&](auto vec) {
             constexpr int VEC = decltype(vec)::value;
             TIMED_LAUNCH("embed_sums", (k_embed_sums<E, VEC>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256),
-                         0, s, (const E*)grad, keys, places, q.s, sum_blocks, grad_W, part);
+                         0, s, (const E*)grad, keys, places, q.s, sum_blocks, grad_W, part, list);
             if (q.s.pieces > 1)
-                TIMED_LAUNCH("embed_join", (k_embed_join<VEC>), dim3((unsigned)items), dim3(kJoinWaves * kWave), 0, s,
-                         keys, q.s, part, grad_W);
+                TIMED_LAUNCH("embed_join", (k_embed_join<VEC>), dim3((unsigned)(items < 1024 ? items : 1024)),
+                             dim3(kJoinWaves * kWave), 0, s, keys, q.s, part, list, grad_W);
         };
         if (vec_of(p->D) == 4) with(Int<4>());
         else with(Int<1>());
