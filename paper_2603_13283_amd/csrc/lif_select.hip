@@ -4,15 +4,16 @@
 //
 // A lane holds one channel, a wave NS of its N states, a workgroup of W waves
 // 64 channels with all their states, in registers for as long as it walks along
-// time.  So B_t and C_t are the same for all lanes, and what a state needs of
-// its step (delta, delta x) is made once per channel: a tile of LIF_SELECT_MARK
-// steps goes through three phases, with a barrier between them:
+// time.  What a state needs of its step (delta, delta x) is made once per channel
+// and shared through LDS: a tile of LIF_SELECT_MARK steps goes through three
+// phases:
 //   A  the waves share out the tile's steps and put delta and delta x of their
-//      steps into LDS, and B and C as float32
+//      steps into LDS
 //   B  each wave runs all steps of the tile on its states and leaves its part
 //      of sum_i C_t[i] h_t[i] in LDS
 //   C  the waves share out the steps again, add up the parts, and write y
-// Raw inputs of the next tile are loaded while a tile is worked on.
+// B_t and C_t are the same for all lanes: those of the tile's 16 steps lie in the
+// 16 lanes of each row, where the vector unit's row broadcast reads them.
 #include "lif_host.hpp"
 #include "lif_types.hpp"
 #include "lif_walk.hpp"
@@ -26,6 +27,7 @@ namespace {
 constexpr int kTile = LIF_SELECT_MARK;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kMaxOrder = 512;         // samples that are put in order
+constexpr int kStepPairs = 8192;       // workgroups of a step from which they take two streams at a time
 // The time axis is cut into segments where there are at most kSplitColumns
 // columns, into as many as give kSplitWaves waves and at least kSplitTiles tiles
 // each; kSplitLeast segments pay for reading the inputs twice.  In us, cut and
@@ -392,9 +394,11 @@ __device__ __forceinline__ void carry(float (&c)[NS], const float (&rate)[NS], c
     }
 }
 
-// A scan is bound by the vector unit and by the rate at which a wave issues
-// instructions (5.5 a state and step: a product and 2^x for the decay, three
-// and a half for state and readout; 60 a channel and step in phases A and C).
+// A scan is bound by the vector unit, 59 to 77 % busy (5.5 instructions a state
+// and step: a product and 2^x for the decay, three and a half for state and
+// readout; 60 a channel and step in phases A and C; an FMA takes 2.9 cycles of a
+// SIMD, one with a broadcast 4.7, 2^x 8.5): 128 x 1000 x 512 x 16 bf16, ragged,
+// 200 us; 8 x 2048 x 2048 x 16 bf16 with marks 230 us, 308 MB at 1.3 TB/s.
 // The phases of three tiles run in one stretch between two barriers (B of a
 // tile, C of the one before, A of the one after), so that the waits of one are
 // filled by the others.  Only whole tiles go through that loop: it has no
@@ -655,12 +659,13 @@ template <typename E> struct BackOut {
     E *gx, *gdt, *gz;
     float *partB, *partC;         // [B G cols][T][N] sums over a column's channels
     float *partA;                 // [S B][D][N]
-    float *partS;                 // [B][2][D]: of skip, of dt_bias
+    float *partS;                 // [S B][2][D]: of skip, of dt_bias
     float *g_first;
 };
 
-// Bound by instructions: 14 a state and step, 4 more for the sums over channels
-// that grad_B and grad_C are, 100 a channel and step in phases A and C.  A wave
+// Bound by the vector unit, 76 % busy: 14 instructions a state and step, 4 more
+// for the sums over channels that grad_B and grad_C are, 100 a channel and step in
+// phases A and C; 8 x 2048 x 2048 x 16 bf16 530 us, 477 MB at 0.9 TB/s.  A wave
 // holds two states at a time, NB times over, so that a tile's states and decays
 // fit its registers.  Between two barriers a tile is walked; then its results
 // are written while the tile before it is made ready and the one before that is
@@ -959,7 +964,8 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
 }
 
 // Adds up the columns' parts of grad_B and grad_C, and the samples' parts of
-// the parameters' gradients, in the order of columns, segments and samples.
+// the parameters' gradients, in the order of columns, segments and samples: 8 x
+// 2048 x 2048 x 16 16 us, 69 MB at 4.3 TB/s.
 template <typename E>
 __global__ __launch_bounds__(256) void k_select_sums(Geometry q, const int32_t* __restrict__ length,
                                                      const float* __restrict__ partB, const float* __restrict__ partC,
@@ -1008,58 +1014,80 @@ __global__ __launch_bounds__(256) void k_select_sums(Geometry q, const int32_t* 
 }
 
 // ---------------------------------------------------------------------------
-// One step.  L lanes share a channel (L a power of two with 4 L >= N), each
-// holds four of its states.
+// One step.  2^shift lanes share a channel, each holds four of its states.
 // ---------------------------------------------------------------------------
 
-template <typename E>
+// The second axis of the grid goes over streams, U at a time, whose loads are in
+// flight together.  Bound by memory: 256 x 4096 x 16 states 28 us, 142 MB at 5.1
+// TB/s; 400 x 3999 x 33 f32 199 us a call with two streams, 238 with one, 235
+// with four.
+template <typename E, int U>
 __global__ __launch_bounds__(256) void k_select_step(Inputs in, const int32_t* __restrict__ slot,
-                                                     float* __restrict__ state, int n_slots, Geometry q, int L,
+                                                     float* __restrict__ state, int n_slots, Geometry q, int shift,
                                                      E* __restrict__ y)
 {
-    const int64_t at = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    const bool live = at < (int64_t)q.B * q.D;
-    const int64_t c = live ? at : (int64_t)q.B * q.D - 1;
-    const int b = (int)(c / q.D), d = (int)(c - (int64_t)b * q.D), g = d / q.Dg, n0 = threadIdx.x % L * 4;
-    const int row = slot ? slot[b] : b;
-    const bool there = row >= 0 && row < n_slots;
-    const float xv = to_f32(((const E*)in.x)[b * q.x_batch + d]);
-    float slope;
-    const float r = to_f32(((const E*)in.dt)[b * q.dt_batch + d]) + (in.bias ? in.bias[d] : 0.0f);
-    const float delta = step_length(q, r, slope), u = delta * xv;
-    float sum = 0.0f;
-    if (there && n0 < q.N) {
-        const E* Bt = (const E*)in.Bm + b * q.b_batch + g * q.N + n0;
-        const E* Ct = (const E*)in.C + b * q.c_batch + g * q.N + n0;
-        float* h = state + ((int64_t)row * q.D + d) * q.N + n0;
-        const float* A = in.A + (int64_t)d * q.N + n0;
-        auto run = [&](float a, float hv, E bv, E cv) {
-            const float v = fmaf(__builtin_amdgcn_exp2f(delta * rate_of(a)), hv, u * to_f32(bv));
-            sum = fmaf(to_f32(cv), v, sum);
-            return v;
-        };
-        if (n0 + 4 <= q.N) {
-            float av[4], hv[4];
-            E bv[4], cv[4];
-            load_elems<float, 4>(A, av);
-            load_elems<float, 4>(h, hv);
-            load_elems<E, 4>(Bt, bv);
-            load_elems<E, 4>(Ct, cv);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) hv[k] = run(av[k], hv[k], bv[k], cv[k]);
-            if (live) store_elems<float, 4>(h, hv);
+    const int at = blockIdx.x * blockDim.x + threadIdx.x, d = at >> shift, n0 = (at & ((1 << shift) - 1)) * 4;
+    const bool live = d < q.D, wide = n0 + 4 <= q.N;
+    const int c = live ? d : q.D - 1, g = q.G > 1 ? c / q.Dg : 0, left = q.N - n0;
+    const float bias = in.bias ? in.bias[c] : 0.0f, skip = in.skip ? in.skip[c] : 0.0f;
+    // four of a channel's or group's values, those past N as 0
+    auto load = [&](auto& v, const auto* from) {
+        if (wide) {
+            load_elems<std::remove_cv_t<std::remove_reference_t<decltype(*from)>>, 4>(from, v);
         } else {
-            for (int k = 0; n0 + k < q.N; ++k) {
-                const float v = run(A[k], h[k], Bt[k], Ct[k]);
-                if (live) h[k] = v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[k] = 0;
+                if (k < left) v[k] = from[k];
             }
         }
-    }
-    for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor(sum, o);
-    if (live && n0 == 0) {
-        sum = fmaf(in.skip ? in.skip[d] : 0.0f, xv, sum);
-        if (in.z) sum *= silu(to_f32(((const E*)in.z)[b * q.z_batch + d]), slope);
-        y[c] = from_f32<E>(there ? sum : 0.0f);
+    };
+    float A[4];
+    load(A, in.A + (int64_t)c * q.N + n0);
+    for (int b0 = blockIdx.y * U; b0 < q.B; b0 += gridDim.y * U) {
+        float h[U][4], z[U];
+        E xv[U], dt[U], Bt[U][4], Ct[U][4];
+        int row[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int b = min(b0 + j, q.B - 1);
+            row[j] = slot ? slot[b] : b;
+            if (row[j] < 0 || row[j] >= n_slots || b0 + j >= q.B) row[j] = -1;
+            xv[j] = ((const E*)in.x + b * q.x_batch)[c];
+            dt[j] = ((const E*)in.dt + b * q.dt_batch)[c];
+            z[j] = in.z ? to_f32(((const E*)in.z + b * q.z_batch)[c]) : 0.0f;
+            load(Bt[j], (const E*)in.Bm + b * q.b_batch + g * q.N + n0);
+            load(Ct[j], (const E*)in.C + b * q.c_batch + g * q.N + n0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) h[j][k] = 0.0f;
+            if (row[j] >= 0) load(h[j], state + ((int64_t)row[j] * q.D + c) * q.N + n0);
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            float slope, sum = 0.0f;
+            const float x = to_f32(xv[j]), delta = step_length(q, to_f32(dt[j]) + bias, slope), u = delta * x;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                h[j][k] = fmaf(__builtin_amdgcn_exp2f(delta * (A[k] * kLog2e)), h[j][k], u * to_f32(Bt[j][k]));
+                sum = k < left ? fmaf(to_f32(Ct[j][k]), h[j][k], sum) : sum;
+            }
+            if (live && row[j] >= 0) {
+                float* to = state + ((int64_t)row[j] * q.D + c) * q.N + n0;
+                if (wide) {
+                    store_elems<float, 4>(to, h[j]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < left) to[k] = h[j][k];
+                }
+            }
+            for (int o = 1 << shift >> 1; o; o >>= 1) sum += __shfl_xor(sum, o);
+            if (live && n0 == 0 && b0 + j < q.B) {
+                sum = fmaf(skip, x, sum);
+                if (in.z) sum *= silu(z[j], slope);
+                (y + (int64_t)(b0 + j) * q.D)[c] = from_f32<E>(row[j] >= 0 ? sum : 0.0f);
+            }
+        }
     }
 }
 
@@ -1275,13 +1303,23 @@ extern "C" int lif_selective_step(const void* x, const void* dt, const float* A,
     if (!x || !dt || !A || !Bm || !C || !y || (n_slots > 0 && !state)) return LIF_ERR_ARG;
     const Geometry q = geometry_of(*p);
     const Inputs in = {x, dt, Bm, C, z, nullptr, A, skip, dt_bias, nullptr};
-    int L = 1;
-    while (4 * L < q.N) L *= 2;
-    const int64_t blocks = ((int64_t)q.B * q.D + 256 / L - 1) / (256 / L);
+    int shift = 0;                                            // 2^shift lanes to a channel
+    while (4 << shift < q.N) ++shift;
+    const int64_t lanes = (int64_t)q.D << shift;
+    const unsigned threads = lanes >= 256 ? 256 : (unsigned)((lanes + kWave - 1) / kWave * kWave);
+    // two streams at a time where that still fills the chip
+    const unsigned blocks = (unsigned)((lanes + threads - 1) / threads);
+    const bool pairs = (int64_t)blocks * q.B >= kStepPairs;
+    const int rows = pairs ? (q.B + 1) / 2 : q.B;
+    const dim3 grid(blocks, rows < 65535 ? rows : 65535);
     with_dtype(p->dtype, [&](auto e) {
         using E = decltype(e);
-        TIMED_LAUNCH("select_step", (k_select_step<E>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, in,
-                     slot, state, n_slots, q, L, (E*)y);
+        if (pairs)
+            TIMED_LAUNCH("select_step", (k_select_step<E, 2>), grid, dim3(threads), 0, (hipStream_t)stream, in, slot,
+                         state, n_slots, q, shift, (E*)y);
+        else
+            TIMED_LAUNCH("select_step", (k_select_step<E, 1>), grid, dim3(threads), 0, (hipStream_t)stream, in, slot,
+                         state, n_slots, q, shift, (E*)y);
     });
     return check_launch();
 }
