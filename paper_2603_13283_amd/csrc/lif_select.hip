@@ -32,7 +32,7 @@ constexpr int kStepPairs = 8192;       // workgroups of a step from which they t
 // columns, into as many as give kSplitWaves waves and at least kSplitTiles tiles
 // each; kSplitLeast segments pay for reading the inputs twice.  In us, cut and
 // not: 8 columns of 65521 steps 302 and 5700, 128 of 1000 (training, 8 states)
-// 185 and 370, 32 of 1000 33 and 118; 192 of 2048 220 and 190.  2 x 4096 x 1024
+// 171 and 370, 32 of 1000 33 and 118; 192 of 2048 220 and 190.  2 x 4096 x 1024
 // x 16, training: 287 us with 4096 waves, 329 with 8192.
 constexpr int kMaxSegments = 256, kSplitColumns = 128, kSplitWaves = 4096, kSplitTiles = 4, kSplitLeast = 4;
 static_assert(kTile == 16, "the sums over lanes below put 16 steps x 4 states into the lanes of a wave");
@@ -1116,11 +1116,13 @@ template <int V> struct Int { static constexpr int value = V; };
 
 // Calls fn(states of a wave, waves) with types that carry them.  Four waves at
 // least share out the steps of a tile, also where fewer hold states: 10 x 2091 x
-// 3069 f16 with one state, training, 650 us (one wave: 1204).
+// 3069 f16 with one state, training, 650 us (one wave: 1204).  Eight waves of one
+// state instead of four of two: 30 x 2283 x 319 x 5 f16 174 -> 146 us; backward the
+// other way, 9 x 1658 x 3230 x 5 631 with four waves, 748 with eight (waves_back).
 template <typename Fn> void with_waves(int N, Fn&& fn)
 {
     if (N <= 4) fn(Int<1>(), Int<4>());
-    else if (N <= 8) fn(Int<2>(), Int<4>());
+    else if (N <= 8) fn(Int<1>(), Int<8>());
     else if (N <= 16) fn(Int<2>(), Int<8>());
     else if (N <= 32) fn(Int<4>(), Int<8>());
     else fn(Int<8>(), Int<8>());
@@ -1134,23 +1136,25 @@ int waves_of(int N)
 }
 
 // Segments of the time axis, by the rule above.
-int segments_of(const lif_select_params& p, int columns)
+int segments_of(const lif_select_params& p, int columns, int waves)
 {
     const int tiles = (p.T + kTile - 1) / kTile;
     if (columns > kSplitColumns) return 1;
-    int S = columns > 0 ? kSplitWaves / (columns * waves_of(p.N)) : 1;
+    int S = columns > 0 ? kSplitWaves / (columns * waves) : 1;
     S = min(min(S, kMaxSegments), tiles / kSplitTiles);
     return S < kSplitLeast ? 1 : S;
 }
 
-Geometry geometry_of(const lif_select_params& p)
+int waves_back(int N) { return N <= 8 ? 4 : 8; }
+
+Geometry geometry_of(const lif_select_params& p, int waves)
 {
     Geometry q;
     q.B = p.B, q.T = p.T, q.D = p.D, q.N = p.N, q.G = p.G;
     q.Dg = p.D / p.G;
     q.cols = (q.Dg + kWave - 1) / kWave;
     q.columns = q.B * q.G * q.cols;
-    const int tiles = (q.T + kTile - 1) / kTile, S = segments_of(p, q.columns);
+    const int tiles = (q.T + kTile - 1) / kTile, S = segments_of(p, q.columns, waves);
     const int per = tiles > 0 ? (tiles + S - 1) / S : 1;
     q.seg_len = per * kTile;
     q.S = tiles > 0 ? (tiles + per - 1) / per : 1;
@@ -1174,7 +1178,7 @@ struct BackLayout {
 
 BackLayout back_layout(const lif_select_params& p)
 {
-    const Geometry q = geometry_of(p);
+    const Geometry q = geometry_of(p, waves_back(p.N));
     BackLayout l;
     const size_t bc = align16(sizeof(float) * q.B * q.G * q.cols * (size_t)q.T * q.N);
     l.partB = 0;
@@ -1194,7 +1198,7 @@ extern "C" size_t lif_selective_scan_workspace_size(const lif_select_params* p)
 {
     using namespace lif;
     if (check_select(p) != LIF_OK) return 0;
-    const Geometry q = geometry_of(*p);
+    const Geometry q = geometry_of(*p, waves_of(p->N));
     return sums_size(q) + ends_size(q);
 }
 
@@ -1212,7 +1216,7 @@ extern "C" int lif_selective_scan(const void* x, const void* dt, const float* A,
     if (need > 0 && (!ws || (uintptr_t)ws % 16)) return LIF_ERR_ARG;
     if (ws_bytes < need) return LIF_ERR_WORKSPACE;
     if (p->B == 0) return LIF_OK;
-    const Geometry q = geometry_of(*p);
+    const Geometry q = geometry_of(*p, waves_of(p->N));
     const Inputs in = {x, dt, Bm, C, z, nullptr, A, skip, dt_bias, length};
     float *sums = (float*)ws, *ends = (float*)((char*)ws + sums_size(q));
     with_dtype(p->dtype, [&](auto e) {
@@ -1254,7 +1258,7 @@ extern "C" int lif_selective_scan_backward(const void* x, const void* dt, const 
     const BackLayout l = back_layout(*p);
     if (l.total > 0 && (!ws || (uintptr_t)ws % 16)) return LIF_ERR_ARG;
     if (ws_bytes < l.total) return LIF_ERR_WORKSPACE;
-    const Geometry q = geometry_of(*p);
+    const Geometry q = geometry_of(*p, waves_back(p->N));
     const Inputs in = {x, dt, Bm, C, z, grad_y, A, skip, dt_bias, length};
     const int64_t bc = (int64_t)q.B * q.G * q.T * q.N;
     const int64_t bc_blocks = bc > ((int64_t)1 << 30) ? 1 << 22 : (bc + 255) / 256;
@@ -1301,7 +1305,7 @@ extern "C" int lif_selective_step(const void* x, const void* dt, const float* A,
     if (p->T != 1 || n_slots < 0 || (!slot && n_slots < p->B)) return LIF_ERR_ARG;
     if (p->B == 0) return LIF_OK;
     if (!x || !dt || !A || !Bm || !C || !y || (n_slots > 0 && !state)) return LIF_ERR_ARG;
-    const Geometry q = geometry_of(*p);
+    const Geometry q = geometry_of(*p, 1);
     const Inputs in = {x, dt, Bm, C, z, nullptr, A, skip, dt_bias, nullptr};
     int shift = 0;                                            // 2^shift lanes to a channel
     while (4 << shift < q.N) ++shift;
