@@ -988,6 +988,11 @@ def _rows_of(name, t, shape, dtype, dev):
     if t.shape != shape or t.dtype != dtype or t.device != dev:
         raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} on {dev}, "
                          f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return _rows(t)
+
+
+def _rows(t):
+    """t, or a copy whose last axis is contiguous."""
     return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
 
 
@@ -1183,6 +1188,19 @@ def distill_top(logits, teacher_logp, teacher_idx, temperature: float = 1.0, tai
 # models over tokens
 # ---------------------------------------------------------------------------
 
+@functools.lru_cache(maxsize=1024)
+def _conv_params(*fields):
+    """A reference to lif_conv_params of these fields (the library only reads
+    them)."""
+    return ctypes.byref(lif_conv_params(*fields))
+
+
+@functools.lru_cache(maxsize=1024)
+def _select_params(*fields):
+    """The same of lif_select_params."""
+    return ctypes.byref(lif_select_params(*fields))
+
+
 @functools.lru_cache(maxsize=256)
 def _embed_ws(B, T, V, D) -> int:
     """lif_embed_backward_workspace_size: it depends on sizes only."""
@@ -1277,7 +1295,7 @@ def _conv_inputs(torch, x, w, bias, dims):
     if x.dim() != dims or not x.is_cuda:
         raise ValueError("x must be a CUDA tensor " + ("[B, T, D]" if dims == 3 else "[B, D]"))
     code, dev, D = _dtype_code("x", x), x.device, x.shape[-1]
-    x = _rows_of("x", x, x.shape, x.dtype, dev)
+    x = _rows(x)
     if w.dim() != 2:
         raise ValueError("w must be [D, K]")
     K = w.shape[1]
@@ -1297,10 +1315,10 @@ def causal_conv(x, w, bias=None, length=None, x_first=None, silu: bool = True, s
         B, T = x.shape[:2]
         length = _expect("length", length, (B,), torch.int32, dev)
         x_first = _expect("x_first", x_first, (B, K - 1, D), x.dtype, dev)
-        p = lif_conv_params(B, T, D, K, code, LIF_CONV_SILU if silu else 0, x.stride(0), x.stride(1), 0, 0)
+        p = _conv_params(B, T, D, K, code, LIF_CONV_SILU if silu else 0, *x.stride()[:2], 0, 0)
         y = torch.empty((B, T, D), dtype=x.dtype, device=dev)
         last = torch.empty((B, max(K - 1, 0), D), dtype=x.dtype, device=dev)
-        rc = lif_causal_conv(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(length), _ptr(x_first), ctypes.byref(p),
+        rc = lif_causal_conv(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(length), _ptr(x_first), p,
                              y.data_ptr(), last.data_ptr(), _raw_stream(torch, dev, stream))
         _check("lif_causal_conv", rc)
         return ConvOut(y, last)
@@ -1319,15 +1337,15 @@ def causal_conv_backward(x, w, grad_y, bias=None, length=None, x_first=None, gra
         grad_last = _expect("grad_last", grad_last, (B, K - 1, D), torch.float32, dev)
         if grad_y is not None:
             grad_y = _rows_of("grad_y", grad_y, x.shape, x.dtype, dev)
-        p = lif_conv_params(B, T, D, K, code, LIF_CONV_SILU if silu else 0, x.stride(0), x.stride(1),
-                            *((0, 0) if grad_y is None else grad_y.stride()[:2]))
+        p = _conv_params(B, T, D, K, code, LIF_CONV_SILU if silu else 0, *x.stride()[:2],
+                         *((0, 0) if grad_y is None else grad_y.stride()[:2]))
         gx = torch.empty((B, T, D), dtype=x.dtype, device=dev)
         gw = torch.empty((D, K), dtype=torch.float32, device=dev)
         gb = None if bias is None else torch.empty(D, dtype=torch.float32, device=dev)
         g0 = torch.empty((B, max(K - 1, 0), D), dtype=torch.float32, device=dev)
         wp, wn, ws = _workspace(torch, _conv_ws(B, T, D, K, code), ws, dev)
         rc = lif_causal_conv_backward(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(length), _ptr(x_first),
-                                      _ptr(grad_y), _ptr(grad_last), ctypes.byref(p), gx.data_ptr(), gw.data_ptr(),
+                                      _ptr(grad_y), _ptr(grad_last), p, gx.data_ptr(), gw.data_ptr(),
                                       _ptr(gb), g0.data_ptr(), wp, wn, _raw_stream(torch, dev, stream))
         _check("lif_causal_conv_backward", rc)
         return ConvGrads(gx, gw, gb, g0)
@@ -1353,10 +1371,10 @@ def causal_conv_step(x, w, state, slot=None, bias=None, silu: bool = True, strea
         B = x.shape[0]
         state = _pool(torch, state, (K - 1, D), x.dtype, dev)
         slot = _expect("slot", slot, (B,), torch.int32, dev)
-        p = lif_conv_params(B, 1, D, K, code, LIF_CONV_SILU if silu else 0, x.stride(0), 0, 0, 0)
+        p = _conv_params(B, 1, D, K, code, LIF_CONV_SILU if silu else 0, x.stride(0), 0, 0, 0)
         y = torch.empty((B, D), dtype=x.dtype, device=dev)
         rc = lif_causal_conv_step(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(slot), state.data_ptr(),
-                                  state.shape[0], ctypes.byref(p), y.data_ptr(), _raw_stream(torch, dev, stream))
+                                  state.shape[0], p, y.data_ptr(), _raw_stream(torch, dev, stream))
         _check("lif_causal_conv_step", rc)
         return y
 
@@ -1383,14 +1401,14 @@ class SelectiveGrads:
 
 def _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, dims, grad_y=None):
     """The checked inputs of the selective scan (dims 3) or its step (dims 2):
-    (pointers of x, dt, A, B, C, D, z, dt_bias and grad_y, the parameters, what
-    has to live until the call is made).  Written out, for these calls are
+    (pointers of x, dt, A, B, C, D, z, dt_bias and grad_y, the parameters, (B, T,
+    D, N, G, type), what has to live until the call is made).  Written out, for these calls are
     short."""
     if x.dim() != dims or not x.is_cuda:
         raise ValueError("x must be a CUDA tensor " + ("[B, T, D]" if dims == 3 else "[B, D]"))
     code, shape, kind, dev = _dtype_code("x", x), x.shape, x.dtype, x.device
     W, lead = shape[-1], shape[:-1]
-    x, dt = _rows_of("x", x, shape, kind, dev), _rows_of("dt", dt, shape, kind, dev)
+    x, dt = _rows(x), _rows_of("dt", dt, shape, kind, dev)
     if z is not None:
         z = _rows_of("z", z, shape, kind, dev)
     if grad_y is not None:
@@ -1410,13 +1428,16 @@ def _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, dims, grad_y=None
     if max(*shape, N, G) > 0x7fffffff:
         _int32(*shape, N, G)
     nb, T = lead if dims == 3 else (lead[0], 1)
-    second = (lambda s: s[1]) if dims == 3 else (lambda s: 0)
     sx, sd, sb, sc = x.stride(), dt.stride(), B.stride(), C.stride()
     sz, sg = (0, 0) if z is None else z.stride(), (0, 0) if grad_y is None else grad_y.stride()
-    p = lif_select_params(nb, T, W, N, G, code, LIF_SELECT_SOFTPLUS if softplus else 0, 0, sx[0], second(sx), sd[0],
-                          second(sd), sz[0], second(sz), sb[0], second(sb), sc[0], second(sc), sg[0], second(sg))
+    if dims == 3:
+        strides = (*sx[:2], *sd[:2], *sz[:2], *sb[:2], *sc[:2], *sg[:2])
+    else:
+        strides = (sx[0], 0, sd[0], 0, sz[0], 0, sb[0], 0, sc[0], 0, 0, 0)
+    sizes = (nb, T, W, N, G, code)
+    p = _select_params(*sizes, LIF_SELECT_SOFTPLUS if softplus else 0, 0, *strides)
     return (x.data_ptr(), dt.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(D), _ptr(z), _ptr(dt_bias),
-            _ptr(grad_y)), p, (x, dt, A, B, C, D, z, dt_bias, grad_y)
+            _ptr(grad_y)), p, sizes, (x, dt, A, B, C, D, z, dt_bias, grad_y)
 
 
 def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, length=None, h_first=None, softplus: bool = True,
@@ -1428,15 +1449,15 @@ def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, length=None, h_
     only."""
     torch = _torch()
     with _on(torch, x, stream):
-        ptrs, p, held = _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, 3)
-        nb, T, W, N, dev = p.B, p.T, p.D, p.N, x.device
+        ptrs, p, (nb, T, W, N, G, code), held = _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, 3)
+        dev = x.device
         length = _expect("length", length, (nb,), torch.int32, dev)
         h_first = _expect("h_first", h_first, (nb, W, N), torch.float32, dev)
         y = torch.empty((nb, T, W), dtype=x.dtype, device=dev) if outputs else None
         last = torch.empty((nb, W, N), dtype=torch.float32, device=dev)
         mk = torch.empty((nb, -(-T // LIF_SELECT_MARK), N, W), dtype=torch.float32, device=dev) if marks else None
-        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, p.G, p.dtype, False), ws, dev)
-        rc = lif_selective_scan(*ptrs[:8], _ptr(length), _ptr(h_first), ctypes.byref(p), _ptr(y), last.data_ptr(),
+        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, G, code, False), ws, dev)
+        rc = lif_selective_scan(*ptrs[:8], _ptr(length), _ptr(h_first), p, _ptr(y), last.data_ptr(),
                                 _ptr(mk), wp, wn, _raw_stream(torch, dev, stream))
         _check("lif_selective_scan", rc)
         return SelectiveOut(y, last, mk)
@@ -1449,8 +1470,8 @@ def selective_scan_backward(x, dt, A, B, C, marks, grad_y=None, D=None, z=None, 
     [B, D, N])."""
     torch = _torch()
     with _on(torch, x, stream):
-        ptrs, p, held = _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, 3, grad_y)
-        nb, T, W, N, dev = p.B, p.T, p.D, p.N, x.device
+        ptrs, p, (nb, T, W, N, G, code), held = _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, 3, grad_y)
+        dev = x.device
         length = _expect("length", length, (nb,), torch.int32, dev)
         marks = _expect("marks", marks, (nb, -(-T // LIF_SELECT_MARK), N, W), torch.float32, dev)
         if marks is None:
@@ -1464,9 +1485,9 @@ def selective_scan_backward(x, dt, A, B, C, marks, grad_y=None, D=None, z=None, 
                            None if z is None else empty((nb, T, W), dtype=kind, device=dev),
                            None if dt_bias is None else empty((W,), dtype=f32, device=dev),
                            empty((nb, W, N), dtype=f32, device=dev))
-        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, p.G, p.dtype, True), ws, dev)
+        wp, wn, ws = _workspace(torch, _select_ws(nb, T, W, N, G, code, True), ws, dev)
         rc = lif_selective_scan_backward(*ptrs[:8], _ptr(length), marks.data_ptr(), ptrs[8], _ptr(grad_last),
-                                         ctypes.byref(p), g.x.data_ptr(), g.dt.data_ptr(), g.A.data_ptr(),
+                                         p, g.x.data_ptr(), g.dt.data_ptr(), g.A.data_ptr(),
                                          g.B.data_ptr(), g.C.data_ptr(), _ptr(g.D), _ptr(g.z), _ptr(g.dt_bias),
                                          g.h_first.data_ptr(), wp, wn, _raw_stream(torch, dev, stream))
         _check("lif_selective_scan_backward", rc)
@@ -1481,12 +1502,12 @@ def selective_step(x, dt, A, B, C, state, slot=None, D=None, z=None, dt_bias=Non
     Returns y [B, D]."""
     torch = _torch()
     with _on(torch, x, stream):
-        ptrs, p, held = _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, 2)
-        nb, dev = p.B, x.device
-        state = _pool(torch, state, (p.D, p.N), torch.float32, dev)
+        ptrs, p, (nb, T, W, N, G, code), held = _selective(torch, x, dt, A, B, C, D, z, dt_bias, softplus, 2)
+        dev = x.device
+        state = _pool(torch, state, (W, N), torch.float32, dev)
         slot = _expect("slot", slot, (nb,), torch.int32, dev)
-        y = torch.empty((nb, p.D), dtype=x.dtype, device=dev)
-        rc = lif_selective_step(*ptrs[:8], _ptr(slot), state.data_ptr(), state.shape[0], ctypes.byref(p),
+        y = torch.empty((nb, W), dtype=x.dtype, device=dev)
+        rc = lif_selective_step(*ptrs[:8], _ptr(slot), state.data_ptr(), state.shape[0], p,
                                 y.data_ptr(), _raw_stream(torch, dev, stream))
         _check("lif_selective_step", rc)
         return y
