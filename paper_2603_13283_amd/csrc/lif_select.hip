@@ -338,10 +338,11 @@ __global__ __launch_bounds__(W* kWave) void k_select_maps(Inputs in, Geometry q,
         for (int i = 0; i < kTile / 2; ++i) v[i] = from[i][lane];
 #pragma unroll
         for (int k = 0; k < NS; ++k) B[k] = n0 + k < q.N ? r.bc[0][0][k].f32() : 0.0f;
+        float part = 0.0f;                                    // of the tile: long sums go in two levels
         auto step = [&](auto at_step) {
             constexpr int i = decltype(at_step)::value;
             const float dl = i % 2 ? v[i / 2].z : v[i / 2].x, u = i % 2 ? v[i / 2].w : v[i / 2].y;
-            total += dl;
+            part += dl;
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
                 const float a = __builtin_amdgcn_exp2f(dl * rate[k]), b = u * of_step<i>(B[k]);
@@ -350,6 +351,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_maps(Inputs in, Geometry q,
         };
         if constexpr (REVERSE) each_step_back(step);
         else each_step(step);
+        total += part;
     };
     const int tiles = (p.n + kTile - 1) / kTile;
     if (tiles > 0) {
@@ -818,6 +820,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         for (int nb = 0; nb < NB; ++nb) {
             if (first(nb) >= q.N) break;
             float h[kTile][NS], a[kTile][NS], sum[kTile], P[kTile], Q[kTile], lam[kTile][NS], part[kTile];
+            float gA_tile[NS] = {};                           // long sums go in two levels
             const float(&B)[NS] = made.B[nb], (&C)[NS] = made.C[nb], (&h0)[NS] = made.h0[nb];
             each_step([&](auto step) {
                 constexpr int i = decltype(step)::value;
@@ -846,7 +849,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                     float f = mu[nb][k] * (i ? h[i ? i - 1 : 0][k] : h0[k]);
                     if (!kWhole) f = i < cnt ? f : 0.0f;
                     P[i] = k ? fmaf(A[nb][k], f, P[i]) : A[nb][k] * f;
-                    gA[nb][k] = fmaf(delta(i), f, gA[nb][k]);
+                    gA_tile[k] = fmaf(delta(i), f, gA_tile[k]);
                 }
                 Q[i] = of_step<i>(B[0]) * lam[i][0];
                 part[i] = merge_states(pb[0], pb[1], pc[0], pc[1]);
@@ -859,6 +862,8 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                     }
                 }
             });
+#pragma unroll
+            for (int k = 0; k < NS; ++k) gA[nb][k] += gA_tile[k];
             // rows 0 .. 3 hold b and c of the first state, b and c of the second
             const float s = merge_steps(part, lane);
             const int row = lane >> 4, i = lane & 15, n = first(nb) + (row >> 1);
@@ -878,14 +883,15 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                 const float2 c = shP[2][j][(s0 + i) / 2][lane];
                 P[i] += a.x, P[i + 1] += a.y, Q[i] += b.x, Q[i + 1] += b.y, Y[i] += c.x, Y[i + 1] += c.y;
             }
-        float g_r[STEPS];
+        float g_r[STEPS], skips = 0.0f, biases = 0.0f;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             g_r[i] = fmaf(made.x[i], Q[i], P[i]) * made.slope[i];
             const bool on = s0 + i < cnt;
-            g_skip = on ? fmaf(made.g[i], made.x[i], g_skip) : g_skip;
-            g_bias = on ? g_bias + g_r[i] : g_bias;
+            skips = on ? fmaf(made.g[i], made.x[i], skips) : skips;
+            biases = on ? biases + g_r[i] : biases;
         }
+        g_skip += skips, g_bias += biases;
         if (p.live)
 #pragma unroll
             for (int i = 0; i < STEPS; ++i)
