@@ -673,8 +673,8 @@ typedef struct lif_embed_params {
     int32_t  B, T;               /* samples and places; either may be 0             */
     int32_t  V, D;               /* rows of the table (>= 1) and their width (>= 1) */
     int32_t  dtype;              /* of out and grad                                 */
-    int32_t  table;              /* of W (forward only)                             */
-    int64_t  w_row;              /* elements between rows of W, >= D (forward only) */
+    int32_t  table;              /* of W                                            */
+    int64_t  w_row;              /* elements between rows of W, >= D                */
     int64_t  g_batch, g_time;    /* strides of grad (backward only)                 */
     double   scale;
     uint32_t flags;              /* must be 0                                       */

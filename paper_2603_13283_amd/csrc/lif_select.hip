@@ -500,7 +500,8 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
     };
     auto put_marks = [&](int t0) {
         if (marks && p.live) {
-            char* to = (char*)(marks + (((int64_t)p.b * ((q.T + kTile - 1) / kTile) + (p.t0 + t0) / kTile) * q.N + n0) * q.D);
+            const int64_t tile = (int64_t)p.b * ((q.T + kTile - 1) / kTile) + (p.t0 + t0) / kTile;
+            char* to = (char*)(marks + (tile * q.N + n0) * q.D);
             const uint32_t o = here(offset4);
 #pragma unroll
             for (int k = 0; k < NS; ++k, to += q.D * (int64_t)4)
@@ -750,7 +751,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
                 raw.v[j][i].load((const E*)from);
-                if (decltype(whole)::value || s0 + i + 1 < left) from += steps[j];     // the last one again past the end
+                if (decltype(whole)::value || s0 + i + 1 < left) from += steps[j];   // the last one again past the end
             }
         }
 #pragma unroll
@@ -927,7 +928,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         load(std::true_type(), kTile);
         ready(kTile);
         if (t0 > 0) back();
-        load(std::true_type(), kTile);                                          // (the first tile again where there is none before it)
+        load(std::true_type(), kTile);                        // (the first tile again where there is none before it)
         for (;;) {
             __syncthreads();
             walk(std::true_type(), t0, kTile);

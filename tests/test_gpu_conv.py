@@ -81,7 +81,8 @@ def steps_of(length, nb, T):
 def run(env, v, dtype, length=None, act=True, label=""):
     torch, lif = env
     nb, T, W = v["x"].shape
-    print(f"[case] conv {label} {tuple(v['x'].shape)} K={v['w'].shape[1]} {dtype} strides={v['x'].stride()}", flush=True)
+    print(f"[case] conv {label} {tuple(v['x'].shape)} K={v['w'].shape[1]} {dtype} strides={v['x'].stride()}",
+          flush=True)
     n = None if length is None else torch.tensor(length, dtype=torch.int32, device="cuda:0")
     kw = dict(bias=v["bias"], length=n, x_first=v["x_first"], silu=act)
     o = lif.causal_conv(v["x"], v["w"], **kw)

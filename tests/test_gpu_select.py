@@ -126,7 +126,8 @@ def segment_of(lif, v, length=None):
 def run(env, v, dtype, length=None, soft=True, label=""):
     torch, lif = env
     nb, T, W = v["x"].shape
-    print(f"[case] select {label} {tuple(v['x'].shape)} N={v['A'].shape[1]} B={tuple(v['B'].shape)} {dtype}", flush=True)
+    print(f"[case] select {label} {tuple(v['x'].shape)} N={v['A'].shape[1]} B={tuple(v['B'].shape)} {dtype}",
+          flush=True)
     n = None if length is None else torch.tensor(length, dtype=torch.int32, device="cuda:0")
     args = [v[k] for k in ("x", "dt", "A", "B", "C")]
     kw = dict(D=v["D"], z=v["z"], dt_bias=v["dt_bias"], length=n, softplus=soft)

@@ -197,7 +197,8 @@ def select_args(**kw):
     dict(dt=Stand((2, 5, 6), F32)), dict(A=Stand((6,), F32)), dict(A=Stand((5, 4), F32)), dict(A=Stand((6, 4))),
     dict(B=Stand((2, 5, 3))), dict(C=Stand((2, 5, 2, 4))), dict(B=Stand((2, 4, 4))), dict(D=Stand((6,))),
     dict(z=Stand((2, 5, 5))), dict(dt_bias=Stand((5,), F32)), dict(length=Stand((3,), I32)),
-    dict(length=Stand((2,), torch.int64)), dict(h_first=Stand((2, 4, 6), F32)), dict(dt=Stand((2, 5, 6), device="cuda:1"))])
+    dict(length=Stand((2,), torch.int64)), dict(h_first=Stand((2, 4, 6), F32)),
+    dict(dt=Stand((2, 5, 6), device="cuda:1"))])
 def test_select_binding(here, kw):
     with pytest.raises(ValueError):
         L.selective_scan(**select_args(**kw))
