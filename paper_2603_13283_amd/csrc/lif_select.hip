@@ -223,9 +223,9 @@ template <typename E> struct Bits {
 // The raw elements of a tile that one lane loads: IN inputs of its channel for
 // the steps that its wave makes ready, w STEPS .. (w + 1) STEPS - 1, and B and
 // C of step lane % 16 for the wave's states.
-template <typename E, int NS, int STEPS, int IN, int NB = 1> struct Raw {
+template <typename E, int NS, int STEPS, int IN> struct Raw {
     Bits<E> v[IN][STEPS];
-    Bits<E> bc[2][NB][NS];
+    Bits<E> bc[2][NS];
 };
 
 // A lane's offset as a value of the place where it is used: otherwise its
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_maps(Inputs in, Geometry q,
         const E* bc = REVERSE ? (const E*)in.C + p.b * q.c_batch + tb * q.c_time
                               : (const E*)in.Bm + p.b * q.b_batch + tb * q.b_time;
 #pragma unroll
-        for (int k = 0; k < NS; ++k) r.bc[0][0][k].load(bc + (int64_t)p.g * q.N + at[k]);
+        for (int k = 0; k < NS; ++k) r.bc[0][k].load(bc + (int64_t)p.g * q.N + at[k]);
     };
     // steps past the end have delta = 0: the identity
     auto ready = [&](const Raw<E, NS, STEPS, IN>& r, float4 (*to)[kWave], int left) {
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_maps(Inputs in, Geometry q,
 #pragma unroll
         for (int i = 0; i < kTile / 2; ++i) v[i] = from[i][lane];
 #pragma unroll
-        for (int k = 0; k < NS; ++k) B[k] = n0 + k < q.N ? r.bc[0][0][k].f32() : 0.0f;
+        for (int k = 0; k < NS; ++k) B[k] = n0 + k < q.N ? r.bc[0][k].f32() : 0.0f;
         float part = 0.0f;                                    // of the tile: long sums go in two levels
         auto step = [&](auto at_step) {
             constexpr int i = decltype(at_step)::value;
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
     };
     auto load_states = [&](Raw<E, NS, STEPS, 3>& r, const E* const (&from)[2][NS]) {
 #pragma unroll
-        for (int k = 0; k < NS; ++k) r.bc[0][0][k].load(from[0][k]), r.bc[1][0][k].load(from[1][k]);
+        for (int k = 0; k < NS; ++k) r.bc[0][k].load(from[0][k]), r.bc[1][k].load(from[1][k]);
     };
     auto ready = [&](const Raw<E, NS, STEPS, 3>& r, float4 (*to)[kWave]) {
 #pragma unroll
@@ -468,8 +468,8 @@ __global__ __launch_bounds__(W* kWave) void k_select_scan(Inputs in, Geometry q,
         float B[NS], Cv[NS], sum[kTile], hs[kTile][NS], a[kTile][NS];
 #pragma unroll
         for (int k = 0; k < NS; ++k) {
-            B[k] = n0 + k < q.N ? r.bc[0][0][k].f32() : 0.0f;
-            Cv[k] = n0 + k < q.N ? r.bc[1][0][k].f32() : 0.0f;
+            B[k] = n0 + k < q.N ? r.bc[0][k].f32() : 0.0f;
+            Cv[k] = n0 + k < q.N ? r.bc[1][k].f32() : 0.0f;
         }
         auto decays = [&](int i) {
             const float dl = i % 2 ? at_step[i / 2].z : at_step[i / 2].x;
@@ -670,9 +670,11 @@ template <typename E> struct BackOut {
 // for the sums over channels that grad_B and grad_C are, 100 a channel and step in
 // phases A and C; 8 x 2048 x 2048 x 16 bf16 530 us, 477 MB at 0.9 TB/s.  A wave
 // holds two states at a time, NB times over, so that a tile's states and decays
-// fit its registers.  Between two barriers a tile is walked; then its results
-// are written while the tile before it is made ready and the one before that is
-// on its way.
+// fit its registers; what lasts from tile to tile is in LDS but for the first two
+// (all in registers spill 113 a lane at 64 states: training, 8 x 2048 x 1024 x 64
+// bf16 2550 us, this 1710; of 32 states 948 and 897).  Between two barriers a tile
+// is walked; then its results are written while the tile before it is made ready
+// and the one before that is on its way.
 template <typename E, int W, int NB>
 __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q, const float* __restrict__ marks,
                                                           const float* __restrict__ grad_last,
@@ -683,40 +685,62 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
     __shared__ float4 shD[kTile / 2][kWave];                  // delta, delta x of two steps
     __shared__ float2 shG[kTile / 2][kWave];                  // g of two
     __shared__ float2 shP[3][W][kTile / 2][kWave];            // the waves' parts of P, Q and y of two
+    __shared__ float2 shS[NB > 1 ? NB - 1 : 1][3][W][kWave];  // mu, the gradient of A, and A of a wave's later states
     const int lane = threadIdx.x & 63, w = wave_index();
     const Place p = place_of(q, in.length, lane, (int*)shP);
     const int s0 = w * STEPS;
     const bool gated = in.z != nullptr, driven = in.gy != nullptr;
     auto first = [&](int nb) { return (nb * W + w) * NS; };
-    float mu[NB][NS], A[NB][NS], rate[NB][NS], gA[NB][NS];
-    int at[NB][NS];                                           // places past N repeat the last state, with B = C = 0
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+    // Of a wave's states, the first two are held in registers, the others in LDS.
+    struct States {
+        float mu[NS], A[NS], gA[NS];
+    } held;
+    const int segments = (p.length + q.seg_len - 1) / q.seg_len;       // that have steps
+    // places past N repeat the last state, with B = C = 0
+    const int at0[NS] = {min(first(0), q.N - 1), min(first(0) + 1, q.N - 1)};
+    auto at = [&](int nb, int k) { return nb ? min(first(nb) + k, q.N - 1) : at0[k]; };
+    auto begin = [&](int nb) {
+        States s;
+        float rate[NS];
 #pragma unroll
         for (int k = 0; k < NS; ++k) {
             const int n = first(nb) + k;
-            at[nb][k] = min(n, q.N - 1);
             const bool on = p.live && n < q.N;
-            A[nb][k] = on ? in.A[(int64_t)p.d * q.N + n] : 0.0f;
-            rate[nb][k] = rate_of(A[nb][k]);
-            mu[nb][k] = on && grad_last ? grad_last[((int64_t)p.b * q.D + p.d) * q.N + n] : 0.0f;
-            gA[nb][k] = 0.0f;
+            s.A[k] = on ? in.A[(int64_t)p.d * q.N + n] : 0.0f;
+            rate[k] = rate_of(s.A[k]);
+            s.mu[k] = on && grad_last ? grad_last[((int64_t)p.b * q.D + p.d) * q.N + n] : 0.0f;
+            s.gA[k] = 0.0f;
         }
-    const int segments = (p.length + q.seg_len - 1) / q.seg_len;       // that have steps
-    if (p.seg + 1 < segments)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-            carry(mu[nb], rate[nb], sums, ends, q, p, first(nb), segments - 1, segments - 1 - p.seg, -1);
+        if (p.seg + 1 < segments)
+            carry(s.mu, rate, sums, ends, q, p, first(nb), segments - 1, segments - 1 - p.seg, -1);
+        return s;
+    };
+    auto keep = [&](int nb, const States& s) {
+        shS[nb - 1][0][w][lane] = make_float2(s.mu[0], s.mu[1]);
+        shS[nb - 1][1][w][lane] = make_float2(s.gA[0], s.gA[1]);
+    };
+    auto kept = [&](int nb) {
+        const float2 mu = shS[nb - 1][0][w][lane], gA = shS[nb - 1][1][w][lane], A = shS[nb - 1][2][w][lane];
+        return States{{mu.x, mu.y}, {A.x, A.y}, {gA.x, gA.y}};
+    };
+    held = begin(0);
+#pragma unroll 1
+    for (int nb = 1; nb < NB; ++nb) {
+        const States s = begin(nb);
+        keep(nb, s);
+        shS[nb - 1][2][w][lane] = make_float2(s.A[0], s.A[1]);
+    }
     const float bias = in.bias ? in.bias[p.d] : 0.0f, skip = in.skip ? in.skip[p.d] : 0.0f;
     float g_skip = 0.0f, g_bias = 0.0f;
 
     // A tile's raw elements and marks on their way, and what phase A makes of
-    // the steps of this wave.
-    Raw<E, NS, STEPS, 4, NB> raw;
-    float mark[NB][NS];
+    // the steps of this wave.  Of the states, the first two only: the others of a
+    // tile are loaded while those before them are walked.
+    Raw<E, NS, STEPS, 4> raw;
+    float mark[NS];
     struct Made {
         float x[STEPS], delta[STEPS], slope[STEPS], g[STEPS], z_slope[STEPS];
-        float B[NB][NS], C[NB][NS], h0[NB][NS];
+        float B[NS], C[NS], h0[NS];
     } made;
     // Where the lane's steps of the tile that is loaded next lie, and where their
     // gradients go: addresses of the lanes, for as scalars they spill the scalar
@@ -744,7 +768,25 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         const int64_t row = ((int64_t)p.b * q.T + p.t0 + t0 + s0) * q.D + p.d;
         out_at[0] = (char*)(out.gx + row), out_at[1] = (char*)(out.gdt + row), out_at[2] = (char*)(out.gz + row);
     };
+    auto load_states = [&](int nb, int tiles, auto& bc, float (&m)[NS]) {      // of the tile `tiles` after Bt
+#pragma unroll
+        for (int k = 0; k < NS; ++k) {
+            bc[0][k].load(Bt + tiles * kTile * q.b_time + at(nb, k));
+            bc[1][k].load(Ct + tiles * kTile * q.c_time + at(nb, k));
+            m[k] = *(const float*)(mark_at + (tiles * q.N + at(nb, k)) * mark_step);
+        }
+    };
+    auto take_states = [&](int nb, auto& bc, const float (&m)[NS]) {
+#pragma unroll
+        for (int k = 0; k < NS; ++k) {
+            const bool on = first(nb) + k < q.N;
+            made.B[k] = on ? bc[0][k].f32() : 0.0f;
+            made.C[k] = on ? bc[1][k].f32() : 0.0f;
+            made.h0[k] = on ? m[k] : 0.0f;
+        }
+    };
     auto load = [&](auto whole, int left) {
+        load_states(0, 0, raw.bc, mark);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const char* from = in_at[j];
@@ -754,14 +796,6 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                 if (decltype(whole)::value || s0 + i + 1 < left) from += steps[j];   // the last one again past the end
             }
         }
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int k = 0; k < NS; ++k) {
-                raw.bc[0][nb][k].load(Bt + at[nb][k]);
-                raw.bc[1][nb][k].load(Ct + at[nb][k]);
-                mark[nb][k] = *(const float*)(mark_at + at[nb][k] * mark_step);
-            }
     };
     auto back = [&] {
 #pragma unroll
@@ -794,21 +828,13 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
             shD[(s0 + i) / 2][lane] = make_float4(v[0][0], v[0][1], v[1][0], v[1][1]);
             shG[(s0 + i) / 2][lane] = make_float2(v[0][2], v[1][2]);
         }
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int k = 0; k < NS; ++k) {
-                const bool on = first(nb) + k < q.N;
-                made.B[nb][k] = on ? raw.bc[0][nb][k].f32() : 0.0f;
-                made.C[nb][k] = on ? raw.bc[1][nb][k].f32() : 0.0f;
-                made.h0[nb][k] = on ? mark[nb][k] : 0.0f;
-            }
+        take_states(0, raw.bc, mark);
     };
-    auto put = [&](int what, int i, int nb, float a, float b) {
+    auto put = [&](auto first_pass, int what, int i, float a, float b) {
         float2* to = &shP[what][w][i / 2][lane];
-        *to = nb ? make_float2(to->x + a, to->y + b) : make_float2(a, b);
+        *to = decltype(first_pass)::value ? make_float2(a, b) : make_float2(to->x + a, to->y + b);
     };
-    auto walk = [&](auto whole, int t0, int cnt) {
+    auto walk = [&](auto whole, int t0, int cnt, int tiles) {
         constexpr bool kWhole = decltype(whole)::value;
         float4 D[kTile / 2];
         float2 G[kTile / 2];
@@ -817,39 +843,42 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         auto delta = [&](int i) { return i % 2 ? D[i / 2].z : D[i / 2].x; };
         auto input = [&](int i) { return i % 2 ? D[i / 2].w : D[i / 2].y; };
         auto grad = [&](int i) { return i % 2 ? G[i / 2].y : G[i / 2].x; };
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            if (first(nb) >= q.N) break;
+        auto pass = [&](auto first_pass, int nb, States& s) {
             float h[kTile][NS], a[kTile][NS], sum[kTile], P[kTile], Q[kTile], lam[kTile][NS], part[kTile];
-            float gA_tile[NS] = {};                           // long sums go in two levels
-            const float(&B)[NS] = made.B[nb], (&C)[NS] = made.C[nb], (&h0)[NS] = made.h0[nb];
+            float gA_tile[NS] = {}, rate[NS];                 // long sums go in two levels
+            const float(&B)[NS] = made.B, (&C)[NS] = made.C, (&h0)[NS] = made.h0;
+            Bits<E> bc[2][NS];
+            float m[NS];
+            if (nb + 1 < NB) load_states(nb + 1, tiles, bc, m);
+#pragma unroll
+            for (int k = 0; k < NS; ++k) rate[k] = rate_of(s.A[k]);
             each_step([&](auto step) {
                 constexpr int i = decltype(step)::value;
 #pragma unroll
                 for (int k = 0; k < NS; ++k) {
-                    a[i][k] = __builtin_amdgcn_exp2f(delta(i) * rate[nb][k]);
+                    a[i][k] = __builtin_amdgcn_exp2f(delta(i) * rate[k]);
                     h[i][k] = fmaf(a[i][k], i ? h[i ? i - 1 : 0][k] : h0[k], input(i) * of_step<i>(B[k]));
                 }
                 sum[i] = of_step<i>(C[0]) * h[i][0];
                 if constexpr (i % 4 == 3) {
                     add_steps<i - 3>(sum + i - 3, C[1], h[i - 3][1], h[i - 2][1], h[i - 1][1], h[i][1]);
-                    put(2, i - 3, nb, sum[i - 3], sum[i - 2]);
-                    put(2, i - 1, nb, sum[i - 1], sum[i]);
+                    put(first_pass, 2, i - 3, sum[i - 3], sum[i - 2]);
+                    put(first_pass, 2, i - 1, sum[i - 1], sum[i]);
                 }
             });
             each_step_back([&](auto step) {
                 constexpr int i = decltype(step)::value;
                 float pb[NS], pc[NS];
-                lam[i][0] = mu[nb][0], lam[i][1] = mu[nb][1];
+                lam[i][0] = s.mu[0], lam[i][1] = s.mu[1];
                 add_step<i>(lam[i][0], lam[i][1], C[0], C[1], grad(i));
 #pragma unroll
                 for (int k = 0; k < NS; ++k) {
                     pc[k] = grad(i) * h[i][k];
                     pb[k] = lam[i][k] * input(i);
-                    mu[nb][k] = a[i][k] * lam[i][k];
-                    float f = mu[nb][k] * (i ? h[i ? i - 1 : 0][k] : h0[k]);
+                    s.mu[k] = a[i][k] * lam[i][k];
+                    float f = s.mu[k] * (i ? h[i ? i - 1 : 0][k] : h0[k]);
                     if (!kWhole) f = i < cnt ? f : 0.0f;
-                    P[i] = k ? fmaf(A[nb][k], f, P[i]) : A[nb][k] * f;
+                    P[i] = k ? fmaf(s.A[k], f, P[i]) : s.A[k] * f;
                     gA_tile[k] = fmaf(delta(i), f, gA_tile[k]);
                 }
                 Q[i] = of_step<i>(B[0]) * lam[i][0];
@@ -858,18 +887,26 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                     add_steps<i>(Q + i, B[1], lam[i][1], lam[i + 1][1], lam[i + 2][1], lam[i + 3][1]);
 #pragma unroll
                     for (int j = 0; j < 4; j += 2) {
-                        put(0, i + j, nb, P[i + j], P[i + j + 1]);
-                        put(1, i + j, nb, Q[i + j], Q[i + j + 1]);
+                        put(first_pass, 0, i + j, P[i + j], P[i + j + 1]);
+                        put(first_pass, 1, i + j, Q[i + j], Q[i + j + 1]);
                     }
                 }
             });
 #pragma unroll
-            for (int k = 0; k < NS; ++k) gA[nb][k] += gA_tile[k];
+            for (int k = 0; k < NS; ++k) s.gA[k] += gA_tile[k];
             // rows 0 .. 3 hold b and c of the first state, b and c of the second
-            const float s = merge_steps(part, lane);
+            const float all = merge_steps(part, lane);
             const int row = lane >> 4, i = lane & 15, n = first(nb) + (row >> 1);
             if (i < cnt && n < q.N)
-                (row & 1 ? out.partC : out.partB)[((int64_t)p.column * q.T + p.t0 + t0 + i) * q.N + n] = s;
+                (row & 1 ? out.partC : out.partB)[((int64_t)p.column * q.T + p.t0 + t0 + i) * q.N + n] = all;
+            if (nb + 1 < NB) take_states(nb + 1, bc, m);
+        };
+        if (first(0) < q.N) pass(std::true_type(), 0, held);
+#pragma unroll 1
+        for (int nb = 1; nb < NB && first(nb) < q.N; ++nb) {
+            States s = kept(nb);
+            pass(std::false_type(), nb, s);
+            keep(nb, s);
         }
     };
     auto write = [&](int cnt) {
@@ -918,7 +955,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         load(std::false_type(), p.n - t0);
         ready(p.n - t0);
         __syncthreads();
-        walk(std::false_type(), t0, p.n - t0);
+        walk(std::false_type(), t0, p.n - t0, 0);
         __syncthreads();
         write(p.n - t0);
     }
@@ -931,7 +968,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         load(std::true_type(), kTile);                        // (the first tile again where there is none before it)
         for (;;) {
             __syncthreads();
-            walk(std::true_type(), t0, kTile);
+            walk(std::true_type(), t0, kTile, t0 > 0);
             __syncthreads();
             write(kTile);
             if (t0 == 0) break;
@@ -948,15 +985,17 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
             if (gated) out.gz[to] = from_f32<E>(0.0f);
         }
         const int64_t states = (int64_t)q.D * q.N;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll 1
+        for (int nb = 0; nb < NB; ++nb) {
+            const States s = nb ? kept(nb) : held;
 #pragma unroll
             for (int k = 0; k < NS; ++k)
                 if (first(nb) + k < q.N) {
                     const int64_t to = (int64_t)p.d * q.N + first(nb) + k;
-                    out.partA[((int64_t)p.seg * q.B + p.b) * states + to] = gA[nb][k];
-                    if (out.g_first && p.seg == 0) out.g_first[p.b * states + to] = mu[nb][k];
+                    out.partA[((int64_t)p.seg * q.B + p.b) * states + to] = s.gA[k];
+                    if (out.g_first && p.seg == 0) out.g_first[p.b * states + to] = s.mu[k];
                 }
+        }
     }
     __syncthreads();
     shP[0][w][0][lane] = make_float2(g_skip, g_bias);
