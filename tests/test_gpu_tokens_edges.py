@@ -67,7 +67,8 @@ def test_sequences_past_32_bits(env):
 
 
 @pytest.mark.parametrize("shape,length", [((3, 1200, 40, 16, 1), [1200, 700, 0]), ((2, 1500, 24, 5, 2), [1, 961]),
-                                          ((1, 2000, 70, 33, 1), [1999])])
+                                          ((1, 2000, 70, 33, 1), [1999]), ((2, 1200, 40, 24, 1), [1200, 333]),
+                                          ((1, 1500, 66, 64, 2), [1490])])
 def test_lengths_in_segments(env, shape, length):
     """Samples that end inside a segment of a time axis that is shared out,
     before the others, or have no step at all."""
