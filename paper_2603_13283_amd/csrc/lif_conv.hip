@@ -290,17 +290,14 @@ __global__ __launch_bounds__(1024) void k_conv_sums(const float* __restrict__ pa
     }
 }
 
+// One step of VEC channels from d on of stream b.
 template <typename E, int K, int VEC>
-__global__ __launch_bounds__(256) void k_conv_step(const E* __restrict__ x, const float* __restrict__ w,
-                                                   const float* __restrict__ bias, const int32_t* __restrict__ slot,
-                                                   E* __restrict__ state, int n_slots, Geometry q, E* __restrict__ y)
+__device__ __forceinline__ void step_at(const E* __restrict__ x, const float* __restrict__ w,
+                                        const float* __restrict__ bias, E* __restrict__ state, int row, bool on,
+                                        const Geometry& q, int b, int d, E* __restrict__ y)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= (int64_t)q.B * q.groups) return;
-    const int b = (int)(at / q.groups), d = min((int)(at - (int64_t)b * q.groups) * VEC, q.D - VEC);
-    const int row = slot ? slot[b] : b;
     E o[VEC];
-    if (row >= 0 && row < n_slots) {
+    if (on) {
         E win[K][VEC];
         E* st = state + (int64_t)row * (K - 1) * q.D + d;
 #pragma unroll
@@ -322,6 +319,23 @@ __global__ __launch_bounds__(256) void k_conv_step(const E* __restrict__ x, cons
         for (int k = 0; k < VEC; ++k) o[k] = from_f32<E>(0.0f);
     }
     store_elems<E, VEC>(y + (int64_t)b * q.D + d, o);
+}
+
+// The state is read and written in place, so every channel has one lane: the
+// first D / VEC lanes of a stream take VEC channels each, the D % VEC after them
+// one each.  Bound by the launch: 64 x 2048 bf16 3.4 us.
+template <typename E, int K, int VEC>
+__global__ __launch_bounds__(256) void k_conv_step(const E* __restrict__ x, const float* __restrict__ w,
+                                                   const float* __restrict__ bias, const int32_t* __restrict__ slot,
+                                                   E* __restrict__ state, int n_slots, Geometry q, E* __restrict__ y)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= (int64_t)q.B * q.groups) return;
+    const int b = (int)(at / q.groups), i = (int)(at - (int64_t)b * q.groups), wide = q.D / VEC;
+    const int row = slot ? slot[b] : b;
+    const bool on = row >= 0 && row < n_slots;
+    if (i < wide) step_at<E, K, VEC>(x, w, bias, state, row, on, q, b, i * VEC, y);
+    else if constexpr (VEC > 1) step_at<E, K, 1>(x, w, bias, state, row, on, q, b, wide * VEC + i - wide, y);
 }
 
 int check_conv(const lif_conv_params* p)
@@ -451,7 +465,8 @@ extern "C" int lif_causal_conv_step(const void* x, const float* w, const float* 
     if (p->T != 1 || n_slots < 0 || (!slot && n_slots < p->B)) return LIF_ERR_ARG;
     if (p->B == 0) return LIF_OK;
     if (!x || !w || !y || (n_slots > 0 && !state)) return LIF_ERR_ARG;
-    const Geometry q = geometry_of(*p, 1);
+    Geometry q = geometry_of(*p, 1);
+    q.groups = p->D / vec_of(*p) + p->D % vec_of(*p);
     const int64_t lanes = (int64_t)q.B * q.groups;
     with_shape(*p, [&](auto e, auto taps, auto vec) {
         using E = decltype(e);
