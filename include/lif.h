@@ -752,7 +752,9 @@ int lif_causal_conv_step(const void* x, const float* w, const float* bias, const
  *   marks     float [B][ceil(T / LIF_SELECT_MARK)][N][D]: the states entering
  *             steps 0, LIF_SELECT_MARK, 2 LIF_SELECT_MARK, ... < n (later ones
  *             are not written); the backward pass needs them; may be NULL
- * Decays e^{delta A} below 2^-126 count as 0.
+ * Decays e^{delta A} below 2^-126 count as 0.  With LIF_SELECT_SOFTPLUS, dt =
+ * -infinity masks a step: delta is 0, the step leaves the state alone, and no
+ * gradient goes through its dt.
  *
  * lif_selective_scan_backward: for dL/dy = grad_y ([B][T][D] of p->dtype, rows
  * contiguous, strides g_batch, g_time; NULL: 0) and dL/dh_last = grad_last

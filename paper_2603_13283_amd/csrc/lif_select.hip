@@ -125,7 +125,7 @@ __device__ __forceinline__ float softplus(float r, float& slope)
     v = fmaf(v, q, 1.0f);
     const float k = __builtin_amdgcn_rcpf(1.0f + e);
     slope = r >= 0.0f ? k : e * k;
-    return fmaf(0.5f, r + fabsf(r), s * v);                           // a NaN stays one
+    return fmaf(s, v, r <= 0.0f ? 0.0f : r);                          // 0 for -infinity, and a NaN stays one
 }
 
 __device__ __forceinline__ float step_length(const Geometry& q, float r, float& slope)

@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 
 import test_gpu_conv as conv
+import test_gpu_select as select
 from rounding import check
 
 pytestmark = pytest.mark.gpu
@@ -34,3 +35,94 @@ def test_step_widths(env, nb, W, K, dtype):
     want = conv.reference({k: conv.arr(t) for k, t in v.items()}, np.full(nb, 6))
     check(conv.arr(torch.stack(ys, 1)), want["y"], dtype, "y")
     assert np.array_equal(conv.arr(state), want["x_last"])
+
+
+def scan(env, v, length=None, soft=True):
+    """Forward and backward on v: results by the names of select.reference."""
+    torch, lif = env
+    n = None if length is None else torch.tensor(length, dtype=torch.int32, device="cuda:0")
+    args = [v[k] for k in ("x", "dt", "A", "B", "C")]
+    kw = dict(D=v["D"], z=v["z"], dt_bias=v["dt_bias"], length=n, softplus=soft)
+    o = lif.selective_scan(*args, h_first=v["h_first"], marks=True, **kw)
+    g = lif.selective_scan_backward(*args, o.marks, v["grad_y"], grad_last=v["grad_last"], **kw)
+    torch.cuda.synchronize()
+    return {"y": o.y, "h_last": o.h_last, **{"grad_" + k: getattr(g, k) for k in
+                                             ("x", "dt", "A", "B", "C", "D", "z", "dt_bias", "h_first")}}
+
+
+def compare(env, got, v, dtype, label, length=None, soft=True):
+    nb, T = v["x"].shape[:2]
+    want = select.reference({k: select.arr(t) for k, t in v.items()}, select.steps_of(length, nb, T), soft,
+                            select.segment_of(env[1], v))
+    for k, w in want.items():
+        check(select.arr(got[k]), w, "f32" if k in select.FLOAT32 else dtype, f"{label} {k}")
+
+
+def masked(torch, v, part):
+    """Which steps of which channels have a step length of 0: single ones, a
+    channel's whole sequence, a whole sample."""
+    g = torch.Generator().manual_seed(5)
+    off = torch.rand(v["dt"].shape, generator=g) < 0.2
+    if part == "sample":
+        off[0] = True
+    off[..., 1] = True
+    return off.to("cuda:0")
+
+
+# few columns share out the time axis in the last two
+MASKED = [(2, 40, 33, 9, 1), (2, 37, 70, 6, 2), (1, 20, 5, 64, 1), (2, 1200, 40, 16, 1), (1, 1100, 20, 33, 1)]
+
+
+@pytest.mark.parametrize("part", ["steps", "sample"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("shape", MASKED)
+def test_masked_steps(env, shape, dtype, part):
+    """dt = -infinity is a step length of 0: the step leaves the state alone,
+    and no gradient goes through dt.  The reference takes -200 there, whose step
+    length is 10^-87."""
+    torch, lif = env
+    print(f"[case] masked {shape} {dtype} {part}", flush=True)
+    v = select.make(torch, shape, dtype, seed=3)
+    off = masked(torch, v, part)
+    v["dt"][off] = float("-inf")
+    got = scan(env, v)
+    assert not got["grad_dt"][off].any() and not got["grad_dt_bias"][1]
+    if part == "sample":
+        assert torch.equal(got["h_last"][0], v["h_first"][0])
+    v["dt"][off] = -200.0
+    compare(env, got, v, dtype, "masked")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_masked_streams(env, dtype):
+    """The same for single steps: such a stream's state keeps its bits."""
+    torch, lif = env
+    v = select.make(torch, (5, 1, 66, 16, 2), dtype, seed=4, step=True)
+    off = masked(torch, v, "sample")
+    v["dt"][off] = float("-inf")
+    state, kept = v["h_first"].clone(), v["h_first"]
+    y = lif.selective_step(*[v[k] for k in ("x", "dt", "A", "B", "C")], state, D=v["D"], z=v["z"],
+                           dt_bias=v["dt_bias"])
+    assert torch.equal(state[off], kept[off])
+    v["dt"][off] = -200.0
+    ref = {k: select.arr(t)[:, None] if k in ("x", "dt", "B", "C", "z", "grad_y") else select.arr(t)
+           for k, t in v.items()}
+    want = select.reference(ref, np.full(5, 1))
+    check(select.arr(y), want["y"][:, 0], dtype, "y")
+    check(select.arr(state), want["h_last"], "f32", "state")
+
+
+def test_longest_steps(env):
+    """Step lengths near the largest float32: the state is forgotten, an input
+    of 0 comes in as 0."""
+    torch, lif = env
+    v = select.make(torch, (2, 40, 33, 9, 1), "f32", seed=6)
+    v["dt"][:, 20], v["x"][:, 20], v["dt_bias"] = 3e38, 0.0, None
+    args = [v[k] for k in ("dt", "A", "B", "C")]
+    o = lif.selective_scan(v["x"][:, :21], *[t if k == 1 else t[:, :21] for k, t in enumerate(args)],
+                           h_first=v["h_first"])
+    assert not o.h_last.any() and torch.isfinite(o.y).all()
+    state = v["h_first"].clone()
+    lif.selective_step(v["x"][:, 20], *[t if k == 1 else t[:, 20, 0] if k > 1 else t[:, 20]
+                                        for k, t in enumerate(args)], state)
+    assert not state.any()
