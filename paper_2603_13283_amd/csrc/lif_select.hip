@@ -145,12 +145,16 @@ __device__ __forceinline__ float silu(float z, float& slope)
 }
 
 // A log2 e, the exponent per unit of delta.  An infinite A keeps a = 1 for
-// delta = 0 (steps past the length inside a tile).
+// delta = 0 (a masked step, steps past the length inside a tile).
 __device__ __forceinline__ float rate_of(float a)
 {
     const float v = a * kLog2e;
     return fabsf(v) > 3.0e38f ? copysignf(3.0e38f, v) : v;
 }
+
+// A as it enters the gradient of delta, A a lambda h: an infinite A has a = 0 and
+// no slope for any delta > 0, and is given none at 0.
+__device__ __forceinline__ float slope_of(float a) { return fabsf(a) == INFINITY ? 0.0f : a; }
 
 template <int CTRL> __device__ __forceinline__ float dpp(float v)
 {
@@ -845,13 +849,13 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
         auto grad = [&](int i) { return i % 2 ? G[i / 2].y : G[i / 2].x; };
         auto pass = [&](auto first_pass, int nb, States& s) {
             float h[kTile][NS], a[kTile][NS], sum[kTile], P[kTile], Q[kTile], lam[kTile][NS], part[kTile];
-            float gA_tile[NS] = {}, rate[NS];                 // long sums go in two levels
+            float gA_tile[NS] = {}, rate[NS], A[NS];          // long sums go in two levels
             const float(&B)[NS] = made.B, (&C)[NS] = made.C, (&h0)[NS] = made.h0;
             Bits<E> bc[2][NS];
             float m[NS];
             if (nb + 1 < NB) load_states(nb + 1, tiles, bc, m);
 #pragma unroll
-            for (int k = 0; k < NS; ++k) rate[k] = rate_of(s.A[k]);
+            for (int k = 0; k < NS; ++k) rate[k] = rate_of(s.A[k]), A[k] = slope_of(s.A[k]);
             each_step([&](auto step) {
                 constexpr int i = decltype(step)::value;
 #pragma unroll
@@ -878,7 +882,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_back(Inputs in, Geometry q,
                     s.mu[k] = a[i][k] * lam[i][k];
                     float f = s.mu[k] * (i ? h[i ? i - 1 : 0][k] : h0[k]);
                     if (!kWhole) f = i < cnt ? f : 0.0f;
-                    P[i] = k ? fmaf(s.A[k], f, P[i]) : s.A[k] * f;
+                    P[i] = k ? fmaf(A[k], f, P[i]) : A[k] * f;
                     gA_tile[k] = fmaf(delta(i), f, gA_tile[k]);
                 }
                 Q[i] = of_step<i>(B[0]) * lam[i][0];
@@ -1088,8 +1092,10 @@ __global__ __launch_bounds__(256) void k_select_step(Inputs in, const int32_t* _
             }
         }
     };
-    float A[4];
-    load(A, in.A + (int64_t)c * q.N + n0);
+    float rate[4];
+    load(rate, in.A + (int64_t)c * q.N + n0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) rate[k] = rate_of(rate[k]);
     for (int b0 = blockIdx.y * U; b0 < q.B; b0 += gridDim.y * U) {
         float h[U][4], z[U];
         E xv[U], dt[U], Bt[U][4], Ct[U][4];
@@ -1114,7 +1120,7 @@ __global__ __launch_bounds__(256) void k_select_step(Inputs in, const int32_t* _
             const float x = to_f32(xv[j]), delta = step_length(q, to_f32(dt[j]) + bias, slope), u = delta * x;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                h[j][k] = fmaf(__builtin_amdgcn_exp2f(delta * (A[k] * kLog2e)), h[j][k], u * to_f32(Bt[j][k]));
+                h[j][k] = fmaf(__builtin_amdgcn_exp2f(delta * rate[k]), h[j][k], u * to_f32(Bt[j][k]));
                 sum = k < left ? fmaf(to_f32(Ct[j][k]), h[j][k], sum) : sum;
             }
             if (live && row[j] >= 0) {

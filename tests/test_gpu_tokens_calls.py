@@ -126,3 +126,38 @@ def test_longest_steps(env):
     lif.selective_step(v["x"][:, 20], *[t if k == 1 else t[:, 20, 0] if k > 1 else t[:, 20]
                                         for k, t in enumerate(args)], state)
     assert not state.any()
+
+
+@pytest.mark.parametrize("shape", MASKED)
+def test_infinite_rates(env, shape):
+    """A = -infinity: a state that keeps nothing over a step of positive length,
+    and stays over one of length 0.  The reference takes -10^30."""
+    torch, lif = env
+    v = select.make(torch, shape, "f32", seed=7)
+    off = masked(torch, v, "steps")
+    v["dt"][off] = float("-inf")
+    v["A"][::3, 0] = float("-inf")
+    v["A"][2, :] = float("-inf")
+    got = scan(env, v)
+    v["dt"][off] = -200.0
+    v["A"][torch.isinf(v["A"])] = -1e30
+    compare(env, got, v, "f32", "infinite rates")
+
+
+def test_infinite_rates_of_streams(env):
+    torch, lif = env
+    v = select.make(torch, (5, 1, 66, 17, 2), "f32", seed=8, step=True)
+    off = masked(torch, v, "steps")
+    v["dt"][off] = float("-inf")
+    v["A"][::3, 0], v["A"][2, :] = float("-inf"), float("-inf")
+    state, kept = v["h_first"].clone(), v["h_first"]
+    y = lif.selective_step(*[v[k] for k in ("x", "dt", "A", "B", "C")], state, D=v["D"], z=v["z"],
+                           dt_bias=v["dt_bias"])
+    assert torch.equal(state[off], kept[off])
+    v["dt"][off] = -200.0
+    v["A"][torch.isinf(v["A"])] = -1e30
+    ref = {k: select.arr(t)[:, None] if k in ("x", "dt", "B", "C", "z", "grad_y") else select.arr(t)
+           for k, t in v.items()}
+    want = select.reference(ref, np.full(5, 1))
+    check(select.arr(y), want["y"][:, 0], "f32", "y")
+    check(select.arr(state), want["h_last"], "f32", "state")
