@@ -55,7 +55,8 @@ def compare(env, got, v, dtype, label, length=None, soft=True):
     want = select.reference({k: select.arr(t) for k, t in v.items()}, select.steps_of(length, nb, T), soft,
                             select.segment_of(env[1], v))
     for k, w in want.items():
-        check(select.arr(got[k]), w, "f32" if k in select.FLOAT32 else dtype, f"{label} {k}")
+        if got[k] is not None:
+            check(select.arr(got[k]), w, "f32" if k in select.FLOAT32 else dtype, f"{label} {k}")
 
 
 def masked(torch, v, part):
@@ -161,3 +162,44 @@ def test_infinite_rates_of_streams(env):
     want = select.reference(ref, np.full(5, 1))
     check(select.arr(y), want["y"][:, 0], "f32", "y")
     check(select.arr(state), want["h_last"], "f32", "state")
+
+
+@pytest.mark.parametrize("N", [4, 20])
+def test_growing_states(env, N):
+    """A > 0 where a shared-out time axis has no state yet: the decay over a
+    segment lies past the largest float32, the state is 0.  Inputs come in the
+    last 40 steps, gradients in the first 40."""
+    torch, lif = env
+    nb, T, W = 1, 2048, 6
+    v = select.make(torch, (nb, T, W, N, 1), "f32", seed=9)
+    p = lif.lif_select_params(nb, T, W, N, 1, 0, 0, 0, *([0] * 12))
+    assert lif.lif_selective_scan_workspace_size(p) > 0, "the time axis is not shared out"
+    v["A"] = torch.full_like(v["A"], 1.5)
+    v["dt"], v["dt_bias"], v["h_first"], v["grad_last"] = torch.ones_like(v["dt"]), None, None, None
+    v["x"][:, :-40] = 0.0
+    v["grad_y"][:, 40:] = 0.0
+    got = scan(env, v, soft=False)
+    # the last 48 steps alone give the outputs, the first 48 the gradients
+    ref = {k: select.arr(t) for k, t in v.items()}
+    part = lambda sl: {k: t[:, sl] if k in ("x", "dt", "B", "C", "z", "grad_y") else t for k, t in ref.items()}  # noqa: E731
+    tail, head = (select.reference(part(sl), np.full(nb, 48), False, 48) for sl in (slice(T - 48, T), slice(0, 48)))
+    assert np.isfinite(tail["h_last"].e).all() and np.isfinite(head["grad_h_first"].e).all()
+    check(select.arr(got["y"][:, -48:]), tail["y"], "f32", "growing y")
+    check(select.arr(got["h_last"]), tail["h_last"], "f32", "growing h_last")
+    for k in ("x", "B", "C", "dt", "z"):
+        check(select.arr(got["grad_" + k][:, :48]), head["grad_" + k], "f32", "growing grad_" + k)
+        assert not got["grad_" + k][:, 48:].any(), k
+    check(select.arr(got["grad_h_first"]), head["grad_h_first"], "f32", "growing grad_h_first")
+    assert not got["y"][:, :-48].any() and not got["grad_A"].any()
+
+
+def test_long_steps_in_segments(env):
+    """Rates of 0 and steps whose sum passes the largest float32: the state
+    stays."""
+    torch, lif = env
+    nb, T, W, N = 1, 2048, 6, 4
+    v = select.make(torch, (nb, T, W, N, 1), "f32", seed=10)
+    v["A"], v["x"] = torch.zeros_like(v["A"]), torch.zeros_like(v["x"])
+    v["dt"] = torch.full_like(v["dt"], 2e38)
+    o = lif.selective_scan(*[v[k] for k in ("x", "dt", "A", "B", "C")], h_first=v["h_first"])
+    assert torch.equal(o.h_last, v["h_first"]) and torch.isfinite(o.y).all()
