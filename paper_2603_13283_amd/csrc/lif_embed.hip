@@ -339,12 +339,13 @@ __global__ __launch_bounds__(256) void k_embed_sums(const E* __restrict__ grad, 
         for (int k = 0; k < VEC; ++k) o[k] = acc[k] * by;
         if (live) store_elems<float, VEC>(to + d, o);
     };
-    for (int i0 = first; i0 < end; i0 += kAhead) {
+    const int n = end - first;                                      // places near 2^31 are counted from the first
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
         E row[kAhead][VEC];
         uint32_t key[kAhead];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            const int i = min(i0 + j, end - 1);
+            const int i = first + min(i0 + j, n - 1);
             key[j] = uniform(keys[i]);
             const int r = (int)uniform(places[i]), b = r / q.T;
             if (key[j] < (uint32_t)q.V)
@@ -352,7 +353,7 @@ __global__ __launch_bounds__(256) void k_embed_sums(const E* __restrict__ grad, 
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            if (i0 + j >= end) break;
+            if (i0 + j >= n) break;
             if (key[j] != run) {
                 if (open) put(part + (int64_t)piece * 2 * q.D, 1.0f);
                 else put(gW + (int64_t)run * q.D, q.scale);

@@ -203,3 +203,22 @@ def test_long_steps_in_segments(env):
     v["dt"] = torch.full_like(v["dt"], 2e38)
     o = lif.selective_scan(*[v[k] for k in ("x", "dt", "A", "B", "C")], h_first=v["h_first"])
     assert torch.equal(o.h_last, v["h_first"]) and torch.isfinite(o.y).all()
+
+
+def test_most_places(env):
+    """As many places as 32 bits count: the last of them lie in pieces whose end
+    is the largest whole number.  Counts below 2^24 are exact; the sum of 2^31 - 8
+    ones takes at most one rounding a piece and one a sum of two."""
+    torch, lif = env
+    R = (1 << 31) - 1
+    print(f"[case] embed {R} places", flush=True)
+    tokens = torch.zeros((1, R), dtype=torch.int32, device="cuda:0")
+    tokens[0, :3], tokens[0, -4:] = 1, 1
+    grad = torch.ones((1, 1, 1), device="cuda:0").expand(1, R, 1)
+    g = lif.embed_backward(tokens, grad, 3)
+    assert g[1, 0] == 7 and g[2, 0] == 0
+    assert abs(float(g[0, 0]) - (R - 7)) <= (R - 7) * 8192 * 2.0 ** -24
+    W = torch.tensor([[2.0], [3.0], [5.0]], device="cuda:0")
+    out = lif.embed(tokens, W, dtype=torch.bfloat16)
+    assert (out[0, :3] == 3).all() and (out[0, -4:] == 3).all()
+    assert all(bool((part == 2).all()) for part in out[0, 3:-4, 0].split(1 << 28))
