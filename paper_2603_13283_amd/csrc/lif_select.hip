@@ -1049,23 +1049,29 @@ __global__ __launch_bounds__(256) void k_select_sums(Geometry q, const int32_t* 
         }
         return;
     }
-    // 64 of the sums to a workgroup, a contiguous quarter of the rows to a wave
+    // 64 of the sums to a workgroup at a time, a contiguous quarter of the rows to a
+    // wave
     __shared__ float sh[4][kWave];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t at = (int64_t)(blockIdx.x - bc_blocks) * kWave + lane, rows = (int64_t)q.S * q.B;
-    const float* from = at < states ? partA + at : partS + (at - states);
-    const int64_t per = at < states ? states : 2 * (int64_t)q.D;
-    float s = 0.0f;
-    if (at < states + 2 * q.D)
+    const int64_t rows = (int64_t)q.S * q.B, sums = states + 2 * (int64_t)q.D;
+    for (int64_t at0 = (int64_t)(blockIdx.x - bc_blocks) * kWave; at0 < sums; at0 += (gridDim.x - bc_blocks) * kWave) {
+        const int64_t at = at0 + lane;
+        const float* from = at < states ? partA + at : partS + (at - states);
+        const int64_t per = at < states ? states : 2 * (int64_t)q.D;
+        float s = 0.0f;
+        if (at < sums)
 #pragma unroll 8
-        for (int64_t i = rows * w / 4; i < rows * (w + 1) / 4; ++i) s += from[i * per];
-    sh[w][lane] = s;
-    __syncthreads();
-    if (w != 0 || at >= states + 2 * q.D) return;
-    s = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
-    const int64_t i = at - states;                            // skip's, then dt_bias'
-    float* to = at < states ? gA : i < q.D ? g_skip : g_bias;
-    if (to) to[at < states ? at : i < q.D ? i : i - q.D] = s;
+            for (int64_t i = rows * w / 4; i < rows * (w + 1) / 4; ++i) s += from[i * per];
+        sh[w][lane] = s;
+        __syncthreads();
+        if (w == 0 && at < sums) {
+            s = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
+            const int64_t i = at - states;                    // skip's, then dt_bias'
+            float* to = at < states ? gA : i < q.D ? g_skip : g_bias;
+            if (to) to[at < states ? at : i < q.D ? i : i - q.D] = s;
+        }
+        __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -1318,8 +1324,9 @@ extern "C" int lif_selective_scan_backward(const void* x, const void* dt, const 
     const Geometry q = geometry_of(*p, waves_back(p->N));
     const Inputs in = {x, dt, Bm, C, z, grad_y, A, skip, dt_bias, length};
     const int64_t bc = (int64_t)q.B * q.G * q.T * q.N;
-    const int64_t bc_blocks = bc > ((int64_t)1 << 30) ? 1 << 22 : (bc + 255) / 256;
-    const int64_t blocks = bc_blocks + ((int64_t)q.D * (q.N + 2) + kWave - 1) / kWave;
+    // the last launch's workgroups, for each of its two halves at most 2^22
+    const int64_t bc_blocks = min((bc + 255) / 256, (int64_t)1 << 22);
+    const int64_t blocks = bc_blocks + min(((int64_t)q.D * (q.N + 2) + kWave - 1) / kWave, (int64_t)1 << 22);
     with_dtype(p->dtype, [&](auto e) {
         using E = decltype(e);
         char* base = (char*)ws;

@@ -222,3 +222,24 @@ def test_most_places(env):
     out = lif.embed(tokens, W, dtype=torch.bfloat16)
     assert (out[0, :3] == 3).all() and (out[0, -4:] == 3).all()
     assert all(bool((part == 2).all()) for part in out[0, 3:-4, 0].split(1 << 28))
+
+
+def test_most_states(env):
+    """The gradient of as many states as the checks accept at one step: its sums
+    are more than a launch has threads.  Channels from every part are compared."""
+    torch, lif = env
+    D, N = 1 << 24, 64
+    print(f"[case] select {D} x {N}", flush=True)
+    g = torch.Generator(device="cuda:0").manual_seed(3)
+    rn = lambda *s: torch.randn(*s, device="cuda:0", generator=g)                         # noqa: E731
+    v = {"x": rn(1, 1, D), "dt": rn(1, 1, D), "A": -torch.rand(D, N, device="cuda:0", generator=g),
+         "B": rn(1, 1, 1, N), "C": rn(1, 1, 1, N), "D": rn(D), "z": None, "dt_bias": rn(D), "h_first": rn(1, D, N),
+         "grad_y": rn(1, 1, D), "grad_last": None}
+    got = scan(env, v)
+    at = torch.cat([torch.arange(i, i + 70) for i in (0, 70000, D // 2 - 35, D - 70)]).to("cuda:0")
+    take = lambda t, axis: t.index_select(axis, at)                                       # noqa: E731
+    axis = {"x": 2, "dt": 2, "A": 0, "D": 0, "dt_bias": 0, "h_first": 1, "grad_y": 2}
+    want = select.reference({k: select.arr(t if k not in axis else take(t, axis[k])) for k, t in v.items()}, np.ones(1))
+    for k, i in {"y": 2, "h_last": 1, "grad_x": 2, "grad_dt": 2, "grad_A": 0, "grad_D": 0, "grad_dt_bias": 0,
+                 "grad_h_first": 1}.items():
+        check(select.arr(take(got[k], i)), want[k], "f32", k)
