@@ -266,27 +266,28 @@ __global__ __launch_bounds__(256) void k_conv_back(const E* __restrict__ x, cons
 }
 
 // Adds up the strips' parts [strips][K + 1][D]: 64 of the (K + 1) D sums to a
-// workgroup, whose 16 waves each take a contiguous range of strips.
+// workgroup at a time, whose 16 waves each take a contiguous range of strips.
 __global__ __launch_bounds__(1024) void k_conv_sums(const float* __restrict__ part, int64_t strips, int K, int D,
                                                     float* __restrict__ gw, float* __restrict__ gb)
 {
     __shared__ float sh[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t sums = (int64_t)(K + 1) * D, at = (int64_t)blockIdx.x * 64 + lane;
-    float s = 0.0f;
-    if (at < sums)
-#pragma unroll 8
-        for (int64_t i = strips * w / 16; i < strips * (w + 1) / 16; ++i) s += part[i * sums + at];
-    sh[w][lane] = s;
-    __syncthreads();
-    if (w != 0 || at >= sums) return;
-    s = 0.0f;
-    for (int j = 0; j < 16; ++j) s += sh[j][lane];
-    const int j = (int)(at / D), d = (int)(at - (int64_t)j * D);
-    if (j < K) {
-        if (gw) gw[(int64_t)d * K + j] = s;
-    } else if (gb) {
-        gb[d] = s;
+    const int64_t sums = (int64_t)(K + 1) * D;
+    for (int64_t at0 = (int64_t)blockIdx.x * 64; at0 < sums; at0 += (int64_t)gridDim.x * 64) {
+        const int64_t at = at0 + lane;
+        sh[w][lane] = at < sums ? sum_rows(part + at, sums, strips * w / 16, strips * (w + 1) / 16) : 0.0f;
+        __syncthreads();
+        if (w == 0 && at < sums) {
+            float s = 0.0f;
+            for (int j = 0; j < 16; ++j) s += sh[j][lane];
+            const int j = (int)(at / D), d = (int)(at - (int64_t)j * D);
+            if (j < K) {
+                if (gw) gw[(int64_t)d * K + j] = s;
+            } else if (gb) {
+                gb[d] = s;
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -450,9 +451,10 @@ extern "C" int lif_causal_conv_backward(const void* x, const float* w, const flo
                          (hipStream_t)stream, (const E*)x, w, bias, length, (const E*)x_first, (const E*)grad_y,
                          grad_last, q, (E*)grad_x, grad_x_first, sums ? (float*)ws : nullptr);
         });
+    const int64_t blocks = min(((int64_t)(p->K + 1) * q.D + 63) / 64, (int64_t)1 << 20);
     if (sums)
-        TIMED_LAUNCH("conv_sums", k_conv_sums, dim3((unsigned)(((int64_t)(p->K + 1) * q.D + 63) / 64)), dim3(1024), 0,
-                     (hipStream_t)stream, (const float*)ws, (int64_t)q.B * q.S, p->K, q.D, grad_w, grad_bias);
+        TIMED_LAUNCH("conv_sums", k_conv_sums, dim3((unsigned)blocks), dim3(1024), 0, (hipStream_t)stream,
+                     (const float*)ws, (int64_t)q.B * q.S, p->K, q.D, grad_w, grad_bias);
     return check_launch();
 }
 

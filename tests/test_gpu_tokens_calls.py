@@ -243,3 +243,24 @@ def test_most_states(env):
     for k, i in {"y": 2, "h_last": 1, "grad_x": 2, "grad_dt": 2, "grad_A": 0, "grad_D": 0, "grad_dt_bias": 0,
                  "grad_h_first": 1}.items():
         check(select.arr(take(got[k], i)), want[k], "f32", k)
+
+
+def test_most_taps(env):
+    """The gradient of so many taps that their sums are more than a launch has
+    threads; channels from every part are compared."""
+    torch, lif = env
+    T, D, K = 3, 30_000_001, 8
+    print(f"[case] conv {D} x {K}", flush=True)
+    g = torch.Generator(device="cuda:0").manual_seed(4)
+    rn = lambda *s: torch.randn(*s, device="cuda:0", generator=g)                         # noqa: E731
+    v = {"x": rn(1, T, D), "w": rn(D, K) / K ** 0.5, "bias": rn(D), "x_first": None, "grad_y": rn(1, T, D),
+         "grad_last": None}
+    o = lif.causal_conv(v["x"], v["w"], v["bias"])
+    grads = lif.causal_conv_backward(v["x"], v["w"], v["grad_y"], v["bias"])
+    got = {"y": o.y, "grad_x": grads.x, "grad_w": grads.w, "grad_bias": grads.bias}
+    at = torch.cat([torch.arange(i, i + 70) for i in (0, 70000, D // 2 - 35, D - 70)]).to("cuda:0")
+    axis = {"x": 2, "w": 0, "bias": 0, "grad_y": 2, "y": 2, "grad_x": 2, "grad_w": 0, "grad_bias": 0}
+    take = lambda k, t: t if t is None else conv.arr(t.index_select(axis[k], at))         # noqa: E731
+    want = conv.reference({k: take(k, t) for k, t in v.items()}, np.full(1, T))
+    for k, t in got.items():
+        check(take(k, t), want[k], "f32", k)
