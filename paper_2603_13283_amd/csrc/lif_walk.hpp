@@ -231,19 +231,25 @@ __device__ __forceinline__ double row_sum8(const double (&v)[kGrp], int lane)
     return dpp_sum<0xb1>(row_fold<0x1b>(q0, q1, b1));                     // quad reverse, then neighbours
 }
 
-// The sum of rows from .. to - 1 of an array, `row` elements apart, in their
-// order.  Eight loads are in flight at once, the last ones too: the compiler
-// unrolls the plain loop inside another one with a wait for each load
-// (lif_causal_conv_backward, 4 x 8192 x 1001 f16 100 us a pass, this 94).
+// The sum of rows from .. to - 1 of an array, `row` elements apart, in two levels:
+// 32 rows in their order, then those sums (3200 equal terms of a gradient: 3.6e-5
+// off in one level, 5e-7 in two).  Eight loads are in flight at once, the last
+// ones too: the compiler unrolls the plain loop inside another one with a wait for
+// each load (lif_causal_conv_backward, 4 x 8192 x 1001 f16 100 us a pass, this 94).
 __device__ __forceinline__ float sum_rows(const float* __restrict__ in, int64_t row, int64_t from, int64_t to)
 {
     float s = 0.0f;
-    for (int64_t i = from; i < to; i += 8) {
-        float v[8];
+    for (int64_t i0 = from; i0 < to; i0 += 32) {
+        const int64_t end = min(i0 + 32, to);
+        float part = 0.0f;
+        for (int64_t i = i0; i < end; i += 8) {
+            float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = in[min(i + j, to - 1) * row];
+            for (int j = 0; j < 8; ++j) v[j] = in[min(i + j, end - 1) * row];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s += i + j < to ? v[j] : 0.0f;
+            for (int j = 0; j < 8; ++j) part += i + j < end ? v[j] : 0.0f;
+        }
+        s += part;
     }
     return s;
 }

@@ -264,3 +264,17 @@ def test_most_taps(env):
     want = conv.reference({k: take(k, t) for k, t in v.items()}, np.full(1, T))
     for k, t in got.items():
         check(take(k, t), want[k], "f32", k)
+
+
+def test_gradients_of_many_steps(env):
+    """Equal terms, whose roundings all go one way, over 51200 strips of 64
+    steps: a term passes 64 roundings of its strip, 32 and 100 of its wave's
+    strips, 16 of the waves and its product's and last one's."""
+    torch, lif = env
+    nb, T, W, gy, x = 50, 65536, 20, 0.123, 0.456
+    one = torch.ones((nb, T, W), device="cuda:0")
+    g = lif.causal_conv_backward(x * one, torch.ones((W, 2), device="cuda:0"), gy * one,
+                                 torch.zeros(W, device="cuda:0"), silu=False)
+    gy, x = float(np.float32(gy)), float(np.float32(x))
+    for got, want in ((g.w[:, 1], nb * T * gy * x), (g.w[:, 0], nb * (T - 1) * gy * x), (g.bias, nb * T * gy)):
+        assert np.abs(conv.arr(got) / want - 1.0).max() <= (64 + 32 + 100 + 16 + 2) * 2.0 ** -24
