@@ -167,7 +167,9 @@ template <int CTRL> __device__ __forceinline__ float dpp(float v)
 template <int I> __device__ __forceinline__ float of_step(float v) { return dpp<0x150 | I>(v); }
 
 // acc[j] += v of step I + j times x[j], for four steps.  The compiler has no
-// such sum; the wait lets a write of v by the instruction before arrive.
+// such sum; the wait lets a write of v by the instruction before arrive.  Sums are
+// written before the last inputs are read: no input may share a register with one,
+// not even where both hold the same value.
 template <int I> __device__ __forceinline__ void add_steps(float* acc, float v, float x0, float x1, float x2, float x3)
 {
     asm("s_nop 1\n\t"
@@ -175,7 +177,7 @@ template <int I> __device__ __forceinline__ void add_steps(float* acc, float v, 
         "v_fmac_f32_dpp %1, %4, %6 row_newbcast:%10 row_mask:0xf bank_mask:0xf\n\t"
         "v_fmac_f32_dpp %2, %4, %7 row_newbcast:%11 row_mask:0xf bank_mask:0xf\n\t"
         "v_fmac_f32_dpp %3, %4, %8 row_newbcast:%12 row_mask:0xf bank_mask:0xf"
-        : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3])
+        : "+&v"(acc[0]), "+&v"(acc[1]), "+&v"(acc[2]), "+&v"(acc[3])
         : "v"(v), "v"(x0), "v"(x1), "v"(x2), "v"(x3), "n"(I), "n"(I + 1), "n"(I + 2), "n"(I + 3));
 }
 
@@ -185,7 +187,7 @@ template <int I> __device__ __forceinline__ void add_step(float& a, float& b, fl
     asm("s_nop 1\n\t"
         "v_fmac_f32_dpp %0, %2, %4 row_newbcast:%5 row_mask:0xf bank_mask:0xf\n\t"
         "v_fmac_f32_dpp %1, %3, %4 row_newbcast:%5 row_mask:0xf bank_mask:0xf"
-        : "+v"(a), "+v"(b)
+        : "+&v"(a), "+&v"(b)
         : "v"(u), "v"(v), "v"(x), "n"(I));
 }
 
