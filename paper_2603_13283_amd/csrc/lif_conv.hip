@@ -53,14 +53,14 @@ template <typename E, int VEC> struct Vec {
     E v[VEC];
 };
 
-// STEPS steps of x or grad_y from t on; those outside the sample as 0.  The
-// loads of a batch are issued together; `first` serves x before t = 0.
+// STEPS steps of x or grad_y from t >= 0 on; those past the sample's end as 0.
+// The loads of a batch are issued together.
 template <typename E, int VEC, int STEPS>
 __device__ __forceinline__ void load_batch(Vec<E, VEC> (&to)[STEPS], const E* __restrict__ in, int64_t time, int t,
                                            int n)
 {
     const E* at = in + t * time;
-    if (t >= 0 && t + STEPS <= n) {
+    if (t + STEPS <= n) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i, at += time) load_elems<E, VEC>(at, to[i].v);
     } else {
@@ -68,7 +68,7 @@ __device__ __forceinline__ void load_batch(Vec<E, VEC> (&to)[STEPS], const E* __
         for (int i = 0; i < STEPS; ++i, at += time) {
 #pragma unroll
             for (int k = 0; k < VEC; ++k) to[i].v[k] = from_f32<E>(0.0f);
-            if (t + i >= 0 && t + i < n) load_elems<E, VEC>(at, to[i].v);
+            if (t + i < n) load_elems<E, VEC>(at, to[i].v);
         }
     }
 }

@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void k_embed(const int32_t* __restrict__ token
 }
 
 struct Sort {
-    int R, T, V, chunk, chunks, bits, shift;
+    int R, T, V, chunk, bits, shift;
 };
 
 // Counts of a chunk's digits.
@@ -559,14 +559,14 @@ extern "C" int lif_embed_backward(const int32_t* token, const void* grad, const 
     if (R <= kFew) {
         int bits = 1;
         while ((1 << bits) <= p->V) ++bits;
-        const Sort o = {(int)R, p->T, p->V, 0, 0, bits, 0};
+        const Sort o = {(int)R, p->T, p->V, 0, bits, 0};
         uint32_t *ko = (uint32_t*)(base + q.keys[0]), *po = (uint32_t*)(base + q.places[0]);
         TIMED_LAUNCH("embed_sort_few", k_sort_few, dim3(1), dim3(kSmallWaves * kWave), 0, s, token, length, o, ko, po,
                      list);
         keys = ko, places = po;
     }
     for (int i = 0; i < q.passes && R > kFew; ++i) {
-        const Sort o = {(int)R, p->T, p->V, q.chunk, q.chunks, q.bits, i * q.bits};
+        const Sort o = {(int)R, p->T, p->V, q.chunk, q.bits, i * q.bits};
         uint32_t *ko = (uint32_t*)(base + q.keys[i & 1]), *po = (uint32_t*)(base + q.places[i & 1]);
         const int bins = 1 << q.bits;
         TIMED_LAUNCH("embed_count", k_count, dim3(q.chunks), dim3(kSortWaves * kWave), 0, s, token, length, keys, o,

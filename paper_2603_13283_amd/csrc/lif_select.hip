@@ -207,15 +207,6 @@ template <typename Fn> __device__ __forceinline__ void each_step_back(Fn&& fn)
     each_of([&](auto i) { fn(Step<kTile - 1 - decltype(i)::value>()); }, std::make_integer_sequence<int, kTile>());
 }
 
-// A row stride that the compiler takes for a new value each time: otherwise it
-// keeps the multiples of every stride for a tile's steps in scalar registers,
-// and spills them.
-__device__ __forceinline__ int64_t fresh(int64_t stride)
-{
-    asm volatile("" : "+s"(stride));
-    return stride;
-}
-
 // An element on its way from memory, in a register of its own: the compiler
 // packs pairs of 16-bit ones into one register, and waits for the loads to do
 // so.
