@@ -271,7 +271,7 @@ __global__ __launch_bounds__(1024) void k_conv_sums(const float* __restrict__ pa
                                                     float* __restrict__ gw, float* __restrict__ gb)
 {
     __shared__ float sh[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t sums = (int64_t)(K + 1) * D;
     for (int64_t at0 = (int64_t)blockIdx.x * 64; at0 < sums; at0 += (int64_t)gridDim.x * 64) {
         const int64_t at = at0 + lane;

@@ -378,8 +378,7 @@ __global__ __launch_bounds__(W* kWave) void k_select_maps(Inputs in, Geometry q,
 
 // c carried through the maps of segments from, from + by, ... (count of them).
 // With A > 0 (or negative step lengths) the factor of a segment can lie past the
-// largest float while the state is 0 or small: what is over 2^126 goes into c
-// first.  Up to there that part is 1, and c keeps its bits.
+// largest float while the state is 0 or small: 2^126 of it goes into c first.
 template <int NS>
 __device__ __forceinline__ void carry(float (&c)[NS], const float (&rate)[NS], const float* __restrict__ sums,
                                       const float* __restrict__ ends, const Geometry& q, const Place& p, int n0,
@@ -391,8 +390,9 @@ __device__ __forceinline__ void carry(float (&c)[NS], const float (&rate)[NS], c
         const float sum = fminf(sums[row * q.D + p.d], 3.0e38f);      // finite, for rates of 0
 #pragma unroll
         for (int k = 0; k < NS; ++k) {
-            const float v = fminf(sum * rate[k], 252.0f), over = fmaxf(v - 126.0f, 0.0f);
-            c[k] = fmaf(__builtin_amdgcn_exp2f(v - over), __builtin_amdgcn_exp2f(over) * c[k],
+            const float v = fminf(sum * rate[k], 252.0f);
+            const bool large = v > 126.0f;
+            c[k] = fmaf(__builtin_amdgcn_exp2f(large ? v - 126.0f : v), large ? c[k] * 0x1p126f : c[k],
                         ends[(row * q.N + min(n0 + k, q.N - 1)) * q.D + p.d]);
         }
     }

@@ -240,14 +240,14 @@ __device__ __forceinline__ float sum_rows(const float* __restrict__ in, int64_t 
 {
     float s = 0.0f;
     for (int64_t i0 = from; i0 < to; i0 += 32) {
-        const int64_t end = min(i0 + 32, to);
+        const float* at = in + i0 * row;
         float part = 0.0f;
-        for (int64_t i = i0; i < end; i += 8) {
+        for (int n = (int)min((int64_t)32, to - i0); n > 0; n -= 8, at += 8 * row) {
             float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = in[min(i + j, end - 1) * row];
+            for (int j = 0; j < 8; ++j) v[j] = at[min(j, n - 1) * row];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) part += i + j < end ? v[j] : 0.0f;
+            for (int j = 0; j < 8; ++j) part += j < n ? v[j] : 0.0f;
         }
         s += part;
     }
