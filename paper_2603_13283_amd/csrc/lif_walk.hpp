@@ -233,21 +233,22 @@ __device__ __forceinline__ double row_sum8(const double (&v)[kGrp], int lane)
 
 // The sum of rows from .. to - 1 of an array, `row` elements apart, in two levels:
 // 32 rows in their order, then those sums (3200 equal terms of a gradient: 3.6e-5
-// off in one level, 5e-7 in two).  Eight loads are in flight at once, the last
-// ones too: the compiler unrolls the plain loop inside another one with a wait for
-// each load (lif_causal_conv_backward, 4 x 8192 x 1001 f16 100 us a pass, this 94).
+// off in one level, 5e-7 in two).  Sixteen loads are in flight at once, the last
+// ones too: the compiler unrolls a plain loop inside another one with a wait for
+// each load (lif_causal_conv_backward, 4 x 8192 x 1001 f16 100 us a pass, this 95;
+// 50 x 65536 x 20 bf16 464, with eight at a time 479, in one level 450).
 __device__ __forceinline__ float sum_rows(const float* __restrict__ in, int64_t row, int64_t from, int64_t to)
 {
     float s = 0.0f;
-    for (int64_t i0 = from; i0 < to; i0 += 32) {
-        const float* at = in + i0 * row;
+    for (int64_t i = from; i < to; i += 32) {
+        const float* at = in + i * row;
         float part = 0.0f;
-        for (int n = (int)min((int64_t)32, to - i0); n > 0; n -= 8, at += 8 * row) {
-            float v[8];
+        for (int n = (int)min((int64_t)32, to - i); n > 0; n -= 16, at += 16 * row) {
+            float v[16];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = at[min(j, n - 1) * row];
+            for (int j = 0; j < 16; ++j) v[j] = at[min(j, n - 1) * row];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) part += j < n ? v[j] : 0.0f;
+            for (int j = 0; j < 16; ++j) part += j < n ? v[j] : 0.0f;
         }
         s += part;
     }
