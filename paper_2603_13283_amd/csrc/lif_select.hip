@@ -398,7 +398,7 @@ __device__ __forceinline__ void carry(float (&c)[NS], const float (&rate)[NS], c
     }
 }
 
-// A scan is bound by the vector unit, 59 to 77 % busy (5.5 instructions a state
+// A scan is bound by the vector unit, 60 to 78 % busy (5.5 instructions a state
 // and step: a product and 2^x for the decay, three and a half for state and
 // readout; 60 a channel and step in phases A and C; an FMA takes 2.9 cycles of a
 // SIMD, one with a broadcast 4.7, 2^x 8.5): 128 x 1000 x 512 x 16 bf16, ragged,
