@@ -753,8 +753,8 @@ int lif_causal_conv_step(const void* x, const float* w, const float* bias, const
  *             steps 0, LIF_SELECT_MARK, 2 LIF_SELECT_MARK, ... < n (later ones
  *             are not written); the backward pass needs them; may be NULL
  * Decays e^{delta A} below 2^-126 count as 0.  With LIF_SELECT_SOFTPLUS, dt =
- * -infinity masks a step: delta is 0, the step leaves the state alone, and no
- * gradient goes through its dt.  A = -infinity is a state that keeps nothing over
+ * -infinity masks a step: delta is 0, finite x and Bm leave the state alone, and
+ * no gradient goes through its dt.  A = -infinity is a state that keeps nothing over
  * a step of positive length and stays over one of length 0; no gradient goes
  * through such a decay.
  *
