@@ -754,9 +754,9 @@ int lif_causal_conv_step(const void* x, const float* w, const float* bias, const
  *             are not written); the backward pass needs them; may be NULL
  * Decays e^{delta A} below 2^-126 count as 0.  With LIF_SELECT_SOFTPLUS, dt =
  * -infinity masks a step: delta is 0, finite x and Bm leave the state alone, and
- * no gradient goes through its dt.  A = -infinity is a state that keeps nothing over
- * a step of positive length and stays over one of length 0; no gradient goes
- * through such a decay.
+ * no gradient goes through its dt.  A = -infinity is a state that keeps nothing
+ * over a step of positive length and stays over one of length 0; no gradient
+ * goes through such a decay.
  *
  * lif_selective_scan_backward: for dL/dy = grad_y ([B][T][D] of p->dtype, rows
  * contiguous, strides g_batch, g_time; NULL: 0) and dL/dh_last = grad_last
